@@ -55,7 +55,9 @@ typedef enum {
   PCTREE_ERR_UNSUPPORTED = -6  /* shape outside the compiled limits          */
 } pctree_status;
 
-typedef enum { PCTREE_F32 = 0, PCTREE_BF16 = 1 } pctree_dtype;
+/* PCTREE_F16 is a type of caches, queries and target logits; the round's head
+ * is F32 or BF16. */
+typedef enum { PCTREE_F32 = 0, PCTREE_BF16 = 1, PCTREE_F16 = 2 } pctree_dtype;
 
 /* Scoring of the tree's children.
  *   PCTREE_MODE_PARENT  PCTree: every frontier parent gets its own Markov bias
@@ -401,6 +403,186 @@ PCTREE_API pctree_status pctree_tree_attention(
     const void* v_cache, const int32_t* prefix_len, const int32_t* n_nodes,
     const int32_t* parent, void* out, void* workspace, size_t workspace_bytes,
     int32_t* status, void* stream);
+
+/*
+ * Rows of several requests, and the cache they belong to.  The entry points
+ * below serve the target's forward outside the tree attention (prompts,
+ * single tokens, chains of drafted tokens: k = 1) and the step before any
+ * attention layer, trees included.
+ *
+ * Rows: request r has n_rows[r] >= 0 consecutive rows from row row_start[r]
+ * of the row tensors (total_rows rows).  Prompts packed one behind the other
+ * have row_start = the running sum of n_rows; a packed tree's nodes
+ * [batch][N] have row_start[r] = r * N and n_rows = n_nodes.  Requests' rows
+ * do not overlap.  Rows of no request are neither read nor written.
+ *
+ * Cache: row j of request r is slot prefix_len[r] + j of the request (as node
+ * i of a tree is slot T + i in pctree_tree_attention).  k_cache and v_cache
+ * are [n_pages][page_size][Hkv][D], dense; slot s of request r is place
+ * s % page_size of page page_table[r][s / page_size], page_table
+ * [batch][max_pages] int32.  page_table NULL: request r's only page is page r
+ * (n_pages >= batch, max_pages = 1), which is the contiguous layout of
+ * pctree_tree_attention with max_slots = page_size.
+ *
+ * A request with n_rows[r] < 0, prefix_len[r] < 0, rows outside
+ * 0 .. total_rows - 1 or slots past max_pages * page_size is left out
+ * (nothing of it is written) and sets the status to PCTREE_ERR_INVALID_ARG,
+ * as a page number outside 0 .. n_pages - 1 does.
+ */
+#define PCTREE_KV_MAX_BATCH 1024   /* requests of one call */
+
+/*
+ * Appends new rows' keys and values to the cache, queries and keys normalised
+ * per head and rotated on the way:
+ *   x' = x                                       without a weight
+ *   x' = x * rsqrt(mean(x^2) + eps) * weight     with q_weight / k_weight [D]
+ *   (y_a, y_b) = rope_scale * (x'_a cos t - x'_b sin t, x'_b cos t + x'_a sin t)
+ *     for the pairs (a, b) = (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if
+ *     interleaved, i < rotary_dim / 2; t = position * inv_freq[i].  Dims past
+ *     rotary_dim are x'.
+ * Queries go to q_out [total_rows][Hq][D], keys and values to their slots.
+ * Arithmetic is float32 with one rounding at the end; the angle is reduced
+ * exactly (64-bit fractions of a turn), so far positions lose nothing.
+ */
+typedef struct {
+  int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
+  int32_t total_rows;    /* rows of q, k, v, q_out and positions             */
+  int32_t Hq, Hkv, D;    /* Hq may be 0 (keys and values only); D 64, 128, 256 */
+  int32_t page_size, n_pages, max_pages;
+  int32_t dtype;         /* PCTREE_BF16 or PCTREE_F16, of every tensor       */
+  int32_t rotary_dim;    /* rotated dims: 0 .. D, a multiple of 16           */
+  int32_t interleaved;   /* 0: pairs (i, i + rotary_dim / 2), 1: (2i, 2i + 1) */
+  int64_t q_stride, k_stride, v_stride;  /* elements from row to row, multiples
+                            of 8, at least heads * D: slices of one projection's
+                            output need no copy                              */
+  float eps;             /* of the norms, >= 0                               */
+  float rope_scale;      /* factor on cos and sin (1: none)                  */
+} pctree_append_config;
+
+/*
+ *   q, k, v         rows as above, 16-byte aligned (q and q_out NULL if Hq = 0);
+ *                   q_out must not overlap q, k or v
+ *   q_weight,
+ *   k_weight        [D] in dtype, 16-byte aligned, or NULL: no norm
+ *   inv_freq        [rotary_dim / 2] double (device): radians per position;
+ *                   NULL only if rotary_dim = 0
+ *   positions       [total_rows] int32, or NULL: the slot, prefix_len + j.
+ *                   For trees the position_ids of pctree_draft (depth + T).
+ *   row_start, n_rows, prefix_len   [batch] int32 (device)
+ *   page_table      [batch][max_pages] int32 (device) or NULL
+ *   status          one device int32 or NULL; written only on an error.  A row
+ *                   whose page number is bad is not appended (its query is
+ *                   still written).
+ * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED for bad arguments
+ * (nothing enqueued) and PCTREE_ERR_CUDA if the launch fails.  No workspace.
+ * Memory bound: every element is read once and written once.
+ */
+PCTREE_API pctree_status pctree_kv_append(
+    const pctree_append_config* cfg, const void* q, const void* k, const void* v,
+    const void* q_weight, const void* k_weight, const double* inv_freq,
+    const int32_t* positions, const int32_t* row_start, const int32_t* n_rows,
+    const int32_t* prefix_len, const int32_t* page_table, void* k_cache,
+    void* v_cache, void* q_out, int32_t* status, void* stream);
+
+/*
+ * Causal attention of new rows over the cache that holds them and their
+ * prefix.  Row j of request r sees the slots 0 .. prefix_len[r] + j:
+ *   out[row][h] = softmax_s(scale * <q[row][h], k[s][h / G]>) . v[s][h / G],
+ * G = Hq / Hkv.  One row a request is decoding, a prompt has any number of
+ * rows (behind a prefix of earlier chunks or none), a drafted chain (k = 1)
+ * is verified as the rows behind its root.  Keys and values of the rows are
+ * in the cache before the call (pctree_kv_append).  Slots past the last row
+ * are never used (their values may be anything); a NaN or infinite score or
+ * value reaches the rows that see it.  Scores, row maxima and sums and the
+ * output's accumulation are float32; probabilities are rounded to dtype for
+ * the product with the values.
+ */
+typedef struct {
+  int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
+  int32_t total_rows;    /* rows of q and out                                */
+  int32_t Hq, Hkv, D;    /* Hq a multiple of Hkv, Hq / Hkv <= 128; D 64, 128 */
+  int32_t page_size, n_pages, max_pages;
+  int32_t dtype;         /* PCTREE_BF16 or PCTREE_F16                        */
+  int64_t q_stride;      /* elements from row to row of q, a multiple of 8,
+                            at least Hq * D                                  */
+  float scale;           /* softmax scale, e.g. 1/sqrt(D), > 0               */
+} pctree_paged_attn_config;
+
+/* Workspace bytes pctree_paged_attention needs on any GPU of this kind; 0 for
+ * a bad config.  256-byte aligned, any prior content. */
+PCTREE_API size_t
+pctree_paged_attention_workspace_bytes(const pctree_paged_attn_config* cfg);
+
+/*
+ *   q               [total_rows] rows of [Hq][D], 16-byte aligned
+ *   out             [total_rows][Hq][D], 16-byte aligned, not overlapping q
+ *   k_cache, v_cache, row_start, n_rows, prefix_len, page_table: as above.
+ *                   A bad page number (see above) stands for a page of zeros.
+ *   workspace       not used concurrently by another call
+ *   status          one device int32 or NULL; written only on an error
+ *                   (PCTREE_ERR_TIMEOUT if a bounded wait ran out)
+ * Any page_size >= 1 works; 8, 16, 32, 64 and multiples of 128 fill the
+ * kernel's blocks of 128 keys.
+ * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED /
+ * PCTREE_ERR_WORKSPACE for bad arguments (nothing enqueued) and
+ * PCTREE_ERR_CUDA if the launch fails.
+ */
+PCTREE_API pctree_status pctree_paged_attention(
+    const pctree_paged_attn_config* cfg, const void* q, const void* k_cache,
+    const void* v_cache, const int32_t* row_start, const int32_t* n_rows,
+    const int32_t* prefix_len, const int32_t* page_table, void* out,
+    void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * The target's tokens from its logits and one given random number a row, the
+ * `target_tokens` of pctree_accept.  (Accepting the drafted child that equals
+ * the token sampled at its parent keeps the target's distribution: every
+ * committed token is a sample of the target at its place.  With temperature 0
+ * this is the greedy rule.)  Per row, with logits z and the row's parameters:
+ *   order    by (z desc, index asc)
+ *   w_i      = exp((z_i - max z) / temperature)
+ *   top-k    keeps the first top_k of the order (<= 0 or >= V: all)
+ *   top-p    keeps the shortest head of what is left whose w reach top_p of
+ *            its sum (>= 1: all; at least one is kept)
+ *   min-p    keeps those with w_i >= min_p (0: all)
+ *   token    the first kept i, by ascending index, whose kept w_0 + .. + w_i
+ *            exceed u times the sum of all kept w.
+ * Temperature 0: the first of the order.  The sums are exact integers of
+ * weights good to 2^-32 and 2^-44 of the largest, so that a token does not
+ * depend on the order of summation or the launch.
+ */
+typedef struct {
+  int32_t rows;          /* rows of logits                                   */
+  int32_t V;             /* vocabulary, 1 .. 2^18                            */
+  int32_t group;         /* consecutive rows that share parameters (a tree's
+                            N nodes; 1: every row has its own)               */
+  int32_t dtype;         /* of the logits: PCTREE_F32, _BF16 or _F16         */
+  int64_t row_stride;    /* elements from row to row, >= V                   */
+} pctree_sample_config;
+
+/*
+ *   logits       [rows][V] in dtype; -inf allowed (weight 0)
+ *   uniform      [rows] float in [0, 1)
+ *   temperature  [ceil(rows / group)] float: 0, or 1e-6 .. 1e6 (NULL: 1)
+ *   top_k        [ceil(rows / group)] int32 (NULL: off)
+ *   top_p        [ceil(rows / group)] float > 0 (NULL: off)
+ *   min_p        [ceil(rows / group)] float in [0, 1] (NULL: off)
+ *   n_rows       [ceil(rows / group)] int32: the group's first n_rows rows are
+ *                sampled (n_nodes of the trees), the others get token -1;
+ *                NULL: all
+ *   tokens       [rows] int32 out
+ *   status       one device int32 or NULL; written only on an error: a row
+ *                with NaN or +inf, or without a finite logit, gets token -1
+ *                and PCTREE_ERR_NONFINITE; one with a parameter or a random
+ *                number outside these ranges -1 and PCTREE_ERR_INVALID_ARG.
+ * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED for bad arguments
+ * (nothing enqueued) and PCTREE_ERR_CUDA if the launch fails.  No workspace.
+ */
+PCTREE_API pctree_status pctree_sample(
+    const pctree_sample_config* cfg, const void* logits, const float* uniform,
+    const float* temperature, const int32_t* top_k, const float* top_p,
+    const float* min_p, const int32_t* n_rows, int32_t* tokens, int32_t* status,
+    void* stream);
 
 /* Human-readable name of a status code. */
 PCTREE_API const char* pctree_status_string(int32_t status);

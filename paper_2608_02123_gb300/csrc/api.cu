@@ -369,7 +369,7 @@ using namespace pct;
 
 extern "C" {
 
-int32_t pctree_version(void) { return 102; }
+int32_t pctree_version(void) { return 103; }
 
 const char* pctree_status_string(int32_t s) {
   switch (s) {

@@ -22,6 +22,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_build",
 PCTREE_OK = 0
 PCTREE_F32 = 0
 PCTREE_BF16 = 1
+PCTREE_F16 = 2
 MAX_K, MAX_N, MAX_POOL, MAX_ROWS = 32, 1024, 16384, 4096
 
 STATUS_NAMES = {0: "ok", -1: "invalid argument", -2: "workspace",
@@ -62,6 +63,31 @@ class AttnConfig(ctypes.Structure):
                 ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("max_slots", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class AppendConfig(ctypes.Structure):
+    """pctree_append_config: rows of several requests and their cache."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "total_rows", "Hq", "Hkv", "D", "page_size", "n_pages",
+        "max_pages", "dtype", "rotary_dim", "interleaved")] + [
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64), ("eps", ctypes.c_float),
+        ("rope_scale", ctypes.c_float)]
+
+
+class PagedAttnConfig(ctypes.Structure):
+    """pctree_paged_attn_config: one causal attention layer over a cache."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "total_rows", "Hq", "Hkv", "D", "page_size", "n_pages",
+        "max_pages", "dtype")] + [
+        ("q_stride", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class SampleConfig(ctypes.Structure):
+    """pctree_sample_config: rows of logits."""
+    _fields_ = [("rows", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64)]
 
 
 class _Tree(ctypes.Structure):
@@ -106,6 +132,15 @@ def _load() -> ctypes.CDLL:
     lib.pctree_tree_attention.argtypes = [ap] + [vp] * 8 + [ctypes.c_size_t,
                                                            vp, vp]
     lib.pctree_tree_attention.restype = ctypes.c_int
+    lib.pctree_kv_append.argtypes = [ctypes.POINTER(AppendConfig)] + [vp] * 16
+    lib.pctree_kv_append.restype = ctypes.c_int
+    pp = ctypes.POINTER(PagedAttnConfig)
+    lib.pctree_paged_attention_workspace_bytes.argtypes = [pp]
+    lib.pctree_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.pctree_paged_attention.argtypes = [pp] + [vp] * 9 + [ctypes.c_size_t, vp, vp]
+    lib.pctree_paged_attention.restype = ctypes.c_int
+    lib.pctree_sample.argtypes = [ctypes.POINTER(SampleConfig)] + [vp] * 10
+    lib.pctree_sample.restype = ctypes.c_int
     lib.pctree_status_string.argtypes = [ctypes.c_int32]
     lib.pctree_status_string.restype = ctypes.c_char_p
     lib.pctree_profile_enable.argtypes = [ctypes.c_int32]
@@ -419,6 +454,178 @@ def pctree_tree_attention(cfg: AttnConfig, q: torch.Tensor, k_cache: torch.Tenso
                                    _stream_ptr(stream))
     if rc != PCTREE_OK:
         raise PctreeError(rc, "pctree_tree_attention")
+
+
+_DTYPES = {torch.float32: PCTREE_F32, torch.bfloat16: PCTREE_BF16,
+           torch.float16: PCTREE_F16}
+_TORCH_TYPE = {code: dt for dt, code in _DTYPES.items()}
+
+
+def _check_tensors(where: str, device: int, specs) -> None:
+    """Each (name, tensor, dtype, elements) of `specs`: a contiguous tensor of
+    that type with at least that many elements on `device`, or None."""
+    for name, t, dt, n in specs:
+        if t is None:
+            continue
+        if (t.dtype is not dt or t.numel() < n or not t.is_contiguous()
+                or t.get_device() != device):
+            raise ValueError(
+                f"{where}: {name} must be a contiguous {dt} tensor of at least {n} "
+                f"elements on the current device cuda:{device}")
+
+
+def _check_rows(where: str, device: int, name: str, t: torch.Tensor, dt, rows: int,
+                heads: int, D: int, stride: int) -> None:
+    """[rows][heads][D] with dense heads and `stride` elements from row to row."""
+    if (t.dtype is not dt or t.get_device() != device or t.dim() != 3
+            or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != D
+            or (rows > 1 and t.stride(0) != stride)
+            or (heads > 1 and t.stride(1) != D) or t.stride(2) != 1):
+        raise ValueError(
+            f"{where}: {name} must be a {dt} tensor [{rows}][{heads}][{D}] on the current "
+            f"device cuda:{device}, {stride} elements from row to row")
+
+
+def append_config(batch: int, total_rows: int, Hq: int, Hkv: int, D: int,
+                  page_size: int, n_pages: int, max_pages: int = 1,
+                  dtype: torch.dtype = torch.bfloat16, rotary_dim: Optional[int] = None,
+                  interleaved: bool = False, q_stride: Optional[int] = None,
+                  k_stride: Optional[int] = None, v_stride: Optional[int] = None,
+                  eps: float = 1e-6, rope_scale: float = 1.0) -> AppendConfig:
+    """``rotary_dim`` defaults to D, the row strides (elements) to dense rows.
+    A contiguous cache [batch][slots][Hkv][D] has page_size = slots, n_pages =
+    batch and no page table."""
+    return AppendConfig(batch, total_rows, Hq, Hkv, D, page_size, n_pages, max_pages,
+                        _DTYPES[dtype], D if rotary_dim is None else rotary_dim,
+                        1 if interleaved else 0,
+                        Hq * D if q_stride is None else q_stride,
+                        Hkv * D if k_stride is None else k_stride,
+                        Hkv * D if v_stride is None else v_stride, eps, rope_scale)
+
+
+def pctree_kv_append(cfg: AppendConfig, q: Optional[torch.Tensor], k: torch.Tensor,
+                     v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                     q_out: Optional[torch.Tensor], row_start: torch.Tensor,
+                     n_rows: torch.Tensor, prefix_len: torch.Tensor,
+                     page_table: Optional[torch.Tensor] = None,
+                     positions: Optional[torch.Tensor] = None,
+                     inv_freq: Optional[torch.Tensor] = None,
+                     q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None,
+                     status: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue the norms and rotation of new rows' queries and keys and the
+    append of their keys and values to the cache (see pctree_kv_append in
+    include/pctree.h).  q, k and v are [total_rows][heads][D], row strides as
+    in ``cfg`` (slices of one projection's output need no copy)."""
+    dev = torch.cuda.current_device()
+    dt = _TORCH_TYPE.get(cfg.dtype)
+    n, D, i32 = cfg.total_rows, cfg.D, torch.int32
+    if cfg.Hq > 0:
+        _check_rows("pctree_kv_append", dev, "q", q, dt, n, cfg.Hq, D, cfg.q_stride)
+    _check_rows("pctree_kv_append", dev, "k", k, dt, n, cfg.Hkv, D, cfg.k_stride)
+    _check_rows("pctree_kv_append", dev, "v", v, dt, n, cfg.Hkv, D, cfg.v_stride)
+    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * D
+    _check_tensors("pctree_kv_append", dev, (
+        ("k_cache", k_cache, dt, slots), ("v_cache", v_cache, dt, slots),
+        ("q_out", q_out, dt, n * cfg.Hq * D), ("row_start", row_start, i32, cfg.batch),
+        ("n_rows", n_rows, i32, cfg.batch), ("prefix_len", prefix_len, i32, cfg.batch),
+        ("page_table", page_table, i32, cfg.batch * cfg.max_pages),
+        ("positions", positions, i32, n),
+        ("inv_freq", inv_freq, torch.float64, cfg.rotary_dim // 2),
+        ("q_weight", q_weight, dt, D), ("k_weight", k_weight, dt, D),
+        ("status", status, i32, 1)))
+    rc = LIB.pctree_kv_append(
+        ctypes.byref(cfg), _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight),
+        _ptr(k_weight), _ptr(inv_freq), _ptr(positions), row_start.data_ptr(),
+        n_rows.data_ptr(), prefix_len.data_ptr(), _ptr(page_table), k_cache.data_ptr(),
+        v_cache.data_ptr(), _ptr(q_out), _ptr(status), _stream_ptr(stream))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_kv_append")
+
+
+def paged_attn_config(batch: int, total_rows: int, Hq: int, Hkv: int, D: int,
+                      page_size: int, n_pages: int, max_pages: int = 1,
+                      dtype: torch.dtype = torch.bfloat16,
+                      q_stride: Optional[int] = None,
+                      scale: Optional[float] = None) -> PagedAttnConfig:
+    """``q_stride`` defaults to dense rows, ``scale`` to 1/sqrt(D); the cache's
+    sizes are those of append_config."""
+    return PagedAttnConfig(batch, total_rows, Hq, Hkv, D, page_size, n_pages, max_pages,
+                           _DTYPES[dtype], Hq * D if q_stride is None else q_stride,
+                           D ** -0.5 if scale is None else scale)
+
+
+def pctree_paged_attention_workspace_bytes(cfg: PagedAttnConfig) -> int:
+    return LIB.pctree_paged_attention_workspace_bytes(ctypes.byref(cfg))
+
+
+def pctree_paged_attention(cfg: PagedAttnConfig, q: torch.Tensor, k_cache: torch.Tensor,
+                           v_cache: torch.Tensor, row_start: torch.Tensor,
+                           n_rows: torch.Tensor, prefix_len: torch.Tensor,
+                           out: torch.Tensor, workspace: torch.Tensor,
+                           page_table: Optional[torch.Tensor] = None,
+                           status: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue causal attention of new rows over the cache (see
+    pctree_paged_attention in include/pctree.h)."""
+    dev = torch.cuda.current_device()
+    dt = _TORCH_TYPE.get(cfg.dtype)
+    n, i32 = cfg.total_rows, torch.int32
+    _check_rows("pctree_paged_attention", dev, "q", q, dt, n, cfg.Hq, cfg.D, cfg.q_stride)
+    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * cfg.D
+    _check_tensors("pctree_paged_attention", dev, (
+        ("k_cache", k_cache, dt, slots), ("v_cache", v_cache, dt, slots),
+        ("out", out, dt, n * cfg.Hq * cfg.D), ("row_start", row_start, i32, cfg.batch),
+        ("n_rows", n_rows, i32, cfg.batch), ("prefix_len", prefix_len, i32, cfg.batch),
+        ("page_table", page_table, i32, cfg.batch * cfg.max_pages),
+        ("workspace", workspace, torch.uint8, 0), ("status", status, i32, 1)))
+    rc = LIB.pctree_paged_attention(
+        ctypes.byref(cfg), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+        row_start.data_ptr(), n_rows.data_ptr(), prefix_len.data_ptr(), _ptr(page_table),
+        out.data_ptr(), workspace.data_ptr(), workspace.numel(), _ptr(status),
+        _stream_ptr(stream))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_paged_attention")
+
+
+def sample_config(rows: int, V: int, group: int = 1, dtype: torch.dtype = torch.float32,
+                  row_stride: Optional[int] = None) -> SampleConfig:
+    """``row_stride`` (elements) defaults to dense rows."""
+    return SampleConfig(rows, V, group, _DTYPES[dtype], V if row_stride is None else row_stride)
+
+
+def pctree_sample(cfg: SampleConfig, logits: torch.Tensor, uniform: torch.Tensor,
+                  tokens: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                  top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                  min_p: Optional[torch.Tensor] = None, n_rows: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue the sampling of a token for every row of logits (see
+    pctree_sample in include/pctree.h).  logits is [rows][V], or any leading
+    shape that has `rows` rows row_stride apart; tokens may be the [batch][N]
+    target tokens that pctree_accept takes."""
+    dev = torch.cuda.current_device()
+    dt = _TORCH_TYPE.get(cfg.dtype)
+    groups = -(-cfg.rows // cfg.group) if cfg.group > 0 else 0
+    f32, i32 = torch.float32, torch.int32
+    if (logits.dtype is not dt or logits.get_device() != dev or logits.dim() < 1
+            or logits.shape[-1] != cfg.V or logits.stride(-1) != 1
+            or logits.numel() < cfg.rows * cfg.V
+            or (logits.dim() > 1 and cfg.rows > 1 and logits.stride(-2) != cfg.row_stride)
+            or (logits.dim() != 2 and not logits.is_contiguous())):
+        raise ValueError(f"pctree_sample: logits must be a {dt} tensor [{cfg.rows}][{cfg.V}] on "
+                         f"the current device cuda:{dev}, {cfg.row_stride} elements from row to row")
+    _check_tensors("pctree_sample", dev, (
+        ("uniform", uniform, f32, cfg.rows), ("tokens", tokens, i32, cfg.rows),
+        ("temperature", temperature, f32, groups), ("top_k", top_k, i32, groups),
+        ("top_p", top_p, f32, groups), ("min_p", min_p, f32, groups),
+        ("n_rows", n_rows, i32, groups), ("status", status, i32, 1)))
+    rc = LIB.pctree_sample(ctypes.byref(cfg), logits.data_ptr(), uniform.data_ptr(),
+                           _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                           _ptr(n_rows), tokens.data_ptr(), _ptr(status), _stream_ptr(stream))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_sample")
 
 
 def pctree_profile_enable(on: bool) -> None:

@@ -1,0 +1,256 @@
+"""pctree_paged_attention against the float64 oracle.
+
+Tolerance per output element, with A = sum_s p_s |v_s| and u the half step of
+the type: probabilities rounded for the product u * A; scores, float32 sums of
+D <= 128 products (at most 128 * 2^-24 of sum |q k| * scale, below 25 here:
+2e-4) and the exponential change a probability by 2.5e-4 relative, numerator
+and sum alike: 5e-4 * A; the output's rounding u * |out|.  In float16 a
+probability below 2^-14 of its row's reference is rounded to 2^-25: keys *
+2^-25 * max |v| more.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle as O
+from tests.kv_util import DTYPES, Batch, f64, half_step
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    from paper_2608_02123_gb300 import pctree
+    return pctree
+
+
+class Call:
+    def __init__(self, P, b, Hq, Hkv, D, dtype="bf16", seed=0, q_pad=0, garbage=True):
+        self.b, self.dt = b, DTYPES[dtype]
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed + 1)
+        rnd = lambda *s: torch.randn(*s, generator=g, dtype=self.dt, device="cuda")
+        wide = rnd(b.total, Hq * D + q_pad) * 1.5
+        self.q = wide[:, :Hq * D].unflatten(1, (Hq, D))
+        self.cfg = P.paged_attn_config(b.batch, b.total, Hq, Hkv, D, b.page_size, b.n_pages,
+                                       b.max_pages, self.dt, q_stride=wide.stride(0))
+        places = b.n_pages * b.page_size
+        self.k, self.v = rnd(places, Hkv, D), rnd(places, Hkv, D)
+        if garbage:                    # what no row sees holds anything
+            free = np.ones(places, bool)
+            for r in range(b.batch):
+                free[b.places(r, 0, int(b.prefix[r] + b.rows[r]))] = False
+            at = torch.from_numpy(np.flatnonzero(free)).cuda()
+            self.k[at] = float("nan")
+            self.v[at] = float("inf")
+        self.out = torch.full((b.total + 2, Hq, D), 9.0, dtype=self.dt, device="cuda")
+        nb = P.pctree_paged_attention_workspace_bytes(self.cfg)
+        self.ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda")
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.dev = b.dev()
+
+    def args(self):
+        return dict(q=self.q, k_cache=self.k, v_cache=self.v, out=self.out[1:-1],
+                    workspace=self.ws, status=self.status, **self.dev)
+
+    def run(self, P, **kw):
+        P.pctree_paged_attention(self.cfg, **{**self.args(), **kw})
+        torch.cuda.synchronize()
+        return int(self.status.item())
+
+    def want(self):
+        b = self.b
+        k, v = f64(self.k), f64(self.v)
+        return O.paged_attention(f64(self.q), k, v, b.start, b.rows, b.prefix, b.page_size,
+                                 b.table, self.cfg.scale)
+
+    def check(self, want=None, rows=None):
+        b, u = self.b, half_step(self.dt)
+        out, size = self.want() if want is None else want
+        got = f64(self.out)
+        used = b.used_rows()
+        assert (got[[0, -1]] == 9).all() and (got[1:-1][~used] == 9).all()
+        tol = (u + 5e-4) * size + u * np.abs(out)
+        if self.dt is torch.float16:
+            tol += float(max(b.prefix + b.rows)) * 2.0 ** -25 * 6
+        at = np.flatnonzero(used) if rows is None else rows
+        err = np.abs(got[1:-1][at] - out[at])
+        assert (err <= tol[at]).all(), (err - tol[at]).max()
+
+
+SHAPES = {
+    "one_key": dict(rows=[1], prefix=[0], page=16, heads=(32, 8)),
+    "token": dict(rows=[1], prefix=[2047], page=16, heads=(32, 8)),
+    "tokens": dict(rows=[1, 1, 1, 1, 1], prefix=[0, 127, 128, 700, 3], page=32, heads=(40, 8)),
+    "tokens_contiguous": dict(rows=[1, 1, 1], prefix=[5, 300, 129], page=0, heads=(16, 16)),
+    "chains": dict(rows=[8, 8, 3, 0, 8], prefix=[100, 250, 0, 9, 121], page=0, heads=(32, 8)),
+    "prompt": dict(rows=[300], prefix=[0], page=16, heads=(10, 2)),
+    "prompts_gaps": dict(rows=[129, 1, 64, 0, 200], prefix=[0, 40, 65, 3, 128], page=64,
+                         heads=(8, 2), gap=2),
+    "page_8": dict(rows=[40, 17], prefix=[90, 3], page=8, heads=(4, 2)),
+    "page_1": dict(rows=[12, 3], prefix=[20, 0], page=1, heads=(4, 2)),
+    "page_23": dict(rows=[40, 17], prefix=[90, 3], page=23, heads=(4, 2)),
+    "page_100": dict(rows=[150, 17], prefix=[90, 203], page=100, heads=(4, 2)),
+    "page_128": dict(rows=[150, 17], prefix=[90, 203], page=128, heads=(4, 2)),
+    "page_200": dict(rows=[150, 17], prefix=[90, 403], page=200, heads=(4, 2)),
+    "one_head": dict(rows=[140, 2], prefix=[7, 260], page=16, heads=(3, 3)),
+    "wide_group": dict(rows=[5, 1], prefix=[130, 0], page=16, heads=(128, 1)),
+    "group_of_48": dict(rows=[5, 9], prefix=[130, 0], page=32, heads=(96, 2)),
+    "many_requests": dict(rows=[1, 2, 1] * 40, prefix=[3, 0, 129] * 40, page=16, heads=(4, 4)),
+}
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "bf16"), (128, "f16"), (64, "f16")])
+@pytest.mark.parametrize("name", sorted(SHAPES))
+def test_shapes(P, name, D, dtype):
+    s = SHAPES[name]
+    b = Batch(s["rows"], s["prefix"], s["page"], gap=s.get("gap", 0))
+    c = Call(P, b, *s["heads"], D, dtype, q_pad=8 if D == 64 else 0)
+    assert c.run(P) == 0
+    c.check()
+
+
+def test_long_prefix_split_over_every_sm(P):
+    b = Batch([1, 3], [20000, 9001], 64)
+    c = Call(P, b, 8, 2, 128)
+    assert c.run(P) == 0
+    c.check()
+
+
+def test_same_result_whatever_the_workspace_held(P):
+    b = Batch([30, 1, 7], [500, 1000, 3], 16)
+    c = Call(P, b, 16, 4, 128)
+    assert c.run(P) == 0
+    first = c.out.clone()
+    c.ws.zero_()
+    assert c.run(P) == 0
+    assert torch.equal(first, c.out)
+
+
+def test_peaked_and_growing_scores(P):
+    """Maxima that grow along the keys move every row's reference, and scores
+    far apart leave one key."""
+    b = Batch([20, 1], [400, 300], 16)
+    for factor in (0.02, 12.0):
+        c = Call(P, b, 4, 2, 128, garbage=False)
+        ramp = torch.arange(c.k.shape[0], device="cuda") / c.k.shape[0]
+        c.q.mul_(0).add_(factor)
+        c.k.copy_((ramp[:, None, None] * torch.ones_like(c.k).float()).to(c.dt))
+        assert c.run(P) == 0
+        out, size = c.want()
+        got, u = f64(c.out[1:-1]), half_step(c.dt)
+        # scores of up to 136 after the float32 sum of 128 equal terms: 1e-5 of
+        # them absolute
+        tol = (u + 2 * 1e-5 * 136 + 5e-4) * size + u * np.abs(out)
+        assert (np.abs(got - out) <= tol).all()
+
+
+def test_non_finite_keys_reach_only_the_rows_that_see_them(P):
+    b = Batch([24, 5], [200, 30], 16)
+    for value in (float("nan"), float("inf")):
+        c = Call(P, b, 8, 2, 128)
+        clean = c.want()
+        slot = 200 + 10                              # row 10's own key, KV head 1
+        at = int(b.places(0, slot, slot + 1)[0])
+        c.k[at, 1, 5] = value
+        with np.errstate(invalid="ignore"):
+            want, size = c.want()
+        assert c.run(P) == 0
+        got = f64(c.out[1:-1])
+        np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+        assert np.isnan(want[10:24, 4:]).any() and not np.isnan(want[:10]).any()
+        fin = ~np.isnan(want)
+        u = half_step(c.dt)
+        tol = (u + 5e-4) * size + u * np.abs(want)
+        assert (np.abs(got - want)[fin] <= tol[fin]).all()
+        del clean
+
+
+def test_bad_requests_and_pages(P):
+    b = Batch([3, 40, 2, 5], [4, 60, 30, 7], 8)
+    c = Call(P, b, 4, 2, 64)
+    full = c.want()
+    for name, value in (("prefix_len", -1), ("prefix_len", b.max_pages * 8 - 4),
+                        ("n_rows", -1), ("n_rows", 6), ("row_start", -1),
+                        ("row_start", b.total - 4)):
+        c = Call(P, b, 4, 2, 64)
+        c.dev[name][3] = value
+        assert c.run(P) == -1, name
+        keep = b.rows.copy()
+        b.rows[3] = 0                                # its rows stay as they were
+        c.check(full)
+        b.rows[:] = keep
+    # a page number that is no page: zeros, no fault, other requests untouched
+    c = Call(P, b, 4, 2, 64)
+    c.dev["page_table"][1, 2] = b.n_pages + 5
+    c.dev["page_table"][1, 3] = -1
+    assert c.run(P) == -1
+    got = f64(c.out[1:-1])
+    assert np.isfinite(got[b.used_rows()]).all()
+    c.check(full, rows=np.r_[0:3, 43:50])
+
+
+def test_no_rows_at_all(P):
+    b = Batch([0, 0], [4, 0], 16, gap=1)
+    c = Call(P, b, 4, 2, 64)
+    assert c.run(P) == 0
+    assert (c.out == 9).all()
+
+
+def test_streams_and_graphs(P):
+    """On another stream, and replayed from two graphs that share a workspace
+    one after the other."""
+    b = Batch([70, 1, 9], [5, 900, 20], 16)
+    c = Call(P, b, 8, 2, 128)
+    want = c.want()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    P.pctree_paged_attention(c.cfg, **c.args(), stream=s)
+    torch.cuda.synchronize()
+    c.check(want)
+    d = Call(P, b, 8, 2, 128, seed=5)
+    d.ws = c.ws
+    graphs = []
+    for x in (c, d):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            P.pctree_paged_attention(x.cfg, **x.args())
+        graphs.append(g)
+    for _ in range(3):
+        c.out.fill_(9)
+        d.out.fill_(9)
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    c.check(want)
+    d.check()
+
+
+def test_pages_past_32_bits(P):
+    """Keys in the last pages of a cache of more than 2^32 elements."""
+    Hkv, D, page = 64, 128, 64
+    pages = (1 << 32) // (Hkv * D * page) + 4
+    kc = torch.zeros(pages, page, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    table = torch.tensor([[pages - 1, 3, pages - 2]], dtype=torch.int32)
+    n = 3 * page - 7
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    rnd = lambda *s: torch.randn(*s, generator=g, dtype=torch.bfloat16, device="cuda")
+    k, v = rnd(3 * page, Hkv, D), rnd(3 * page, Hkv, D)
+    for i, p in enumerate(table[0].tolist()):
+        kc[p], vc[p] = k[i * page:(i + 1) * page], v[i * page:(i + 1) * page]
+    q = rnd(1, Hkv, D)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cfg = P.paged_attn_config(1, 1, Hkv, Hkv, D, page, pages, 3)
+    ws = torch.empty(P.pctree_paged_attention_workspace_bytes(cfg), dtype=torch.uint8,
+                     device="cuda")
+    out = torch.empty_like(q)
+    P.pctree_paged_attention(cfg, q, kc, vc, torch.zeros(1, **i32), torch.ones(1, **i32),
+                             torch.full((1,), n - 1, **i32), out, ws, page_table=table.cuda())
+    s = torch.einsum("hd,shd->hs", q[0].double(), k[:n].double()) * D ** -0.5
+    p = s.softmax(-1)
+    want = torch.einsum("hs,shd->hd", p, v[:n].double())
+    size = torch.einsum("hs,shd->hd", p, v[:n].double().abs())
+    u = half_step(torch.bfloat16)
+    assert bool(((out[0].double() - want).abs() <= (u + 5e-4) * size + u * want.abs()).all())

@@ -1,0 +1,242 @@
+"""pctree_sample against the float64 oracle: tokens are equal.
+
+A row's cumulative weights are good to 2^-36.5 of their sum, so a random number
+lands on the other side of one of V borders with a chance of about V * 2^-37 a
+row (1e-6 at V = 151936); the inputs are fixed, and no row of them is that
+close.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle as O
+from tests.kv_util import DTYPES
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    from paper_2608_02123_gb300 import pctree
+    return pctree
+
+
+def draw(rows, V, dtype, seed=0, scale=3.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    z = torch.randn(rows, V, generator=g, device="cuda").mul_(scale)
+    z -= torch.rand(rows, V, generator=g, device="cuda").mul_(V).floor_().add_(1).log_().mul_(1.1)
+    u = torch.rand(rows, generator=g, device="cuda")
+    return z.to(DTYPES[dtype]), u
+
+
+def run(P, z, u, group=1, n_rows=None, rows=None, **params):
+    rows = z.shape[0] if rows is None else rows
+    cfg = P.sample_config(rows, z.shape[1], group, z.dtype, z.stride(0))
+    groups = -(-rows // group)
+    types = dict(temperature=torch.float32, top_k=torch.int32, top_p=torch.float32,
+                 min_p=torch.float32)
+    dev = {k: torch.tensor(np.broadcast_to(v, (groups,)).copy(), dtype=types[k], device="cuda")
+           for k, v in params.items()}
+    tokens = torch.full((rows + 2,), -99, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nr = None if n_rows is None else torch.tensor(n_rows, dtype=torch.int32, device="cuda")
+    P.pctree_sample(cfg, z, u, tokens[1:-1], n_rows=nr, status=status, **dev)
+    torch.cuda.synchronize()
+    got = tokens.cpu().numpy()
+    assert got[0] == -99 and got[-1] == -99
+    return got[1:-1], int(status.item())
+
+
+def want(z, u, group=1, n_rows=None, **params):
+    z, u = z.double().cpu().numpy(), u.double().cpu().numpy()
+    out = np.full(len(u), -1, np.int32)
+    for i in range(len(u)):
+        g = i // group
+        if n_rows is not None and i - g * group >= n_rows[g]:
+            continue
+        par = {}
+        for k, v in params.items():
+            x = np.broadcast_to(v, (-(-len(u) // group),))[g]
+            par[k] = int(x) if k == "top_k" else float(np.float32(x))
+        out[i] = O.sample_row(z[i], u[i], **par)
+    return out
+
+
+FILTERS = {
+    "plain": {},
+    "cold": dict(temperature=0.05),
+    "hot": dict(temperature=4.0),
+    "greedy": dict(temperature=0.0, top_k=5, top_p=0.3),
+    "top_1": dict(top_k=1),
+    "top_k": dict(temperature=0.8, top_k=50),
+    "top_k_many": dict(temperature=1.3, top_k=3000),
+    "top_p": dict(top_p=0.9),
+    "top_p_small": dict(temperature=0.7, top_p=0.05),
+    "top_p_hot": dict(temperature=3.0, top_p=0.97),
+    "min_p": dict(min_p=0.05),
+    "min_p_one": dict(min_p=1.0),
+    "all": dict(temperature=0.9, top_k=200, top_p=0.95, min_p=0.01),
+    "k_and_p": dict(temperature=2.0, top_k=1000, top_p=0.5),
+    "off": dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0),
+    "k_is_all": dict(top_k=1 << 20, top_p=2.0),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 1000, 4099, 32003, 151936])
+def test_filters(P, V, dtype):
+    """Every filter on rows of every length (odd ones are not aligned)."""
+    for i, (name, params) in enumerate(sorted(FILTERS.items())):
+        z, u = draw(4, V, dtype, seed=17 * i + V)
+        got, st = run(P, z, u, **params)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, **params), err_msg=name)
+
+
+@pytest.mark.parametrize("params", [{}, dict(temperature=0.6), dict(temperature=2.5),
+                                    dict(top_p=0.95), dict(top_k=40)])
+def test_many_rows(P, params):
+    """Rows with many borders near the random number."""
+    z, u = draw(700, 20011, "f32", seed=5)
+    got, st = run(P, z, u, **params)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, **params))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 3001, 151936])
+def test_equal_logits(P, V, dtype):
+    """Rows of one value, two values or few values: the order is the index."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    u = torch.rand(6, generator=g, device="cuda")
+    z = torch.zeros(6, V, device="cuda")
+    z[1] = -3.5
+    z[2, ::3] = 1.0
+    z[3] = torch.randint(0, 3, (V,), generator=g, device="cuda").float()
+    z[4, V // 2:] = -0.0                              # equal to +0
+    z[5] = torch.randint(0, 40, (V,), generator=g, device="cuda").float() * 0.125
+    z = z.to(DTYPES[dtype])
+    for params in ({}, dict(top_k=max(1, V // 2 - 1)), dict(top_k=2), dict(top_p=0.5),
+                   dict(top_p=0.9, top_k=max(1, V - 3)), dict(temperature=0.0), dict(min_p=0.9)):
+        got, st = run(P, z, u, **params)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, **params), err_msg=str(params))
+
+
+def test_random_numbers_at_the_ends(P):
+    z, _ = draw(4, 5000, "f32", seed=9)
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 2.0 ** -24, 0.5], device="cuda")
+    for params in ({}, dict(top_k=7), dict(top_p=0.8)):
+        got, st = run(P, z, u, **params)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, **params))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_masked_vocabularies(P, dtype):
+    """Logits masked with -inf or the type's lowest value, down to one."""
+    dt = DTYPES[dtype]
+    lowest = torch.finfo(dt).min
+    for value in (float("-inf"), lowest):
+        for keep in (1, 3, 400):
+            z, u = draw(5, 30011, "f32", seed=keep)
+            mask = torch.ones_like(z, dtype=torch.bool)
+            g = torch.Generator(device="cuda")
+            g.manual_seed(keep)
+            for r in range(5):
+                mask[r, torch.randperm(30011, generator=g, device="cuda")[:keep]] = False
+            z = z.to(dt).masked_fill_(mask, value)
+            for params in ({}, dict(top_k=2), dict(top_k=1000), dict(top_p=0.7),
+                           dict(temperature=0.0), dict(top_k=401, top_p=0.999)):
+                got, st = run(P, z, u, **params)
+                assert st == 0
+                np.testing.assert_array_equal(got, want(z, u, **params), err_msg=str(params))
+    z = torch.full((2, 999), lowest, dtype=dt, device="cuda")     # nothing but masks
+    u = torch.tensor([0.25, 0.75], device="cuda")
+    got, st = run(P, z, u)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u))
+
+
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 0.02, 30.0, 1e6])
+@pytest.mark.parametrize("shift", [0.0, 88.0, -3e4, 1e7, 1e30])
+def test_extreme_scales(P, temperature, shift):
+    """Far from zero, and temperatures at their limits."""
+    z, u = draw(3, 7001, "f32", seed=3)
+    z = z + shift
+    for params in ({}, dict(top_p=0.8), dict(top_k=11)):
+        got, st = run(P, z, u, temperature=temperature, **params)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, temperature=temperature, **params))
+
+
+def test_groups_padding_and_strides(P):
+    """Trees' rows: parameters per request, unused rows -1, rows of a wider
+    tensor."""
+    wide, u = draw(3 * 16, 4000, "f32", seed=21)
+    z = wide[:, 5:3105]                              # rows not aligned to 16 bytes
+    par = dict(temperature=[0.0, 0.7, 1.2], top_k=[0, 30, 0], top_p=[1.0, 1.0, 0.9],
+               min_p=[0.0, 0.0, 0.02])
+    for n_rows in (None, [16, 0, 5], [3, 99, -2]):
+        got, st = run(P, z, u, group=16, n_rows=n_rows, **par)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, group=16, n_rows=n_rows, **par))
+    got, st = run(P, z, u, group=16, rows=37, **par)   # the last group is cut short
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, group=16, **par)[:37])
+
+
+def test_bad_rows_and_parameters(P):
+    z, u = draw(8, 3000, "f32", seed=2)
+    good = want(z, u)
+    z[1, 77] = float("nan")
+    z[2, 0] = float("inf")
+    z[3] = float("-inf")
+    got, st = run(P, z, u)
+    assert st == -5
+    assert (got[1:4] == -1).all()
+    np.testing.assert_array_equal(got[[0, 4, 5, 6, 7]], good[[0, 4, 5, 6, 7]])
+    nan = float("nan")
+    for name, bad in (("temperature", [-1.0, nan, 1e-7, 1e7, float("inf")]),
+                      ("top_p", [0.0, -0.5, nan]), ("min_p", [-0.1, 1.5, nan])):
+        for x in bad:
+            z, u = draw(2, 500, "bf16", seed=4)
+            ok = want(z, u)
+            got, st = run(P, z, u, **{name: [1.0 if name != "min_p" else 0.0, x]})
+            assert st == -1 and got[1] == -1 and got[0] == ok[0], (name, x)
+    for x in (1.0, -0.1, nan):
+        z, u = draw(2, 500, "f32", seed=4)
+        ok = want(z, u)
+        u[1] = x
+        got, st = run(P, z, u)
+        assert st == -1 and got[1] == -1 and got[0] == ok[0]
+
+
+def test_largest_vocabulary(P):
+    z, u = draw(3, 1 << 18, "f32", seed=8, scale=0.01)
+    for params in ({}, dict(top_p=0.9), dict(top_k=100000)):
+        got, st = run(P, z, u, **params)
+        assert st == 0
+        np.testing.assert_array_equal(got, want(z, u, **params))
+
+
+def test_stream_and_graph(P):
+    z, u = draw(9, 9001, "bf16", seed=6)
+    ref = want(z, u, top_k=20)
+    cfg = P.sample_config(9, 9001, dtype=z.dtype)
+    tokens = torch.empty(9, dtype=torch.int32, device="cuda")
+    k = torch.full((9,), 20, dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    P.pctree_sample(cfg, z, u, tokens, top_k=k, stream=s)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(tokens.cpu().numpy(), ref)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        P.pctree_sample(cfg, z, u, tokens, top_k=k)
+    tokens.fill_(-3)
+    g.replay()
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(tokens.cpu().numpy(), ref)
