@@ -1,10 +1,13 @@
 // pctree_sample: the target's token at every row of its logits, from given
 // random numbers, with temperature, top-k, top-p and min-p.
 //
-// A row belongs to a cluster of up to eight CTAs, each of which keeps its slice
-// of the row in shared memory: the logits are read from memory once, and every
-// later pass (maximum, weights, selection, draw) runs on shared memory, with
-// the CTAs' results exchanged through distributed shared memory.
+// Two placements of a row, the same code:
+//   cluster  (few rows) a row belongs to up to eight CTAs, each of which keeps
+//            its slice in shared memory: logits are read once, and the CTAs'
+//            results meet through distributed shared memory;
+//   stream   (many rows) a row belongs to one CTA, which reads it from memory
+//            in the first pass and from L2 in the others: no cluster barriers,
+//            and as many rows in flight as L2 holds.
 //
 // Weights w = exp((z - max) / T) are summed as integers in units of 2^-45 of
 // the largest weight, so sums are exact and in any order the same.  A token is
@@ -19,13 +22,18 @@
 // Tokens above 2^-12 of the total use the fine form (there are at most 4096);
 // the errors of the light ones then add up to at most 2^-36.5 of the total.
 //
-// Selection: every filter keeps a head of the order (z desc, index asc), which
-// is the set of keys K >= K* for K = (z, -index) as one 64-bit integer, K* the
-// largest key whose head reaches a target count (top-k) or weight (top-p).
-// The logits are binned linearly below the maximum (512 bins over 16 octaves
-// of weight, over all 46 where that is too few); the bin that the target falls
-// in is gathered and ranked.  A bin too full for that (long runs of equal
-// logits) is left to a bisection over the keys.
+// Selection: every filter keeps a head of the order (z desc, index asc).
+//   Few candidates: where a logit is known that nothing kept is below, the
+//   logits from it on (a little over top_k of them) are ranked against one
+//   another by one CTA, with their exact weights.
+//   Else a head is the set of keys K >= K* for K = (z, -index) as one 64-bit
+//   integer, K* the largest key whose head reaches a target count (top-k) or
+//   weight (top-p): the logits are binned linearly below the maximum, by count
+//   and by weight in single precision; the bins that the target can fall in
+//   are gathered and ranked on top of the exact sums above them.  Bins too full
+//   for that (long runs of equal logits) are left to a bisection over the keys.
+#include <type_traits>
+
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
@@ -37,9 +45,10 @@ constexpr int kSmpWarps = kSmpThreads / 32;
 constexpr int kSmpMaxCluster = 8;
 constexpr int kSmpBins = 512;
 constexpr int kSmpList = 512;               // gathered keys of a bin
+constexpr int kSmpGroups = kSmpThreads / 8; // groups of eight lanes per CTA
+constexpr int kSmpCand = 832;               // candidates one CTA can rank
 constexpr int kSmpMaxV = 1 << 18;           // sums of 2^45-scaled weights fit 64 bits
-constexpr int kOctaves = 46;                // below: weight 0
-constexpr int kNarrow = 16;                 // octaves of the first binning
+constexpr int kOctaves = 46;                // below the largest: weight 0
 constexpr float kMagic = 12582912.0f;       // 1.5 * 2^23: adds as round to integer
 constexpr float kMagic2 = 0.0234375f;       // 1.5 * 2^-6: rounds to 2^-29
 constexpr float kLn2 = 0.693147180559945f / 128.0f;
@@ -81,71 +90,100 @@ struct SampleArgs {
   int V, group, slice;                      // slice: elements per CTA of the cluster
 };
 
-// What a row's passes need, the same in every CTA of its cluster.
+// What a row's passes need, the same in every CTA of its cluster.  Logits are
+// taken relative to `base`.
 struct RowFacts {
   float c_hi, c_lo;                         // 128 log2(e) / T
-  float base;                               // subtracted from z before scaling
-  float m;                                  // max - base
-  float cut;                                // z - base below it has weight 0
-  float fine_from;                          // z - base from it on uses the fine form
-  int k0;                                   // round(m * 128 log2(e) / T)
+  float base;
+  float m;                                  // the maximum
+  float low;                                // 60 octaves below: clamped to, weight 0
+  float cut;                                // 46 octaves below: weight 0 from here down
+  float fine_from;                          // from it on the fine form
+  float min_z;                              // min_p keeps logits (not relative) from it on
+  int k;                                    // round(m * 128 log2(e) / T)
 };
 
 struct alignas(16) SampleShared {
   uint64_t bar;
   RowFacts row;
-  float warp_max[kSmpWarps];
-  float cta_max[kSmpMaxCluster];
+  float warp_max[kSmpMaxCluster * kSmpWarps];       // of every warp of the cluster
+  alignas(16) float group_max[kSmpMaxCluster * kSmpGroups];   // of every 8 lanes, or thread
+  float from;                               // logits from it on are candidates
   int cta_first[kSmpMaxCluster];            // lowest index of the maximum (T = 0)
+  unsigned cta_n[kSmpMaxCluster];           // candidates of every CTA
   unsigned long long warp_sum[kSmpMaxCluster * kSmpWarps];
-  // found by the leader, written to every CTA
-  int bin;                                  // -1: the target lies past the bins
-  unsigned long long above_n, above_w;      // count and weight before the bin
+  int bin0, bin1;                           // the bins a target can fall in (-1: past all)
   unsigned long long border, border_w;      // K* and the weight of its head
-  unsigned long long total_w;               // weight of all bins
-  unsigned list_n;
-  unsigned long long part_n[kSmpMaxCluster], part_w[kSmpMaxCluster];
-  unsigned long long red[2 * kSmpWarps];
-  // the leader's sum of all CTAs' bins
-  unsigned bin_n[kSmpBins];
-  unsigned long long bin_w[kSmpBins];
+  int found;
+  unsigned list_n, local_n;
+  unsigned long long part[kSmpMaxCluster];
+  unsigned long long red[kSmpWarps];
   union {
-    unsigned hist[4][kSmpBins];             // count, weight in 15-bit limbs
+    struct {                                // one CTA's candidates
+      unsigned long long key[kSmpCand], w[kSmpCand];
+    } cand;
     struct {
-      unsigned long long key[kSmpList], w[kSmpList];
-    } list;
+      unsigned bin_n[kSmpBins], bin_w[kSmpBins];    // the leader's sum of all CTAs' bins
+      union {
+        unsigned hist[2][kSmpBins];         // count, weight in 2^-32 of the total
+        struct {
+          unsigned long long key[kSmpList], w[kSmpList];
+        } list;
+      };
+    };
   };
   uint2 tab[128][16];                       // light table, a column per lane pair
 };
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ T* cluster_ptr(T* p, int rank) {
-  uint64_t r;
-  asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
-  return reinterpret_cast<T*>(r);
+  if constexpr (STREAM) {
+    return p;
+  } else {
+    uint64_t r;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+    return reinterpret_cast<T*>(r);
+  }
 }
 
-// Barrier of the cluster's CTAs, with the warp's lanes together.
+// Barrier of the row's CTAs, with the warp's lanes together.
+template <bool STREAM>
 __device__ __forceinline__ void csync() {
-  __syncwarp();
-  cluster_sync();
+  if constexpr (STREAM) {
+    __syncthreads();
+  } else {
+    __syncwarp();
+    cluster_sync();
+  }
 }
 
-__device__ __forceinline__ unsigned long long light_weight(const SampleShared* S,
-                                                           const RowFacts& f, float x) {
-  const float t = fmaf(x, f.c_hi, kMagic);
-  const float kf = t - kMagic;
-  float r = fmaf(x, f.c_hi, -kf);
-  r = fmaf(x, f.c_lo, r);
-  float p = fmaf(r, kLn2 * kLn2 * kLn2 / 6.0f, kLn2 * kLn2 / 2.0f);
-  p = fmaf(r, p, kLn2);
-  const float s = r * p;
-  const int n = __float_as_int(t) - 0x4b400000 - f.k0;      // <= 0
-  const uint2 e = S->tab[n & 127][threadIdx.x & 15];
-  const float b = fmaf(__uint_as_float(e.y), s, kMagic2);
-  const uint32_t w = e.x + (static_cast<uint32_t>(__float_as_int(b)) << 2);
-  const int sh = -(n >> 7);
-  return ((static_cast<unsigned long long>(w) << 14) + ((1ull << sh) >> 1)) >> sh;
+// Light weights of two logits (relative to base, at least f.low).
+__device__ __forceinline__ void light_weights(const SampleShared* S, const RowFacts& f, float x0,
+                                              float x1, unsigned long long& w0,
+                                              unsigned long long& w1) {
+  const uint64_t x = pack2(x0, x1), c = pack2(f.c_hi, f.c_hi);
+  const uint64_t t = fma2(x, c, pack2(kMagic, kMagic));
+  const uint64_t nk = fma2(t, pack2(-1.0f, -1.0f), pack2(kMagic, kMagic));
+  uint64_t r = fma2(x, c, nk);
+  r = fma2(x, pack2(f.c_lo, f.c_lo), r);
+  constexpr float a2 = kLn2 * kLn2 / 2.0f, a3 = kLn2 * kLn2 * kLn2 / 6.0f;
+  uint64_t p = fma2(r, pack2(a3, a3), pack2(a2, a2));
+  p = fma2(r, p, pack2(kLn2, kLn2));
+  const uint64_t s = mul2(r, p);
+  float t0, t1;
+  unpack2(t, t0, t1);
+  // n = round(x c) - k <= 0 is -(128 sh - j): sh = ceil(-n / 128), and the
+  // table is stored backwards
+  const int n0 = f.k + (0x4b400000 + 127) - __float_as_int(t0);
+  const int n1 = f.k + (0x4b400000 + 127) - __float_as_int(t1);
+  const uint2 e0 = S->tab[n0 & 127][threadIdx.x & 15], e1 = S->tab[n1 & 127][threadIdx.x & 15];
+  float b0, b1;
+  unpack2(fma2(pack2(__uint_as_float(e0.y), __uint_as_float(e1.y)), s, pack2(kMagic2, kMagic2)),
+          b0, b1);
+  const uint32_t v0 = e0.x + (static_cast<uint32_t>(__float_as_int(b0)) << 2);
+  const uint32_t v1 = e1.x + (static_cast<uint32_t>(__float_as_int(b1)) << 2);
+  w0 = (((static_cast<unsigned long long>(v0) << 15) >> (n0 >> 7)) + 1) >> 1;
+  w1 = (((static_cast<unsigned long long>(v1) << 15) >> (n1 >> 7)) + 1) >> 1;
 }
 
 __device__ __forceinline__ unsigned long long fine_weight(const RowFacts& f, float x) {
@@ -161,7 +199,7 @@ __device__ __forceinline__ unsigned long long fine_weight(const RowFacts& f, flo
   const float yh = r * l_hi;
   const float yl = fmaf(r, l_hi, -yh) + fmaf(r, l_lo, rl * l_hi);
   const float sl = fmaf(yh * yh, fmaf(yh, fmaf(yh, 1.0f / 24.0f, 1.0f / 6.0f), 0.5f), yl);
-  const int n = static_cast<int>(kf) - f.k0;
+  const int n = static_cast<int>(kf) - f.k;
   const int j = n & 127;
   const float th = kPow2.hi[j], tl = kPow2.lo[j];
   const float q = th * yh;
@@ -173,17 +211,29 @@ __device__ __forceinline__ unsigned long long fine_weight(const RowFacts& f, flo
   return (static_cast<unsigned long long>(w) + ((1ull << sh) >> 1)) >> sh;
 }
 
-__device__ __forceinline__ unsigned long long weight(const SampleShared* S, const RowFacts& f,
-                                                     float x) {
-  if (x < f.cut) return 0ull;
-  return x >= f.fine_from ? fine_weight(f, x) : light_weight(S, f, x);
-}
 
 // Order (z desc, index asc) as integers, largest first.
 __device__ __forceinline__ unsigned long long order_key(float z, int index) {
   const unsigned b = __float_as_uint(z + 0.0f);             // -0 ranks as 0
   const unsigned o = (b & 0x80000000u) ? ~b : b | 0x80000000u;
   return (static_cast<unsigned long long>(o) << 32) | (0xffffffffu - static_cast<unsigned>(index));
+}
+
+// x in [0, 1) as a 64-bit fraction (exact from 2^-41 on).
+__device__ __forceinline__ unsigned long long fraction64(float x) {
+  const unsigned b = __float_as_uint(x);
+  const int e = static_cast<int>(b >> 23);
+  const unsigned long long m = (b & 0x7fffffu) | 0x800000u;
+  return e >= 86 ? m << (e - 86) : e > 62 ? m >> (86 - e) : 0ull;
+}
+// The smallest weight that reaches p of `all`, and the place of u in `total`.
+__device__ __forceinline__ unsigned long long reach_of(float p, unsigned long long all) {
+  const unsigned long long f = fraction64(p);
+  const unsigned long long t = __umul64hi(f, all) + (f * all != 0 ? 1ull : 0ull);
+  return t < 1 ? 1 : t;
+}
+__device__ __forceinline__ unsigned long long place_of(float u, unsigned long long total) {
+  return __umul64hi(fraction64(u), total);
 }
 
 __device__ __forceinline__ unsigned long long warp_sum64(unsigned long long v) {
@@ -199,6 +249,9 @@ struct Elem<PCTREE_F32> {
   using type = float;
   static constexpr int kVec = 4;
   static __device__ __forceinline__ float low() { return -INFINITY; }
+  static __device__ __forceinline__ uint4 low_vec() {
+    return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+  }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x);
     x[1] = __uint_as_float(v.y);
@@ -211,6 +264,10 @@ struct Elem16 {
   using type = uint16_t;
   static constexpr int kVec = 8;
   static __device__ __forceinline__ uint16_t low() { return F16 ? 0xfc00 : 0xff80; }
+  static __device__ __forceinline__ uint4 low_vec() {
+    constexpr uint32_t two = F16 ? 0xfc00fc00u : 0xff80ff80u;
+    return make_uint4(two, two, two, two);
+  }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -226,8 +283,37 @@ struct Elem<PCTREE_BF16> : Elem16<false> {};
 template <>
 struct Elem<PCTREE_F16> : Elem16<true> {};
 
-template <int DT>
-__global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
+// The weights of a lane's logits: the light form of all without branches (so
+// that the chains overlap), then the fine form of the few that use it.
+template <int N>
+__device__ __forceinline__ void weights(const SampleShared* S, const RowFacts& f,
+                                        const float (&x)[N], unsigned long long (&w)[N]) {
+  bool fine = false;
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    const float z0 = x[e] - f.base, z1 = x[e + 1] - f.base;
+    light_weights(S, f, fmaxf(z0, f.low), fmaxf(z1, f.low), w[e], w[e + 1]);
+    fine |= z0 >= f.fine_from || z1 >= f.fine_from;
+  }
+  if (fine) {
+#pragma unroll 1
+    for (int e = 0; e < N; ++e) {
+      float z = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i == e) z = x[i] - f.base;
+      if (z >= f.fine_from) {
+        const unsigned long long v = fine_weight(f, z);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i == e) w[i] = v;
+      }
+    }
+  }
+}
+
+template <int DT, bool STREAM>
+__global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   using E = Elem<DT>;
   using T = typename E::type;
   constexpr int kVec = E::kVec;
@@ -235,20 +321,16 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
   SampleShared* S = reinterpret_cast<SampleShared*>(smem);
   T* data = reinterpret_cast<T*>(smem + sizeof(SampleShared));
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n_cta = static_cast<int>(a.V + a.slice - 1) / a.slice;   // = the cluster's size
-  const int rank = static_cast<int>(cluster_ctarank());
+  const int n_cta = STREAM ? 1 : (a.V + a.slice - 1) / a.slice;       // = the cluster's size
+  const int rank = STREAM ? 0 : static_cast<int>(cluster_ctarank());
   const int row = blockIdx.x / n_cta;
-  SampleShared* L = cluster_ptr(S, 0);                      // the leader's
+  SampleShared* L = cluster_ptr<STREAM>(S, 0);              // the leader's
   pdl_launch_dependents();
   if (tid == 0) {
     mbar_init(&S->bar, 1);
     fence_barrier_init();
-  }
-  for (int i = tid; i < 128 * 16; i += kSmpThreads) {
-    const int j = i >> 4;
-    S->tab[j][i & 15] = make_uint2(
-        kPow2.fix[j] - (static_cast<uint32_t>(__float_as_int(kMagic2)) << 2),
-        __float_as_uint(kPow2.hi[j]));
+    S->list_n = 0;
+    S->local_n = 0;
   }
   pdl_wait();
   const int g = row / a.group;
@@ -261,32 +343,35 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
   const T* src = static_cast<const T*>(a.logits) + row * a.row_stride + e0;
   // element i lies at data[pad + i], so that global and shared addresses agree
   // modulo 16 bytes; the vectors' places outside the slice hold -inf
-  const int pad = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15u) / sizeof(T));
+  const int pad =
+      STREAM ? 0 : static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15u) / sizeof(T));
   const int n_vec = (pad + n_el + kVec - 1) / kVec;
   const int head = pad == 0 ? 0 : min(n_el, kVec - pad);
-  const int body = (n_el - head) / kVec;                    // whole vectors
+  const int body = STREAM ? 0 : (n_el - head) / kVec;       // whole vectors
   __syncthreads();
-  if (tid == 0 && body > 0) {
-    mbar_arrive_expect_tx(&S->bar, static_cast<uint32_t>(body) * 16u);
-    const uint32_t bar = smem_u32(&S->bar);
-    const T* from = src + head;
-    uint32_t to = smem_u32(data + pad + head);
-    for (int left = body; left > 0;) {
-      const int v = left < 1024 ? left : 1024;              // 16 KB a copy
-      asm volatile(
-          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
-              "r"(to), "l"(reinterpret_cast<uint64_t>(from)), "r"(v * 16), "r"(bar)
-          : "memory");
-      to += v * 16;
-      from += v * kVec;
-      left -= v;
+  if constexpr (!STREAM) {
+    if (tid == 0 && body > 0) {
+      mbar_arrive_expect_tx(&S->bar, static_cast<uint32_t>(body) * 16u);
+      const uint32_t bar = smem_u32(&S->bar);
+      const T* from = src + head;
+      uint32_t to = smem_u32(data + pad + head);
+      for (int left = body; left > 0;) {
+        const int v = left < 1024 ? left : 1024;            // 16 KB a copy
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+            "[%3];" ::"r"(to), "l"(reinterpret_cast<uint64_t>(from)), "r"(v * 16), "r"(bar)
+            : "memory");
+        to += v * 16;
+        from += v * kVec;
+        left -= v;
+      }
     }
+    if (tid < head) data[pad + tid] = src[tid];
+    const int tail0 = head + body * kVec;
+    if (tid >= 32 && tid < 32 + n_el - tail0) data[pad + tail0 + tid - 32] = src[tail0 + tid - 32];
+    if (tid >= 64 && tid < 64 + pad) data[tid - 64] = E::low();
+    if (tid >= 96 && tid < 96 + n_vec * kVec - pad - n_el) data[pad + n_el + tid - 96] = E::low();
   }
-  if (tid < head) data[pad + tid] = src[tid];
-  const int tail0 = head + body * kVec;
-  if (tid >= 32 && tid < 32 + n_el - tail0) data[pad + tail0 + tid - 32] = src[tail0 + tid - 32];
-  if (tid >= 64 && tid < 64 + pad) data[tid - 64] = E::low();
-  if (tid >= 96 && tid < 96 + n_vec * kVec - pad - n_el) data[pad + n_el + tid - 96] = E::low();
   // the row's parameters
   const float temp = a.temperature != nullptr ? a.temperature[g] : 1.0f;
   const int top_k = a.top_k != nullptr ? a.top_k[g] : 0;
@@ -295,6 +380,31 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
   const float u = a.uniform[row];
   const bool params_ok = (temp == 0.0f || (temp >= 1e-6f && temp <= 1e6f)) && top_p > 0.0f &&
                          min_p >= 0.0f && min_p <= 1.0f && u >= 0.0f && u < 1.0f;
+  const bool by_k = top_k > 0 && top_k < a.V, by_p = top_p < 1.0f, by_m = min_p > 0.0f;
+  // lanes per group of the maxima that bound the top_k-th logit (0: too many)
+  const int group_lanes = !by_k || temp == 0.0f              ? 0
+                          : top_k <= n_cta * kSmpWarps / 2   ? 32
+                          : top_k <= n_cta * kSmpGroups * 3 / 4 ? 8
+                          : STREAM && top_k <= kSmpThreads * 3 / 4 ? 1
+                                                                : 0;
+  const bool few = group_lanes != 0 || (by_m && (!by_k || !by_p));
+  // the scale, and min_p's border below the maximum (one thread: 64-bit
+  // arithmetic of a whole CTA would take longer than a pass over the row)
+  double c = 1.0, below = 0.0;
+  if (tid == 0 && params_ok && temp > 0.0f) {
+    c = 128.0 * 1.4426950408889634074 / static_cast<double>(temp);
+    if (by_m) below = static_cast<double>(temp) * log(static_cast<double>(min_p));
+  }
+  auto make_table = [&]() {
+    for (int i = tid; i < 128 * 16; i += kSmpThreads) {
+      const int q = i >> 4, j = 127 - q;
+      S->tab[q][i & 15] = make_uint2(
+          kPow2.fix[j] - (static_cast<uint32_t>(__float_as_int(kMagic2)) << 2),
+          __float_as_uint(kPow2.hi[j]));
+    }
+  };
+  const bool all_light = temp > 0.0f && !by_k && (by_p || !by_m);   // weights of the whole row
+  if (all_light) make_table();
   bool landed = true;
   if (body > 0) {
     volatile int never = 0;
@@ -304,49 +414,77 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
   // each warp has a run of the slice's vectors
   const int per_warp = (n_vec + kSmpWarps - 1) / kSmpWarps;
   const int v0 = min(n_vec, warp * per_warp), v1 = min(n_vec, v0 + per_warp);
-  const uint4* vec = reinterpret_cast<const uint4*>(data);
+  const uint4* vec = STREAM ? reinterpret_cast<const uint4*>(src)
+                            : reinterpret_cast<const uint4*>(data);
   const int first = e0 - pad;                               // row index of data[0]
+  // body_fn(x, row index of x[0]) over the lane's vectors, `ahead` loads in
+  // flight; lanes past the run's end get -inf, so the warp stays together
+  constexpr std::integral_constant<int, 4> kFar{};          // little work per vector
+  constexpr std::integral_constant<int, 2> kNear{};
+  constexpr std::integral_constant<int, 1> kNext{};
+  auto pass = [&](auto ahead, auto&& body_fn) {
+    constexpr int kAhead = STREAM ? decltype(ahead)::value : 1;
+    for (int vb = v0; vb < v1; vb += 32 * kAhead) {
+      uint4 raw[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int v = vb + i * 32 + lane;
+        raw[i] = v < v1 ? vec[v] : E::low_vec();
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        float x[kVec];
+        E::unpack(raw[i], x);
+        body_fn(x, first + (vb + i * 32 + lane) * kVec);
+      }
+    }
+  };
 
   // ---------------- maximum ----------------
   float m = -INFINITY;
-  for (int v = v0 + lane; v < v1; v += 32) {
-    float x[kVec];
-    E::unpack(vec[v], x);
+  pass(kFar, [&](const float (&x)[kVec], int) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) m = max_nan(m, x[e]);
+    for (int e = 0; e < kVec; e += 2) m = max_nan(m, x[e], x[e + 1]);
+  });
+  if (!landed) m = __int_as_float(0x7fc00000);
+  const float m1 = m;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
+  const float m8 = m;
+#pragma unroll
+  for (int o = 8; o < 32; o <<= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
+  // every CTA of the cluster has started before its memory is written
+  if constexpr (!STREAM) csync<STREAM>();
+  if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->warp_max[rank * kSmpWarps + warp] = m;
+  if (group_lanes == 8) {
+    for (int i = lane & 7; i < n_cta; i += 8)
+      cluster_ptr<STREAM>(S, i)->group_max[rank * kSmpGroups + warp * 4 + (lane >> 3)] = m8;
+  } else if (group_lanes == 1) {
+    S->group_max[tid] = m1;
   }
+  csync<STREAM>();
+  m = -INFINITY;
+  for (int i = lane; i < n_cta * kSmpWarps; i += 32) m = max_nan(m, S->warp_max[i]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
-  if (lane == 0) S->warp_max[warp] = m;
-  __syncthreads();
-  // every CTA of the cluster has started before its memory is written
-  csync();
-  if (warp == 0) {
-    m = lane < kSmpWarps ? S->warp_max[lane] : -INFINITY;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
-    if (!landed) m = __int_as_float(0x7fc00000);
-    if (lane < n_cta) cluster_ptr(S, lane)->cta_max[rank] = m;
-  }
-  csync();
-  m = S->cta_max[0];
-  for (int c = 1; c < n_cta; ++c) m = max_nan(m, S->cta_max[c]);
   if (!params_ok || !(fabsf(m) < INFINITY)) {
     if (rank == 0 && tid == 0) {
       a.tokens[row] = -1;
       if (a.status != nullptr)
-        atomicCAS(a.status, 0, !params_ok ? PCTREE_ERR_INVALID_ARG : PCTREE_ERR_NONFINITE);
+        atomicCAS(a.status, 0, !landed      ? PCTREE_ERR_TIMEOUT
+                               : !params_ok ? PCTREE_ERR_INVALID_ARG
+                                            : PCTREE_ERR_NONFINITE);
     }
     return;
   }
   if (temp == 0.0f) {                                       // the lowest index of the maximum
     int at = 0x7fffffff;
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
+    if (__any_sync(kFull, m8 == m)) {                       // in this warp's run
+      pass(kFar, [&](const float (&x)[kVec], int i0) {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (x[e] == m) at = min(at, first + v * kVec + e);
+        for (int e = 0; e < kVec; ++e)
+          if (x[e] == m) at = min(at, i0 + e);
+      });
     }
     at = __reduce_min_sync(kFull, at);
     int* best = reinterpret_cast<int*>(S->red);
@@ -356,9 +494,9 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
       for (int w = 1; w < kSmpWarps; ++w) at = min(at, best[w]);
       L->cta_first[rank] = at;
     }
-    csync();
+    csync<STREAM>();
     if (rank == 0 && tid == 0) {
-      for (int c = 0; c < n_cta; ++c) at = min(at, S->cta_first[c]);
+      for (int r = 0; r < n_cta; ++r) at = min(at, S->cta_first[r]);
       a.tokens[row] = at;
     }
     return;
@@ -366,7 +504,6 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
 
   // ---------------- the row's facts ----------------
   if (tid == 0) {
-    const double c = 128.0 * 1.4426950408889634074 / static_cast<double>(temp);
     RowFacts f;
     f.c_hi = static_cast<float>(c);
     f.c_lo = static_cast<float>(c - static_cast<double>(f.c_hi));
@@ -375,14 +512,22 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
     // so the difference is exact.
     f.base = fabsf(m) * f.c_hi > 16384.0f ? m : 0.0f;
     f.m = m - f.base;
-    f.k0 = __float_as_int(fmaf(f.m, f.c_hi, kMagic)) - 0x4b400000;
-    f.cut = static_cast<float>(static_cast<double>(f.m) - kOctaves * 128.0 / c);
-    f.fine_from = -INFINITY;
+    f.k = __float_as_int(fmaf(f.m, f.c_hi, kMagic)) - 0x4b400000;
+    f.cut = f.m - kOctaves * 128.0f / f.c_hi;
+    f.low = f.m - 60.0f * 128.0f / f.c_hi;
+    f.fine_from = f.cut;
+    f.min_z = -INFINITY;
+    if (by_m) {
+      // the smallest float z with exp((z - max) / T) >= min_p
+      const double from = static_cast<double>(m) + below;
+      float z = static_cast<float>(from);
+      if (static_cast<double>(z) < from) z = nextafterf(z, INFINITY);
+      f.min_z = fminf(z, m);
+    }
     S->row = f;
   }
   __syncthreads();
   RowFacts f = S->row;
-  const bool by_k = top_k > 0 && top_k < a.V, by_p = top_p < 1.0f;
 
   // sums the cluster's values (one per thread) for everyone
   auto cluster_total = [&](unsigned long long v) -> unsigned long long {
@@ -391,286 +536,446 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
     __syncthreads();
     if (warp == 0) {
       v = warp_sum64(lane < kSmpWarps ? S->red[lane] : 0ull);
-      if (lane < n_cta) cluster_ptr(S, lane)->part_w[rank] = v;
+      if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->part[rank] = v;
     }
-    csync();
+    csync<STREAM>();
     unsigned long long t = 0;
-    for (int c = 0; c < n_cta; ++c) t += S->part_w[c];
-    csync();                                         // part_w may be written again
+    for (int r = 0; r < n_cta; ++r) t += S->part[r];
+    csync<STREAM>();                                        // part may be written again
     return t;
   };
+  // the weight of the whole row: light weights of all, then the fine form of
+  // those above 2^-12 of the total; leaves this lane's sum in `mine`
+  unsigned long long all_w = 0, mine = 0;
+  auto sum_all = [&]() {
+    mine = 0;
+    pass(kNear, [&](const float (&x)[kVec], int) {
+#pragma unroll
+      for (int e = 0; e < kVec; e += 2) {
+        unsigned long long w0, w1;
+        light_weights(S, f, fmaxf(x[e] - f.base, f.low), fmaxf(x[e + 1] - f.base, f.low), w0, w1);
+        mine += w0 + w1;
+      }
+    });
+    const unsigned long long rough = cluster_total(mine);
+    f.fine_from =
+        fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * 128.0f / f.c_hi);
+    if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
+      pass(kFar, [&](const float (&x)[kVec], int) {
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < kVec; ++e) top = fmaxf(top, x[e]);
+        if (top - f.base >= f.fine_from) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const float z = x[e] - f.base;
+            if (z >= f.fine_from) {
+              unsigned long long w0, w1;
+              light_weights(S, f, z, z, w0, w1);
+              mine += fine_weight(f, z) - w0;
+            }
+          }
+        }
+      });
+    }
+    all_w = cluster_total(mine);
+  };
+  if (all_light) sum_all();
 
-  unsigned long long all_w = 0;                             // weight of the whole row
-  unsigned long long mine = 0;                              // of this lane's elements
-  if (!by_k) {
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float z = x[e] - f.base;
-        if (z >= f.cut) mine += light_weight(S, f, z);
+  // ---------------- few candidates: one CTA alone ----------------
+  // A logit that nothing kept is below: min_p's border; for top_k the top_k-th
+  // largest of the maxima of disjoint groups, which as many logits reach (a
+  // little over top_k of them, while there are more groups than that).
+  if (few) {
+    float from = -INFINITY;
+    if (group_lanes == 32) {
+      const int n = n_cta * kSmpWarps, i = tid >> 2;        // four threads a maximum
+      const float x = i < n ? S->warp_max[i] : -INFINITY;
+      int ahead = 0;
+      for (int j = tid & 3; j < n; j += 4) {
+        const float y = S->warp_max[j];
+        ahead += y > x || (y == x && j < i) ? 1 : 0;
       }
+      ahead += __shfl_xor_sync(kFull, ahead, 1);
+      ahead += __shfl_xor_sync(kFull, ahead, 2);
+      if (i < n && (tid & 3) == 0 && ahead == top_k - 1) S->from = x;
+      __syncthreads();
+      from = S->from;
+    } else if (group_lanes == 8) {
+      // each CTA ranks its own groups: eight threads a maximum
+      const int n = n_cta * kSmpGroups, i = rank * kSmpGroups + (tid >> 3);
+      const float x = S->group_max[i];
+      int ahead = 0;
+      for (int j = tid & 7; j < n; j += 8) {
+        const float y = S->group_max[j];
+        ahead += y > x || (y == x && j < i) ? 1 : 0;
+      }
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) ahead += __shfl_xor_sync(kFull, ahead, o);
+      if ((tid & 7) == 0 && ahead == top_k - 1)
+        for (int r = 0; r < n_cta; ++r) cluster_ptr<STREAM>(S, r)->from = x;
+      csync<STREAM>();
+      from = S->from;
+    } else if (group_lanes == 1) {
+      const float x = m1;
+      int ahead = 0;
+      for (int j = 0; j < kSmpThreads; j += 4) {
+        const float4 y = *reinterpret_cast<const float4*>(&S->group_max[j]);
+        ahead += (y.x > x || (y.x == x && j < tid) ? 1 : 0) +
+                 (y.y > x || (y.y == x && j + 1 < tid) ? 1 : 0) +
+                 (y.z > x || (y.z == x && j + 2 < tid) ? 1 : 0) +
+                 (y.w > x || (y.w == x && j + 3 < tid) ? 1 : 0);
+      }
+      if (ahead == top_k - 1) S->from = x;
+      __syncthreads();
+      from = S->from;
     }
-    const unsigned long long z0 = cluster_total(mine);
-    // fine weights from 2^-12 of the total on
-    if (tid == 0)
-      S->row.fine_from = static_cast<float>(
-          static_cast<double>(f.m) +
-          (log2(static_cast<double>(z0)) - 45.0 - 12.0) * 128.0 / static_cast<double>(f.c_hi));
+    // (top_p needs the weight of all that top_k leaves)
+    if (by_m && (group_lanes == 0 || !by_p)) from = fmaxf(from, f.min_z);
+    unsigned mine_n = 0;
+    if (__any_sync(kFull, m1 >= from)) {                    // some in this warp's run
+      pass(kFar, [&](const float (&x)[kVec], int i0) {
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < kVec; ++e) top = fmaxf(top, x[e]);
+        if (top >= from) {
+          unsigned hits = 0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            hits |= (x[e] >= from && x[e] - f.base >= f.cut ? 1u : 0u) << e;
+          const unsigned n = __popc(hits);
+          if (n != 0) {
+            mine_n += n;
+            unsigned at = atomicAdd(&L->list_n, n);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+              if ((hits >> e) & 1u) {
+                if (at < kSmpCand) L->cand.key[at] = order_key(x[e], i0 + e);
+                ++at;
+              }
+          }
+        }
+      });
+    }
+    mine_n = __reduce_add_sync(kFull, mine_n);
+    if (lane == 0 && mine_n != 0) atomicAdd(&S->local_n, mine_n);
     __syncthreads();
-    f.fine_from = S->row.fine_from;
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float z = x[e] - f.base;
-        if (z >= f.fine_from && z >= f.cut) mine += fine_weight(f, z) - light_weight(S, f, z);
+    if (tid < n_cta) cluster_ptr<STREAM>(S, tid)->cta_n[rank] = S->local_n;
+    csync<STREAM>();
+    unsigned n = 0;
+    for (int r = 0; r < n_cta; ++r) n += S->cta_n[r];
+    if (n <= kSmpCand) {
+      if (rank != 0) return;
+      // threads per candidate (a power of two), so that few are ranked fast
+      int split = 1;
+      while (split < 32 && n * split * 2 <= kSmpThreads) split *= 2;
+      const int per = kSmpThreads / split, sub = tid & (split - 1);
+      for (unsigned i = tid; i < n; i += kSmpThreads) {
+        const unsigned o = static_cast<unsigned>(S->cand.key[i] >> 32);
+        S->cand.w[i] = fine_weight(
+            f, __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o) - f.base);
       }
+      __syncthreads();
+      auto over_split = [&](unsigned long long v) {
+        for (int o = 1; o < split; o <<= 1) v += __shfl_xor_sync(kFull, v, o);
+        return v;
+      };
+      constexpr int kMine = (kSmpCand + kSmpThreads - 1) / kSmpThreads;
+      unsigned hn[kMine];                                   // count and weight of the head
+      unsigned long long hw[kMine];                         // that ends at a candidate
+#pragma unroll
+      for (int t = 0; t < kMine; ++t) {
+        const unsigned i = tid / split + t * per;
+        const unsigned long long key = i < n ? S->cand.key[i] : ~0ull;
+        unsigned long long w = 0;
+        unsigned c1 = 0;
+        if (t * per < static_cast<int>(n))
+          for (unsigned j = sub; j < n; j += split)
+            if (S->cand.key[j] >= key) {
+              ++c1;
+              w += S->cand.w[j];
+            }
+        hw[t] = over_split(w);
+        hn[t] = static_cast<unsigned>(over_split(c1));
+      }
+      if (by_k) {
+        const unsigned last = min(static_cast<unsigned>(top_k), n);
+#pragma unroll
+        for (int t = 0; t < kMine; ++t)
+          if (tid / split + t * per < n && hn[t] == last && sub == 0) S->border_w = hw[t];
+        __syncthreads();
+        all_w = S->border_w;
+      }
+      const unsigned long long want = by_p ? reach_of(top_p, all_w) : ~0ull;
+      const unsigned long long least = by_m ? order_key(f.min_z, 0x7fffffff) : 0ull;
+      unsigned long long own[kMine], sum = 0;
+#pragma unroll
+      for (int t = 0; t < kMine; ++t) {
+        const unsigned i = tid / split + t * per;
+        own[t] = i < n ? S->cand.w[i] : 0ull;
+        if (i < n && ((by_k && hn[t] > static_cast<unsigned>(top_k)) ||
+                      hw[t] - own[t] >= want || S->cand.key[i] < least))
+          own[t] = 0;
+        if (sub == 0) sum += own[t];
+      }
+      __syncthreads();                                      // the weights have been read
+#pragma unroll
+      for (int t = 0; t < kMine; ++t) {
+        const unsigned i = tid / split + t * per;
+        if (i < n && sub == 0) S->cand.w[i] = own[t];
+      }
+      sum = warp_sum64(sum);
+      if (lane == 0) S->red[warp] = sum;
+      __syncthreads();
+      unsigned long long total = 0;
+#pragma unroll
+      for (int w = 0; w < kSmpWarps; ++w) total += S->red[w];
+      const unsigned long long target = place_of(u, total);
+      // ascending index is descending lower half of the key
+#pragma unroll
+      for (int t = 0; t < kMine; ++t) {
+        const unsigned i = tid / split + t * per;
+        const unsigned place = i < n ? static_cast<unsigned>(S->cand.key[i]) : ~0u;
+        unsigned long long w = 0;
+        if (t * per < static_cast<int>(n))
+          for (unsigned j = sub; j < n; j += split)
+            if (static_cast<unsigned>(S->cand.key[j]) >= place) w += S->cand.w[j];
+        w = over_split(w);
+        if (i < n && sub == 0 && w > target && w - own[t] <= target)
+          a.tokens[row] = static_cast<int>(0xffffffffu - place);
+      }
+      return;
     }
-    if (by_p) all_w = cluster_total(mine);
+    // too many: every CTA selects among its own, below
+    csync<STREAM>();
   }
 
-  // ---------------- selection ----------------
-  unsigned long long border = 0;                            // keep keys >= border
-  float bin_scale = 0.0f;
-  auto bin_of = [&](float z) -> unsigned {
-    return __float_as_uint(fmaf(f.m - z, bin_scale, 8388608.0f)) - 0x4b000000u;
-  };
-  auto build_bins = [&](int octaves) {
-    bin_scale = f.c_hi * (static_cast<float>(kSmpBins) / (128.0f * octaves));
-    for (int i = tid; i < 4 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
+  // ---------------- selection by bins ----------------
+  if (!all_light) {                                         // binning needs the total
+    make_table();
     __syncthreads();
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
+    sum_all();
+  }
+  unsigned long long border = 0;                            // keep keys >= border
+  if (by_k || by_p) {
+    // top-p alone: as many octaves as tokens below them cannot reach half of
+    // 1 - top_p of the weight, were all of them that heavy
+    const int octaves =
+        by_k ? kOctaves
+             : max(4, min(kOctaves, 2 + static_cast<int>(ceilf(
+                                        45.0f + log2f(static_cast<float>(a.V)) -
+                                        log2f((1.0f - top_p) * static_cast<float>(all_w))))));
+    const float bin_scale = f.c_hi * (static_cast<float>(kSmpBins) / (128.0f * octaves));
+    auto bin_of = [&](float z) -> unsigned {                // monotone in z
+      return __float_as_uint(fmaf(f.m - z, bin_scale, 8388608.0f)) - 0x4b000000u;
+    };
+    // weights in 2^-31.9 of the total, in single precision: off by at most half
+    // a unit a token and 2^-18 of their sum
+    // (the exact weights are relative to 2^(k/128), not to the maximum's)
+    const float log_total = log2f(static_cast<float>(all_w)) - 45.0f;
+    const float scale2 = f.c_hi * (1.0f / 128.0f);
+    const float log_unit =
+        31.9f - log_total +
+        fmaf(f.m, f.c_lo, fmaf(f.m, f.c_hi, -static_cast<float>(f.k))) * (1.0f / 128.0f);
+    const unsigned long long unit_total = 4007346184ull;    // 2^31.9
+    const unsigned long long slack = (unit_total >> 18) + a.V / 2 + 4096;
+    for (int i = tid; i < 2 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
+    __syncthreads();
+    pass(kNear, [&](const float (&x)[kVec], int) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const float z = x[e] - f.base;
-        if (z >= f.cut) {
-          const unsigned b = bin_of(z);
-          if (b < kSmpBins) {
-            const unsigned long long w = weight(S, f, z);
-            atomicAdd(&S->hist[0][b], 1u);
-            atomicAdd(&S->hist[1][b], static_cast<unsigned>(w) & 0x7fffu);
-            atomicAdd(&S->hist[2][b], static_cast<unsigned>(w >> 15) & 0x7fffu);
-            atomicAdd(&S->hist[3][b], static_cast<unsigned>(w >> 30));
-          }
+        const unsigned b = bin_of(z);
+        if (z >= f.cut && b < kSmpBins) {
+          atomicAdd(&S->hist[1][b],
+                    __float2uint_rn(ex2_approx((z - f.m) * scale2 + log_unit)));
+          if (by_k) atomicAdd(&S->hist[0][b], 1u);
         }
       }
-    }
-    csync();
+    });
+    csync<STREAM>();
     // each CTA adds up a share of the bins, for the leader
-    const int share = kSmpBins / kSmpMaxCluster;
-    for (int s = rank; s < kSmpMaxCluster; s += n_cta) {
-      for (int i = tid; i < share; i += kSmpThreads) {
-        const int b = s * share + i;
-        unsigned n = 0;
-        unsigned long long w = 0;
-        for (int c = 0; c < n_cta; ++c) {
-          const SampleShared* R = cluster_ptr(S, c);
-          n += R->hist[0][b];
-          w += R->hist[1][b] + (static_cast<unsigned long long>(R->hist[2][b]) << 15) +
-               (static_cast<unsigned long long>(R->hist[3][b]) << 30);
-        }
-        L->bin_n[b] = n;
-        L->bin_w[b] = w;
+    constexpr int share = kSmpBins / kSmpMaxCluster;
+    for (int i = rank * share + tid; i < kSmpBins; i += kSmpThreads) {
+      // (a CTA takes every n_cta-th share)
+      const int s = i / share;
+      if (s % n_cta != rank && !STREAM) continue;
+      unsigned n = 0, w = 0;
+      for (int r = 0; r < n_cta; ++r) {
+        const SampleShared* R = cluster_ptr<STREAM>(S, r);
+        n += R->hist[0][i];
+        w += R->hist[1][i];
       }
+      L->bin_n[i] = n;
+      L->bin_w[i] = w;
     }
-    csync();
-  };
-  // the bin in which the bins' sum reaches `target` (counts or weights)
-  auto find_bin = [&](unsigned long long target, bool weights) {
-    if (rank == 0 && warp == 0) {
-      constexpr int kPer = kSmpBins / 32;
-      unsigned long long n = 0, w = 0;
-      for (int i = 0; i < kPer; ++i) {
-        n += S->bin_n[lane * kPer + i];
-        w += S->bin_w[lane * kPer + i];
-      }
-      unsigned long long n_in = n, w_in = w;                // inclusive over lanes
+    csync<STREAM>();
+    // the bins in which the head of `target` (a count, or a weight in units)
+    // can end, give or take `loose`
+    auto find_bins = [&](unsigned long long target, bool by_weight, unsigned long long loose) {
+      if (rank == 0 && warp == 0) {
+        const unsigned* bins = by_weight ? S->bin_w : S->bin_n;
+        unsigned long long base = 0;
+        int b0 = -1, b1 = -1;
+        for (int b = 0; b < kSmpBins; b += 32) {
+          unsigned long long in = bins[b + lane];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long pn = __shfl_up_sync(kFull, n_in, o);
-        const unsigned long long pw = __shfl_up_sync(kFull, w_in, o);
-        if (lane >= o) {
-          n_in += pn;
-          w_in += pw;
-        }
-      }
-      const unsigned reach = __ballot_sync(kFull, (weights ? w_in : n_in) >= target);
-      const unsigned long long total = __shfl_sync(kFull, w_in, 31);
-      if (reach == 0) {
-        if (lane == 0)
-          for (int c = 0; c < n_cta; ++c) {
-            cluster_ptr(S, c)->bin = -1;
-            cluster_ptr(S, c)->total_w = total;
+          for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long p = __shfl_up_sync(kFull, in, o);
+            if (lane >= o) in += p;
           }
-      } else if (lane == __ffs(reach) - 1) {
-        unsigned long long an = n_in - n, aw = w_in - w;
-        int b = lane * kPer;
-        while (b < lane * kPer + kPer - 1 &&
-               (weights ? aw + S->bin_w[b] : an + S->bin_n[b]) < target) {
-          an += S->bin_n[b];
-          aw += S->bin_w[b];
-          ++b;
+          in += base;
+          const unsigned lo = __ballot_sync(kFull, in + loose >= target);
+          const unsigned hi = __ballot_sync(kFull, in >= target + loose);
+          if (b0 < 0 && lo != 0) b0 = b + __ffs(lo) - 1;
+          if (b1 < 0 && hi != 0) b1 = b + __ffs(hi) - 1;
+          base = __shfl_sync(kFull, in, 31);
         }
-        for (int c = 0; c < n_cta; ++c) {
-          SampleShared* R = cluster_ptr(S, c);
-          R->bin = b;
-          R->above_n = an;
-          R->above_w = aw;
-          R->total_w = total;
+        if (by_weight && b1 < 0) b1 = kSmpBins - 1;
+        if (lane < n_cta) {
+          SampleShared* R = cluster_ptr<STREAM>(S, lane);
+          R->bin0 = b0;
+          R->bin1 = b1;
           R->list_n = 0;
+          R->found = 0;
         }
       }
-    }
-    csync();
-  };
-  // K* of `target` and the weight of its head, once find_bin has found its bin
-  auto resolve = [&](unsigned long long target, bool weights) {
-    const unsigned bin = static_cast<unsigned>(S->bin);
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
+      csync<STREAM>();
+    };
+    // K* of `target` (a count, or an exact weight) and the weight of its head,
+    // once its bins are known
+    auto resolve = [&](unsigned long long target, bool by_weight) {
+      const unsigned b0 = static_cast<unsigned>(S->bin0), b1 = static_cast<unsigned>(S->bin1);
+      unsigned long long above_w = 0;
+      unsigned above = 0;
+      pass(kNext, [&](const float (&x)[kVec], int i0) {
+        unsigned up = 0, in = 0;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float z = x[e] - f.base;
-        if (z >= f.cut && bin_of(z) == bin) {
-          const unsigned at = atomicAdd(&L->list_n, 1u);
-          if (at < kSmpList) {
-            L->list.key[at] = order_key(x[e], first + v * kVec + e);
-            L->list.w[at] = weight(S, f, z);
+        for (int e = 0; e < kVec; ++e) {
+          const float z = x[e] - f.base;
+          const unsigned b = bin_of(z);
+          const bool live = z >= f.cut;
+          up |= (live && b < b0 ? 1u : 0u) << e;
+          in |= (live && b >= b0 && b <= b1 ? 1u : 0u) << e;
+        }
+        if (!__any_sync(kFull, (up | in) != 0)) return;
+        unsigned long long w[kVec];
+        weights(S, f, x, w);
+        above += __popc(up);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          above_w += (up >> e) & 1u ? w[e] : 0ull;
+          if ((in >> e) & 1u) {
+            const unsigned at = atomicAdd(&L->list_n, 1u);
+            if (at < kSmpList) {
+              L->list.key[at] = order_key(x[e], i0 + e);
+              L->list.w[at] = w[e];
+            }
           }
         }
-      }
-    }
-    csync();
-    const unsigned n = L->list_n;
-    csync();
-    if (n <= kSmpList) {
-      if (rank == 0 && tid < n) {
+      });
+      above_w = cluster_total(above_w);
+      const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
+      const unsigned n = L->list_n;
+      csync<STREAM>();
+      if (rank == 0 && n <= kSmpList && tid < n) {
         const unsigned long long key = S->list.key[tid], own = S->list.w[tid];
-        unsigned long long hn = S->above_n, hw = S->above_w;   // up to and with this key
+        unsigned long long hn = above_n, hw = above_w;      // up to and with this key
         for (unsigned i = 0; i < n; ++i)
           if (S->list.key[i] >= key) {
             ++hn;
             hw += S->list.w[i];
           }
-        const bool here = weights ? hw >= target && hw - own < target : hn == target;
-        if (here)
-          for (int c = 0; c < n_cta; ++c) {
-            cluster_ptr(S, c)->border = key;
-            cluster_ptr(S, c)->border_w = hw;
-          }
-      }
-      csync();
-      return;
-    }
-    // too many keys in the bin: K* bit by bit, the largest key whose head
-    // reaches the target
-    unsigned long long key = 0, key_w = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const unsigned long long trial = key | (1ull << bit);
-      unsigned long long hn = 0, hw = 0;
-      for (int v = v0 + lane; v < v1; v += 32) {
-        float x[kVec];
-        E::unpack(vec[v], x);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float z = x[e] - f.base;
-          if (z >= f.cut && order_key(x[e], first + v * kVec + e) >= trial) {
-            ++hn;
-            hw += weight(S, f, z);
+        if (by_weight ? hw >= target && hw - own < target : hn == target) {
+          for (int r = 0; r < n_cta; ++r) {
+            SampleShared* R = cluster_ptr<STREAM>(S, r);
+            R->border = key;
+            R->border_w = hw;
+            R->found = 1;
           }
         }
       }
-      hw = cluster_total(hw);
-      if (!weights) hn = cluster_total(hn);
-      if ((weights ? hw : hn) >= target) {
-        key = trial;
-        key_w = hw;
+      csync<STREAM>();
+      if (S->found != 0) return;
+      // too many keys in the bins: K* bit by bit, the largest key whose head
+      // reaches the target
+      unsigned long long key = 0, key_w = 0;
+      for (int bit = 63; bit >= 0; --bit) {
+        const unsigned long long trial = key | (1ull << bit);
+        unsigned long long hw = 0;
+        unsigned hn = 0;
+        pass(kNext, [&](const float (&x)[kVec], int i0) {
+          unsigned up = 0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            up |= (x[e] - f.base >= f.cut && order_key(x[e], i0 + e) >= trial ? 1u : 0u) << e;
+          if (!__any_sync(kFull, up != 0)) return;
+          unsigned long long w[kVec];
+          weights(S, f, x, w);
+          hn += __popc(up);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) hw += (up >> e) & 1u ? w[e] : 0ull;
+        });
+        hw = cluster_total(hw);
+        const unsigned long long reached = by_weight ? hw : cluster_total(hn);
+        if (reached >= target) {
+          key = trial;
+          key_w = hw;
+        }
       }
-    }
-    if (tid == 0) {
-      S->border = key;
-      S->border_w = key_w;
-    }
-    __syncthreads();
-  };
-
-  if (by_k || by_p) {
-    build_bins(kNarrow);
-    bool wide = false;
+      if (tid == 0) {
+        S->border = key;
+        S->border_w = key_w;
+      }
+      __syncthreads();
+    };
     if (by_k) {
-      find_bin(static_cast<unsigned long long>(top_k), false);
-      if (S->bin < 0) {
-        wide = true;
-        build_bins(kOctaves);
-        find_bin(static_cast<unsigned long long>(top_k), false);
-      }
-      if (S->bin >= 0) {
+      find_bins(static_cast<unsigned long long>(top_k), false, 0);
+      if (S->bin1 >= 0) {                                   // else fewer have a weight
         resolve(static_cast<unsigned long long>(top_k), false);
         border = S->border;
         all_w = S->border_w;
-      } else {
-        all_w = S->total_w;                                 // all that have a weight
       }
+      csync<STREAM>();                                      // the results are read
     }
     if (by_p) {
-      double want = ceil(static_cast<double>(top_p) * static_cast<double>(all_w));
-      unsigned long long target = static_cast<unsigned long long>(want);
-      if (target < 1) target = 1;
-      if (target > all_w) target = all_w;
-      csync();                                       // the results above are read
-      find_bin(target, true);
-      if (S->bin < 0 && !wide) {
-        build_bins(kOctaves);
-        find_bin(target, true);
-      }
-      if (S->bin >= 0) {
-        resolve(target, true);
-        const unsigned long long b = S->border;
-        border = b > border ? b : border;
-      }
+      const unsigned long long target = reach_of(top_p, all_w);
+      // in the bins' units
+      const float scaled = static_cast<float>(target) * exp2f(31.9f - log_total - 45.0f);
+      find_bins(static_cast<unsigned long long>(scaled), true, slack);
+      resolve(target, true);
+      const unsigned long long b = S->border;
+      border = b > border ? b : border;
     }
   }
-  if (min_p > 0.0f) {
-    // the smallest float z with exp((z - max) / T) >= min_p
-    if (tid == 0) {
-      const double from = static_cast<double>(m) +
-                          static_cast<double>(temp) * log(static_cast<double>(min_p));
-      float z = static_cast<float>(from);
-      if (static_cast<double>(z) < from) z = nextafterf(z, INFINITY);
-      S->red[0] = order_key(fminf(z, m), 0x7fffffff);
-    }
-    __syncthreads();
-    const unsigned long long b = S->red[0];
-    border = b > border ? b : border;
-    __syncthreads();
+  if (by_m) {
+    const unsigned long long least = order_key(f.min_z, 0x7fffffff);
+    border = least > border ? least : border;
   }
 
   // ---------------- draw ----------------
-  const bool filtered = border != 0;
   const unsigned ob = static_cast<unsigned>(border >> 32);
-  const float border_z = __uint_as_float((ob & 0x80000000u) ? ob & 0x7fffffffu : ~ob);
+  const float border_z = border == 0 ? -INFINITY
+                                     : __uint_as_float((ob & 0x80000000u) ? ob & 0x7fffffffu : ~ob);
   auto kept = [&](float z, int index) {
     return z > border_z || (z == border_z && order_key(z, index) >= border);
   };
-  if (filtered || by_k) {
+  if (border != 0) {
     mine = 0;
-    for (int v = v0 + lane; v < v1; v += 32) {
-      float x[kVec];
-      E::unpack(vec[v], x);
+    pass(kNext, [&](const float (&x)[kVec], int i0) {
+      unsigned keep = 0;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (!filtered || kept(x[e], first + v * kVec + e)) mine += weight(S, f, x[e] - f.base);
-    }
+      for (int e = 0; e < kVec; ++e) keep |= (kept(x[e], i0 + e) ? 1u : 0u) << e;
+      if (!__any_sync(kFull, keep != 0)) return;
+      unsigned long long w[kVec];
+      weights(S, f, x, w);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) mine += (keep >> e) & 1u ? w[e] : 0ull;
+    });
   }
   mine = warp_sum64(mine);
-  if (lane < n_cta) cluster_ptr(S, lane)->warp_sum[rank * kSmpWarps + warp] = mine;
-  csync();
+  if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->warp_sum[rank * kSmpWarps + warp] = mine;
+  csync<STREAM>();
   // the warp in whose run the cumulative weight passes u * total
   constexpr int kPer = kSmpMaxCluster * kSmpWarps / 32;     // runs a lane adds up
   unsigned long long lane_in = 0, upto[kPer];
@@ -693,20 +998,19 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
   for (int i = 0; i < kPer; ++i)
     if (i == self % kPer) before = scan - lane_in + upto[i];
   before = __shfl_sync(kFull, before, self / kPer) - mine;
-  const unsigned long long target =
-      static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(total));
+  const unsigned long long target = place_of(u, total);
   if (before > target || before + mine <= target) return;
   unsigned long long cum = before;
   for (int vb = v0; vb < v1; vb += 32) {
     const int v = vb + lane;
     float x[kVec];
+    E::unpack(v < v1 ? vec[v] : E::low_vec(), x);
+    const int i0 = first + v * kVec;
     unsigned long long w[kVec], sum = 0;
-    if (v < v1) E::unpack(vec[v], x);
+    weights(S, f, x, w);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-      w[e] = 0;
-      if (v < v1 && (!filtered || kept(x[e], first + v * kVec + e)))
-        w[e] = weight(S, f, x[e] - f.base);
+      if (!kept(x[e], i0 + e)) w[e] = 0;
       sum += w[e];
     }
     unsigned long long in = sum;
@@ -715,15 +1019,15 @@ __global__ void __launch_bounds__(kSmpThreads) sample_kernel(SampleArgs a) {
       const unsigned long long p = __shfl_up_sync(kFull, in, o);
       if (lane >= o) in += p;
     }
-    const unsigned pass = __ballot_sync(kFull, cum + in > target);
-    if (pass != 0) {
-      if (lane == __ffs(pass) - 1) {
-        unsigned long long c = cum + in - sum;
+    const unsigned past = __ballot_sync(kFull, cum + in > target);
+    if (past != 0) {
+      if (lane == __ffs(past) - 1) {
+        unsigned long long at = cum + in - sum;
         int token = -1;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          c += w[e];
-          if (token < 0 && c > target) token = first + v * kVec + e;
+          at += w[e];
+          if (token < 0 && at > target) token = i0 + e;
         }
         a.tokens[row] = token;
       }
@@ -742,6 +1046,14 @@ pctree_status sample_check(const pctree_sample_config* c) {
   if (c->V > kSmpMaxV || c->rows > (1 << 27) || c->row_stride > (1ll << 40))
     return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
+}
+
+// Resident rows of the streamed placement: what a second pass finds in L2.
+constexpr size_t kStreamBytes = 104u << 20;
+
+template <int DT, bool STREAM>
+const void* sample_fn() {
+  return reinterpret_cast<const void*>(sample_kernel<DT, STREAM>);
 }
 
 }  // namespace
@@ -766,16 +1078,28 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   int num_sms = 0;
   st = device_facts(&num_sms);
   if (st != PCTREE_OK) return st;
-  // CTAs per row: slices of at most 80 KB (two CTAs an SM), and of at least
-  // 8 KB
-  int ctas = 1;
-  while (ctas < kSmpMaxCluster &&
-         static_cast<long long>(c.V) * el > ctas * 8192ll)
-    ctas *= 2;
   const int vec = 16 / el;
+  const size_t row_bytes = static_cast<size_t>(c.V) * el;
+  // streamed: whole 16-byte vectors, a row for every CTA place of the GPU, and
+  // (two CTAs an SM, or one) the rows in flight in L2
+  const bool aligned = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && c.V % vec == 0 &&
+                       (c.row_stride * el) % 16 == 0;
+  const int per_sm = row_bytes * 2 * num_sms <= kStreamBytes ? 2 : 1;
+  const bool streamed = aligned && row_bytes * num_sms <= kStreamBytes &&
+                        c.rows >= num_sms * per_sm;
+  // cluster: slices of at least 8 KB, up to eight of them
+  int ctas = 1;
   SampleArgs a{};
-  a.slice = ((c.V + ctas - 1) / ctas + vec - 1) / vec * vec;
-  ctas = (c.V + a.slice - 1) / a.slice;
+  size_t bytes = sizeof(SampleShared);
+  if (streamed) {
+    a.slice = c.V;
+    if (per_sm == 1) bytes = 120 * 1024;                    // keeps a second CTA off the SM
+  } else {
+    while (ctas < kSmpMaxCluster && row_bytes > ctas * 8192ull) ctas *= 2;
+    a.slice = ((c.V + ctas - 1) / ctas + vec - 1) / vec * vec;
+    ctas = (c.V + a.slice - 1) / a.slice;
+    bytes += static_cast<size_t>(a.slice + 2 * vec) * el;
+  }
   a.logits = logits;
   a.uniform = uniform;
   a.temperature = temperature;
@@ -788,14 +1112,15 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   a.row_stride = c.row_stride;
   a.V = c.V;
   a.group = c.group;
-  const size_t bytes = sizeof(SampleShared) + static_cast<size_t>(a.slice + 2 * vec) * el;
-  const void* fn = c.dtype == PCTREE_F32    ? reinterpret_cast<const void*>(sample_kernel<PCTREE_F32>)
-                   : c.dtype == PCTREE_BF16 ? reinterpret_cast<const void*>(sample_kernel<PCTREE_BF16>)
-                                            : reinterpret_cast<const void*>(sample_kernel<PCTREE_F16>);
+  const void* fn =
+      c.dtype == PCTREE_F32 ? (streamed ? sample_fn<PCTREE_F32, true>() : sample_fn<PCTREE_F32, false>())
+      : c.dtype == PCTREE_BF16
+          ? (streamed ? sample_fn<PCTREE_BF16, true>() : sample_fn<PCTREE_BF16, false>())
+          : (streamed ? sample_fn<PCTREE_F16, true>() : sample_fn<PCTREE_F16, false>());
   constexpr size_t kMost = sizeof(SampleShared) + (kSmpMaxV / kSmpMaxCluster + 8) * 4;
-  static_assert(kMost <= 227 * 1024, "shared memory per CTA");
-  static SmemLimit limits[3];
-  if (limits[c.dtype].ensure(fn, kMost) != cudaSuccess) return PCTREE_ERR_CUDA;
+  static_assert(kMost <= 227 * 1024 && kMost >= 120 * 1024, "shared memory per CTA");
+  static SmemLimit limits[2][3];
+  if (limits[streamed][c.dtype].ensure(fn, kMost) != cudaSuccess) return PCTREE_ERR_CUDA;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -809,7 +1134,7 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   lc.dynamicSmemBytes = bytes;
   lc.stream = static_cast<cudaStream_t>(stream);
   lc.attrs = attr;
-  lc.numAttrs = 2;
+  lc.numAttrs = streamed ? 1 : 2;
   void* params[] = {&a};
   return cudaLaunchKernelExC(&lc, fn, params) == cudaSuccess ? PCTREE_OK : PCTREE_ERR_CUDA;
 }

@@ -461,29 +461,57 @@ _DTYPES = {torch.float32: PCTREE_F32, torch.bfloat16: PCTREE_BF16,
 _TORCH_TYPE = {code: dt for dt, code in _DTYPES.items()}
 
 
-def _check_tensors(where: str, device: int, specs) -> None:
-    """Each (name, tensor, dtype, elements) of `specs`: a contiguous tensor of
-    that type with at least that many elements on `device`, or None."""
-    for name, t, dt, n in specs:
-        if t is None:
-            continue
-        if (t.dtype is not dt or t.numel() < n or not t.is_contiguous()
-                or t.get_device() != device):
-            raise ValueError(
-                f"{where}: {name} must be a contiguous {dt} tensor of at least {n} "
-                f"elements on the current device cuda:{device}")
+# The checks of the calls below run in front of kernels of a few microseconds:
+# each is written so that a good call takes the fewest steps in Python, and
+# what is wrong with a bad one is worked out afterwards.
+
+_RAW_DEVICE = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _check_rows(where: str, device: int, name: str, t: torch.Tensor, dt, rows: int,
-                heads: int, D: int, stride: int) -> None:
-    """[rows][heads][D] with dense heads and `stride` elements from row to row."""
-    if (t.dtype is not dt or t.get_device() != device or t.dim() != 3
-            or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != D
-            or (rows > 1 and t.stride(0) != stride)
-            or (heads > 1 and t.stride(1) != D) or t.stride(2) != 1):
-        raise ValueError(
-            f"{where}: {name} must be a {dt} tensor [{rows}][{heads}][{D}] on the current "
-            f"device cuda:{device}, {stride} elements from row to row")
+def _device_index() -> int:
+    if _RAW_DEVICE is not None and torch.cuda.is_initialized():
+        return _RAW_DEVICE()
+    return torch.cuda.current_device()
+
+
+def _device_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    if stream is None and _RAW_STREAM is not None:
+        return _RAW_STREAM(device)
+    return _stream_ptr(stream)
+
+
+def _flat(t: Optional[torch.Tensor], dt, n: int, device: int) -> bool:
+    """None, or a contiguous tensor of type dt and at least n elements there."""
+    return t is None or (t.dtype is dt and t.numel() >= n and t.get_device() == device
+                         and t.is_contiguous())
+
+
+def _rows(t: torch.Tensor, dt, rows: int, heads: int, D: int, stride: int,
+          device: int) -> bool:
+    """[rows][heads][D] there, heads dense and rows `stride` elements apart."""
+    if t.dtype is not dt or t.get_device() != device or t.dim() != 3:
+        return False
+    n, h, d = t.shape
+    a, b, c = t.stride()
+    return (n >= rows and h == heads and d == D and c == 1 and (b == D or heads == 1)
+            and (a == stride or rows == 1))
+
+
+def _refuse(where: str, device: int, checks) -> None:
+    """Names the first of the (name, good, wanted) that is not good."""
+    for name, good, wanted in checks:
+        if not good:
+            raise ValueError(f"{where}: {name} must be {wanted}, on the current device "
+                             f"cuda:{device}")
+
+
+def _flat_check(name, t, dt, n, device):
+    return name, _flat(t, dt, n, device), f"a contiguous {dt} tensor of at least {n} elements"
+
+
+def _rows_check(name, t, dt, rows, heads, D, stride, device):
+    return (name, _rows(t, dt, rows, heads, D, stride, device),
+            f"a {dt} tensor [{rows}][{heads}][{D}], {stride} elements from row to row")
 
 
 def append_config(batch: int, total_rows: int, Hq: int, Hkv: int, D: int,
@@ -518,28 +546,44 @@ def pctree_kv_append(cfg: AppendConfig, q: Optional[torch.Tensor], k: torch.Tens
     append of their keys and values to the cache (see pctree_kv_append in
     include/pctree.h).  q, k and v are [total_rows][heads][D], row strides as
     in ``cfg`` (slices of one projection's output need no copy)."""
-    dev = torch.cuda.current_device()
+    dev = _device_index()
     dt = _TORCH_TYPE.get(cfg.dtype)
-    n, D, i32 = cfg.total_rows, cfg.D, torch.int32
-    if cfg.Hq > 0:
-        _check_rows("pctree_kv_append", dev, "q", q, dt, n, cfg.Hq, D, cfg.q_stride)
-    _check_rows("pctree_kv_append", dev, "k", k, dt, n, cfg.Hkv, D, cfg.k_stride)
-    _check_rows("pctree_kv_append", dev, "v", v, dt, n, cfg.Hkv, D, cfg.v_stride)
-    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * D
-    _check_tensors("pctree_kv_append", dev, (
-        ("k_cache", k_cache, dt, slots), ("v_cache", v_cache, dt, slots),
-        ("q_out", q_out, dt, n * cfg.Hq * D), ("row_start", row_start, i32, cfg.batch),
-        ("n_rows", n_rows, i32, cfg.batch), ("prefix_len", prefix_len, i32, cfg.batch),
-        ("page_table", page_table, i32, cfg.batch * cfg.max_pages),
-        ("positions", positions, i32, n),
-        ("inv_freq", inv_freq, torch.float64, cfg.rotary_dim // 2),
-        ("q_weight", q_weight, dt, D), ("k_weight", k_weight, dt, D),
-        ("status", status, i32, 1)))
+    n, D, Hq, Hkv, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.Hkv, cfg.batch, torch.int32
+    slots = cfg.n_pages * cfg.page_size * Hkv * D
+    if not ((Hq == 0 or (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
+                         and _flat(q_out, dt, n * Hq * D, dev)))
+            and _rows(k, dt, n, Hkv, D, cfg.k_stride, dev)
+            and _rows(v, dt, n, Hkv, D, cfg.v_stride, dev)
+            and _flat(k_cache, dt, slots, dev) and _flat(v_cache, dt, slots, dev)
+            and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
+            and _flat(prefix_len, i32, batch, dev)
+            and _flat(page_table, i32, batch * cfg.max_pages, dev)
+            and _flat(positions, i32, n, dev)
+            and _flat(inv_freq, torch.float64, cfg.rotary_dim // 2, dev)
+            and _flat(q_weight, dt, D, dev) and _flat(k_weight, dt, D, dev)
+            and _flat(status, i32, 1, dev)):
+        _refuse("pctree_kv_append", dev, [
+            *([_rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
+               _flat_check("q_out", q_out, dt, n * Hq * D, dev)] if Hq else []),
+            _rows_check("k", k, dt, n, Hkv, D, cfg.k_stride, dev),
+            _rows_check("v", v, dt, n, Hkv, D, cfg.v_stride, dev),
+            _flat_check("k_cache", k_cache, dt, slots, dev),
+            _flat_check("v_cache", v_cache, dt, slots, dev),
+            _flat_check("row_start", row_start, i32, batch, dev),
+            _flat_check("n_rows", n_rows, i32, batch, dev),
+            _flat_check("prefix_len", prefix_len, i32, batch, dev),
+            _flat_check("page_table", page_table, i32, batch * cfg.max_pages, dev),
+            _flat_check("positions", positions, i32, n, dev),
+            _flat_check("inv_freq", inv_freq, torch.float64, cfg.rotary_dim // 2, dev),
+            _flat_check("q_weight", q_weight, dt, D, dev),
+            _flat_check("k_weight", k_weight, dt, D, dev),
+            _flat_check("status", status, i32, 1, dev)])
     rc = LIB.pctree_kv_append(
         ctypes.byref(cfg), _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight),
         _ptr(k_weight), _ptr(inv_freq), _ptr(positions), row_start.data_ptr(),
         n_rows.data_ptr(), prefix_len.data_ptr(), _ptr(page_table), k_cache.data_ptr(),
-        v_cache.data_ptr(), _ptr(q_out), _ptr(status), _stream_ptr(stream))
+        v_cache.data_ptr(), _ptr(q_out), _ptr(status),
+        _device_stream(stream, dev))
     if rc != PCTREE_OK:
         raise PctreeError(rc, "pctree_kv_append")
 
@@ -569,22 +613,32 @@ def pctree_paged_attention(cfg: PagedAttnConfig, q: torch.Tensor, k_cache: torch
                            stream: Optional[torch.cuda.Stream] = None) -> None:
     """Enqueue causal attention of new rows over the cache (see
     pctree_paged_attention in include/pctree.h)."""
-    dev = torch.cuda.current_device()
+    dev = _device_index()
     dt = _TORCH_TYPE.get(cfg.dtype)
-    n, i32 = cfg.total_rows, torch.int32
-    _check_rows("pctree_paged_attention", dev, "q", q, dt, n, cfg.Hq, cfg.D, cfg.q_stride)
-    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * cfg.D
-    _check_tensors("pctree_paged_attention", dev, (
-        ("k_cache", k_cache, dt, slots), ("v_cache", v_cache, dt, slots),
-        ("out", out, dt, n * cfg.Hq * cfg.D), ("row_start", row_start, i32, cfg.batch),
-        ("n_rows", n_rows, i32, cfg.batch), ("prefix_len", prefix_len, i32, cfg.batch),
-        ("page_table", page_table, i32, cfg.batch * cfg.max_pages),
-        ("workspace", workspace, torch.uint8, 0), ("status", status, i32, 1)))
+    n, D, Hq, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.batch, torch.int32
+    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * D
+    if not (_rows(q, dt, n, Hq, D, cfg.q_stride, dev) and _flat(out, dt, n * Hq * D, dev)
+            and _flat(k_cache, dt, slots, dev) and _flat(v_cache, dt, slots, dev)
+            and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
+            and _flat(prefix_len, i32, batch, dev)
+            and _flat(page_table, i32, batch * cfg.max_pages, dev)
+            and _flat(workspace, torch.uint8, 0, dev) and _flat(status, i32, 1, dev)):
+        _refuse("pctree_paged_attention", dev, [
+            _rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
+            _flat_check("out", out, dt, n * Hq * D, dev),
+            _flat_check("k_cache", k_cache, dt, slots, dev),
+            _flat_check("v_cache", v_cache, dt, slots, dev),
+            _flat_check("row_start", row_start, i32, batch, dev),
+            _flat_check("n_rows", n_rows, i32, batch, dev),
+            _flat_check("prefix_len", prefix_len, i32, batch, dev),
+            _flat_check("page_table", page_table, i32, batch * cfg.max_pages, dev),
+            _flat_check("workspace", workspace, torch.uint8, 0, dev),
+            _flat_check("status", status, i32, 1, dev)])
     rc = LIB.pctree_paged_attention(
         ctypes.byref(cfg), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
         row_start.data_ptr(), n_rows.data_ptr(), prefix_len.data_ptr(), _ptr(page_table),
         out.data_ptr(), workspace.data_ptr(), workspace.numel(), _ptr(status),
-        _stream_ptr(stream))
+        _device_stream(stream, dev))
     if rc != PCTREE_OK:
         raise PctreeError(rc, "pctree_paged_attention")
 
@@ -593,6 +647,16 @@ def sample_config(rows: int, V: int, group: int = 1, dtype: torch.dtype = torch.
                   row_stride: Optional[int] = None) -> SampleConfig:
     """``row_stride`` (elements) defaults to dense rows."""
     return SampleConfig(rows, V, group, _DTYPES[dtype], V if row_stride is None else row_stride)
+
+
+def _logit_rows(t: torch.Tensor, dt, rows: int, V: int, stride: int, device: int) -> bool:
+    """[rows][V] there, rows `stride` apart, or a dense tensor of that many
+    rows of V."""
+    if t.dtype is not dt or t.get_device() != device or t.dim() < 1 or t.shape[-1] != V:
+        return False
+    if t.dim() == 2 and t.shape[0] >= rows:
+        return (V == 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) == stride)
+    return t.is_contiguous() and t.numel() >= rows * V and (rows <= 1 or stride == V)
 
 
 def pctree_sample(cfg: SampleConfig, logits: torch.Tensor, uniform: torch.Tensor,
@@ -605,25 +669,30 @@ def pctree_sample(cfg: SampleConfig, logits: torch.Tensor, uniform: torch.Tensor
     pctree_sample in include/pctree.h).  logits is [rows][V], or any leading
     shape that has `rows` rows row_stride apart; tokens may be the [batch][N]
     target tokens that pctree_accept takes."""
-    dev = torch.cuda.current_device()
+    dev = _device_index()
     dt = _TORCH_TYPE.get(cfg.dtype)
-    groups = -(-cfg.rows // cfg.group) if cfg.group > 0 else 0
-    f32, i32 = torch.float32, torch.int32
-    if (logits.dtype is not dt or logits.get_device() != dev or logits.dim() < 1
-            or logits.shape[-1] != cfg.V or logits.stride(-1) != 1
-            or logits.numel() < cfg.rows * cfg.V
-            or (logits.dim() > 1 and cfg.rows > 1 and logits.stride(-2) != cfg.row_stride)
-            or (logits.dim() != 2 and not logits.is_contiguous())):
-        raise ValueError(f"pctree_sample: logits must be a {dt} tensor [{cfg.rows}][{cfg.V}] on "
-                         f"the current device cuda:{dev}, {cfg.row_stride} elements from row to row")
-    _check_tensors("pctree_sample", dev, (
-        ("uniform", uniform, f32, cfg.rows), ("tokens", tokens, i32, cfg.rows),
-        ("temperature", temperature, f32, groups), ("top_k", top_k, i32, groups),
-        ("top_p", top_p, f32, groups), ("min_p", min_p, f32, groups),
-        ("n_rows", n_rows, i32, groups), ("status", status, i32, 1)))
+    rows, V, group, f32, i32 = cfg.rows, cfg.V, cfg.group, torch.float32, torch.int32
+    groups = rows if group == 1 else -(-rows // group) if group > 0 else 0
+    if not (_logit_rows(logits, dt, rows, V, cfg.row_stride, dev)
+            and _flat(uniform, f32, rows, dev) and _flat(tokens, i32, rows, dev)
+            and _flat(temperature, f32, groups, dev) and _flat(top_k, i32, groups, dev)
+            and _flat(top_p, f32, groups, dev) and _flat(min_p, f32, groups, dev)
+            and _flat(n_rows, i32, groups, dev) and _flat(status, i32, 1, dev)):
+        _refuse("pctree_sample", dev, [
+            ("logits", _logit_rows(logits, dt, rows, V, cfg.row_stride, dev),
+             f"a {dt} tensor [{rows}][{V}], {cfg.row_stride} elements from row to row"),
+            _flat_check("uniform", uniform, f32, rows, dev),
+            _flat_check("tokens", tokens, i32, rows, dev),
+            _flat_check("temperature", temperature, f32, groups, dev),
+            _flat_check("top_k", top_k, i32, groups, dev),
+            _flat_check("top_p", top_p, f32, groups, dev),
+            _flat_check("min_p", min_p, f32, groups, dev),
+            _flat_check("n_rows", n_rows, i32, groups, dev),
+            _flat_check("status", status, i32, 1, dev)])
     rc = LIB.pctree_sample(ctypes.byref(cfg), logits.data_ptr(), uniform.data_ptr(),
                            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-                           _ptr(n_rows), tokens.data_ptr(), _ptr(status), _stream_ptr(stream))
+                           _ptr(n_rows), tokens.data_ptr(), _ptr(status),
+                           _device_stream(stream, dev))
     if rc != PCTREE_OK:
         raise PctreeError(rc, "pctree_sample")
 

@@ -240,3 +240,93 @@ def test_stream_and_graph(P):
     g.replay()
     torch.cuda.synchronize()
     np.testing.assert_array_equal(tokens.cpu().numpy(), ref)
+
+
+def mixed_params(repeat=1):
+    """One parameter set per group: every filter above."""
+    sets = [FILTERS[n] for n in sorted(FILTERS)] * repeat
+    return dict(temperature=[s.get("temperature", 1.0) for s in sets],
+                top_k=[s.get("top_k", 0) for s in sets],
+                top_p=[s.get("top_p", 1.0) for s in sets],
+                min_p=[s.get("min_p", 0.0) for s in sets])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["drawn", "few_values", "masked", "one_value"])
+def test_many_aligned_rows(P, dtype, kind):
+    """As many rows as the GPU has places for CTAs (each row on one CTA): every
+    filter, on drawn logits, on long runs of equal ones and on masked ones."""
+    group, V = 24, 6000
+    z, u = draw(16 * group, V, "f32", seed=31)
+    if kind == "few_values":
+        z = (z * 2).round() * 0.5
+    elif kind == "masked":
+        g = torch.Generator(device="cuda")
+        g.manual_seed(7)
+        z.masked_fill_(torch.rand(z.shape, generator=g, device="cuda") < 0.99, float("-inf"))
+        z[::3] = z[::3].nan_to_num(neginf=-6e4)
+        z[:, 11] = -1.0
+    elif kind == "one_value":
+        z.fill_(-2.5)
+    z = z.to(DTYPES[dtype])
+    par = mixed_params()
+    got, st = run(P, z, u, group=group, **par)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, group=group, **par))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tree_logits_full_size(P, dtype):
+    """A serving batch's rows of Qwen3's vocabulary; the oracle takes two rows
+    of every group."""
+    group, V = 20, 151936
+    z, u = draw(16 * group, V, dtype, seed=41)
+    par = mixed_params()
+    n_rows = [group - (i % 3) for i in range(16)]
+    got, st = run(P, z, u, group=group, n_rows=n_rows, **par)
+    assert st == 0
+    at = [i * group + j for i in range(16) for j in (i, group - 1)]
+    for i in at:
+        g = i // group
+        if i - g * group >= n_rows[g]:
+            assert got[i] == -1
+            continue
+        ref = want(z[i:i + 1], u[i:i + 1], **{k: [v[g]] for k, v in par.items()})
+        assert got[i] == ref[0], i
+
+
+def test_streamed_rows_report_errors(P):
+    z, u = draw(400, 4096, "f32", seed=3)
+    good = want(z, u, top_k=30)
+    z[7, 4095] = float("nan")
+    z[399, 0] = float("inf")
+    z[200] = float("-inf")
+    got, st = run(P, z, u, top_k=30)
+    assert st == -5
+    bad = [7, 200, 399]
+    assert (got[bad] == -1).all()
+    rest = np.delete(np.arange(400), bad)
+    np.testing.assert_array_equal(got[rest], good[rest])
+
+
+def test_top_p_needs_no_bisection(P):
+    """Rows whose nucleus holds thousands of tokens take about as long as a few
+    passes over them, not as the 64 of the bisection that only long runs of
+    equal logits need."""
+    z, u = draw(64, 151936, "f32", seed=12)
+
+    def ms(**params):
+        cfg = P.sample_config(64, 151936)
+        tokens = torch.empty(64, dtype=torch.int32, device="cuda")
+        dev = {k: torch.full((64,), v, device="cuda") for k, v in params.items()}
+        best = 1e9
+        for _ in range(5):
+            a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+            a.record()
+            P.pctree_sample(cfg, z, u, tokens, **dev)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    assert ms(top_p=0.95) < 10 * ms()
