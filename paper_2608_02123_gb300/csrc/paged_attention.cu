@@ -67,6 +67,8 @@ struct PagedArgs {
   int Hq, Hkv, G, npt;
   int packed;             // pages per block (page_size 8 .. 64), 0: parts of pages
   int page_blocks;        // blocks per page if not packed
+  int box_rows;           // rows of a K/V box: a page, or part of one
+  int join_step;          // CTAs from one piece of a unit to the next
   float scale_log2;
 };
 
@@ -136,7 +138,7 @@ __host__ __device__ constexpr uint32_t idesc(int M, int N) {
   return idesc_bf16_f32(M, N) & (F16 ? ~((1u << 7) | (1u << 10)) : ~0u);
 }
 
-template <int D, bool F16>
+template <int D, bool F16, bool PAIR>
 __global__ void __maxnreg__(112)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k,
@@ -151,13 +153,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   Tail* T = reinterpret_cast<Tail*>(skv + kSlots * kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = a.G * a.npt;                       // rows of a tile
+  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
+  constexpr int kTiles = PAIR ? 2 : 1;             // tiles of a unit
+  const int unit_rows = kTiles * a.npt;
   volatile int* abort_v = &T->abort;
 
   // ---------------- set-up ----------------
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(&T->kv_full[s], 1);
-      mbar_init(&T->kv_empty[s], 1);
+      mbar_init(&T->kv_empty[s], kTiles);          // the MMAs of every CTA that got the block
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&T->q_full[s], 1);
@@ -195,8 +200,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     const int n = a.rows.n_rows[r], prefix = a.rows.prefix_len[r];
     long long w = 0;
     if (kv_request_ok(a.rows, a.rows.row_start[r], n, prefix)) {
-      for (int j = lane * a.npt; j < n; j += 32 * a.npt)
-        w += blocks_of(a, prefix + min(n, j + a.npt)) + kUnitCharge;
+      for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
+        w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
     } else if (blockIdx.x == 0 && lane == 0) {
       report(a.status, PCTREE_ERR_INVALID_ARG);
     }
@@ -222,6 +227,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  if constexpr (PAIR) cluster_sync();              // both CTAs' barriers are initialised
   const uint32_t tmem = T->tmem_base;
 
   auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
@@ -265,19 +271,18 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       }
       ++q;
       for (int b = it.b0; ok && b < it.b1; ++b) {
-        // this lane's page of the block: its number, place and rows
-        int page = -1, off = 0, rows, boxes = 1, at = 0;
+        // this lane's box of the block: its page, place and rows
+        int page = -1, off = 0, rows = a.box_rows, boxes;
+        const int at = lane * rows;
         if (a.packed) {
-          const int keys = min(kBK, it.key_end - b * kBK);
-          rows = a.rows.page_size;
-          boxes = (keys + rows - 1) / rows;
-          at = lane * rows;
+          boxes = (min(kBK, it.key_end - b * kBK) + rows - 1) / rows;
           if (lane < boxes) page = kv_page(a.rows, it.r, b * a.packed + lane);
         } else {
           const int entry = b / a.page_blocks;
           off = (b - entry * a.page_blocks) * kBK;
-          rows = min(kBK, a.rows.page_size);
-          if (lane == 0) page = kv_page(a.rows, it.r, entry);
+          boxes = (min(kBK, a.rows.page_size - off) + rows - 1) / rows;
+          off += at;
+          if (lane < boxes) page = kv_page(a.rows, it.r, entry);
         }
         if (lane < boxes && page < 0) {
           report(a.status, PCTREE_ERR_INVALID_ARG);
@@ -292,10 +297,17 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
             mbar_arrive_expect_tx(&T->kv_full[slot],
                                   static_cast<uint32_t>(kHalves * boxes * rows) * 128u);
           __syncwarp();
-          if (lane < boxes) {
+          // a pair's CTAs take the boxes in turn, each for both of them
+          if (lane < boxes && (!PAIR || (lane & 1) == rank)) {
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h)
-              tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, it.kvh, off, page);
+            for (int h = 0; h < kHalves; ++h) {
+              if constexpr (PAIR)
+                tma_load_4d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h,
+                                      it.kvh, off, page, 3);
+              else
+                tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, it.kvh, off,
+                            page);
+            }
           }
           ++issued;
           if (++slot == kSlots) {
@@ -315,6 +327,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         (void)mbar_wait_bounded(&T->kv_full[x % kSlots], (x / kSlots) & 1, &never, kLimitNs);
       for (int x = q > 2 ? q - 2 : 0; x < q; ++x)
         (void)mbar_wait_bounded(&T->q_full[x & 1], (x >> 1) & 1, &never, kLimitNs);
+      // and so do the other CTA's arrivals
+      if constexpr (PAIR) {
+        for (int x = issued > kSlots ? issued - kSlots : 0; ok && x < issued; ++x)
+          (void)mbar_wait_bounded(&T->kv_empty[x % kSlots], (x / kSlots) & 1, &never, kLimitNs);
+      }
     }
   } else if (warp == 1 && lane == 0) {
     // ---------------- S issuer ----------------
@@ -344,7 +361,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
           tc_mma_bf16(tmem + sb * kBK, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
         }
         tc_commit(&T->s_full[sb]);
-        tc_commit(&T->kv_empty[slot]);
+        if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
+        else tc_commit(&T->kv_empty[slot]);
         slot += 2;
         if (slot >= kSlots) {
           slot -= kSlots;
@@ -385,7 +403,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         tc_commit(&T->p_empty[sb]);
         if (b + 1 == it.b1) tc_commit(&T->o_full);
-        tc_commit(&T->kv_empty[slot]);
+        if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
+        else tc_commit(&T->kv_empty[slot]);
         slot += 2;
         if (slot >= kSlots) {
           slot -= kSlots;
@@ -400,9 +419,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   } else if (warp == 3) {
     // ---------------- planner ----------------
     const long long total = T->upto[a.rows.batch - 1];
-    long long stretch = (total + gridDim.x - 1) / gridDim.x;
+    const int places = gridDim.x / kTiles, place = blockIdx.x / kTiles;
+    long long stretch = (total + places - 1) / places;
     if (stretch < kMinStretch) stretch = kMinStretch;
-    long long x = blockIdx.x * stretch;
+    long long x = place * stretch;
     const long long x_end = min(total, x + stretch);
     Join join = {0, 0, 0, 0};
     int k = 0;
@@ -437,8 +457,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       kvh = static_cast<int>(in / per_head);
       in -= kvh * per_head;                        // place inside the head's tiles
       for (;;) {
-        const int j = (tile + lane) * a.npt;
-        const int cost = j < n ? blocks_of(a, prefix + min(n, j + a.npt)) + kUnitCharge : 0;
+        const int j = (tile + lane) * unit_rows;
+        const int cost = j < n ? blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge : 0;
         long long c = cost;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -456,15 +476,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         tile += 32;
       }
       while (ok && x < x_end) {
-        const int j0 = tile * a.npt, j1 = min(n, j0 + a.npt);
+        // this CTA's tile of the unit; the keys are those of the whole unit
+        const int j0 = tile * unit_rows + rank * a.npt, j1 = min(n, j0 + a.npt);
         Item it;
         it.r = r;
         it.kvh = kvh;
         it.row0 = start + j0;
-        it.n_rows = j1 - j0;
+        it.n_rows = max(0, j1 - j0);
         it.j0 = j0;
         it.prefix = prefix;
-        it.key_end = prefix + j1;
+        it.key_end = prefix + min(n, (tile + 1) * unit_rows);
         it.nblk = blocks_of(a, it.key_end);
         const long long left = it.nblk + kUnitCharge - in;
         const long long take = min(left, x_end - x);
@@ -473,7 +494,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         if (it.b1 > it.b0) {
           if (it.b0 == 0 && it.b1 < it.nblk) {
             // joined from here: the unit's end lies `left` past x
-            join.pieces = static_cast<int>((x + left - 1) / stretch) - static_cast<int>(blockIdx.x) + 1;
+            join.pieces = static_cast<int>((x + left - 1) / stretch) - place + 1;
             join.kvh = kvh;
             join.row0 = it.row0;
             join.n_rows = it.n_rows;
@@ -483,7 +504,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         x += take;
         in = 0;
         ++tile;
-        if (x < x_end && tile * a.npt >= n) {
+        if (x < x_end && tile * unit_rows >= n) {
           tile = 0;
           if (++kvh == a.Hkv) {
             kvh = 0;
@@ -715,6 +736,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   __syncthreads();
   tc_fence_after_sync();
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
+  if constexpr (PAIR) {
+    // the other CTA's copies and commits no longer reach this one's memory
+    __syncwarp();
+    cluster_sync();
+  }
 }
 
 // Joins the pieces of the units that end in another CTA than they began in: a
@@ -742,7 +768,8 @@ __global__ void __launch_bounds__(kJoinThreads, 8) paged_join_kernel(PagedArgs a
     for (int u = 0; u < 4; ++u) {
       const bool in = s0 + u < j.pieces;
       // the first piece is its CTA's last, every other one its CTA's first
-      const size_t part = static_cast<size_t>(c0 + s0 + u) * 2 + (s0 + u == 0 ? 1 : 0);
+      const size_t part =
+          static_cast<size_t>(c0 + (s0 + u) * a.join_step) * 2 + (s0 + u == 0 ? 1 : 0);
       w[u] = in ? a.part_ml[part * 128 + row] : make_float2(-INFINITY, 0.0f);
       v[u] = in ? po[(part * (D / 4) + quad) * 128 + row] : acc;
     }
@@ -804,7 +831,7 @@ PagedWs paged_ws(const pctree_paged_attn_config& c) {
   return w;
 }
 
-template <int D, bool F16>
+template <int D, bool F16, bool PAIR>
 pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                            const CUtensorMap& tm_v, const PagedArgs& a, int num_sms,
                            cudaStream_t stream) {
@@ -812,26 +839,40 @@ pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
       (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
   static SmemLimit limit;
-  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16>);
+  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16, PAIR>);
   if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t lc = {};
-  const int ctas = num_sms < kMaxCtas ? num_sms : kMaxCtas;
+  int ctas = num_sms < kMaxCtas ? num_sms : kMaxCtas;
+  if (PAIR) ctas &= ~1;
   lc.gridDim = dim3(static_cast<unsigned>(ctas));
   lc.blockDim = dim3(kThreads);
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
   lc.attrs = attr;
-  lc.numAttrs = 1;
-  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16>, tm_q, tm_k, tm_v, a) != cudaSuccess)
+  lc.numAttrs = PAIR ? 2 : 1;
+  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16, PAIR>, tm_q, tm_k, tm_v, a) != cudaSuccess)
     return PCTREE_ERR_CUDA;
+  lc.numAttrs = 1;
   lc.gridDim = dim3(static_cast<unsigned>(ctas), (a.G * a.npt + kJoinRows - 1) / kJoinRows, D / 32);
   lc.blockDim = dim3(kJoinThreads);
   lc.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&lc, paged_join_kernel<D, F16>, a) == cudaSuccess ? PCTREE_OK
                                                                              : PCTREE_ERR_CUDA;
+}
+
+template <int D, bool F16>
+pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                           const CUtensorMap& tm_v, const PagedArgs& a, int num_sms, bool pair,
+                           cudaStream_t stream) {
+  return pair ? paged_launch<D, F16, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
+              : paged_launch<D, F16, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
 }
 
 }  // namespace
@@ -893,6 +934,12 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   a.packed = c.page_size == 8 || c.page_size == 16 || c.page_size == 32 || c.page_size == 64
                  ? kBK / c.page_size : 0;
   a.page_blocks = (c.page_size + kBK - 1) / kBK;
+  // Requests of more than a tile of rows, on average: pairs of CTAs take two
+  // tiles of a head at a time and each loads half of the keys for both.
+  const bool pair = num_sms >= 2 && c.total_rows > static_cast<long long>(c.batch) * a.npt;
+  const int most = pair ? kBK / 2 : kBK;           // so that both CTAs have boxes to load
+  a.box_rows = c.page_size < most ? c.page_size : most;
+  a.join_step = pair ? 2 : 1;
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
   CUtensorMap tm_q, tm_k, tm_v;
   const uint64_t D = static_cast<uint64_t>(c.D), head = D * 2;   // bytes of one head row
@@ -907,7 +954,7 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
     const uint64_t dims[4] = {D, static_cast<uint64_t>(c.Hkv), static_cast<uint64_t>(c.page_size),
                               static_cast<uint64_t>(c.n_pages)};
     const uint64_t str[3] = {head, head * c.Hkv, head * c.Hkv * c.page_size};
-    const uint32_t box[4] = {64, 1, static_cast<uint32_t>(c.page_size < kBK ? c.page_size : kBK), 1};
+    const uint32_t box[4] = {64, 1, static_cast<uint32_t>(a.box_rows), 1};
     st = encode_bf16_map_nd(&tm_k, k_cache, 4, dims, str, box);
     if (st != PCTREE_OK) return st;
     st = encode_bf16_map_nd(&tm_v, v_cache, 4, dims, str, box);
@@ -916,10 +963,10 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
   const bool f16 = c.dtype == PCTREE_F16;
   if (c.D == 64)
-    return f16 ? paged_launch<64, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
-               : paged_launch<64, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
-  return f16 ? paged_launch<128, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
-             : paged_launch<128, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
+    return f16 ? paged_launch<64, true>(tm_q, tm_k, tm_v, a, num_sms, pair, stream)
+               : paged_launch<64, false>(tm_q, tm_k, tm_v, a, num_sms, pair, stream);
+  return f16 ? paged_launch<128, true>(tm_q, tm_k, tm_v, a, num_sms, pair, stream)
+             : paged_launch<128, false>(tm_q, tm_k, tm_v, a, num_sms, pair, stream);
 }
 
 }  // extern "C"

@@ -96,8 +96,17 @@ SHAPES = {
     "one_head": dict(rows=[140, 2], prefix=[7, 260], page=16, heads=(3, 3)),
     "wide_group": dict(rows=[5, 1], prefix=[130, 0], page=16, heads=(128, 1)),
     "group_of_48": dict(rows=[5, 9], prefix=[130, 0], page=32, heads=(96, 2)),
+    # several tiles a request: pairs of CTAs, an odd tile, a last tile of one row
+    "pairs_odd_tiles": dict(rows=[161, 33, 0, 70], prefix=[0, 300, 5, 77], page=16, heads=(16, 4)),
+    "pairs_long_prefix": dict(rows=[65, 129], prefix=[1900, 3], page=64, heads=(16, 4), gap=1),
+    "pairs_one_head": dict(rows=[500], prefix=[130], page=32, heads=(2, 2)),
+    "pairs_wide_group": dict(rows=[9, 4], prefix=[250, 0], page=16, heads=(96, 2)),
     "many_requests": dict(rows=[1, 2, 1] * 40, prefix=[3, 0, 129] * 40, page=16, heads=(4, 4)),
 }
+
+
+for _page in (0, 1, 8, 16, 23, 32, 48, 64, 100, 128, 200):
+    SHAPES[f"pairs_page_{_page}"] = dict(rows=[70, 41], prefix=[190, 3], page=_page, heads=(16, 2))
 
 
 @pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "bf16"), (128, "f16"), (64, "f16")])
