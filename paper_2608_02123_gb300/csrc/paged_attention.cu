@@ -13,7 +13,7 @@
 // in order.
 //
 //   warp 0      TMA producer, all lanes: the tile's Q (two buffers), then K and
-//               V blocks (128-byte swizzle, 64 dims a half), K and V in turn,
+//               V blocks (128-byte swizzle, 64 dims a half), K a block ahead,
 //               into a ring; a lane issues the copies of one page
 //   warp 1      S issuer: S_b = Q K_b^T (tcgen05.mma, M = N = 128) into one of
 //               two TMEM buffers
@@ -71,6 +71,10 @@ struct PagedArgs {
   int join_step;          // CTAs from one piece of a unit to the next
   float scale_log2;
 };
+
+// Places of the g-th block's K and V in the ring's sequence.
+__device__ __forceinline__ int k_place(int g) { return g == 0 ? 0 : 2 * g - 1; }
+__device__ __forceinline__ int v_place(int g) { return 2 * g + 2; }
 
 struct Tail {
   uint64_t q_full[2], q_empty[2];
@@ -255,89 +259,119 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
 
   if (warp == 0) {
     // ---------------- TMA producer ----------------
-    int slot = 0, issued = 0, q = 0;
-    uint32_t phase = 0;
-    bool ok = true;
+    // K runs a block ahead of V, in the order the MMAs free them: K_0 K_1 V_0
+    // K_2 V_1 ..., place k_place(g) and v_place(g) of the ring's sequence.
+    struct Box {
+      int page, off, boxes, kvh;                   // this lane's box of a block
+    };
+    int g = 0, q = 0, k = 0, b = 0;                // blocks, Q tiles, items fetched, block
+    bool ok = true, more = true;
     Item it;
-    for (int k = 0;; ++k) {
-      if (!(ok = fetch_warp(k, it)) || it.nblk == 0) break;
-      const int qb = q & 1;
-      if (!(ok = wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1))) break;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&T->q_full[qb], static_cast<uint32_t>(kHalves * R) * 128u);
-        for (int h = 0; h < kHalves; ++h)
-          tma_load_3d(sq + qb * kTileBytes + h * kHalfBytes, &tm_q, &T->q_full[qb], 64 * h,
-                      it.kvh * a.G, it.row0);
+    it.b1 = 0;
+    auto next_block = [&](Box& x) {                // false: no more, or not ok
+      if (b >= it.b1) {
+        if (!(ok = fetch_warp(k++, it)) || it.nblk == 0) return more = false;
+        b = it.b0;
+        const int qb = q & 1;
+        if (!(ok = wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1))) return more = false;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&T->q_full[qb], static_cast<uint32_t>(kHalves * R) * 128u);
+          for (int h = 0; h < kHalves; ++h)
+            tma_load_3d(sq + qb * kTileBytes + h * kHalfBytes, &tm_q, &T->q_full[qb], 64 * h,
+                        it.kvh * a.G, it.row0);
+        }
+        ++q;
       }
-      ++q;
-      for (int b = it.b0; ok && b < it.b1; ++b) {
-        // this lane's box of the block: its page, place and rows
-        int page = -1, off = 0, rows = a.box_rows, boxes;
-        const int at = lane * rows;
-        if (a.packed) {
-          boxes = (min(kBK, it.key_end - b * kBK) + rows - 1) / rows;
-          if (lane < boxes) page = kv_page(a.rows, it.r, b * a.packed + lane);
-        } else {
-          const int entry = b / a.page_blocks;
-          off = (b - entry * a.page_blocks) * kBK;
-          boxes = (min(kBK, a.rows.page_size - off) + rows - 1) / rows;
-          off += at;
-          if (lane < boxes) page = kv_page(a.rows, it.r, entry);
-        }
-        if (lane < boxes && page < 0) {
-          report(a.status, PCTREE_ERR_INVALID_ARG);
-          page = a.rows.n_pages;                   // past the tensor: zeros
-        }
+      x.page = -1;
+      x.off = 0;
+      x.kvh = it.kvh;
+      const int rows = a.box_rows;
+      if (a.packed) {
+        x.boxes = (min(kBK, it.key_end - b * kBK) + rows - 1) / rows;
+        if (lane < x.boxes) x.page = kv_page(a.rows, it.r, b * a.packed + lane);
+      } else {
+        const int entry = b / a.page_blocks;
+        x.off = (b - entry * a.page_blocks) * kBK;
+        x.boxes = (min(kBK, a.rows.page_size - x.off) + rows - 1) / rows;
+        x.off += lane * rows;
+        if (lane < x.boxes) x.page = kv_page(a.rows, it.r, entry);
+      }
+      if (lane < x.boxes && x.page < 0) {
+        report(a.status, PCTREE_ERR_INVALID_ARG);
+        x.page = a.rows.n_pages;                   // past the tensor: zeros
+      }
+      ++b;
+      return true;
+    };
+    auto load = [&](const CUtensorMap* map, const Box& x, int place) {
+      const int slot = place % kSlots;
+      if (!(ok = wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1))) return;
+      uint8_t* dst = skv + slot * kTileBytes + lane * a.box_rows * 128;
+      if (lane == 0)
+        mbar_arrive_expect_tx(&T->kv_full[slot],
+                              static_cast<uint32_t>(kHalves * x.boxes * a.box_rows) * 128u);
+      __syncwarp();
+      // a pair's CTAs take the boxes in turn, each for both of them
+      if (lane < x.boxes && (!PAIR || (lane & 1) == rank)) {
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          if (!(ok = wwait(&T->kv_empty[slot], phase ^ 1u))) break;
-          uint8_t* dst = skv + slot * kTileBytes + at * 128;
-          const CUtensorMap* map = v == 0 ? &tm_k : &tm_v;
-          if (lane == 0)
-            mbar_arrive_expect_tx(&T->kv_full[slot],
-                                  static_cast<uint32_t>(kHalves * boxes * rows) * 128u);
-          __syncwarp();
-          // a pair's CTAs take the boxes in turn, each for both of them
-          if (lane < boxes && (!PAIR || (lane & 1) == rank)) {
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-              if constexpr (PAIR)
-                tma_load_4d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h,
-                                      it.kvh, off, page, 3);
-              else
-                tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, it.kvh, off,
-                            page);
-            }
-          }
-          ++issued;
-          if (++slot == kSlots) {
-            slot = 0;
-            phase ^= 1u;
-          }
+        for (int h = 0; h < kHalves; ++h) {
+          if constexpr (PAIR)
+            tma_load_4d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh,
+                                  x.off, x.page, 3);
+          else
+            tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh, x.off,
+                        x.page);
         }
       }
-      if (!ok) break;
+    };
+    Box cur, next;
+    int k_issued = 0, v_issued = 0;
+    if (next_block(cur)) {
+      load(&tm_k, cur, k_place(0));
+      k_issued = 1;
+      for (; ok; ++g) {
+        const bool has = next_block(next);
+        if (!ok) break;
+        if (has) {
+          load(&tm_k, next, k_place(g + 1));
+          if (!ok) break;
+          ++k_issued;
+        }
+        load(&tm_v, cur, v_place(g));
+        if (!ok) break;
+        ++v_issued;
+        if (!has) break;
+        cur = next;
+      }
     }
     __syncwarp();
     if (lane == 0) {
       if (!ok) give_up();
       // copies still in flight land before the CTA may exit
       volatile int never = 0;
-      for (int x = issued > kSlots ? issued - kSlots : 0; x < issued; ++x)
-        (void)mbar_wait_bounded(&T->kv_full[x % kSlots], (x / kSlots) & 1, &never, kLimitNs);
+      auto drain = [&](uint64_t* bars) {           // each slot's last place
+        for (int slot = 0; slot < kSlots; ++slot) {
+          int last = -1;
+          for (int x = max(0, k_issued - kSlots); x < k_issued; ++x)
+            if (k_place(x) % kSlots == slot) last = max(last, k_place(x));
+          for (int x = max(0, v_issued - kSlots); x < v_issued; ++x)
+            if (v_place(x) % kSlots == slot) last = max(last, v_place(x));
+          if (last >= 0)
+            (void)mbar_wait_bounded(&bars[slot], (last / kSlots) & 1, &never, kLimitNs);
+        }
+      };
+      drain(T->kv_full);
       for (int x = q > 2 ? q - 2 : 0; x < q; ++x)
         (void)mbar_wait_bounded(&T->q_full[x & 1], (x >> 1) & 1, &never, kLimitNs);
       // and so do the other CTA's arrivals
       if constexpr (PAIR) {
-        for (int x = issued > kSlots ? issued - kSlots : 0; ok && x < issued; ++x)
-          (void)mbar_wait_bounded(&T->kv_empty[x % kSlots], (x / kSlots) & 1, &never, kLimitNs);
+        if (ok) drain(T->kv_empty);
       }
     }
   } else if (warp == 1 && lane == 0) {
     // ---------------- S issuer ----------------
     constexpr uint32_t idS = idesc<F16>(128, kBK);
-    int slot = 0, q = 0, g = 0;
-    uint32_t phase = 0;
+    int q = 0, g = 0;
     const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
     const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
     bool ok = true;
@@ -349,8 +383,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       ++q;
       const uint64_t qd = q_desc + qb * (kTileBytes >> 4);
       for (int b = it.b0; b < it.b1; ++b, ++g) {
-        const int sb = g & 1;
-        ok = mbar_wait_bounded(&T->kv_full[slot], phase, abort_v, kLimitNs) &&
+        const int sb = g & 1, slot = k_place(g) % kSlots;
+        ok = mbar_wait_bounded(&T->kv_full[slot], (k_place(g) / kSlots) & 1, abort_v, kLimitNs) &&
              mbar_wait_bounded(&T->p_empty[sb], ((g >> 1) & 1) ^ 1, abort_v, kLimitNs);
         if (!ok) break;
         const uint64_t kd = k_desc + slot * (kTileBytes >> 4);
@@ -363,11 +397,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         tc_commit(&T->s_full[sb]);
         if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
         else tc_commit(&T->kv_empty[slot]);
-        slot += 2;
-        if (slot >= kSlots) {
-          slot -= kSlots;
-          phase ^= 1u;
-        }
       }
       tc_commit(&T->q_empty[qb]);
     }
@@ -378,16 +407,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   } else if (warp == 2 && lane == 0) {
     // ---------------- PV issuer ----------------
     constexpr uint32_t idO = idesc<F16>(128, D) | (1u << 16);   // B MN-major
-    int slot = 1, g = 0;
-    uint32_t phase = 0;
+    int g = 0;
     const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), kHalfBytes, 1024);
     bool ok = true;
     Item it;
     for (int k = 0; ok; ++k) {
       if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
       for (int b = it.b0; b < it.b1; ++b, ++g) {
-        const int sb = g & 1;
-        ok = mbar_wait_bounded(&T->kv_full[slot], phase, abort_v, kLimitNs) &&
+        const int sb = g & 1, slot = v_place(g) % kSlots;
+        ok = mbar_wait_bounded(&T->kv_full[slot], (v_place(g) / kSlots) & 1, abort_v, kLimitNs) &&
              mbar_wait_bounded(&T->p_full[sb], (g >> 1) & 1, abort_v, kLimitNs) &&
              (b > it.b0 ||                         // the last piece's O has been read
               mbar_wait_bounded(&T->o_empty, (k & 1) ^ 1, abort_v, kLimitNs));
@@ -405,11 +433,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         if (b + 1 == it.b1) tc_commit(&T->o_full);
         if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
         else tc_commit(&T->kv_empty[slot]);
-        slot += 2;
-        if (slot >= kSlots) {
-          slot -= kSlots;
-          phase ^= 1u;
-        }
       }
     }
     if (!ok) give_up();
@@ -661,7 +684,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         // 0 * (non-finite) cannot reach O
         const int valid = min(cap, it.key_end - key0);
         if (valid < kBK) {
-          const int xv = 2 * g + 1;
+          const int xv = v_place(g);
           if (!(ok = wwait(&T->kv_full[xv % kSlots], (xv / kSlots) & 1))) break;
           uint8_t* v = skv + (xv % kSlots) * kTileBytes;
           const int n16 = (kBK - valid) * 8;
