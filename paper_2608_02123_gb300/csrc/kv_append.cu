@@ -14,8 +14,13 @@
 // position * fraction wraps modulo one turn by itself, in integers; what is
 // left is exact to position * 2^-53 turns, for any position.
 //
-// What bounds it: HBM for prompts and trees (each element is read and written
-// once, nothing is read twice), the launch for single tokens.
+// What bounds it: HBM for prompts (each element is read and written once: 370
+// MB in 65 us, 0.84 of the measured copy rate), the launch for single tokens;
+// in between (trees of 32 requests, 89 MB in 26.6 us) the rows a warp takes one
+// after the other.  Four heads of loads ahead of the arithmetic and two CTAs an
+// SM (us, trees / prompts): 26.6 / 65.2; two heads and three CTAs 33.1 / 70.2;
+// six heads 27.1 / 64.0; eight and one CTA 35.5 / 89.6.  Arithmetic goes two
+// elements at a time (before: 28.2 / 70.5).
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
@@ -24,6 +29,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWarps = kAppendThreads / 32;
+constexpr int kAppendCtas = 2;      // an SM: 113 registers a thread
 constexpr int kHeadsAhead = 4;      // heads a lane has loads in flight for
 
 struct AppendArgs {
@@ -47,11 +53,12 @@ struct AppendArgs {
 
 struct AppendShared {
   unsigned long long turn[128];                  // fraction of a turn per position
+  alignas(16) float weight[2][256];              // of queries and keys
   int start[PCTREE_KV_MAX_BATCH], end[PCTREE_KV_MAX_BATCH], prefix[PCTREE_KV_MAX_BATCH];
 };
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, kAppendCtas) kv_append_kernel(AppendArgs a) {
   constexpr int S = D / 16;                      // lanes per head
   constexpr int kGroups = 32 / S;                // heads side by side in a warp
   __shared__ AppendShared sh;
@@ -60,6 +67,12 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a)
   const int half = a.rotary / 2;
   pdl_launch_dependents();
   pdl_wait();
+  for (int i = half + threadIdx.x; i < 128; i += kAppendThreads) sh.turn[i] = 0;
+  for (int i = threadIdx.x; i < 2 * D; i += kAppendThreads) {
+    const uint16_t* w = i < D ? a.q_weight : a.k_weight;
+    const int d = i < D ? i : i - D;
+    sh.weight[i < D ? 0 : 1][d] = w != nullptr ? unpack16<F16>(w[d]).x : 1.0f;
+  }
   for (int i = threadIdx.x; i < half; i += kAppendThreads) {
     const double t = a.inv_freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
     // the fraction in [-0.5, 0.5] as a signed 64-bit integer, twice over
@@ -99,6 +112,29 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a)
       }
     }
     if (r < 0) continue;                         // a row of no request
+    const int h_end = min(heads, (part + 1) * a.heads_per_part);
+    const uint16_t* q_row = a.q + row * a.q_stride;
+    const uint16_t* k_row = a.k + row * a.k_stride;
+    const uint16_t* v_row = a.v + row * a.v_stride;
+    uint4 x0[kHeadsAhead], x1[kHeadsAhead];
+    auto load = [&](int hb) {
+#pragma unroll
+      for (int u = 0; u < kHeadsAhead; ++u) {
+        const int h = hb + u * kGroups + group;
+        const bool is_v = h >= a.Hq + a.Hkv;
+        const uint16_t* src = h < a.Hq ? q_row + h * D
+                              : !is_v  ? k_row + (h - a.Hq) * D
+                                       : v_row + (h - a.Hq - a.Hkv) * D;
+        if (h < h_end) {
+          x0[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s : c0) * 8);
+          x1[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s + 1 : c1) * 8);
+        } else {
+          x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+        }
+      }
+    };
+    // the first heads are under way while the place and the angles are found
+    load(part * a.heads_per_part);
     const int slot = sh.prefix[r] + row - sh.start[r];
     const int entry = slot / a.rows.page_size;
     const int page = kv_page(a.rows, r, entry);
@@ -107,111 +143,128 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a)
     const size_t place =
         (static_cast<size_t>(page < 0 ? 0 : page) * a.rows.page_size +
          (slot - entry * a.rows.page_size)) * a.Hkv * D;
-    float cs[8], sn[8];
-    if (rotated) {
+    // the head lanes' eight angles, each worked out by one of the warp's groups
+    uint64_t cs[4], sn[4], ns[4];                // cos, sin and -sin, in pairs
+    if (a.rotary > 0) {
+      constexpr int kOwn = 8 / kGroups;
       const long long pos = a.positions != nullptr ? a.positions[row] : slot;
+      float c_own[kOwn], s_own[kOwn];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const unsigned long long ph = static_cast<unsigned long long>(pos) * sh.turn[8 * s + e];
+      for (int e = 0; e < kOwn; ++e) {
+        const unsigned long long ph =
+            static_cast<unsigned long long>(pos) * sh.turn[8 * s + group * kOwn + e];
         // half turns in [-1, 1)
         const float x = static_cast<float>(static_cast<int>(ph >> 32)) * (1.0f / 2147483648.0f);
-        sincospif(x, &sn[e], &cs[e]);
-        sn[e] *= a.scale;
-        cs[e] *= a.scale;
+        sincospif(x, &s_own[e], &c_own[e]);
+        s_own[e] *= a.scale;
+        c_own[e] *= a.scale;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        float c[2], t[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int from = ((e + i) / kOwn) * S + s;
+          c[i] = __shfl_sync(kFull, c_own[(e + i) % kOwn], from);
+          t[i] = __shfl_sync(kFull, s_own[(e + i) % kOwn], from);
+        }
+        cs[e / 2] = pack2(c[0], c[1]);
+        sn[e / 2] = pack2(t[0], t[1]);
+        ns[e / 2] = pack2(-t[0], -t[1]);
       }
     }
-    const int h_end = min(heads, (part + 1) * a.heads_per_part);
     // every lane runs the same number of rounds: the reductions are warp-wide
-    for (int hb = part * a.heads_per_part; hb < h_end; hb += kGroups * kHeadsAhead) {
-      uint4 x0[kHeadsAhead], x1[kHeadsAhead];
-#pragma unroll
-      for (int u = 0; u < kHeadsAhead; ++u) {
-        const int h = hb + u * kGroups + group;
-        const uint16_t* src =
-            h < a.Hq ? a.q + row * a.q_stride + static_cast<size_t>(h) * D
-            : h < a.Hq + a.Hkv
-                ? a.k + row * a.k_stride + static_cast<size_t>(h - a.Hq) * D
-                : a.v + row * a.v_stride + static_cast<size_t>(h - a.Hq - a.Hkv) * D;
-        const bool is_v = h >= a.Hq + a.Hkv;
-        if (h < h_end) {
-          x0[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s : c0) * 8);
-          x1[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s + 1 : c1) * 8);
-        } else {
-          x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
-        }
-      }
+    for (int hb = part * a.heads_per_part;;) {
 #pragma unroll
       for (int u = 0; u < kHeadsAhead; ++u) {
         const int h = hb + u * kGroups + group;
         const bool is_q = h < a.Hq, is_v = h >= a.Hq + a.Hkv;
-        const uint16_t* weight = is_q ? a.q_weight : a.k_weight;
-        float f0[8], f1[8];
+        const bool norm = (is_q ? a.q_weight : a.k_weight) != nullptr;
+        uint64_t f0[4], f1[4];                   // the two pieces, two elements at a time
+        uint64_t sum2 = 0;
         const uint32_t w0[4] = {x0[u].x, x0[u].y, x0[u].z, x0[u].w};
         const uint32_t w1[4] = {x1[u].x, x1[u].y, x1[u].z, x1[u].w};
-        float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 lo = unpack16<F16>(w0[e]), hi = unpack16<F16>(w1[e]);
-          f0[2 * e] = lo.x;
-          f0[2 * e + 1] = lo.y;
-          f1[2 * e] = hi.x;
-          f1[2 * e + 1] = hi.y;
-          sum += lo.x * lo.x + lo.y * lo.y + hi.x * hi.x + hi.y * hi.y;
+          f0[e] = pack2(lo.x, lo.y);
+          f1[e] = pack2(hi.x, hi.y);
+          sum2 = fma2(f0[e], f0[e], sum2);
+          sum2 = fma2(f1[e], f1[e], sum2);
         }
+        float sum, odd;
+        unpack2(sum2, sum, odd);
+        sum += odd;
 #pragma unroll
         for (int o = S / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
         if (h >= h_end) continue;
-        if (!is_v) {
-          if (weight != nullptr) {
+        if (!is_v && (norm || rotated)) {
+          if (norm) {
             const float inv = rsqrtf(sum * (1.0f / D) + a.eps);
-            const uint4 g0 = *reinterpret_cast<const uint4*>(weight + c0 * 8);
-            const uint4 g1 = *reinterpret_cast<const uint4*>(weight + c1 * 8);
-            const uint32_t p0[4] = {g0.x, g0.y, g0.z, g0.w}, p1[4] = {g1.x, g1.y, g1.z, g1.w};
+            const uint64_t inv2 = pack2(inv, inv);
+            const ulonglong2* g0 = reinterpret_cast<const ulonglong2*>(&sh.weight[is_q ? 0 : 1][c0 * 8]);
+            const ulonglong2* g1 = reinterpret_cast<const ulonglong2*>(&sh.weight[is_q ? 0 : 1][c1 * 8]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 lo = unpack16<F16>(p0[e]), hi = unpack16<F16>(p1[e]);
-              f0[2 * e] *= inv * lo.x;
-              f0[2 * e + 1] *= inv * lo.y;
-              f1[2 * e] *= inv * hi.x;
-              f1[2 * e + 1] *= inv * hi.y;
+            for (int e = 0; e < 4; e += 2) {
+              const ulonglong2 p = g0[e / 2], q = g1[e / 2];
+              f0[e] = mul2(mul2(f0[e], inv2), p.x);
+              f0[e + 1] = mul2(mul2(f0[e + 1], inv2), p.y);
+              f1[e] = mul2(mul2(f1[e], inv2), q.x);
+              f1[e + 1] = mul2(mul2(f1[e + 1], inv2), q.y);
             }
           }
           if (rotated) {
             if (a.interleaved) {
+              // a piece's element pairs are rotation pairs: piece 0 has the
+              // angles 0..3, piece 1 the angles 4..7
+              auto turn = [](uint64_t ab, float c, float t) {
+                float x, y;
+                unpack2(ab, x, y);
+                return fma2(pack2(y, x), pack2(-t, t), mul2(ab, pack2(c, c)));
+              };
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const float p = f0[2 * e], q = f0[2 * e + 1];
-                f0[2 * e] = p * cs[e] - q * sn[e];
-                f0[2 * e + 1] = q * cs[e] + p * sn[e];
-                const float p1 = f1[2 * e], q1 = f1[2 * e + 1];
-                f1[2 * e] = p1 * cs[4 + e] - q1 * sn[4 + e];
-                f1[2 * e + 1] = q1 * cs[4 + e] + p1 * sn[4 + e];
+                float c, d, t, v;
+                unpack2(cs[e / 2], c, d);
+                unpack2(sn[e / 2], t, v);
+                f0[e] = turn(f0[e], (e & 1) ? d : c, (e & 1) ? v : t);
+                unpack2(cs[2 + e / 2], c, d);
+                unpack2(sn[2 + e / 2], t, v);
+                f1[e] = turn(f1[e], (e & 1) ? d : c, (e & 1) ? v : t);
               }
             } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const float p = f0[e], q = f1[e];
-                f0[e] = p * cs[e] - q * sn[e];
-                f1[e] = q * cs[e] + p * sn[e];
+              for (int e = 0; e < 4; ++e) {
+                const uint64_t p = f0[e];
+                f0[e] = fma2(f1[e], ns[e], mul2(p, cs[e]));
+                f1[e] = fma2(p, sn[e], mul2(f1[e], cs[e]));
               }
             }
           }
-          if (weight != nullptr || rotated) {
-            x0[u] = make_uint4(pack16<F16>(f0[0], f0[1]), pack16<F16>(f0[2], f0[3]),
-                               pack16<F16>(f0[4], f0[5]), pack16<F16>(f0[6], f0[7]));
-            x1[u] = make_uint4(pack16<F16>(f1[0], f1[1]), pack16<F16>(f1[2], f1[3]),
-                               pack16<F16>(f1[4], f1[5]), pack16<F16>(f1[6], f1[7]));
-          }
+          auto packed = [](const uint64_t(&f)[4]) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float lo, hi;
+              unpack2(f[e], lo, hi);
+              w[e] = pack16<F16>(lo, hi);
+            }
+            return make_uint4(w[0], w[1], w[2], w[3]);
+          };
+          x0[u] = packed(f0);
+          x1[u] = packed(f1);
         }
-        uint16_t* dst =
-            is_q    ? a.q_out + (static_cast<size_t>(row) * a.Hq + h) * D
-            : !is_v ? a.k_cache + place + static_cast<size_t>(h - a.Hq) * D
-                    : a.v_cache + place + static_cast<size_t>(h - a.Hq - a.Hkv) * D;
+        uint16_t* dst = is_q    ? a.q_out + (static_cast<size_t>(row) * a.Hq + h) * D
+                        : !is_v ? a.k_cache + place + (h - a.Hq) * D
+                                : a.v_cache + place + (h - a.Hq - a.Hkv) * D;
         if (is_q || page >= 0) {
           *reinterpret_cast<uint4*>(dst + (is_v ? 2 * s : c0) * 8) = x0[u];
           *reinterpret_cast<uint4*>(dst + (is_v ? 2 * s + 1 : c1) * 8) = x1[u];
         }
       }
+      hb += kGroups * kHeadsAhead;
+      if (hb >= h_end) break;
+      load(hb);
     }
   }
 }
@@ -312,17 +365,16 @@ pctree_status pctree_kv_append(const pctree_append_config* cfg, const void* q, c
   // runs of heads: as many warps as the SMs hold while rows are few, whole
   // rows (one set of sines and cosines) once there are enough of them
   const int heads = c.Hq + 2 * c.Hkv, groups = 512 / c.D;
-  const long long warps = static_cast<long long>(num_sms) * kAppendWarps * 4;
-  long long parts = warps / c.total_rows;
+  const long long warps = static_cast<long long>(num_sms) * kAppendWarps * kAppendCtas;
+  long long parts = (warps + c.total_rows - 1) / c.total_rows;
   const int most = (heads + groups - 1) / groups;
-  if (parts < 1) parts = 1;
   if (parts > most) parts = most;
   a.heads_per_part = (heads + static_cast<int>(parts) - 1) / static_cast<int>(parts);
   a.heads_per_part = (a.heads_per_part + groups - 1) / groups * groups;
   a.parts = (heads + a.heads_per_part - 1) / a.heads_per_part;
   const long long items = static_cast<long long>(c.total_rows) * a.parts;
   long long blocks = (items + kAppendWarps - 1) / kAppendWarps;
-  if (blocks > num_sms * 4ll) blocks = num_sms * 4ll;
+  if (blocks > num_sms * kAppendCtas) blocks = num_sms * kAppendCtas;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
