@@ -186,7 +186,7 @@ __device__ __forceinline__ void light_weights(const SampleShared* S, const RowFa
   w1 = (((static_cast<unsigned long long>(v1) << 15) >> (n1 >> 7)) + 1) >> 1;
 }
 
-__device__ __forceinline__ unsigned long long fine_weight(const RowFacts& f, float x) {
+__device__ __noinline__ unsigned long long fine_weight(const RowFacts& f, float x) {
   const float ph = x * f.c_hi;
   const float pl = fmaf(x, f.c_lo, fmaf(x, f.c_hi, -ph));
   const float kf = rintf(ph);
@@ -252,6 +252,14 @@ struct Elem<PCTREE_F32> {
   static __device__ __forceinline__ uint4 low_vec() {
     return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
   }
+  // the largest of a vector's elements and `m` (NaN if any is)
+  using Max = float;
+  static __device__ __forceinline__ Max none() { return -INFINITY; }
+  static __device__ __forceinline__ Max larger(const uint4& v, Max m) {
+    m = max_nan(m, __uint_as_float(v.x), __uint_as_float(v.y));
+    return max_nan(m, __uint_as_float(v.z), __uint_as_float(v.w));
+  }
+  static __device__ __forceinline__ float value(Max m) { return m; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x);
     x[1] = __uint_as_float(v.y);
@@ -267,6 +275,22 @@ struct Elem16 {
   static __device__ __forceinline__ uint4 low_vec() {
     constexpr uint32_t two = F16 ? 0xfc00fc00u : 0xff80ff80u;
     return make_uint4(two, two, two, two);
+  }
+  // (pairs: even and odd elements)
+  using Max = uint32_t;
+  static __device__ __forceinline__ Max none() { return low_vec().x; }
+  static __device__ __forceinline__ Max max2(Max a, Max b) {
+    Max r;
+    if constexpr (F16) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ Max larger(const uint4& v, Max m) {
+    return max2(max2(max2(v.x, v.y), max2(v.z, v.w)), m);
+  }
+  static __device__ __forceinline__ float value(Max m) {
+    const float2 p = unpack16<F16>(m);
+    return max_nan(p.x, p.y);
   }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -417,35 +441,39 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   const uint4* vec = STREAM ? reinterpret_cast<const uint4*>(src)
                             : reinterpret_cast<const uint4*>(data);
   const int first = e0 - pad;                               // row index of data[0]
-  // body_fn(x, row index of x[0]) over the lane's vectors, `ahead` loads in
-  // flight; lanes past the run's end get -inf, so the warp stays together
-  constexpr std::integral_constant<int, 4> kFar{};          // little work per vector
-  constexpr std::integral_constant<int, 2> kNear{};
-  constexpr std::integral_constant<int, 1> kNext{};
-  auto pass = [&](auto ahead, auto&& body_fn) {
-    constexpr int kAhead = STREAM ? decltype(ahead)::value : 1;
-    for (int vb = v0; vb < v1; vb += 32 * kAhead) {
-      uint4 raw[kAhead];
+  // fn(vector, row index of its first element) over the lane's vectors; lanes
+  // past the run's end get -inf, so the warp stays together.  Little work per
+  // vector (kFar): several loads, then their work; else the next load ahead of
+  // the work and one copy of it (unrolled heavy passes waited for instructions).
+  constexpr std::true_type kFar{};
+  constexpr std::false_type kNear{};
+  auto pass = [&](auto far, auto&& fn) {
+    auto load = [&](int v) { return v < v1 ? vec[v] : E::low_vec(); };
+    if constexpr (decltype(far)::value && STREAM) {
+      constexpr int kAhead = 6;
+#pragma unroll 1
+      for (int vb = v0; vb < v1; vb += 32 * kAhead) {
+        uint4 raw[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int v = vb + i * 32 + lane;
-        raw[i] = v < v1 ? vec[v] : E::low_vec();
+        for (int i = 0; i < kAhead; ++i) raw[i] = load(vb + i * 32 + lane);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fn(raw[i], first + (vb + i * 32 + lane) * kVec);
       }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        float x[kVec];
-        E::unpack(raw[i], x);
-        body_fn(x, first + (vb + i * 32 + lane) * kVec);
+    } else {
+      uint4 next = load(v0 + lane);
+#pragma unroll 1
+      for (int vb = v0; vb < v1; vb += 32) {
+        const uint4 now = next;
+        next = load(vb + 32 + lane);
+        fn(now, first + (vb + lane) * kVec);
       }
     }
   };
 
   // ---------------- maximum ----------------
-  float m = -INFINITY;
-  pass(kFar, [&](const float (&x)[kVec], int) {
-#pragma unroll
-    for (int e = 0; e < kVec; e += 2) m = max_nan(m, x[e], x[e + 1]);
-  });
+  typename E::Max largest = E::none();
+  pass(kFar, [&](const uint4& raw, int) { largest = E::larger(raw, largest); });
+  float m = E::value(largest);
   if (!landed) m = __int_as_float(0x7fc00000);
   const float m1 = m;
 #pragma unroll
@@ -480,7 +508,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   if (temp == 0.0f) {                                       // the lowest index of the maximum
     int at = 0x7fffffff;
     if (__any_sync(kFull, m8 == m)) {                       // in this warp's run
-      pass(kFar, [&](const float (&x)[kVec], int i0) {
+      pass(kFar, [&](const uint4& raw, int i0) {
+        if (E::value(E::larger(raw, E::none())) != m) return;
+        float x[kVec];
+        E::unpack(raw, x);
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
           if (x[e] == m) at = min(at, i0 + e);
@@ -549,7 +580,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   unsigned long long all_w = 0, mine = 0;
   auto sum_all = [&]() {
     mine = 0;
-    pass(kNear, [&](const float (&x)[kVec], int) {
+    pass(kNear, [&](const uint4& raw, int) {
+      float x[kVec];
+      E::unpack(raw, x);
 #pragma unroll
       for (int e = 0; e < kVec; e += 2) {
         unsigned long long w0, w1;
@@ -561,11 +594,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     f.fine_from =
         fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * 128.0f / f.c_hi);
     if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
-      pass(kFar, [&](const float (&x)[kVec], int) {
-        float top = x[0];
-#pragma unroll
-        for (int e = 1; e < kVec; ++e) top = fmaxf(top, x[e]);
-        if (top - f.base >= f.fine_from) {
+      pass(kFar, [&](const uint4& raw, int) {
+        if (E::value(E::larger(raw, E::none())) - f.base >= f.fine_from) {
+          float x[kVec];
+          E::unpack(raw, x);
 #pragma unroll
           for (int e = 0; e < kVec; ++e) {
             const float z = x[e] - f.base;
@@ -634,11 +666,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     if (by_m && (group_lanes == 0 || !by_p)) from = fmaxf(from, f.min_z);
     unsigned mine_n = 0;
     if (__any_sync(kFull, m1 >= from)) {                    // some in this warp's run
-      pass(kFar, [&](const float (&x)[kVec], int i0) {
-        float top = x[0];
-#pragma unroll
-        for (int e = 1; e < kVec; ++e) top = fmaxf(top, x[e]);
-        if (top >= from) {
+      pass(kFar, [&](const uint4& raw, int i0) {
+        if (E::value(E::larger(raw, E::none())) >= from) {
+          float x[kVec];
+          E::unpack(raw, x);
           unsigned hits = 0;
 #pragma unroll
           for (int e = 0; e < kVec; ++e)
@@ -757,6 +788,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     sum_all();
   }
   unsigned long long border = 0;                            // keep keys >= border
+  bool summed = true;                                       // `mine` is of what is kept
   if (by_k || by_p) {
     // top-p alone: as many octaves as tokens below them cannot reach half of
     // 1 - top_p of the weight, were all of them that heavy
@@ -781,7 +813,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     const unsigned long long slack = (unit_total >> 18) + a.V / 2 + 4096;
     for (int i = tid; i < 2 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
     __syncthreads();
-    pass(kNear, [&](const float (&x)[kVec], int) {
+    pass(kNear, [&](const uint4& raw, int) {
+      float x[kVec];
+      E::unpack(raw, x);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const float z = x[e] - f.base;
@@ -848,7 +882,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       const unsigned b0 = static_cast<unsigned>(S->bin0), b1 = static_cast<unsigned>(S->bin1);
       unsigned long long above_w = 0;
       unsigned above = 0;
-      pass(kNext, [&](const float (&x)[kVec], int i0) {
+      pass(kNear, [&](const uint4& raw, int i0) {
+        float x[kVec];
+        E::unpack(raw, x);
         unsigned up = 0, in = 0;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
@@ -874,6 +910,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           }
         }
       });
+      mine = above_w;
       above_w = cluster_total(above_w);
       const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
       const unsigned n = L->list_n;
@@ -896,7 +933,20 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         }
       }
       csync<STREAM>();
-      if (S->found != 0) return;
+      if (S->found != 0) {
+        // this warp's share of the bins' kept keys
+        const unsigned long long least = S->border;
+        for (unsigned i = lane; i < n; i += 32) {
+          const unsigned long long key = L->list.key[i];
+          // (a run's vectors reach past the slice's ends)
+          const int at = static_cast<int>(0xffffffffu - static_cast<unsigned>(key));
+          if (key >= least && at >= max(e0, first + v0 * kVec) &&
+              at < min(e0 + n_el, first + v1 * kVec))
+            mine += L->list.w[i];
+        }
+        return;
+      }
+      summed = false;
       // too many keys in the bins: K* bit by bit, the largest key whose head
       // reaches the target
       unsigned long long key = 0, key_w = 0;
@@ -904,7 +954,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         const unsigned long long trial = key | (1ull << bit);
         unsigned long long hw = 0;
         unsigned hn = 0;
-        pass(kNext, [&](const float (&x)[kVec], int i0) {
+        pass(kNear, [&](const uint4& raw, int i0) {
+          float x[kVec];
+          E::unpack(raw, x);
           unsigned up = 0;
 #pragma unroll
           for (int e = 0; e < kVec; ++e)
@@ -950,7 +1002,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   }
   if (by_m) {
     const unsigned long long least = order_key(f.min_z, 0x7fffffff);
-    border = least > border ? least : border;
+    if (least > border) {
+      border = least;
+      summed = false;
+    }
   }
 
   // ---------------- draw ----------------
@@ -960,9 +1015,11 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   auto kept = [&](float z, int index) {
     return z > border_z || (z == border_z && order_key(z, index) >= border);
   };
-  if (border != 0) {
+  if (!summed) {
     mine = 0;
-    pass(kNext, [&](const float (&x)[kVec], int i0) {
+    pass(kNear, [&](const uint4& raw, int i0) {
+      float x[kVec];
+      E::unpack(raw, x);
       unsigned keep = 0;
 #pragma unroll
       for (int e = 0; e < kVec; ++e) keep |= (kept(x[e], i0 + e) ? 1u : 0u) << e;
