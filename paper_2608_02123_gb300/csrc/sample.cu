@@ -44,9 +44,9 @@ constexpr int kSmpThreads = 512;
 constexpr int kSmpWarps = kSmpThreads / 32;
 constexpr int kSmpMaxCluster = 8;
 constexpr int kSmpBins = 512;
-constexpr int kSmpList = 512;               // gathered keys of a bin
-constexpr int kSmpGroups = kSmpThreads / 8; // groups of eight lanes per CTA
-constexpr int kSmpCand = 832;               // candidates one CTA can rank
+constexpr int kSmpList = 384;               // gathered keys of a bin
+constexpr int kSmpMaxGroups = 512;          // groups of lanes whose maxima are ranked
+constexpr int kSmpCand = 640;               // candidates one CTA can rank
 constexpr int kSmpMaxV = 1 << 18;           // sums of 2^45-scaled weights fit 64 bits
 constexpr int kOctaves = 46;                // below the largest: weight 0
 constexpr float kMagic = 12582912.0f;       // 1.5 * 2^23: adds as round to integer
@@ -107,7 +107,7 @@ struct alignas(16) SampleShared {
   uint64_t bar;
   RowFacts row;
   float warp_max[kSmpMaxCluster * kSmpWarps];       // of every warp of the cluster
-  alignas(16) float group_max[kSmpMaxCluster * kSmpGroups];   // of every 8 lanes, or thread
+  float group_max[kSmpMaxGroups];           // of every group of lanes
   float from;                               // logits from it on are candidates
   int cta_first[kSmpMaxCluster];            // lowest index of the maximum (T = 0)
   unsigned cta_n[kSmpMaxCluster];           // candidates of every CTA
@@ -132,6 +132,7 @@ struct alignas(16) SampleShared {
       };
     };
   };
+  float pending[kSmpWarps][64];             // logits of a warp, until 32 are together
   uint2 tab[128][16];                       // light table, a column per lane pair
 };
 
@@ -336,6 +337,15 @@ __device__ __forceinline__ void weights(const SampleShared* S, const RowFacts& f
   }
 }
 
+__device__ __forceinline__ unsigned long long weight(const SampleShared* S, const RowFacts& f,
+                                                     float x) {
+  const float z = x - f.base;
+  if (z >= f.fine_from) return fine_weight(f, z);
+  unsigned long long w, same;
+  light_weights(S, f, fmaxf(z, f.low), fmaxf(z, f.low), w, same);
+  return w;
+}
+
 template <int DT, bool STREAM>
 __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   using E = Elem<DT>;
@@ -405,12 +415,19 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   const bool params_ok = (temp == 0.0f || (temp >= 1e-6f && temp <= 1e6f)) && top_p > 0.0f &&
                          min_p >= 0.0f && min_p <= 1.0f && u >= 0.0f && u < 1.0f;
   const bool by_k = top_k > 0 && top_k < a.V, by_p = top_p < 1.0f, by_m = min_p > 0.0f;
-  // lanes per group of the maxima that bound the top_k-th logit (0: too many)
-  const int group_lanes = !by_k || temp == 0.0f              ? 0
-                          : top_k <= n_cta * kSmpWarps / 2   ? 32
-                          : top_k <= n_cta * kSmpGroups * 3 / 4 ? 8
-                          : STREAM && top_k <= kSmpThreads * 3 / 4 ? 1
-                                                                : 0;
+  // lanes per group of the maxima that bound the top_k-th logit (0: too many):
+  // of G groups in the row, about -G ln(1 - top_k / G) logits reach the
+  // top_k-th largest maximum
+  int group_lanes = 0;
+  if (by_k && temp > 0.0f) {
+#pragma unroll
+    for (int lanes = 1; lanes <= 32; lanes *= 2) {
+      const int groups = n_cta * (kSmpThreads / lanes);
+      if (groups <= kSmpMaxGroups &&
+          top_k <= (groups <= 128 ? groups / 16 * 15 : groups / 8 * 5))
+        group_lanes = lanes;
+    }
+  }
   const bool few = group_lanes != 0 || (by_m && (!by_k || !by_p));
   // the scale, and min_p's border below the maximum (one thread: 64-bit
   // arithmetic of a whole CTA would take longer than a pass over the row)
@@ -447,8 +464,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   // the work and one copy of it (unrolled heavy passes waited for instructions).
   constexpr std::true_type kFar{};
   constexpr std::false_type kNear{};
-  auto pass = [&](auto far, auto&& fn) {
-    auto load = [&](int v) { return v < v1 ? vec[v] : E::low_vec(); };
+  auto pass = [&](auto far, auto&& fn, bool reads = true) { // reads: else the lane gets -inf
+    auto load = [&](int v) { return v < v1 && reads ? vec[v] : E::low_vec(); };
     if constexpr (decltype(far)::value && STREAM) {
       constexpr int kAhead = 6;
 #pragma unroll 1
@@ -476,19 +493,20 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   float m = E::value(largest);
   if (!landed) m = __int_as_float(0x7fc00000);
   const float m1 = m;
+  float mg = m;                                             // of this lane's group
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
-  const float m8 = m;
-#pragma unroll
-  for (int o = 8; o < 32; o <<= 1) m = max_nan(m, __shfl_xor_sync(kFull, m, o));
+  for (int o = 1; o < 32; o <<= 1) {
+    m = max_nan(m, __shfl_xor_sync(kFull, m, o));
+    if (2 * o == group_lanes) mg = m;
+  }
+  const float mw = m;                                       // of this warp's run
   // every CTA of the cluster has started before its memory is written
   if constexpr (!STREAM) csync<STREAM>();
-  if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->warp_max[rank * kSmpWarps + warp] = m;
-  if (group_lanes == 8) {
-    for (int i = lane & 7; i < n_cta; i += 8)
-      cluster_ptr<STREAM>(S, i)->group_max[rank * kSmpGroups + warp * 4 + (lane >> 3)] = m8;
-  } else if (group_lanes == 1) {
-    S->group_max[tid] = m1;
+  if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->warp_max[rank * kSmpWarps + warp] = mw;
+  const int own_group = group_lanes == 0 ? 0 : (rank * kSmpThreads + tid) / group_lanes;
+  if (group_lanes != 0 && group_lanes != 32) {
+    for (int r = lane & (group_lanes - 1); r < n_cta; r += group_lanes)
+      cluster_ptr<STREAM>(S, r)->group_max[own_group] = mg;
   }
   csync<STREAM>();
   m = -INFINITY;
@@ -507,7 +525,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   }
   if (temp == 0.0f) {                                       // the lowest index of the maximum
     int at = 0x7fffffff;
-    if (__any_sync(kFull, m8 == m)) {                       // in this warp's run
+    if (mw == m) {                                          // in this warp's run
       pass(kFar, [&](const uint4& raw, int i0) {
         if (E::value(E::larger(raw, E::none())) != m) return;
         float x[kVec];
@@ -621,7 +639,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   if (few) {
     float from = -INFINITY;
     if (group_lanes == 32) {
-      const int n = n_cta * kSmpWarps, i = tid >> 2;        // four threads a maximum
+      // every CTA ranks all warps' maxima, four threads each
+      const int n = n_cta * kSmpWarps, i = tid >> 2;
       const float x = i < n ? S->warp_max[i] : -INFINITY;
       int ahead = 0;
       for (int j = tid & 3; j < n; j += 4) {
@@ -633,33 +652,18 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       if (i < n && (tid & 3) == 0 && ahead == top_k - 1) S->from = x;
       __syncthreads();
       from = S->from;
-    } else if (group_lanes == 8) {
-      // each CTA ranks its own groups: eight threads a maximum
-      const int n = n_cta * kSmpGroups, i = rank * kSmpGroups + (tid >> 3);
-      const float x = S->group_max[i];
+    } else if (group_lanes != 0) {
+      // a group's lanes rank its maximum, for all CTAs
+      const int n = n_cta * (kSmpThreads / group_lanes);
       int ahead = 0;
-      for (int j = tid & 7; j < n; j += 8) {
+      for (int j = lane & (group_lanes - 1); j < n; j += group_lanes) {
         const float y = S->group_max[j];
-        ahead += y > x || (y == x && j < i) ? 1 : 0;
+        ahead += y > mg || (y == mg && j < own_group) ? 1 : 0;
       }
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) ahead += __shfl_xor_sync(kFull, ahead, o);
-      if ((tid & 7) == 0 && ahead == top_k - 1)
-        for (int r = 0; r < n_cta; ++r) cluster_ptr<STREAM>(S, r)->from = x;
+      for (int o = 1; o < group_lanes; o <<= 1) ahead += __shfl_xor_sync(kFull, ahead, o);
+      if ((lane & (group_lanes - 1)) == 0 && ahead == top_k - 1)
+        for (int r = 0; r < n_cta; ++r) cluster_ptr<STREAM>(S, r)->from = mg;
       csync<STREAM>();
-      from = S->from;
-    } else if (group_lanes == 1) {
-      const float x = m1;
-      int ahead = 0;
-      for (int j = 0; j < kSmpThreads; j += 4) {
-        const float4 y = *reinterpret_cast<const float4*>(&S->group_max[j]);
-        ahead += (y.x > x || (y.x == x && j < tid) ? 1 : 0) +
-                 (y.y > x || (y.y == x && j + 1 < tid) ? 1 : 0) +
-                 (y.z > x || (y.z == x && j + 2 < tid) ? 1 : 0) +
-                 (y.w > x || (y.w == x && j + 3 < tid) ? 1 : 0);
-      }
-      if (ahead == top_k - 1) S->from = x;
-      __syncthreads();
       from = S->from;
     }
     // (top_p needs the weight of all that top_k leaves)
@@ -686,7 +690,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
               }
           }
         }
-      });
+      }, m1 >= from);
     }
     mine_n = __reduce_add_sync(kFull, mine_n);
     if (lane == 0 && mine_n != 0) atomicAdd(&S->local_n, mine_n);
@@ -879,9 +883,13 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     // K* of `target` (a count, or an exact weight) and the weight of its head,
     // once its bins are known
     auto resolve = [&](unsigned long long target, bool by_weight) {
-      const unsigned b0 = static_cast<unsigned>(S->bin0), b1 = static_cast<unsigned>(S->bin1);
+      // bin < b0 is above, b0 <= bin <= b1 in the list
+      const float to_b0 = 8388608.0f + static_cast<float>(S->bin0);
+      const float to_b1 = 8388608.0f + static_cast<float>(S->bin1);
       unsigned long long above_w = 0;
       unsigned above = 0;
+      int waiting = 0;                                      // logits in `pending`
+      float* pending = S->pending[warp];
       pass(kNear, [&](const uint4& raw, int i0) {
         float x[kVec];
         E::unpack(raw, x);
@@ -889,27 +897,53 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const float z = x[e] - f.base;
-          const unsigned b = bin_of(z);
-          const bool live = z >= f.cut;
-          up |= (live && b < b0 ? 1u : 0u) << e;
-          in |= (live && b >= b0 && b <= b1 ? 1u : 0u) << e;
+          const float t = fmaf(f.m - z, bin_scale, 8388608.0f);      // as bin_of
+          up |= (t < to_b0 ? 1u : 0u) << e;
+          in |= (t >= to_b0 && t <= to_b1 ? 1u : 0u) << e;
         }
-        if (!__any_sync(kFull, (up | in) != 0)) return;
-        unsigned long long w[kVec];
-        weights(S, f, x, w);
+        if (in != 0) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            if (((in >> e) & 1u) && x[e] - f.base >= f.cut) {
+              const unsigned at = atomicAdd(&L->list_n, 1u);
+              if (at < kSmpList) {
+                L->list.key[at] = order_key(x[e], i0 + e);
+                L->list.w[at] = weight(S, f, x[e]);
+              }
+            }
+        }
+        __syncwarp();
+        const unsigned n_up = __reduce_add_sync(kFull, __popc(up));
+        if (n_up == 0) return;
         above += __popc(up);
+        if (n_up > 16 * kVec) {                             // many: all of the vector
+          unsigned long long w[kVec];
+          weights(S, f, x, w);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) above_w += (up >> e) & 1u ? w[e] : 0ull;
+          return;
+        }
+        // few: gathered until every lane has one
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          above_w += (up >> e) & 1u ? w[e] : 0ull;
-          if ((in >> e) & 1u) {
-            const unsigned at = atomicAdd(&L->list_n, 1u);
-            if (at < kSmpList) {
-              L->list.key[at] = order_key(x[e], i0 + e);
-              L->list.w[at] = w[e];
-            }
+          const bool mine_up = (up >> e) & 1u;
+          const unsigned who = __ballot_sync(kFull, mine_up);
+          if (who == 0) continue;
+          if (mine_up) pending[waiting + __popc(who & ((1u << lane) - 1u))] = x[e];
+          waiting += __popc(who);
+          if (waiting >= 32) {
+            __syncwarp();
+            above_w += weight(S, f, pending[lane]);
+            const float rest = pending[32 + lane];
+            __syncwarp();
+            pending[lane] = rest;
+            waiting -= 32;
           }
         }
+        __syncwarp();
       });
+      __syncwarp();
+      if (lane < waiting) above_w += weight(S, f, pending[lane]);
       mine = above_w;
       above_w = cluster_total(above_w);
       const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
