@@ -2,7 +2,7 @@
 // random numbers, with temperature, top-k, top-p and min-p.
 //
 // Two placements of a row, the same code:
-//   cluster  (few rows) a row belongs to up to eight CTAs, each of which keeps
+//   cluster  (few rows) a row belongs to up to 16 CTAs, each of which keeps
 //            its slice in shared memory: logits are read once, and the CTAs'
 //            results meet through distributed shared memory;
 //   stream   (many rows) a row belongs to one CTA, which reads it from memory
@@ -42,7 +42,7 @@ namespace {
 
 constexpr int kSmpThreads = 512;
 constexpr int kSmpWarps = kSmpThreads / 32;
-constexpr int kSmpMaxCluster = 8;
+constexpr int kSmpMaxCluster = 16;
 constexpr int kSmpBins = 512;
 constexpr int kSmpList = 384;               // gathered keys of a bin
 constexpr int kSmpMaxGroups = 512;          // groups of lanes whose maxima are ranked
@@ -116,7 +116,7 @@ struct alignas(16) SampleShared {
   unsigned long long border, border_w;      // K* and the weight of its head
   int found;
   unsigned list_n, local_n;
-  unsigned long long part[kSmpMaxCluster];
+  unsigned long long part[2][kSmpMaxCluster];
   unsigned long long red[kSmpWarps];
   union {
     struct {                                // one CTA's candidates
@@ -145,6 +145,14 @@ __device__ __forceinline__ T* cluster_ptr(T* p, int rank) {
     asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
     return reinterpret_cast<T*>(r);
   }
+}
+
+// The two halves of csync below.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Barrier of the row's CTAs, with the warp's lanes together.
@@ -203,11 +211,15 @@ __device__ __noinline__ unsigned long long fine_weight(const RowFacts& f, float 
   const int n = static_cast<int>(kf) - f.k;
   const int j = n & 127;
   const float th = kPow2.hi[j], tl = kPow2.lo[j];
+  // th + q + rest in units of 2^-45: th's bits, q in units of 2^-30 and what is
+  // left
   const float q = th * yh;
-  const float rest = fmaf(th, yh, -q) + fmaf(th, sl, tl);
-  const float unit = 35184372088832.0f;                     // 2^45
-  const long long w = __float2ll_rn(th * unit) + __float2ll_rn(q * unit) +
-                      __float2ll_rn(rest * unit);
+  const int qi = __float2int_rn(q * 1073741824.0f);
+  const float rest = fmaf(static_cast<float>(qi), -1.0f / 1073741824.0f, q) +
+                     (fmaf(th, yh, -q) + fmaf(th, sl, tl));
+  const long long w =
+      (static_cast<long long>((__float_as_uint(th) & 0x7fffffu) | 0x800000u) << 22) +
+      (static_cast<long long>(qi) << 15) + __float2int_rn(rest * 35184372088832.0f);
   const int sh = -(n >> 7);
   return (static_cast<unsigned long long>(w) + ((1ull << sh) >> 1)) >> sh;
 }
@@ -383,6 +395,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   const int head = pad == 0 ? 0 : min(n_el, kVec - pad);
   const int body = STREAM ? 0 : (n_el - head) / kVec;       // whole vectors
   __syncthreads();
+  if constexpr (!STREAM) cluster_arrive();                  // this CTA has started
   if constexpr (!STREAM) {
     if (tid == 0 && body > 0) {
       mbar_arrive_expect_tx(&S->bar, static_cast<uint32_t>(body) * 16u);
@@ -429,6 +442,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     }
   }
   const bool few = group_lanes != 0 || (by_m && (!by_k || !by_p));
+  const float octave = temp * 0.693147181f;                 // of weight, in logits
   // the scale, and min_p's border below the maximum (one thread: 64-bit
   // arithmetic of a whole CTA would take longer than a pass over the row)
   double c = 1.0, below = 0.0;
@@ -501,7 +515,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   }
   const float mw = m;                                       // of this warp's run
   // every CTA of the cluster has started before its memory is written
-  if constexpr (!STREAM) csync<STREAM>();
+  if constexpr (!STREAM) {
+    __syncwarp();
+    cluster_wait();
+  }
   if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->warp_max[rank * kSmpWarps + warp] = mw;
   const int own_group = group_lanes == 0 ? 0 : (rank * kSmpThreads + tid) / group_lanes;
   if (group_lanes != 0 && group_lanes != 32) {
@@ -562,8 +579,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     f.base = fabsf(m) * f.c_hi > 16384.0f ? m : 0.0f;
     f.m = m - f.base;
     f.k = __float_as_int(fmaf(f.m, f.c_hi, kMagic)) - 0x4b400000;
-    f.cut = f.m - kOctaves * 128.0f / f.c_hi;
-    f.low = f.m - 60.0f * 128.0f / f.c_hi;
+    f.cut = f.m - kOctaves * octave;
+    f.low = f.m - 60.0f * octave;
     f.fine_from = f.cut;
     f.min_z = -INFINITY;
     if (by_m) {
@@ -578,19 +595,21 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   __syncthreads();
   RowFacts f = S->row;
 
-  // sums the cluster's values (one per thread) for everyone
+  // sums the cluster's values (one per thread) for everyone; the next sum but
+  // one writes the same words, with a barrier in between
+  int sums = 0;
   auto cluster_total = [&](unsigned long long v) -> unsigned long long {
+    unsigned long long* part = S->part[sums++ & 1];
     v = warp_sum64(v);
     if (lane == 0) S->red[warp] = v;
     __syncthreads();
     if (warp == 0) {
       v = warp_sum64(lane < kSmpWarps ? S->red[lane] : 0ull);
-      if (lane < n_cta) cluster_ptr<STREAM>(S, lane)->part[rank] = v;
+      if (lane < n_cta) cluster_ptr<STREAM>(part, lane)[rank] = v;
     }
     csync<STREAM>();
     unsigned long long t = 0;
-    for (int r = 0; r < n_cta; ++r) t += S->part[r];
-    csync<STREAM>();                                        // part may be written again
+    for (int r = 0; r < n_cta; ++r) t += part[r];
     return t;
   };
   // the weight of the whole row: light weights of all, then the fine form of
@@ -610,7 +629,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     });
     const unsigned long long rough = cluster_total(mine);
     f.fine_from =
-        fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * 128.0f / f.c_hi);
+        fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * octave);
     if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
       pass(kFar, [&](const uint4& raw, int) {
         if (E::value(E::larger(raw, E::none())) - f.base >= f.fine_from) {
@@ -628,7 +647,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         }
       });
     }
-    all_w = cluster_total(mine);
+    if (by_k || by_p) all_w = cluster_total(mine);          // else the draw adds up
   };
   if (all_light) sum_all();
 
@@ -639,17 +658,16 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   if (few) {
     float from = -INFINITY;
     if (group_lanes == 32) {
-      // every CTA ranks all warps' maxima, four threads each
-      const int n = n_cta * kSmpWarps, i = tid >> 2;
+      // every CTA ranks all warps' maxima (16 to 256), 32 to 2 threads each
+      const int n = n_cta * kSmpWarps, split = kSmpThreads / n, i = tid / split;
       const float x = i < n ? S->warp_max[i] : -INFINITY;
       int ahead = 0;
-      for (int j = tid & 3; j < n; j += 4) {
+      for (int j = tid % split; j < n; j += split) {
         const float y = S->warp_max[j];
         ahead += y > x || (y == x && j < i) ? 1 : 0;
       }
-      ahead += __shfl_xor_sync(kFull, ahead, 1);
-      ahead += __shfl_xor_sync(kFull, ahead, 2);
-      if (i < n && (tid & 3) == 0 && ahead == top_k - 1) S->from = x;
+      for (int o = 1; o < split; o <<= 1) ahead += __shfl_xor_sync(kFull, ahead, o);
+      if (i < n && tid % split == 0 && ahead == top_k - 1) S->from = x;
       __syncthreads();
       from = S->from;
     } else if (group_lanes != 0) {
@@ -833,7 +851,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     });
     csync<STREAM>();
     // each CTA adds up a share of the bins, for the leader
-    constexpr int share = kSmpBins / kSmpMaxCluster;
+    constexpr int share = kSmpBins / 16;
     for (int i = rank * share + tid; i < kSmpBins; i += kSmpThreads) {
       // (a CTA takes every n_cta-th share)
       const int s = i / share;
@@ -947,8 +965,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       mine = above_w;
       above_w = cluster_total(above_w);
       const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
-      const unsigned n = L->list_n;
-      csync<STREAM>();
+      const unsigned n = S->list_n;                         // (the leader's counts)
       if (rank == 0 && n <= kSmpList && tid < n) {
         const unsigned long long key = S->list.key[tid], own = S->list.w[tid];
         unsigned long long hn = above_n, hw = above_w;      // up to and with this key
@@ -962,7 +979,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
             SampleShared* R = cluster_ptr<STREAM>(S, r);
             R->border = key;
             R->border_w = hw;
-            R->found = 1;
+            R->found = static_cast<int>(n);
           }
         }
       }
@@ -970,7 +987,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       if (S->found != 0) {
         // this warp's share of the bins' kept keys
         const unsigned long long least = S->border;
-        for (unsigned i = lane; i < n; i += 32) {
+        for (int i = lane; i < S->found; i += 32) {
           const unsigned long long key = L->list.key[i];
           // (a run's vectors reach past the slice's ends)
           const int at = static_cast<int>(0xffffffffu - static_cast<unsigned>(key));
@@ -1146,6 +1163,51 @@ template <int DT, bool STREAM>
 const void* sample_fn() {
   return reinterpret_cast<const void*>(sample_kernel<DT, STREAM>);
 }
+const void* sample_fn(int dtype, bool streamed) {
+  return dtype == PCTREE_F32
+             ? (streamed ? sample_fn<PCTREE_F32, true>() : sample_fn<PCTREE_F32, false>())
+         : dtype == PCTREE_BF16
+             ? (streamed ? sample_fn<PCTREE_BF16, true>() : sample_fn<PCTREE_BF16, false>())
+             : (streamed ? sample_fn<PCTREE_F16, true>() : sample_fn<PCTREE_F16, false>());
+}
+
+constexpr size_t kSampleSmem = sizeof(SampleShared) + (kSmpMaxV / 8 + 8) * 4;
+static_assert(kSampleSmem <= 227 * 1024 && kSampleSmem >= 120 * 1024, "shared memory per CTA");
+
+// Whether clusters of 16 CTAs (more than is portable) fit on the current
+// device; asked once per device and type.
+bool wide_clusters(int dtype) {
+  static std::mutex mu;
+  static signed char known[64][3];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  std::lock_guard<std::mutex> lk(mu);
+  signed char& k = known[dev][dtype];
+  if (k == 0) {
+    const void* fn = sample_fn(dtype, false);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 16;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(16);
+    lc.blockDim = dim3(kSmpThreads);
+    lc.dynamicSmemBytes = sizeof(SampleShared) + (kSmpMaxV / 16 + 8) * 4;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    int clusters = 0;
+    const bool fits =
+        cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(kSampleSmem)) == cudaSuccess &&
+        cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) ==
+            cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&clusters, fn, &lc) == cudaSuccess && clusters > 0;
+    if (!fits) (void)cudaGetLastError();
+    k = fits ? 1 : -1;
+  }
+  return k > 0;
+}
 
 }  // namespace
 }  // namespace pct
@@ -1178,7 +1240,8 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   const int per_sm = row_bytes * 2 * num_sms <= kStreamBytes ? 2 : 1;
   const bool streamed = aligned && row_bytes * num_sms <= kStreamBytes &&
                         c.rows >= num_sms * per_sm;
-  // cluster: slices of at least 8 KB, up to eight of them
+  // cluster: slices of at least 8 KB, up to eight of them, 16 while the SMs
+  // have room
   int ctas = 1;
   SampleArgs a{};
   size_t bytes = sizeof(SampleShared);
@@ -1186,7 +1249,12 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
     a.slice = c.V;
     if (per_sm == 1) bytes = 120 * 1024;                    // keeps a second CTA off the SM
   } else {
-    while (ctas < kSmpMaxCluster && row_bytes > ctas * 8192ull) ctas *= 2;
+    const int most = c.rows * 16ll <= num_sms && wide_clusters(c.dtype) ? 16 : 8;
+    while (ctas < most && row_bytes > ctas * 8192ull) ctas *= 2;
+    // fewer where that keeps all rows on the GPU at once, two CTAs an SM
+    while (ctas > 1 && static_cast<long long>(c.rows) * ctas > 2 * num_sms &&
+           row_bytes <= ctas / 2 * 78000ull)
+      ctas /= 2;
     a.slice = ((c.V + ctas - 1) / ctas + vec - 1) / vec * vec;
     ctas = (c.V + a.slice - 1) / a.slice;
     bytes += static_cast<size_t>(a.slice + 2 * vec) * el;
@@ -1203,15 +1271,9 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   a.row_stride = c.row_stride;
   a.V = c.V;
   a.group = c.group;
-  const void* fn =
-      c.dtype == PCTREE_F32 ? (streamed ? sample_fn<PCTREE_F32, true>() : sample_fn<PCTREE_F32, false>())
-      : c.dtype == PCTREE_BF16
-          ? (streamed ? sample_fn<PCTREE_BF16, true>() : sample_fn<PCTREE_BF16, false>())
-          : (streamed ? sample_fn<PCTREE_F16, true>() : sample_fn<PCTREE_F16, false>());
-  constexpr size_t kMost = sizeof(SampleShared) + (kSmpMaxV / kSmpMaxCluster + 8) * 4;
-  static_assert(kMost <= 227 * 1024 && kMost >= 120 * 1024, "shared memory per CTA");
+  const void* fn = sample_fn(c.dtype, streamed);
   static SmemLimit limits[2][3];
-  if (limits[streamed][c.dtype].ensure(fn, kMost) != cudaSuccess) return PCTREE_ERR_CUDA;
+  if (limits[streamed][c.dtype].ensure(fn, kSampleSmem) != cudaSuccess) return PCTREE_ERR_CUDA;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
