@@ -88,7 +88,8 @@ struct Tail {
   Item item[kItemRing];
   float row_l[2][128], row_m[2][128];
   alignas(16) uint8_t stage[4][32 * 64];
-  long long upto[PCTREE_KV_MAX_BATCH];       // work of requests 0 .. r
+  unsigned upto[PCTREE_KV_MAX_BATCH];        // work of requests 0 .. r (the host checks the sum)
+  int start[PCTREE_KV_MAX_BATCH], n[PCTREE_KV_MAX_BATCH], prefix[PCTREE_KV_MAX_BATCH];
 };
 
 // Blocks that hold the keys 0 .. end-1, the first key of block b, and the keys
@@ -199,29 +200,36 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   if (warp == 1) tmem_alloc(&T->tmem_base, kTmemCols);
   pdl_launch_dependents();
   pdl_wait();
-  // the work of every request, a warp each
+  // the requests, then the work of each, a warp each
+  for (int r = threadIdx.x; r < a.rows.batch; r += kThreads) {
+    const int start = a.rows.row_start[r], n = a.rows.n_rows[r], prefix = a.rows.prefix_len[r];
+    const bool good = kv_request_ok(a.rows, start, n, prefix);
+    if (!good && blockIdx.x == 0) report(a.status, PCTREE_ERR_INVALID_ARG);
+    T->start[r] = start;
+    T->n[r] = good ? n : 0;
+    T->prefix[r] = prefix;
+  }
+  __syncthreads();
   for (int r = warp; r < a.rows.batch; r += kThreads / 32) {
-    const int n = a.rows.n_rows[r], prefix = a.rows.prefix_len[r];
-    long long w = 0;
-    if (kv_request_ok(a.rows, a.rows.row_start[r], n, prefix)) {
-      for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
-        w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
-    } else if (blockIdx.x == 0 && lane == 0) {
-      report(a.status, PCTREE_ERR_INVALID_ARG);
-    }
+    const int n = T->n[r], prefix = T->prefix[r];
+    unsigned w = 0;
+    for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
+      w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
+    if (n > unit_rows) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
+      for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
+    }
     if (lane == 0) T->upto[r] = w * a.Hkv;
   }
   __syncthreads();
   if (warp == 0) {
-    long long base = 0;
+    unsigned base = 0;
     for (int r0 = 0; r0 < a.rows.batch; r0 += 32) {
       const int r = r0 + lane;
-      long long w = r < a.rows.batch ? T->upto[r] : 0;
+      unsigned w = r < a.rows.batch ? T->upto[r] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long p = __shfl_up_sync(kFull, w, o);
+        const unsigned p = __shfl_up_sync(kFull, w, o);
         if (lane >= o) w += p;
       }
       if (r < a.rows.batch) T->upto[r] = base + w;
@@ -441,12 +449,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     (void)mbar_wait_bounded(&T->done, 0, &never, kLimitNs);
   } else if (warp == 3) {
     // ---------------- planner ----------------
-    const long long total = T->upto[a.rows.batch - 1];
-    const int places = gridDim.x / kTiles, place = blockIdx.x / kTiles;
-    long long stretch = (total + places - 1) / places;
-    if (stretch < kMinStretch) stretch = kMinStretch;
-    long long x = place * stretch;
-    const long long x_end = min(total, x + stretch);
+    const unsigned total = T->upto[a.rows.batch - 1];
+    const unsigned places = gridDim.x / kTiles, place = blockIdx.x / kTiles;
+    const unsigned stretch = max((total + places - 1) / places, static_cast<unsigned>(kMinStretch));
+    // (place * stretch is at most total + places * kMinStretch)
+    unsigned x = place * stretch;
+    const unsigned x_end = min(total, x + stretch);
     Join join = {0, 0, 0, 0};
     int k = 0;
     bool ok = true;
@@ -470,22 +478,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       int r = lo, kvh = 0, tile = 0;
       int start = 0, n = 0, prefix = 0;
       auto load = [&]() {
-        start = a.rows.row_start[r];
-        n = a.rows.n_rows[r];
-        prefix = a.rows.prefix_len[r];
+        start = T->start[r];
+        n = T->n[r];
+        prefix = T->prefix[r];
       };
       load();
-      long long in = x - (r > 0 ? T->upto[r - 1] : 0);
-      const long long per_head = (T->upto[r] - (r > 0 ? T->upto[r - 1] : 0)) / a.Hkv;
+      const unsigned before = r > 0 ? T->upto[r - 1] : 0;
+      const unsigned per_head = (T->upto[r] - before) / a.Hkv;
+      unsigned in = x - before;                    // place inside the head's tiles
       kvh = static_cast<int>(in / per_head);
-      in -= kvh * per_head;                        // place inside the head's tiles
+      in -= kvh * per_head;
       for (;;) {
         const int j = (tile + lane) * unit_rows;
-        const int cost = j < n ? blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge : 0;
-        long long c = cost;
+        const unsigned cost = j < n ? blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge : 0;
+        unsigned c = cost;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long p = __shfl_up_sync(kFull, c, o);
+          const unsigned p = __shfl_up_sync(kFull, c, o);
           if (lane >= o) c += p;
         }
         const unsigned past = __ballot_sync(kFull, c > in);
@@ -510,14 +519,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         it.prefix = prefix;
         it.key_end = prefix + min(n, (tile + 1) * unit_rows);
         it.nblk = blocks_of(a, it.key_end);
-        const long long left = it.nblk + kUnitCharge - in;
-        const long long take = min(left, x_end - x);
+        const unsigned left = it.nblk + kUnitCharge - in;
+        const unsigned take = min(left, x_end - x);
         it.b0 = max(0, static_cast<int>(in) - kUnitCharge);
         it.b1 = max(0, static_cast<int>(in + take) - kUnitCharge);
         if (it.b1 > it.b0) {
           if (it.b0 == 0 && it.b1 < it.nblk) {
             // joined from here: the unit's end lies `left` past x
-            join.pieces = static_cast<int>((x + left - 1) / stretch) - place + 1;
+            join.pieces = static_cast<int>((x + left - 1) / stretch - place) + 1;
             join.kvh = kvh;
             join.row0 = it.row0;
             join.n_rows = it.n_rows;
@@ -767,63 +776,92 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
 }
 
 // Joins the pieces of the units that end in another CTA than they began in: a
-// thread has four dims of a row.
-constexpr int kJoinThreads = 128;
-constexpr int kJoinRows = 16;
+// thread has four dims of a row at a time.  Few CTAs, since most find nothing to
+// join (152 x 32 of them took 3 us of a batch of short chains).
+constexpr int kJoinThreads = 256;
+constexpr int kJoinCtas = 4;                 // per CTA of the attention
 
 template <int D, bool F16>
-__global__ void __launch_bounds__(kJoinThreads, 8) paged_join_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(PagedArgs a) {
   pdl_launch_dependents();
   pdl_wait();
   const int c0 = blockIdx.x;
   const Join j = a.join[c0];
-  const int row = blockIdx.y * kJoinRows + (threadIdx.x >> 3);
-  const int quad = blockIdx.z * 8 + (threadIdx.x & 7);
-  const int nl = row / a.G, g = row - nl * a.G;
-  if (j.pieces == 0 || nl >= j.n_rows) return;
+  if (j.pieces == 0) return;
+  constexpr int kQuads = D / 4;
   const float4* po = reinterpret_cast<const float4*>(a.part_o);
-  float m = -INFINITY, lsum = 0.0f;
-  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = 0; s0 < j.pieces; s0 += 4) {
-    float2 w[4];
-    float4 v[4];
+  const int n = j.n_rows * a.G * kQuads;
+  for (int i = blockIdx.y * kJoinThreads + threadIdx.x; i < n; i += kJoinCtas * kJoinThreads) {
+    // neighbouring threads have neighbouring dims (their stores) of a row
+    const int row = i / kQuads, quad = i - row * kQuads;
+    const int nl = row / a.G, g = row - nl * a.G;
+    float m = -INFINITY, lsum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s0 = 0; s0 < j.pieces; s0 += 4) {
+      float2 w[4];
+      float4 v[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bool in = s0 + u < j.pieces;
-      // the first piece is its CTA's last, every other one its CTA's first
-      const size_t part =
-          static_cast<size_t>(c0 + (s0 + u) * a.join_step) * 2 + (s0 + u == 0 ? 1 : 0);
-      w[u] = in ? a.part_ml[part * 128 + row] : make_float2(-INFINITY, 0.0f);
-      v[u] = in ? po[(part * (D / 4) + quad) * 128 + row] : acc;
-    }
-    float mn = m;
+      for (int u = 0; u < 4; ++u) {
+        const bool in = s0 + u < j.pieces;
+        // the first piece is its CTA's last, every other one its CTA's first
+        const size_t part =
+            static_cast<size_t>(c0 + (s0 + u) * a.join_step) * 2 + (s0 + u == 0 ? 1 : 0);
+        w[u] = in ? a.part_ml[part * 128 + row] : make_float2(-INFINITY, 0.0f);
+        v[u] = in ? po[(part * kQuads + quad) * 128 + row] : acc;
+      }
+      float mn = m;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (w[u].y != 0.0f) mn = fmaxf(mn, w[u].x);
-    const float f0 = mn > m && m > -INFINITY ? exp2f(m - mn) : 1.0f;
-    lsum *= f0;
-    acc.x *= f0;
-    acc.y *= f0;
-    acc.z *= f0;
-    acc.w *= f0;
-    m = mn;
+      for (int u = 0; u < 4; ++u)
+        if (w[u].y != 0.0f) mn = fmaxf(mn, w[u].x);
+      const float f0 = mn > m && m > -INFINITY ? exp2f(m - mn) : 1.0f;
+      lsum *= f0;
+      acc.x *= f0;
+      acc.y *= f0;
+      acc.z *= f0;
+      acc.w *= f0;
+      m = mn;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (w[u].y != 0.0f) {
-        const float f = exp2f(w[u].x - m);
-        lsum = fmaf(w[u].y, f, lsum);
-        acc.x = fmaf(v[u].x, f, acc.x);
-        acc.y = fmaf(v[u].y, f, acc.y);
-        acc.z = fmaf(v[u].z, f, acc.z);
-        acc.w = fmaf(v[u].w, f, acc.w);
+      for (int u = 0; u < 4; ++u) {
+        if (w[u].y != 0.0f) {
+          const float f = exp2f(w[u].x - m);
+          lsum = fmaf(w[u].y, f, lsum);
+          acc.x = fmaf(v[u].x, f, acc.x);
+          acc.y = fmaf(v[u].y, f, acc.y);
+          acc.z = fmaf(v[u].z, f, acc.z);
+          acc.w = fmaf(v[u].w, f, acc.w);
+        }
       }
     }
+    const float inv = lsum != 0.0f ? 1.0f / lsum : 0.0f;
+    uint16_t* orow =
+        a.out + ((static_cast<size_t>(j.row0) + nl) * a.Hq + j.kvh * a.G + g) * D + quad * 4;
+    *reinterpret_cast<uint2*>(orow) = make_uint2(pack16<F16>(acc.x * inv, acc.y * inv),
+                                                 pack16<F16>(acc.z * inv, acc.w * inv));
   }
-  const float inv = lsum != 0.0f ? 1.0f / lsum : 0.0f;
-  uint16_t* orow =
-      a.out + ((static_cast<size_t>(j.row0) + nl) * a.Hq + j.kvh * a.G + g) * D + quad * 4;
-  *reinterpret_cast<uint2*>(orow) = make_uint2(pack16<F16>(acc.x * inv, acc.y * inv),
-                                               pack16<F16>(acc.z * inv, acc.w * inv));
+}
+
+// Rows per tile: one where requests have one row each, on average (a tile's
+// rows are loaded whether or not they are the request's), else as many as fit.
+int rows_per_tile(const pctree_paged_attn_config& c) {
+  const int fit = 128 / (c.Hq / c.Hkv);
+  return c.total_rows <= c.batch ? 1 : fit < c.total_rows ? fit : c.total_rows;
+}
+
+// Pages per block of keys where several fill one, else 0.
+int packed_pages(int page_size) {
+  return page_size == 8 || page_size == 16 || page_size == 32 || page_size == 64 ? kBK / page_size
+                                                                                 : 0;
+}
+
+// Whether the planner can count the most work a configuration can have in 32
+// bits.
+bool paged_work_ok(const pctree_paged_attn_config& c) {
+  const long long units = c.total_rows / rows_per_tile(c) + 1ll + c.batch;
+  const long long blocks =
+      (packed_pages(c.page_size) != 0
+           ? (static_cast<long long>(c.max_pages) * c.page_size + kBK - 1) / kBK
+           : static_cast<long long>(c.max_pages) * ((c.page_size + kBK - 1) / kBK)) + kUnitCharge;
+  return units * blocks < (1ll << 32) / c.Hkv - 1024;
 }
 
 pctree_status paged_check(const pctree_paged_attn_config* c) {
@@ -836,7 +874,8 @@ pctree_status paged_check(const pctree_paged_attn_config* c) {
   if (c->Hq % c->Hkv != 0 || c->q_stride % 8 != 0 ||
       c->q_stride < static_cast<int64_t>(c->Hq) * c->D)
     return PCTREE_ERR_INVALID_ARG;
-  if ((c->D != 64 && c->D != 128) || c->Hq / c->Hkv > 128 || c->q_stride > (1ll << 38))
+  if ((c->D != 64 && c->D != 128) || c->Hq / c->Hkv > 128 || c->q_stride > (1ll << 38) ||
+      !paged_work_ok(*c))
     return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }
@@ -883,7 +922,7 @@ pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
   if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16, PAIR>, tm_q, tm_k, tm_v, a) != cudaSuccess)
     return PCTREE_ERR_CUDA;
   lc.numAttrs = 1;
-  lc.gridDim = dim3(static_cast<unsigned>(ctas), (a.G * a.npt + kJoinRows - 1) / kJoinRows, D / 32);
+  lc.gridDim = dim3(static_cast<unsigned>(ctas), kJoinCtas);
   lc.blockDim = dim3(kJoinThreads);
   lc.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&lc, paged_join_kernel<D, F16>, a) == cudaSuccess ? PCTREE_OK
@@ -951,11 +990,8 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   a.Hq = c.Hq;
   a.Hkv = c.Hkv;
   a.G = c.Hq / c.Hkv;
-  // rows per tile: one where requests have one row each, on average (a tile's
-  // rows are loaded whether or not they are the request's), else as many as fit
-  a.npt = c.total_rows <= c.batch ? 1 : 128 / a.G < c.total_rows ? 128 / a.G : c.total_rows;
-  a.packed = c.page_size == 8 || c.page_size == 16 || c.page_size == 32 || c.page_size == 64
-                 ? kBK / c.page_size : 0;
+  a.npt = rows_per_tile(c);
+  a.packed = packed_pages(c.page_size);
   a.page_blocks = (c.page_size + kBK - 1) / kBK;
   // Requests of more than a tile of rows, on average: pairs of CTAs take two
   // tiles of a head at a time and each loads half of the keys for both.
