@@ -777,6 +777,8 @@ class Drafter:
         self.accepted_idx = self.tree.extra["accepted_idx"]
         self.accepted_len = self.tree.extra["accepted_len"]
         self.bonus = self.tree.extra["bonus"]
+        self.target = torch.full((cfg.batch, cfg.N), -1, dtype=torch.int32,
+                                 device=self.device)
 
     def draft(self, base_logits, head_emb, head_out, root_token, stream=None):
         pctree_draft(self.cfg, base_logits, head_emb, head_out, root_token,
@@ -787,6 +789,20 @@ class Drafter:
         pctree_accept(self.cfg, self.tree, target_tokens, self.accepted_idx,
                       self.accepted_len, self.bonus, stream)
         return self.accepted_idx, self.accepted_len, self.bonus
+
+    def sample_accept(self, logits, uniform, temperature=None, top_k=None, top_p=None,
+                      min_p=None, status=None, stream=None):
+        """Acceptance against tokens sampled from the target's logits
+        [batch][N][V] of the tree's nodes, with one random number in [0, 1) per
+        node (uniform [batch][N]) and the parameters [batch] of pctree_sample:
+        the committed tokens and the bonus are samples of the target.  Rows
+        past a tree's nodes are not read; the sampled tokens are in
+        ``self.target``."""
+        cfg = self.cfg
+        sc = sample_config(cfg.batch * cfg.N, logits.shape[-1], cfg.N, logits.dtype)
+        pctree_sample(sc, logits, uniform, self.target, temperature, top_k, top_p, min_p,
+                      self.tree.n_nodes, status, stream)
+        return self.accept(self.target, stream)
 
     def check_status(self) -> None:
         code = int(self.tree.status.item())
