@@ -143,7 +143,7 @@ __host__ __device__ constexpr uint32_t idesc(int M, int N) {
   return idesc_bf16_f32(M, N) & (F16 ? ~((1u << 7) | (1u << 10)) : ~0u);
 }
 
-template <int D, bool F16, bool PAIR>
+template <int D, bool F16, int CTAS>
 __global__ void __maxnreg__(112)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k,
@@ -158,16 +158,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   Tail* T = reinterpret_cast<Tail*>(skv + kSlots * kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = a.G * a.npt;                       // rows of a tile
-  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
-  constexpr int kTiles = PAIR ? 2 : 1;             // tiles of a unit
-  const int unit_rows = kTiles * a.npt;
+  const int rank = CTAS > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  constexpr uint16_t kAll = (1 << CTAS) - 1;       // the CTAs that share a block's loads
+  const int unit_rows = CTAS * a.npt;              // a tile for each of them
   volatile int* abort_v = &T->abort;
 
   // ---------------- set-up ----------------
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(&T->kv_full[s], 1);
-      mbar_init(&T->kv_empty[s], kTiles);          // the MMAs of every CTA that got the block
+      mbar_init(&T->kv_empty[s], CTAS);          // the MMAs of every CTA that got the block
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&T->q_full[s], 1);
@@ -239,7 +239,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  if constexpr (PAIR) cluster_sync();              // both CTAs' barriers are initialised
+  if constexpr (CTAS > 1) cluster_sync();          // all CTAs' barriers are initialised
   const uint32_t tmem = T->tmem_base;
 
   auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
@@ -319,13 +319,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         mbar_arrive_expect_tx(&T->kv_full[slot],
                               static_cast<uint32_t>(kHalves * x.boxes * a.box_rows) * 128u);
       __syncwarp();
-      // a pair's CTAs take the boxes in turn, each for both of them
-      if (lane < x.boxes && (!PAIR || (lane & 1) == rank)) {
+      // a cluster's CTAs take the boxes in turn, each for all of them
+      if (lane < x.boxes && (lane & (CTAS - 1)) == rank) {
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
-          if constexpr (PAIR)
+          if constexpr (CTAS > 1)
             tma_load_4d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh,
-                                  x.off, x.page, 3);
+                                  x.off, x.page, kAll);
           else
             tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh, x.off,
                         x.page);
@@ -371,8 +371,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       drain(T->kv_full);
       for (int x = q > 2 ? q - 2 : 0; x < q; ++x)
         (void)mbar_wait_bounded(&T->q_full[x & 1], (x >> 1) & 1, &never, kLimitNs);
-      // and so do the other CTA's arrivals
-      if constexpr (PAIR) {
+      // and so do the other CTAs' arrivals
+      if constexpr (CTAS > 1) {
         if (ok) drain(T->kv_empty);
       }
     }
@@ -403,7 +403,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
           tc_mma_bf16(tmem + sb * kBK, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
         }
         tc_commit(&T->s_full[sb]);
-        if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
+        if constexpr (CTAS > 1) tc_commit_multicast(&T->kv_empty[slot], kAll);
         else tc_commit(&T->kv_empty[slot]);
       }
       tc_commit(&T->q_empty[qb]);
@@ -439,7 +439,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         tc_commit(&T->p_empty[sb]);
         if (b + 1 == it.b1) tc_commit(&T->o_full);
-        if constexpr (PAIR) tc_commit_both(&T->kv_empty[slot]);
+        if constexpr (CTAS > 1) tc_commit_multicast(&T->kv_empty[slot], kAll);
         else tc_commit(&T->kv_empty[slot]);
       }
     }
@@ -450,7 +450,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   } else if (warp == 3) {
     // ---------------- planner ----------------
     const unsigned total = T->upto[a.rows.batch - 1];
-    const unsigned places = gridDim.x / kTiles, place = blockIdx.x / kTiles;
+    const unsigned places = gridDim.x / CTAS, place = blockIdx.x / CTAS;
     const unsigned stretch = max((total + places - 1) / places, static_cast<unsigned>(kMinStretch));
     // (place * stretch is at most total + places * kMinStretch)
     unsigned x = place * stretch;
@@ -768,8 +768,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   __syncthreads();
   tc_fence_after_sync();
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  if constexpr (PAIR) {
-    // the other CTA's copies and commits no longer reach this one's memory
+  if constexpr (CTAS > 1) {
+    // the other CTAs' copies and commits no longer reach this one's memory
     __syncwarp();
     cluster_sync();
   }
@@ -893,7 +893,27 @@ PagedWs paged_ws(const pctree_paged_attn_config& c) {
   return w;
 }
 
-template <int D, bool F16, bool PAIR>
+// CTAs of a grid of clusters that are on the GPU together (at most kMaxCtas);
+// asked once per device.
+template <int CTAS>
+int resident_ctas(const void* fn, const cudaLaunchConfig_t& lc, int num_sms) {
+  const int most = num_sms < kMaxCtas ? num_sms : kMaxCtas;
+  if (CTAS == 1) return most;
+  static std::mutex mu;
+  static int known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return CTAS;
+  std::lock_guard<std::mutex> lk(mu);
+  if (known[dev] == 0) {
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, fn, &lc) != cudaSuccess || clusters < 1)
+      clusters = 1;
+    known[dev] = clusters * CTAS < most ? clusters * CTAS : most / CTAS * CTAS;
+  }
+  return known[dev];
+}
+
+template <int D, bool F16, int CTAS>
 pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                            const CUtensorMap& tm_v, const PagedArgs& a, int num_sms,
                            cudaStream_t stream) {
@@ -901,25 +921,25 @@ pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
       (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
   static SmemLimit limit;
-  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16, PAIR>);
+  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16, CTAS>);
   if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.x = CTAS;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t lc = {};
-  int ctas = num_sms < kMaxCtas ? num_sms : kMaxCtas;
-  if (PAIR) ctas &= ~1;
-  lc.gridDim = dim3(static_cast<unsigned>(ctas));
+  lc.gridDim = dim3(static_cast<unsigned>(kMaxCtas / CTAS * CTAS));
   lc.blockDim = dim3(kThreads);
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
   lc.attrs = attr;
-  lc.numAttrs = PAIR ? 2 : 1;
-  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16, PAIR>, tm_q, tm_k, tm_v, a) != cudaSuccess)
+  lc.numAttrs = CTAS > 1 ? 2 : 1;
+  const int ctas = resident_ctas<CTAS>(fn, lc, num_sms);
+  lc.gridDim = dim3(static_cast<unsigned>(ctas));
+  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16, CTAS>, tm_q, tm_k, tm_v, a) != cudaSuccess)
     return PCTREE_ERR_CUDA;
   lc.numAttrs = 1;
   lc.gridDim = dim3(static_cast<unsigned>(ctas), kJoinCtas);
@@ -931,10 +951,11 @@ pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
 
 template <int D, bool F16>
 pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
-                           const CUtensorMap& tm_v, const PagedArgs& a, int num_sms, bool pair,
+                           const CUtensorMap& tm_v, const PagedArgs& a, int num_sms,
                            cudaStream_t stream) {
-  return pair ? paged_launch<D, F16, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
-              : paged_launch<D, F16, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
+  return a.join_step == 4   ? paged_launch<D, F16, 4>(tm_q, tm_k, tm_v, a, num_sms, stream)
+         : a.join_step == 2 ? paged_launch<D, F16, 2>(tm_q, tm_k, tm_v, a, num_sms, stream)
+                            : paged_launch<D, F16, 1>(tm_q, tm_k, tm_v, a, num_sms, stream);
 }
 
 }  // namespace
@@ -993,12 +1014,16 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   a.npt = rows_per_tile(c);
   a.packed = packed_pages(c.page_size);
   a.page_blocks = (c.page_size + kBK - 1) / kBK;
-  // Requests of more than a tile of rows, on average: pairs of CTAs take two
-  // tiles of a head at a time and each loads half of the keys for both.
-  const bool pair = num_sms >= 2 && c.total_rows > static_cast<long long>(c.batch) * a.npt;
-  const int most = pair ? kBK / 2 : kBK;           // so that both CTAs have boxes to load
+  // Requests of more than a tile of rows, on average: the CTAs of a cluster take
+  // tiles of a head side by side, and each loads a share of the keys for all.
+  // Four of them where pages are small and requests have tiles enough.
+  const long long tiles = c.total_rows / (static_cast<long long>(c.batch) * a.npt);
+  // (us, four prompts of up to 4096 rows, two / four: pages of 8 674 / 556,
+  // 16 513 / 479, 32 425 / 430; 36 clusters of four fit, 144 of 152 SMs.)
+  a.join_step = num_sms < 4 || c.total_rows <= static_cast<long long>(c.batch) * a.npt ? 1
+                : c.page_size <= 16 && tiles >= 6 ? 4 : 2;
+  const int most = kBK / a.join_step;              // so that every CTA has boxes to load
   a.box_rows = c.page_size < most ? c.page_size : most;
-  a.join_step = pair ? 2 : 1;
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
   CUtensorMap tm_q, tm_k, tm_v;
   const uint64_t D = static_cast<uint64_t>(c.D), head = D * 2;   // bytes of one head row
@@ -1022,10 +1047,10 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
   const bool f16 = c.dtype == PCTREE_F16;
   if (c.D == 64)
-    return f16 ? paged_launch<64, true>(tm_q, tm_k, tm_v, a, num_sms, pair, stream)
-               : paged_launch<64, false>(tm_q, tm_k, tm_v, a, num_sms, pair, stream);
-  return f16 ? paged_launch<128, true>(tm_q, tm_k, tm_v, a, num_sms, pair, stream)
-             : paged_launch<128, false>(tm_q, tm_k, tm_v, a, num_sms, pair, stream);
+    return f16 ? paged_launch<64, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
+               : paged_launch<64, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
+  return f16 ? paged_launch<128, true>(tm_q, tm_k, tm_v, a, num_sms, stream)
+             : paged_launch<128, false>(tm_q, tm_k, tm_v, a, num_sms, stream);
 }
 
 }  // extern "C"

@@ -364,13 +364,13 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
       : "memory");
 }
 
-// tc_commit that arrives on the barrier at this place in both CTAs of a pair,
-// for MMAs of this CTA alone.
-__device__ __forceinline__ void tc_commit_both(uint64_t* bar) {
+// tc_commit that arrives on the barrier at this place in every CTA of `mask`
+// (bits are cluster ranks), for MMAs of this CTA alone.
+__device__ __forceinline__ void tc_commit_multicast(uint64_t* bar, uint16_t mask) {
   asm volatile(
       "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
       "[%0], %1;" ::"r"(smem_u32(bar)),
-      "h"(static_cast<uint16_t>(3))
+      "h"(mask)
       : "memory");
 }
 

@@ -108,6 +108,11 @@ SHAPES = {
 for _page in (0, 1, 8, 16, 23, 32, 48, 64, 100, 128, 200):
     SHAPES[f"pairs_page_{_page}"] = dict(rows=[70, 41], prefix=[190, 3], page=_page, heads=(16, 2))
 
+# clusters of four: many tiles a request, small pages
+for _page in (1, 5, 8, 16):
+    SHAPES[f"fours_page_{_page}"] = dict(rows=[205, 97, 0, 129], prefix=[40, 301, 7, 0],
+                                         page=_page, heads=(16, 2), gap=1)
+
 
 @pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "bf16"), (128, "f16"), (64, "f16")])
 @pytest.mark.parametrize("name", sorted(SHAPES))
