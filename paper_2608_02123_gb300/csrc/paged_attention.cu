@@ -68,9 +68,19 @@ struct PagedArgs {
   int packed;             // pages per block (page_size 8 .. 64), 0: parts of pages
   int page_blocks;        // blocks per page if not packed
   int box_rows;           // rows of a K/V box: a page, or part of one
+  // Rows of the groups in which K and V lie in a ring slot, [group][64-dim half]
+  // [row]: 128 (each half in one piece), or box_rows where one box brings both
+  // halves of the dims.  A group of V is at least 8 keys, of K 8 or all (the
+  // 8-key steps of an MMA operand are equally far apart).
+  int k_group, v_group;
   int join_step;          // CTAs from one piece of a unit to the next
   float scale_log2;
 };
+
+// Bytes from the start of a slot to key r of its V (first half of the dims).
+__device__ __forceinline__ int v_place_of(int r, int group, int halves) {
+  return ((r & -group) * halves + (r & (group - 1))) * 128;
+}
 
 // Places of the g-th block's K and V in the ring's sequence.
 __device__ __forceinline__ int k_place(int g) { return g == 0 ? 0 : 2 * g - 1; }
@@ -314,21 +324,29 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     auto load = [&](const CUtensorMap* map, const Box& x, int place) {
       const int slot = place % kSlots;
       if (!(ok = wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1))) return;
-      uint8_t* dst = skv + slot * kTileBytes + lane * a.box_rows * 128;
+      const bool both = kHalves == 2 && (map == &tm_k ? a.k_group : a.v_group) != kBK;
+      uint8_t* dst = skv + slot * kTileBytes + lane * a.box_rows * (both ? 256 : 128);
       if (lane == 0)
         mbar_arrive_expect_tx(&T->kv_full[slot],
                               static_cast<uint32_t>(kHalves * x.boxes * a.box_rows) * 128u);
       __syncwarp();
       // a cluster's CTAs take the boxes in turn, each for all of them
       if (lane < x.boxes && (lane & (CTAS - 1)) == rank) {
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
+        if (both) {
           if constexpr (CTAS > 1)
-            tma_load_4d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh,
-                                  x.off, x.page, kAll);
+            tma_load_5d_multicast(dst, map, &T->kv_full[slot], 0, x.off, 0, x.kvh, x.page, kAll);
           else
-            tma_load_4d(dst + h * kHalfBytes, map, &T->kv_full[slot], 64 * h, x.kvh, x.off,
-                        x.page);
+            tma_load_5d(dst, map, &T->kv_full[slot], 0, x.off, 0, x.kvh, x.page);
+        } else {
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) {
+            if constexpr (CTAS > 1)
+              tma_load_5d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 0, x.off, h,
+                                    x.kvh, x.page, kAll);
+            else
+              tma_load_5d(dst + h * kHalfBytes, map, &T->kv_full[slot], 0, x.off, h, x.kvh,
+                          x.page);
+          }
         }
       }
     };
@@ -381,7 +399,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     constexpr uint32_t idS = idesc<F16>(128, kBK);
     int q = 0, g = 0;
     const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
-    const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
+    // 8 keys are a row group; groups of 8 with both halves are twice as far apart
+    const bool k_both = kHalves == 2 && a.k_group == 8;
+    const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv)) +
+                            (k_both ? static_cast<uint64_t>(1024 >> 4) << 32 : 0ull);
+    const int k_half = (k_both ? 1024 : kHalfBytes) >> 4;
     bool ok = true;
     Item it;
     for (int k = 0; ok; ++k) {
@@ -399,8 +421,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         tc_fence_after_sync();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          const int off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-          tc_mma_bf16(tmem + sb * kBK, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
+          const int q_off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+          const int k_off = (kk >> 2) * k_half + (kk & 3) * 2;
+          tc_mma_bf16(tmem + sb * kBK, qd + q_off, kd + k_off, idS, kk > 0 ? 1u : 0u);
         }
         tc_commit(&T->s_full[sb]);
         if constexpr (CTAS > 1) tc_commit_multicast(&T->kv_empty[slot], kAll);
@@ -416,7 +439,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     // ---------------- PV issuer ----------------
     constexpr uint32_t idO = idesc<F16>(128, D) | (1u << 16);   // B MN-major
     int g = 0;
-    const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), kHalfBytes, 1024);
+    // (with groups of 8 keys the next 8 are in the next group)
+    const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), a.v_group * 128,
+                                               kHalves == 2 && a.v_group == 8 ? 2048 : 1024);
+    int v_off[kBK / 16];                           // of every 16 keys in a slot
+#pragma unroll
+    for (int kk = 0; kk < kBK / 16; ++kk) v_off[kk] = v_place_of(16 * kk, a.v_group, kHalves) >> 4;
     bool ok = true;
     Item it;
     for (int k = 0; ok; ++k) {
@@ -434,7 +462,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         for (int kk = 0; kk < kBK / 16; ++kk) {
           const int h = kk >> 2;
           tc_mma_tmem_a(tmem + kOCol + h * D, tmem + sb * kBK + h * 64 + (kk & 3) * 8,
-                        vd + ((kk * 16 * 128) >> 4), idO,
+                        vd + v_off[kk], idO,
                         (b > it.b0 || (kk & 3) > 0) ? 1u : 0u);
         }
         tc_commit(&T->p_empty[sb]);
@@ -699,8 +727,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
           const int n16 = (kBK - valid) * 8;
           for (int i = half * 128 + t; i < kHalves * n16; i += 256) {
             const int vh = i >= n16 ? 1 : 0, rem = i - vh * n16;
-            *reinterpret_cast<uint4*>(v + vh * kHalfBytes + (valid + rem / 8) * 128 +
-                                      (rem % 8) * 16) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(v + v_place_of(valid + rem / 8, a.v_group, kHalves) +
+                                      vh * a.v_group * 128 + (rem % 8) * 16) =
+                make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
         }
@@ -1024,6 +1053,8 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
                 : c.page_size <= 16 && tiles >= 6 ? 4 : 2;
   const int most = kBK / a.join_step;              // so that every CTA has boxes to load
   a.box_rows = c.page_size < most ? c.page_size : most;
+  a.v_group = a.packed != 0 && a.box_rows < kBK ? a.box_rows : kBK;
+  a.k_group = a.v_group == 8 ? 8 : kBK;
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
   CUtensorMap tm_q, tm_k, tm_v;
   const uint64_t D = static_cast<uint64_t>(c.D), head = D * 2;   // bytes of one head row
@@ -1035,13 +1066,17 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
     if (st != PCTREE_OK) return st;
   }
   {
-    const uint64_t dims[4] = {D, static_cast<uint64_t>(c.Hkv), static_cast<uint64_t>(c.page_size),
-                              static_cast<uint64_t>(c.n_pages)};
-    const uint64_t str[3] = {head, head * c.Hkv, head * c.Hkv * c.page_size};
-    const uint32_t box[4] = {64, 1, static_cast<uint32_t>(a.box_rows), 1};
-    st = encode_bf16_map_nd(&tm_k, k_cache, 4, dims, str, box);
+    // 64 dims, slots of a page, halves of the dims, heads, pages
+    const uint64_t dims[5] = {64, static_cast<uint64_t>(c.page_size), D / 64,
+                              static_cast<uint64_t>(c.Hkv), static_cast<uint64_t>(c.n_pages)};
+    const uint64_t str[4] = {head * c.Hkv, 128, head, head * c.Hkv * c.page_size};
+    const uint32_t rows = static_cast<uint32_t>(a.box_rows);
+    const uint32_t half = 1, all = static_cast<uint32_t>(c.D / 64);
+    const uint32_t k_box[5] = {64, rows, a.k_group == kBK ? half : all, 1, 1};
+    const uint32_t v_box[5] = {64, rows, a.v_group == kBK ? half : all, 1, 1};
+    st = encode_bf16_map_nd(&tm_k, k_cache, 5, dims, str, k_box);
     if (st != PCTREE_OK) return st;
-    st = encode_bf16_map_nd(&tm_v, v_cache, 4, dims, str, box);
+    st = encode_bf16_map_nd(&tm_v, v_cache, 5, dims, str, v_box);
     if (st != PCTREE_OK) return st;
   }
   cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
