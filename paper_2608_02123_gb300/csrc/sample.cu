@@ -273,6 +273,9 @@ struct Elem<PCTREE_F32> {
     return max_nan(m, __uint_as_float(v.z), __uint_as_float(v.w));
   }
   static __device__ __forceinline__ float value(Max m) { return m; }
+  static __device__ __forceinline__ void unpack4(const uint4& v, int, float (&x)[4]) {
+    unpack(v, x);
+  }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x);
     x[1] = __uint_as_float(v.y);
@@ -304,6 +307,13 @@ struct Elem16 {
   static __device__ __forceinline__ float value(Max m) {
     const float2 p = unpack16<F16>(m);
     return max_nan(p.x, p.y);
+  }
+  static __device__ __forceinline__ void unpack4(const uint4& v, int part, float (&x)[4]) {
+    const float2 lo = unpack16<F16>(part ? v.z : v.x), hi = unpack16<F16>(part ? v.w : v.y);
+    x[0] = lo.x;
+    x[1] = lo.y;
+    x[2] = hi.x;
+    x[3] = hi.y;
   }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -618,13 +628,19 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   auto sum_all = [&]() {
     mine = 0;
     pass(kNear, [&](const uint4& raw, int) {
-      float x[kVec];
-      E::unpack(raw, x);
+      // four logits at a time: the loop then stays in the innermost
+      // instruction cache
+#pragma unroll 1
+      for (int part = 0; part < kVec / 4; ++part) {
+        float x[4];
+        E::unpack4(raw, part, x);
 #pragma unroll
-      for (int e = 0; e < kVec; e += 2) {
-        unsigned long long w0, w1;
-        light_weights(S, f, fmaxf(x[e] - f.base, f.low), fmaxf(x[e + 1] - f.base, f.low), w0, w1);
-        mine += w0 + w1;
+        for (int e = 0; e < 4; e += 2) {
+          unsigned long long w0, w1;
+          light_weights(S, f, fmaxf(x[e] - f.base, f.low), fmaxf(x[e + 1] - f.base, f.low), w0,
+                        w1);
+          mine += w0 + w1;
+        }
       }
     });
     const unsigned long long rough = cluster_total(mine);
