@@ -427,7 +427,8 @@ PCTREE_API pctree_status pctree_tree_attention(
  * A request with n_rows[r] < 0, prefix_len[r] < 0, rows outside
  * 0 .. total_rows - 1 or slots past max_pages * page_size is left out
  * (nothing of it is written) and sets the status to PCTREE_ERR_INVALID_ARG,
- * as a page number outside 0 .. n_pages - 1 does.
+ * as a page number outside 0 .. n_pages - 1 does.  Requests may share pages
+ * (of a common prefix); the slots that one call appends to are distinct places.
  */
 #define PCTREE_KV_MAX_BATCH 1024   /* requests of one call */
 
@@ -492,10 +493,12 @@ PCTREE_API pctree_status pctree_kv_append(
  * rows (behind a prefix of earlier chunks or none), a drafted chain (k = 1)
  * is verified as the rows behind its root.  Keys and values of the rows are
  * in the cache before the call (pctree_kv_append).  Slots past the last row
- * are never used (their values may be anything); a NaN or infinite score or
- * value reaches the rows that see it.  Scores, row maxima and sums and the
- * output's accumulation are float32; probabilities are rounded to dtype for
- * the product with the values.
+ * are never used (their values may be anything).  A NaN or infinite score or
+ * value reaches the rows that see it and no others (where one tile's new rows,
+ * at most 128 / G, hold non-finite values in more than 64 groups of 8 dims of
+ * a head, every dim of the rows that see the first of them is NaN).  Scores,
+ * row maxima and sums and the output's accumulation are float32; probabilities
+ * are rounded to dtype for the product with the values.
  */
 typedef struct {
   int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */

@@ -19,7 +19,7 @@
 //               two TMEM buffers
 //   warp 2      PV issuer: O_h += P_b V_b over each half h of the block's keys
 //               (P read from TMEM)
-//   warp 3      planner: the CTA's pieces, in order, two ahead
+//   warp 3      planner: the CTA's pieces, in order, up to kItemRing ahead
 //   warps 4..7  output: the two O of a finished piece, combined, to rows of out
 //               or the piece's partial, while the softmax goes on
 //   warps 8..15 softmax, two threads per tile row, 64 keys of a block each with
@@ -38,6 +38,7 @@ constexpr uint64_t kLimitNs = 1000000000ull;
 constexpr int kThreads = 512;
 constexpr int kSlots = 4;                    // K or V blocks in the ring
 constexpr int kItemRing = 4;
+constexpr int kMaxBad = 64;                  // 16-byte places of V told apart (clean_v)
 constexpr int kMaxCtas = 152;                // SMs of a GB300: partials the workspace holds
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kOCol = 2 * kBK;
@@ -82,6 +83,28 @@ __device__ __forceinline__ int v_place_of(int r, int group, int halves) {
   return ((r & -group) * halves + (r & (group - 1))) * 128;
 }
 
+// Eight values (16 bytes of V) with a NaN or infinity among them: key (counted
+// from the first that not every row of the tile sees), place of the eight in
+// the row, and for each value 0 (finite), 1 (+inf), 2 (-inf) or 3 (NaN).  The
+// non-finite ones are replaced by 0.  Returns 0 if all are finite.
+template <bool F16>
+__device__ __forceinline__ uint32_t bad_entry(uint4& v, int key, int place) {
+  constexpr uint32_t top = F16 ? 0x7c00u : 0x7f80u;
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t kinds = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t x = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+    if ((x & top) == top) {
+      kinds |= ((x & (0x7fffu ^ top)) != 0 ? 3u : (x & 0x8000u) != 0 ? 2u : 1u) << (2 * e);
+      w[e >> 1] &= ~(0xffffu << (16 * (e & 1)));
+    }
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+  return kinds == 0 ? 0u
+                    : kinds | static_cast<uint32_t>(place) << 16 | static_cast<uint32_t>(key) << 20;
+}
+
 // Places of the g-th block's K and V in the ring's sequence.
 __device__ __forceinline__ int k_place(int g) { return g == 0 ? 0 : 2 * g - 1; }
 __device__ __forceinline__ int v_place(int g) { return 2 * g + 2; }
@@ -97,6 +120,11 @@ struct Tail {
   int abort;
   Item item[kItemRing];
   float row_l[2][128], row_m[2][128];
+  // Non-finite values at keys that only some rows of the piece's tile see, by
+  // piece parity and output warp (each resets its own copy): entries of
+  // bad_entry, their number and the first such key.
+  int bad_n[2][4], bad_first[2][4];
+  uint32_t bad[2][4][kMaxBad];
   alignas(16) uint8_t stage[4][32 * 64];
   unsigned upto[PCTREE_KV_MAX_BATCH];        // work of requests 0 .. r (the host checks the sum)
   int start[PCTREE_KV_MAX_BATCH], n[PCTREE_KV_MAX_BATCH], prefix[PCTREE_KV_MAX_BATCH];
@@ -153,6 +181,37 @@ __host__ __device__ constexpr uint32_t idesc(int M, int N) {
   return idesc_bf16_f32(M, N) & (F16 ? ~((1u << 7) | (1u << 10)) : ~0u);
 }
 
+// Readies a V block whose keys `valid` .. 127 no row of the tile sees and whose
+// keys by_some .. valid - 1 only some rows do (see its call; not inline: its
+// registers would be the loop's).  rel0: key 0 counted from the first key that
+// not every row sees.
+template <int HALVES, bool F16>
+__device__ __noinline__ void clean_v(uint8_t* v, Tail* T, int parity, int thread, int valid,
+                                     int by_some, int rel0, int group) {
+  const int n16 = (kBK - valid) * 8;
+  for (int i = thread; i < HALVES * n16; i += 256) {
+    const int vh = i >= n16 ? 1 : 0, rem = i - vh * n16;
+    *reinterpret_cast<uint4*>(v + v_place_of(valid + rem / 8, group, HALVES) + vh * group * 128 +
+                              (rem % 8) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  for (int i = thread; i < (valid - by_some) * 8 * HALVES; i += 256) {
+    const int key = by_some + i / (8 * HALVES), place = i % (8 * HALVES);
+    // (the 128-byte rows are swizzled: 16-byte place p of row r at p ^ (r & 7))
+    const int at = v_place_of(key, group, HALVES) + (place >> 3) * group * 128;
+    uint4* p = reinterpret_cast<uint4*>(v + at + (((place & 7) ^ ((at >> 7) & 7)) * 16));
+    uint4 x = *p;
+    const uint32_t entry = bad_entry<F16>(x, rel0 + key, place);
+    if (entry != 0) {
+      *p = x;
+      for (int q = 0; q < 4; ++q) {
+        atomicMin(&T->bad_first[parity][q], rel0 + key);
+        const int n = atomicAdd(&T->bad_n[parity][q], 1);
+        if (n < kMaxBad) T->bad[parity][q][n] = entry;
+      }
+    }
+  }
+}
+
 template <int D, bool F16, int CTAS>
 __global__ void __maxnreg__(112)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
@@ -194,6 +253,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     mbar_init(&T->o_empty, 4);
     mbar_init(&T->done, 2);
     T->abort = 0;
+    for (int i = 0; i < 8; ++i) {
+      T->bad_n[i >> 2][i & 3] = 0;
+      T->bad_first[i >> 2][i & 3] = kBK;
+    }
     fence_barrier_init();
     tma_prefetch_desc(&tm_q);
     tma_prefetch_desc(&tm_k);
@@ -603,6 +666,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       tc_fence_after_sync();
       uint16_t* oitem = a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G) * D;
       const bool whole = it.b0 == 0 && it.b1 == it.nblk;
+      const int n_bad = T->bad_n[k & 1][quad];
       const size_t part = static_cast<size_t>(blockIdx.x) * 2 + (it.b0 == 0 ? 1 : 0);
       // the halves' sums and O relative to the larger of their references
       const float l0 = T->row_l[0][t], l1 = T->row_l[1][t];
@@ -635,6 +699,35 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
             const uint64_t a0 = pack2(__uint_as_float(y0[i]), __uint_as_float(y0[i + 1]));
             const uint64_t a1 = pack2(__uint_as_float(y1[i]), __uint_as_float(y1[i + 1]));
             unpack2(fma2(a0, pack2(f0, f0), mul2(a1, pack2(f1, f1))), y[i], y[i + 1]);
+          }
+        }
+        // values taken out of V reach the rows that see their keys
+        if (n_bad != 0) {
+          uint32_t pos = 0, neg = 0, nan = 0;
+          const int seen = t / a.G - 1;            // the last such key the row sees
+          for (int i = 0; i < min(n_bad, kMaxBad); ++i) {
+            const uint32_t e = T->bad[k & 1][quad][i];
+            const int place = (e >> 16) & 15;
+            if (static_cast<int>(e >> 20) > seen || place / 4 != c) continue;
+            for (int x = 0; x < 8; ++x) {
+              const uint32_t kind = (e >> (2 * x)) & 3u, bit = 1u << ((place & 3) * 8 + x);
+              if (kind == 1) pos |= bit;
+              if (kind == 2) neg |= bit;
+              if (kind == 3) nan |= bit;
+            }
+          }
+          if (n_bad > kMaxBad && T->bad_first[k & 1][quad] <= seen) nan = 0xffffffffu;
+          nan |= pos & neg;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if ((pos >> i) & 1u) y[i] = INFINITY;
+            if ((neg >> i) & 1u) y[i] = -INFINITY;
+            if ((nan >> i) & 1u) y[i] = __int_as_float(0x7fc00000);
+          }
+          __syncwarp();
+          if (c == D / 32 - 1 && lane == 0) {
+            T->bad_n[k & 1][quad] = 0;
+            T->bad_first[k & 1][quad] = kBK;
           }
         }
         if (c == D / 32 - 1) {
@@ -717,22 +810,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         for (int k2 = 8; k2 < 64; ++k2) m8[k2 & 7] = fmaxf(m8[k2 & 7], x[k2]);
         const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
                          fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * sc;
-        // V rows no row of the tile sees hold anything: zero them, so that
-        // 0 * (non-finite) cannot reach O
-        const int valid = min(cap, it.key_end - key0);
-        if (valid < kBK) {
-          const int xv = v_place(g);
-          if (!(ok = wwait(&T->kv_full[xv % kSlots], (xv / kSlots) & 1))) break;
-          uint8_t* v = skv + (xv % kSlots) * kTileBytes;
-          const int n16 = (kBK - valid) * 8;
-          for (int i = half * 128 + t; i < kHalves * n16; i += 256) {
-            const int vh = i >= n16 ? 1 : 0, rem = i - vh * n16;
-            *reinterpret_cast<uint4*>(v + v_place_of(valid + rem / 8, a.v_group, kHalves) +
-                                      vh * a.v_group * 128 + (rem % 8) * 16) =
-                make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async_smem();
-        }
         if (__any_sync(kFull, mx > m_used + 8.0f)) {
           const bool mine = mx > m_used + 8.0f;
           const float alpha = mine ? ex2_approx(m_used - mx) : 1.0f;
@@ -777,6 +854,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
           float s0, s1;
           unpack2(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), s0, s1);
           l_sum += s0 + s1;
+        }
+        // V rows no row of the tile sees hold anything: zero them, so that
+        // 0 * (non-finite) cannot reach O.  Those that only some rows see (the
+        // tile's own keys) must not reach the others either: their non-finite
+        // values are taken out and noted for the output warps.
+        const int valid = min(cap, max(0, it.prefix + it.j0 + it.n_rows - key0));
+        const int by_some = max(0, it.prefix + it.j0 + 1 - key0);
+        if (min(valid, by_some) < kBK) {
+          const int xv = v_place(g);
+          if (!(ok = wwait(&T->kv_full[xv % kSlots], (xv / kSlots) & 1))) break;
+          uint8_t* v = skv + (xv % kSlots) * kTileBytes;
+          clean_v<D / 64, F16>(v, T, k & 1, half * 128 + t, valid, by_some,
+                               key0 - (it.prefix + it.j0 + 1), a.v_group);
+          fence_proxy_async_smem();
         }
         tc_fence_before_sync();
         __syncwarp();

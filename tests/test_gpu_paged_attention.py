@@ -180,6 +180,64 @@ def test_non_finite_keys_reach_only_the_rows_that_see_them(P):
         del clean
 
 
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "f16")])
+@pytest.mark.parametrize("page", [0, 8, 16, 100])
+@pytest.mark.parametrize("rows,prefix", [([24, 5], [200, 30]), ([150, 90, 1], [0, 130, 40])])
+def test_non_finite_values_reach_only_the_rows_that_see_them(P, rows, prefix, page, D, dtype):
+    """Values of new rows' slots, seen by the later rows of their tile alone, and
+    of prefix slots, seen by all."""
+    b = Batch(rows, prefix, page)
+    inf, nan = float("inf"), float("nan")
+    c = Call(P, b, 8, 2, D, dtype)
+    # (request, slot past the prefix, KV head, dim, value); row 0's own slot is
+    # seen by every row, a pair of opposite infinities is NaN where both are seen
+    places = [(0, 5, 1, 3, inf), (0, 9, 1, 3, -inf), (0, 12, 0, D - 1, nan), (0, 23, 1, 17, -inf),
+              (1, 0, 0, 40, inf), (1, 4, 1, 0, nan), (0, rows[0] - 1, 0, 8, inf)]
+    if prefix[1] > 3:
+        places.append((1, -3, 1, 63, inf))
+    for r, j, h, d, x in places:
+        at = int(b.places(r, prefix[r] + j, prefix[r] + j + 1)[0])
+        c.v[at, h, d] = x
+    assert c.run(P) == 0
+    # the reference without 0 * inf: finite values, then what each row sees
+    k, v = f64(c.k), f64(c.v)
+    finite = np.where(np.isfinite(v), v, 0.0)
+    want, size = O.paged_attention(f64(c.q), k, finite, b.start, b.rows, b.prefix, b.page_size,
+                                   b.table, c.cfg.scale)
+    special = np.zeros(want.shape)
+    with np.errstate(invalid="ignore"):
+        for r, j, h, d, x in places:
+            first = int(b.start[r]) + max(j, 0)
+            special[first:int(b.start[r]) + rows[r], 4 * h:4 * h + 4, d] += x
+        want = want + special
+    got = f64(c.out[1:-1])
+    used = b.used_rows()
+    np.testing.assert_array_equal(np.isnan(got[used]), np.isnan(want[used]))
+    np.testing.assert_array_equal(np.isinf(got[used]), np.isinf(want[used]))
+    np.testing.assert_array_equal(np.sign(got[used][np.isinf(want[used])]),
+                                  np.sign(want[used][np.isinf(want[used])]))
+    fin = used[:, None, None] & np.isfinite(want)
+    u = half_step(c.dt)
+    tol = (u + 5e-4) * size + u * np.abs(np.where(fin, want, 0))
+    if dtype == "f16":
+        tol += float(max(b.prefix + b.rows)) * 2.0 ** -25 * 6
+    assert (np.abs(np.where(fin, got - want, 0)) <= tol).all()
+
+
+def test_many_non_finite_values(P):
+    """More of them in a tile than are told apart: rows from the first on are
+    NaN, those before it untouched."""
+    b = Batch([32], [64], 16)
+    c = Call(P, b, 8, 2, 128)
+    clean = c.want()
+    at = torch.from_numpy(b.places(0, 64 + 10, 64 + 32)).cuda()
+    c.v[at] = float("nan")
+    assert c.run(P) == 0
+    got = f64(c.out[1:-1])
+    assert np.isnan(got[10:]).all()
+    c.check(clean, rows=np.arange(10))
+
+
 def test_bad_requests_and_pages(P):
     b = Batch([3, 40, 2, 5], [4, 60, 30, 7], 8)
     c = Call(P, b, 4, 2, 64)
