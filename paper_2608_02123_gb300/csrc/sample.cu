@@ -31,7 +31,8 @@
 //   weight (top-p): the logits are binned linearly below the maximum, by count
 //   and by weight in single precision; the bins that the target can fall in
 //   are gathered and ranked on top of the exact sums above them.  Bins too full
-//   for that (long runs of equal logits) are left to a bisection over the keys.
+//   for that (flat rows, long runs of equal logits) are searched digit by digit,
+//   nine bits of the key a pass.
 #include <type_traits>
 
 #include "kv_rows.cuh"
@@ -44,7 +45,7 @@ constexpr int kSmpThreads = 512;
 constexpr int kSmpWarps = kSmpThreads / 32;
 constexpr int kSmpMaxCluster = 16;
 constexpr int kSmpBins = 512;
-constexpr int kSmpList = 384;               // gathered keys of a bin
+constexpr int kSmpList = 512;               // gathered keys of a bin
 constexpr int kSmpMaxGroups = 512;          // groups of lanes whose maxima are ranked
 constexpr int kSmpCand = 640;               // candidates one CTA can rank
 constexpr int kSmpMaxV = 1 << 18;           // sums of 2^45-scaled weights fit 64 bits
@@ -232,6 +233,11 @@ __device__ __forceinline__ unsigned long long order_key(float z, int index) {
   return (static_cast<unsigned long long>(o) << 32) | (0xffffffffu - static_cast<unsigned>(index));
 }
 
+// The same in 50 bits.
+__device__ __forceinline__ unsigned long long short_key(unsigned long long key) {
+  return (key >> 32) << 18 | (key & (kSmpMaxV - 1));
+}
+
 // x in [0, 1) as a 64-bit fraction (exact from 2^-41 on).
 __device__ __forceinline__ unsigned long long fraction64(float x) {
   const unsigned b = __float_as_uint(x);
@@ -367,6 +373,8 @@ __device__ __forceinline__ unsigned long long weight(const SampleShared* S, cons
   light_weights(S, f, fmaxf(z, f.low), fmaxf(z, f.low), w, same);
   return w;
 }
+
+static_assert(kSmpBins == kSmpThreads && kSmpMaxV == 1 << 18, "digits: a bin a thread");
 
 template <int DT, bool STREAM>
 __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
@@ -1013,38 +1021,95 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         }
         return;
       }
-      summed = false;
-      // too many keys in the bins: K* bit by bit, the largest key whose head
-      // reaches the target
-      unsigned long long key = 0, key_w = 0;
-      for (int bit = 63; bit >= 0; --bit) {
-        const unsigned long long trial = key | (1ull << bit);
-        unsigned long long hw = 0;
-        unsigned hn = 0;
+      // Too many keys in the bins (a flat row, or long runs of equal logits): K*
+      // digit by digit from the highest, the keys as numbers of 50 bits (the
+      // logit's order, then 2^18 - 1 - index)
+      auto in_bins = [&](float z) {
+        const float t = fmaf(f.m - z, bin_scale, 8388608.0f);
+        return t >= to_b0 && t <= to_b1 && z >= f.cut;
+      };
+      unsigned long long base = by_weight ? above_w : above_n;       // of what is above
+      unsigned long long digits = 0;                        // K*'s, so far
+#pragma unroll 1
+      for (int shift = 45; shift >= 0; shift -= 9) {
+        for (int i = tid; i < 2 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
+        __syncthreads();
+        if (tid == 0) {
+          S->bin0 = 0;
+          S->border_w = base;
+        }
+        auto add = [&](int d, unsigned long long v) {       // 64 bits in two words
+          const unsigned lo = static_cast<unsigned>(v);
+          const unsigned old = atomicAdd(&S->hist[0][d], lo);
+          atomicAdd(&S->hist[1][d], static_cast<unsigned>(v >> 32) + (old + lo < old ? 1u : 0u));
+        };
         pass(kNear, [&](const uint4& raw, int i0) {
           float x[kVec];
           E::unpack(raw, x);
-          unsigned up = 0;
+          unsigned in = 0;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            up |= (x[e] - f.base >= f.cut && order_key(x[e], i0 + e) >= trial ? 1u : 0u) << e;
-          if (!__any_sync(kFull, up != 0)) return;
-          unsigned long long w[kVec];
-          weights(S, f, x, w);
-          hn += __popc(up);
+          for (int e = 0; e < kVec; ++e) in |= (in_bins(x[e] - f.base) ? 1u : 0u) << e;
+          if (!__any_sync(kFull, in != 0)) return;
+#pragma unroll 1
+          for (int e = 0; e < kVec; ++e) {
+            float z = 0.0f;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) hw += (up >> e) & 1u ? w[e] : 0ull;
+            for (int i = 0; i < kVec; ++i)
+              if (i == e) z = x[i];
+            const unsigned long long key = short_key(order_key(z, i0 + e));
+            const bool mine_in = ((in >> e) & 1u) && (key >> (shift + 9)) == digits;
+            const unsigned who = __ballot_sync(kFull, mine_in);
+            if (who == 0) continue;
+            unsigned long long v = 0;
+            if (mine_in) v = by_weight ? weight(S, f, z) : 1ull;
+            const int d = static_cast<int>(key >> shift) & (kSmpBins - 1);
+            const int d0 = __shfl_sync(kFull, d, __ffs(who) - 1);
+            if (__any_sync(kFull, mine_in && d != d0)) {
+              if (mine_in) add(d, v);
+            } else {                                        // one digit: one addition
+              v = warp_sum64(v);
+              if (lane == 0) add(d0, v);
+            }
+          }
         });
-        hw = cluster_total(hw);
-        const unsigned long long reached = by_weight ? hw : cluster_total(hn);
-        if (reached >= target) {
-          key = trial;
-          key_w = hw;
+        csync<STREAM>();
+        // the digit with which the target is reached, the same in every CTA
+        const int d = kSmpBins - 1 - tid;
+        unsigned long long own = 0;
+        for (int r = 0; r < n_cta; ++r) {
+          const SampleShared* R = cluster_ptr<STREAM>(S, r);
+          own += (static_cast<unsigned long long>(R->hist[1][d]) << 32) + R->hist[0][d];
         }
+        unsigned long long upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned long long p = __shfl_up_sync(kFull, upto, o);
+          if (lane >= o) upto += p;
+        }
+        if (lane == 31) S->red[warp] = upto;
+        __syncthreads();
+        upto += base;
+        for (int w = 0; w < warp; ++w) upto += S->red[w];
+        if (upto >= target && upto - own < target) {
+          S->bin0 = d;
+          S->border_w = upto - own;
+        }
+        csync<STREAM>();
+        digits = digits << 9 | static_cast<unsigned>(S->bin0);
+        base = S->border_w;
       }
+      pass(kNear, [&](const uint4& raw, int i0) {           // the weights kept of the bins
+        float x[kVec];
+        E::unpack(raw, x);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (in_bins(x[e] - f.base) && short_key(order_key(x[e], i0 + e)) >= digits)
+            mine += weight(S, f, x[e]);
+      });
+      above_w = cluster_total(mine);
       if (tid == 0) {
-        S->border = key;
-        S->border_w = key_w;
+        S->border = (digits >> 18) << 32 | 0xfffc0000u | (digits & 0x3ffffu);
+        S->border_w = above_w;
       }
       __syncthreads();
     };

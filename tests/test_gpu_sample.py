@@ -309,6 +309,25 @@ def test_streamed_rows_report_errors(P):
     np.testing.assert_array_equal(got[rest], good[rest])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [10, 308])
+def test_flat_rows(P, rows, dtype):
+    """Borders among thousands of equal or nearly equal logits, a row to a
+    cluster and a row to a CTA."""
+    z, u = draw(rows, 151936, dtype, seed=rows)
+    n = rows // 2
+    z[1::7] = torch.randint(0, 3, z[1::7].shape, device="cuda").to(z.dtype)
+    z[4::7] = (z[4::7].float() / 100).to(z.dtype)
+    # a request of two rows each
+    params = dict(temperature=np.array([1.0, 1.5, 2.5, 40.0])[np.arange(n) % 4],
+                  top_p=np.array([0.95, 0.6, 1.0, 0.99, 0.3])[np.arange(n) % 5],
+                  top_k=np.array([0, 5000, 0, 70000, 0, 0])[np.arange(n) % 6],
+                  min_p=np.array([0.0, 0.0, 0.0, 0.5])[np.arange(n) % 4])
+    got, st = run(P, z, u, group=2, **params)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, group=2, **params))
+
+
 def test_top_p_needs_no_bisection(P):
     """Rows whose nucleus holds thousands of tokens take about as long as a few
     passes over them, not as the 64 of the bisection that only long runs of
