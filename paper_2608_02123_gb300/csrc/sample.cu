@@ -117,6 +117,8 @@ struct alignas(16) SampleShared {
   unsigned long long border, border_w;      // K* and the weight of its head
   int found;
   unsigned list_n, local_n;
+  int run;                                  // the warp whose run holds the token (-1: none)
+  unsigned long long run_before;            // the weight before that run
   unsigned long long part[2][kSmpMaxCluster];
   unsigned long long red[kSmpWarps];
   union {
@@ -133,7 +135,7 @@ struct alignas(16) SampleShared {
       };
     };
   };
-  float pending[kSmpWarps][64];             // logits of a warp, until 32 are together
+  int pending[kSmpWarps][64];               // a warp's elements, until 32 are together
   uint2 tab[128][16];                       // light table, a column per lane pair
 };
 
@@ -167,10 +169,11 @@ __device__ __forceinline__ void csync() {
   }
 }
 
-// Light weights of two logits (relative to base, at least f.low).
-__device__ __forceinline__ void light_weights(const SampleShared* S, const RowFacts& f, float x0,
-                                              float x1, unsigned long long& w0,
-                                              unsigned long long& w1) {
+// Light weights of two logits (relative to base, at least f.low) in units of
+// 2^-46, cut off: rounded to units of 2^-45 they are (w + 1) / 2.
+__device__ __forceinline__ void light_halves(const SampleShared* S, const RowFacts& f, float x0,
+                                             float x1, unsigned long long& w0,
+                                             unsigned long long& w1) {
   const uint64_t x = pack2(x0, x1), c = pack2(f.c_hi, f.c_hi);
   const uint64_t t = fma2(x, c, pack2(kMagic, kMagic));
   const uint64_t nk = fma2(t, pack2(-1.0f, -1.0f), pack2(kMagic, kMagic));
@@ -192,8 +195,15 @@ __device__ __forceinline__ void light_weights(const SampleShared* S, const RowFa
           b0, b1);
   const uint32_t v0 = e0.x + (static_cast<uint32_t>(__float_as_int(b0)) << 2);
   const uint32_t v1 = e1.x + (static_cast<uint32_t>(__float_as_int(b1)) << 2);
-  w0 = (((static_cast<unsigned long long>(v0) << 15) >> (n0 >> 7)) + 1) >> 1;
-  w1 = (((static_cast<unsigned long long>(v1) << 15) >> (n1 >> 7)) + 1) >> 1;
+  w0 = (static_cast<unsigned long long>(v0) << 15) >> (n0 >> 7);
+  w1 = (static_cast<unsigned long long>(v1) << 15) >> (n1 >> 7);
+}
+__device__ __forceinline__ void light_weights(const SampleShared* S, const RowFacts& f, float x0,
+                                              float x1, unsigned long long& w0,
+                                              unsigned long long& w1) {
+  light_halves(S, f, x0, x1, w0, w1);
+  w0 = (w0 + 1) >> 1;
+  w1 = (w1 + 1) >> 1;
 }
 
 __device__ __noinline__ unsigned long long fine_weight(const RowFacts& f, float x) {
@@ -279,9 +289,14 @@ struct Elem<PCTREE_F32> {
     return max_nan(m, __uint_as_float(v.z), __uint_as_float(v.w));
   }
   static __device__ __forceinline__ float value(Max m) { return m; }
-  static __device__ __forceinline__ void unpack4(const uint4& v, int, float (&x)[4]) {
-    unpack(v, x);
+  // the first two elements, which leave the vector
+  static __device__ __forceinline__ float2 next2(uint4& v) {
+    const float2 x = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+    v.x = v.z;
+    v.y = v.w;
+    return x;
   }
+  static __device__ __forceinline__ float one(float v) { return v; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x);
     x[1] = __uint_as_float(v.y);
@@ -314,13 +329,14 @@ struct Elem16 {
     const float2 p = unpack16<F16>(m);
     return max_nan(p.x, p.y);
   }
-  static __device__ __forceinline__ void unpack4(const uint4& v, int part, float (&x)[4]) {
-    const float2 lo = unpack16<F16>(part ? v.z : v.x), hi = unpack16<F16>(part ? v.w : v.y);
-    x[0] = lo.x;
-    x[1] = lo.y;
-    x[2] = hi.x;
-    x[3] = hi.y;
+  static __device__ __forceinline__ float2 next2(uint4& v) {
+    const float2 x = unpack16<F16>(v.x);
+    v.x = v.y;
+    v.y = v.z;
+    v.z = v.w;
+    return x;
   }
+  static __device__ __forceinline__ float one(uint16_t v) { return unpack16<F16>(v).x; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -395,6 +411,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     fence_barrier_init();
     S->list_n = 0;
     S->local_n = 0;
+    S->run = -1;
   }
   pdl_wait();
   const int g = row / a.group;
@@ -613,6 +630,37 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   __syncthreads();
   RowFacts f = S->row;
 
+  // Element `index` of the row (of this CTA's slice).
+  auto element = [&](int index) { return E::one(reinterpret_cast<const T*>(vec)[index - first]); };
+  // Gathers the elements of the lanes' `hits` (bits, from index i0) until every
+  // lane has one for fn, so that little of a warp idles where few are wanted.
+  int waiting = 0;
+  int* pending = S->pending[warp];
+  auto gather = [&](unsigned hits, int i0, auto&& fn) {
+    for (;;) {
+      const unsigned who = __ballot_sync(kFull, hits != 0);
+      if (who == 0) return;
+      if (hits != 0) {
+        pending[waiting + __popc(who & ((1u << lane) - 1u))] = i0 + __ffs(hits) - 1;
+        hits &= hits - 1;
+      }
+      waiting += __popc(who);
+      __syncwarp();
+      if (waiting >= 32) {
+        fn(element(pending[lane]));
+        const int rest = pending[32 + lane];
+        __syncwarp();
+        pending[lane] = rest;
+        waiting -= 32;
+        __syncwarp();
+      }
+    }
+  };
+  auto gather_rest = [&](auto&& fn) {
+    if (lane < waiting) fn(element(pending[lane]));
+    waiting = 0;
+    __syncwarp();
+  };
   // sums the cluster's values (one per thread) for everyone; the next sum but
   // one writes the same words, with a barrier in between
   int sums = 0;
@@ -634,42 +682,42 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   // those above 2^-12 of the total; leaves this lane's sum in `mine`
   unsigned long long all_w = 0, mine = 0;
   auto sum_all = [&]() {
+    // two logits at a time: the loop stays in the innermost instruction cache
+    // (the sum of rounded weights is the sum of w + (w & 1), halved)
     mine = 0;
-    pass(kNear, [&](const uint4& raw, int) {
-      // four logits at a time: the loop then stays in the innermost
-      // instruction cache
+    pass(kNear, [&](uint4 raw, int) {
 #pragma unroll 1
-      for (int part = 0; part < kVec / 4; ++part) {
-        float x[4];
-        E::unpack4(raw, part, x);
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          unsigned long long w0, w1;
-          light_weights(S, f, fmaxf(x[e] - f.base, f.low), fmaxf(x[e + 1] - f.base, f.low), w0,
-                        w1);
-          mine += w0 + w1;
-        }
+      for (int i = 0; i < kVec / 2; ++i) {
+        const float2 x = E::next2(raw);
+        unsigned long long w0, w1;
+        light_halves(S, f, fmaxf(x.x - f.base, f.low), fmaxf(x.y - f.base, f.low), w0, w1);
+        mine += w0 + (w0 & 1);
+        mine += w1 + (w1 & 1);
       }
     });
+    mine >>= 1;
     const unsigned long long rough = cluster_total(mine);
     f.fine_from =
         fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * octave);
     if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
-      pass(kFar, [&](const uint4& raw, int) {
+      auto more = [&](float x) {
+        const float z = x - f.base;
+        unsigned long long w0, w1;
+        light_weights(S, f, z, z, w0, w1);
+        mine += fine_weight(f, z) - w0;
+      };
+      pass(kFar, [&](const uint4& raw, int i0) {
+        unsigned hits = 0;
         if (E::value(E::larger(raw, E::none())) - f.base >= f.fine_from) {
           float x[kVec];
           E::unpack(raw, x);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const float z = x[e] - f.base;
-            if (z >= f.fine_from) {
-              unsigned long long w0, w1;
-              light_weights(S, f, z, z, w0, w1);
-              mine += fine_weight(f, z) - w0;
-            }
-          }
+          for (int e = 0; e < kVec; ++e)
+            hits |= (x[e] - f.base >= f.fine_from ? 1u : 0u) << e;
         }
+        gather(hits, i0, more);
       });
+      gather_rest(more);
     }
     if (by_k || by_p) all_w = cluster_total(mine);          // else the draw adds up
   };
@@ -930,8 +978,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       const float to_b1 = 8388608.0f + static_cast<float>(S->bin1);
       unsigned long long above_w = 0;
       unsigned above = 0;
-      int waiting = 0;                                      // logits in `pending`
-      float* pending = S->pending[warp];
+      auto more = [&](float x) { above_w += weight(S, f, x); };
       pass(kNear, [&](const uint4& raw, int i0) {
         float x[kVec];
         E::unpack(raw, x);
@@ -965,27 +1012,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           for (int e = 0; e < kVec; ++e) above_w += (up >> e) & 1u ? w[e] : 0ull;
           return;
         }
-        // few: gathered until every lane has one
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const bool mine_up = (up >> e) & 1u;
-          const unsigned who = __ballot_sync(kFull, mine_up);
-          if (who == 0) continue;
-          if (mine_up) pending[waiting + __popc(who & ((1u << lane) - 1u))] = x[e];
-          waiting += __popc(who);
-          if (waiting >= 32) {
-            __syncwarp();
-            above_w += weight(S, f, pending[lane]);
-            const float rest = pending[32 + lane];
-            __syncwarp();
-            pending[lane] = rest;
-            waiting -= 32;
-          }
-        }
-        __syncwarp();
+        gather(up, i0, more);
       });
-      __syncwarp();
-      if (lane < waiting) above_w += weight(S, f, pending[lane]);
+      gather_rest(more);
       mine = above_w;
       above_w = cluster_total(above_w);
       const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
@@ -1188,20 +1217,39 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     if (i == self % kPer) before = scan - lane_in + upto[i];
   before = __shfl_sync(kFull, before, self / kPer) - mine;
   const unsigned long long target = place_of(u, total);
-  if (before > target || before + mine <= target) return;
-  unsigned long long cum = before;
-  for (int vb = v0; vb < v1; vb += 32) {
+  // that warp's run, divided among the CTA's warps
+  if (lane == 0 && before <= target && before + mine > target) {
+    S->run = warp;
+    S->run_before = before;
+  }
+  __syncthreads();
+  if (S->run < 0) return;
+  const int r0 = min(n_vec, S->run * per_warp), r1 = min(n_vec, r0 + per_warp);
+  const int part = (r1 - r0 + kSmpWarps - 1) / kSmpWarps;
+  const int s0 = min(r1, r0 + warp * part), s1 = min(r1, s0 + part);
+  auto kept_weights = [&](int vb, int v1, unsigned long long (&w)[kVec]) {
     const int v = vb + lane;
     float x[kVec];
     E::unpack(v < v1 ? vec[v] : E::low_vec(), x);
-    const int i0 = first + v * kVec;
-    unsigned long long w[kVec], sum = 0;
     weights(S, f, x, w);
+    unsigned long long sum = 0;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-      if (!kept(x[e], i0 + e)) w[e] = 0;
+      if (!kept(x[e], first + v * kVec + e)) w[e] = 0;
       sum += w[e];
     }
+    return sum;
+  };
+  unsigned long long w[kVec], part_w = 0;
+  for (int vb = s0; vb < s1; vb += 32) part_w += kept_weights(vb, s1, w);
+  part_w = warp_sum64(part_w);
+  if (lane == 0) S->red[warp] = part_w;
+  __syncthreads();
+  unsigned long long cum = S->run_before;
+  for (int i = 0; i < warp; ++i) cum += S->red[i];
+  if (cum > target || cum + part_w <= target) return;
+  for (int vb = s0; vb < s1; vb += 32) {
+    const unsigned long long sum = kept_weights(vb, s1, w);
     unsigned long long in = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -1216,7 +1264,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           at += w[e];
-          if (token < 0 && at > target) token = i0 + e;
+          if (token < 0 && at > target) token = first + (vb + lane) * kVec + e;
         }
         a.tokens[row] = token;
       }
