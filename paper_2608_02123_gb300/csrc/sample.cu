@@ -97,7 +97,6 @@ struct RowFacts {
   float c_hi, c_lo;                         // 128 log2(e) / T
   float base;
   float m;                                  // the maximum
-  float low;                                // 60 octaves below: clamped to, weight 0
   float cut;                                // 46 octaves below: weight 0 from here down
   float fine_from;                          // from it on the fine form
   float min_z;                              // min_p keeps logits (not relative) from it on
@@ -169,8 +168,18 @@ __device__ __forceinline__ void csync() {
   }
 }
 
-// Light weights of two logits (relative to base, at least f.low) in units of
-// 2^-46, cut off: rounded to units of 2^-45 they are (w + 1) / 2.
+// v * 2^(32 - n) cut off, 0 from n = 64 on.
+__device__ __forceinline__ unsigned long long high_shifted(uint32_t v, uint32_t n) {
+  unsigned long long r;
+  asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tshr.u64 %0, t, %3;\n\t}"
+      : "=l"(r) : "r"(0u), "r"(v), "r"(n));
+  return r;
+}
+
+// Light weights of two logits (relative to base, or -inf) in units of 2^-46,
+// cut off: rounded to units of 2^-45 they are (w + 1) / 2.  Logits so far below
+// that t leaves [2^23, 2^24) need no clamp: its bits, as an integer, are then
+// so far from kMagic's that n shifts all of v out.
 __device__ __forceinline__ void light_halves(const SampleShared* S, const RowFacts& f, float x0,
                                              float x1, unsigned long long& w0,
                                              unsigned long long& w1) {
@@ -185,18 +194,19 @@ __device__ __forceinline__ void light_halves(const SampleShared* S, const RowFac
   const uint64_t s = mul2(r, p);
   float t0, t1;
   unpack2(t, t0, t1);
-  // n = round(x c) - k <= 0 is -(128 sh - j): sh = ceil(-n / 128), and the
-  // table is stored backwards
-  const int n0 = f.k + (0x4b400000 + 127) - __float_as_int(t0);
-  const int n1 = f.k + (0x4b400000 + 127) - __float_as_int(t1);
+  // round(x c) - k <= 0 is -(128 sh - j), sh = ceil of its 128th part, and the
+  // table is stored backwards; n = 128 (sh + 17) + 127 - j, for a shift from the
+  // upper word
+  const uint32_t top = static_cast<uint32_t>(f.k) + 0x4b400000u + 127u + 17u * 128u;
+  const uint32_t n0 = top - __float_as_uint(t0), n1 = top - __float_as_uint(t1);
   const uint2 e0 = S->tab[n0 & 127][threadIdx.x & 15], e1 = S->tab[n1 & 127][threadIdx.x & 15];
   float b0, b1;
   unpack2(fma2(pack2(__uint_as_float(e0.y), __uint_as_float(e1.y)), s, pack2(kMagic2, kMagic2)),
           b0, b1);
   const uint32_t v0 = e0.x + (static_cast<uint32_t>(__float_as_int(b0)) << 2);
   const uint32_t v1 = e1.x + (static_cast<uint32_t>(__float_as_int(b1)) << 2);
-  w0 = (static_cast<unsigned long long>(v0) << 15) >> (n0 >> 7);
-  w1 = (static_cast<unsigned long long>(v1) << 15) >> (n1 >> 7);
+  w0 = high_shifted(v0, n0 >> 7);
+  w1 = high_shifted(v1, n1 >> 7);
 }
 __device__ __forceinline__ void light_weights(const SampleShared* S, const RowFacts& f, float x0,
                                               float x1, unsigned long long& w0,
@@ -361,7 +371,7 @@ __device__ __forceinline__ void weights(const SampleShared* S, const RowFacts& f
 #pragma unroll
   for (int e = 0; e < N; e += 2) {
     const float z0 = x[e] - f.base, z1 = x[e + 1] - f.base;
-    light_weights(S, f, fmaxf(z0, f.low), fmaxf(z1, f.low), w[e], w[e + 1]);
+    light_weights(S, f, z0, z1, w[e], w[e + 1]);
     fine |= z0 >= f.fine_from || z1 >= f.fine_from;
   }
   if (fine) {
@@ -386,7 +396,7 @@ __device__ __forceinline__ unsigned long long weight(const SampleShared* S, cons
   const float z = x - f.base;
   if (z >= f.fine_from) return fine_weight(f, z);
   unsigned long long w, same;
-  light_weights(S, f, fmaxf(z, f.low), fmaxf(z, f.low), w, same);
+  light_weights(S, f, z, z, w, same);
   return w;
 }
 
@@ -615,7 +625,6 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     f.m = m - f.base;
     f.k = __float_as_int(fmaf(f.m, f.c_hi, kMagic)) - 0x4b400000;
     f.cut = f.m - kOctaves * octave;
-    f.low = f.m - 60.0f * octave;
     f.fine_from = f.cut;
     f.min_z = -INFINITY;
     if (by_m) {
@@ -685,17 +694,18 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     // two logits at a time: the loop stays in the innermost instruction cache
     // (the sum of rounded weights is the sum of w + (w & 1), halved)
     mine = 0;
+    unsigned odd = 0;
     pass(kNear, [&](uint4 raw, int) {
 #pragma unroll 1
       for (int i = 0; i < kVec / 2; ++i) {
         const float2 x = E::next2(raw);
         unsigned long long w0, w1;
-        light_halves(S, f, fmaxf(x.x - f.base, f.low), fmaxf(x.y - f.base, f.low), w0, w1);
-        mine += w0 + (w0 & 1);
-        mine += w1 + (w1 & 1);
+        light_halves(S, f, x.x - f.base, x.y - f.base, w0, w1);
+        mine += w0 + w1;
+        odd += (static_cast<unsigned>(w0) & 1u) + (static_cast<unsigned>(w1) & 1u);
       }
     });
-    mine >>= 1;
+    mine = (mine + odd) >> 1;
     const unsigned long long rough = cluster_total(mine);
     f.fine_from =
         fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * octave);
