@@ -253,11 +253,6 @@ __device__ __forceinline__ unsigned long long order_key(float z, int index) {
   return (static_cast<unsigned long long>(o) << 32) | (0xffffffffu - static_cast<unsigned>(index));
 }
 
-// The same in 50 bits.
-__device__ __forceinline__ unsigned long long short_key(unsigned long long key) {
-  return (key >> 32) << 18 | (key & (kSmpMaxV - 1));
-}
-
 // x in [0, 1) as a 64-bit fraction (exact from 2^-41 on).
 __device__ __forceinline__ unsigned long long fraction64(float x) {
   const unsigned b = __float_as_uint(x);
@@ -286,6 +281,7 @@ struct Elem;
 template <>
 struct Elem<PCTREE_F32> {
   using type = float;
+  static constexpr int kLowBits = 0;        // of a float that the type has not
   static constexpr int kVec = 4;
   static __device__ __forceinline__ float low() { return -INFINITY; }
   static __device__ __forceinline__ uint4 low_vec() {
@@ -317,6 +313,7 @@ struct Elem<PCTREE_F32> {
 template <bool F16>
 struct Elem16 {
   using type = uint16_t;
+  static constexpr int kLowBits = F16 ? 13 : 16;
   static constexpr int kVec = 8;
   static __device__ __forceinline__ uint16_t low() { return F16 ? 0xfc00 : 0xff80; }
   static __device__ __forceinline__ uint4 low_vec() {
@@ -642,7 +639,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   // Element `index` of the row (of this CTA's slice).
   auto element = [&](int index) { return E::one(reinterpret_cast<const T*>(vec)[index - first]); };
   // Gathers the elements of the lanes' `hits` (bits, from index i0) until every
-  // lane has one for fn, so that little of a warp idles where few are wanted.
+  // lane has one, so that little of a warp idles where few are wanted; then
+  // fn(element, its index, whether the lane has one) by the whole warp.
   int waiting = 0;
   int* pending = S->pending[warp];
   auto gather = [&](unsigned hits, int i0, auto&& fn) {
@@ -656,7 +654,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       waiting += __popc(who);
       __syncwarp();
       if (waiting >= 32) {
-        fn(element(pending[lane]));
+        fn(element(pending[lane]), pending[lane], true);
         const int rest = pending[32 + lane];
         __syncwarp();
         pending[lane] = rest;
@@ -666,7 +664,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     }
   };
   auto gather_rest = [&](auto&& fn) {
-    if (lane < waiting) fn(element(pending[lane]));
+    const bool have = lane < waiting;
+    fn(have ? element(pending[lane]) : -INFINITY, have ? pending[lane] : 0, have);
     waiting = 0;
     __syncwarp();
   };
@@ -710,7 +709,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     f.fine_from =
         fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * octave);
     if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
-      auto more = [&](float x) {
+      auto more = [&](float x, int, bool have) {
+        if (!have) return;
         const float z = x - f.base;
         unsigned long long w0, w1;
         light_weights(S, f, z, z, w0, w1);
@@ -988,7 +988,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       const float to_b1 = 8388608.0f + static_cast<float>(S->bin1);
       unsigned long long above_w = 0;
       unsigned above = 0;
-      auto more = [&](float x) { above_w += weight(S, f, x); };
+      auto more = [&](float x, int, bool have) {
+        if (have) above_w += weight(S, f, x);
+      };
       pass(kNear, [&](const uint4& raw, int i0) {
         float x[kVec];
         E::unpack(raw, x);
@@ -1061,16 +1063,29 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         return;
       }
       // Too many keys in the bins (a flat row, or long runs of equal logits): K*
-      // digit by digit from the highest, the keys as numbers of 50 bits (the
-      // logit's order, then 2^18 - 1 - index)
+      // by nine bits a pass from the highest, a key as a short number: the order
+      // of the logit (without the bits that its type has not) from the bins' end
+      // on, and 2^18 - 1 - index
       auto in_bins = [&](float z) {
         const float t = fmaf(f.m - z, bin_scale, 8388608.0f);
         return t >= to_b0 && t <= to_b1 && z >= f.cut;
       };
+      auto order_at = [&](float bin) {                      // a bin's place, at its upper end
+        const float z = f.base + (f.m - bin / bin_scale);
+        return static_cast<unsigned>(order_key(z, 0) >> 32) >> E::kLowBits;
+      };
+      const unsigned o_end = order_at(to_b1 - 8388608.0f + 1.0f);
+      const unsigned o_top = order_at(to_b0 - 8388608.0f - 1.0f);
+      auto short_key = [&](float x, int index) {
+        const unsigned o = static_cast<unsigned>(order_key(x, 0) >> 32) >> E::kLowBits;
+        return static_cast<unsigned long long>(o - o_end) << 18 |
+               static_cast<unsigned>(kSmpMaxV - 1 - index);
+      };
+      const int bits = 18 + 32 - __clz(o_top - o_end);
       unsigned long long base = by_weight ? above_w : above_n;       // of what is above
       unsigned long long digits = 0;                        // K*'s, so far
 #pragma unroll 1
-      for (int shift = 45; shift >= 0; shift -= 9) {
+      for (int shift = (bits - 1) / 9 * 9; shift >= 0; shift -= 9) {
         for (int i = tid; i < 2 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
         __syncthreads();
         if (tid == 0) {
@@ -1082,35 +1097,31 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           const unsigned old = atomicAdd(&S->hist[0][d], lo);
           atomicAdd(&S->hist[1][d], static_cast<unsigned>(v >> 32) + (old + lo < old ? 1u : 0u));
         };
+        auto count = [&](float x, int index, bool have) {
+          const unsigned long long key = short_key(x, index);
+          const bool in = have && (key >> (shift + 9)) == digits;
+          const unsigned who = __ballot_sync(kFull, in);
+          if (who == 0) return;
+          unsigned long long v = 0;
+          if (in) v = by_weight ? weight(S, f, x) : 1ull;
+          const int d = static_cast<int>(key >> shift) & (kSmpBins - 1);
+          const int d0 = __shfl_sync(kFull, d, __ffs(who) - 1);
+          if (__any_sync(kFull, in && d != d0)) {
+            if (in) add(d, v);
+          } else {                                          // one digit: one addition
+            v = warp_sum64(v);
+            if (lane == 0) add(d0, v);
+          }
+        };
         pass(kNear, [&](const uint4& raw, int i0) {
           float x[kVec];
           E::unpack(raw, x);
           unsigned in = 0;
 #pragma unroll
           for (int e = 0; e < kVec; ++e) in |= (in_bins(x[e] - f.base) ? 1u : 0u) << e;
-          if (!__any_sync(kFull, in != 0)) return;
-#pragma unroll 1
-          for (int e = 0; e < kVec; ++e) {
-            float z = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-              if (i == e) z = x[i];
-            const unsigned long long key = short_key(order_key(z, i0 + e));
-            const bool mine_in = ((in >> e) & 1u) && (key >> (shift + 9)) == digits;
-            const unsigned who = __ballot_sync(kFull, mine_in);
-            if (who == 0) continue;
-            unsigned long long v = 0;
-            if (mine_in) v = by_weight ? weight(S, f, z) : 1ull;
-            const int d = static_cast<int>(key >> shift) & (kSmpBins - 1);
-            const int d0 = __shfl_sync(kFull, d, __ffs(who) - 1);
-            if (__any_sync(kFull, mine_in && d != d0)) {
-              if (mine_in) add(d, v);
-            } else {                                        // one digit: one addition
-              v = warp_sum64(v);
-              if (lane == 0) add(d0, v);
-            }
-          }
+          gather(in, i0, count);
         });
+        gather_rest(count);
         csync<STREAM>();
         // the digit with which the target is reached, the same in every CTA
         const int d = kSmpBins - 1 - tid;
@@ -1137,17 +1148,25 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         digits = digits << 9 | static_cast<unsigned>(S->bin0);
         base = S->border_w;
       }
+      auto more_kept = [&](float x, int index, bool have) {
+        if (have && short_key(x, index) >= digits) mine += weight(S, f, x);
+      };
       pass(kNear, [&](const uint4& raw, int i0) {           // the weights kept of the bins
         float x[kVec];
         E::unpack(raw, x);
+        unsigned in = 0;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (in_bins(x[e] - f.base) && short_key(order_key(x[e], i0 + e)) >= digits)
-            mine += weight(S, f, x[e]);
+        for (int e = 0; e < kVec; ++e) in |= (in_bins(x[e] - f.base) ? 1u : 0u) << e;
+        gather(in, i0, more_kept);
       });
+      gather_rest(more_kept);
       above_w = cluster_total(mine);
       if (tid == 0) {
-        S->border = (digits >> 18) << 32 | 0xfffc0000u | (digits & 0x3ffffu);
+        const unsigned o = (static_cast<unsigned>(digits >> 18) + o_end) << E::kLowBits;
+        // (the bits that the type has not are ones in the order of negative logits)
+        const unsigned rest = (o & 0x80000000u) != 0 ? 0u : (1u << E::kLowBits) - 1u;
+        S->border = static_cast<unsigned long long>(o | rest) << 32 |
+                    (0xffffffffu - (kSmpMaxV - 1) + static_cast<unsigned>(digits & (kSmpMaxV - 1)));
         S->border_w = above_w;
       }
       __syncthreads();
