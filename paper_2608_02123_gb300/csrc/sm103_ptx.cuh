@@ -134,20 +134,8 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map,
       : "memory");
 }
 
-// tma_load_4d into the shared memory of every CTA of `mask` (bits are cluster
-// ranks), each completing on the barrier at the same place of its own.
-__device__ __forceinline__ void tma_load_4d_multicast(void* dst, const CUtensorMap* map,
-                                                      uint64_t* bar, int32_t x, int32_t y,
-                                                      int32_t z, int32_t w, uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::"
-      "bytes.multicast::cluster [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y),
-      "r"(z), "r"(w), "h"(mask)
-      : "memory");
-}
-
-// 5-D box loads; as tma_load_4d and tma_load_4d_multicast.
+// 5-D box loads; multicast: into the shared memory of every CTA of `mask` (bits are
+// cluster ranks), each completing on the barrier at the same place of its own.
 __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, uint64_t* bar,
                                             int32_t x, int32_t y, int32_t z, int32_t w,
                                             int32_t v) {
