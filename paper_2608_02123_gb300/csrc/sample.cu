@@ -902,9 +902,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
                                         45.0f + log2f(static_cast<float>(a.V)) -
                                         log2f((1.0f - top_p) * static_cast<float>(all_w))))));
     const float bin_scale = f.c_hi * (static_cast<float>(kSmpBins) / (128.0f * octaves));
-    auto bin_of = [&](float z) -> unsigned {                // monotone in z
-      return __float_as_uint(fmaf(f.m - z, bin_scale, 8388608.0f)) - 0x4b000000u;
-    };
+    // 2^23 + the bin of a logit `below` the maximum (monotone; a bin below
+    // kSmpBins is above the cut)
+    auto place = [&](float below) { return fmaf(below, bin_scale, 8388608.0f); };
     // weights in 2^-31.9 of the total, in single precision: off by at most half
     // a unit a token and 2^-18 of their sum
     // (the exact weights are relative to 2^(k/128), not to the maximum's)
@@ -922,11 +922,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       E::unpack(raw, x);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
-        const float z = x[e] - f.base;
-        const unsigned b = bin_of(z);
-        if (z >= f.cut && b < kSmpBins) {
-          atomicAdd(&S->hist[1][b],
-                    __float2uint_rn(ex2_approx((z - f.m) * scale2 + log_unit)));
+        const float below = m - x[e];
+        const unsigned b = __float_as_uint(place(below)) - 0x4b000000u;
+        if (b < kSmpBins) {
+          atomicAdd(&S->hist[1][b], __float2uint_rn(ex2_approx(fmaf(below, -scale2, log_unit))));
           if (by_k) atomicAdd(&S->hist[0][b], 1u);
         }
       }
@@ -988,43 +987,31 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       const float to_b1 = 8388608.0f + static_cast<float>(S->bin1);
       unsigned long long above_w = 0;
       unsigned above = 0;
-      auto more = [&](float x, int, bool have) {
-        if (have) above_w += weight(S, f, x);
+      // what the logits of the bins, and those above, are not below: a bin's
+      // place, at its upper end
+      auto logit_at = [&](float t) { return f.base + (f.m - (t - 8388608.0f) / bin_scale); };
+      const float from = logit_at(to_b1 + 1.0f);
+      auto more = [&](float x, int index, bool have) {
+        const float t = place(m - x);
+        if (have && t < to_b0) {
+          ++above;
+          above_w += weight(S, f, x);
+        } else if (have && t <= to_b1) {
+          const unsigned at = atomicAdd(&L->list_n, 1u);
+          if (at < kSmpList) {
+            L->list.key[at] = order_key(x, index);
+            L->list.w[at] = weight(S, f, x);
+          }
+        }
+        __syncwarp();
       };
       pass(kNear, [&](const uint4& raw, int i0) {
         float x[kVec];
         E::unpack(raw, x);
-        unsigned up = 0, in = 0;
+        unsigned hits = 0;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float z = x[e] - f.base;
-          const float t = fmaf(f.m - z, bin_scale, 8388608.0f);      // as bin_of
-          up |= (t < to_b0 ? 1u : 0u) << e;
-          in |= (t >= to_b0 && t <= to_b1 ? 1u : 0u) << e;
-        }
-        if (in != 0) {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            if (((in >> e) & 1u) && x[e] - f.base >= f.cut) {
-              const unsigned at = atomicAdd(&L->list_n, 1u);
-              if (at < kSmpList) {
-                L->list.key[at] = order_key(x[e], i0 + e);
-                L->list.w[at] = weight(S, f, x[e]);
-              }
-            }
-        }
-        __syncwarp();
-        const unsigned n_up = __reduce_add_sync(kFull, __popc(up));
-        if (n_up == 0) return;
-        above += __popc(up);
-        if (n_up > 16 * kVec) {                             // many: all of the vector
-          unsigned long long w[kVec];
-          weights(S, f, x, w);
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) above_w += (up >> e) & 1u ? w[e] : 0ull;
-          return;
-        }
-        gather(up, i0, more);
+        for (int e = 0; e < kVec; ++e) hits |= (x[e] >= from ? 1u : 0u) << e;
+        gather(hits, i0, more);
       });
       gather_rest(more);
       mine = above_w;
@@ -1066,22 +1053,20 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       // by nine bits a pass from the highest, a key as a short number: the order
       // of the logit (without the bits that its type has not) from the bins' end
       // on, and 2^18 - 1 - index
-      auto in_bins = [&](float z) {
-        const float t = fmaf(f.m - z, bin_scale, 8388608.0f);
-        return t >= to_b0 && t <= to_b1 && z >= f.cut;
+      const float to = logit_at(to_b0 - 1.0f);              // and not above
+      auto order_of = [&](float x) {
+        return static_cast<unsigned>(order_key(x, 0) >> 32) >> E::kLowBits;
       };
-      auto order_at = [&](float bin) {                      // a bin's place, at its upper end
-        const float z = f.base + (f.m - bin / bin_scale);
-        return static_cast<unsigned>(order_key(z, 0) >> 32) >> E::kLowBits;
+      const unsigned o_end = order_of(from);
+      auto in_bins = [&](float x) {
+        const float t = place(m - x);
+        return t >= to_b0 && t <= to_b1;
       };
-      const unsigned o_end = order_at(to_b1 - 8388608.0f + 1.0f);
-      const unsigned o_top = order_at(to_b0 - 8388608.0f - 1.0f);
       auto short_key = [&](float x, int index) {
-        const unsigned o = static_cast<unsigned>(order_key(x, 0) >> 32) >> E::kLowBits;
-        return static_cast<unsigned long long>(o - o_end) << 18 |
+        return static_cast<unsigned long long>(order_of(x) - o_end) << 18 |
                static_cast<unsigned>(kSmpMaxV - 1 - index);
       };
-      const int bits = 18 + 32 - __clz(o_top - o_end);
+      const int bits = 18 + 32 - __clz(order_of(to) - o_end);
       unsigned long long base = by_weight ? above_w : above_n;       // of what is above
       unsigned long long digits = 0;                        // K*'s, so far
 #pragma unroll 1
@@ -1099,7 +1084,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         };
         auto count = [&](float x, int index, bool have) {
           const unsigned long long key = short_key(x, index);
-          const bool in = have && (key >> (shift + 9)) == digits;
+          const bool in = have && in_bins(x) && (key >> (shift + 9)) == digits;
           const unsigned who = __ballot_sync(kFull, in);
           if (who == 0) return;
           unsigned long long v = 0;
@@ -1118,7 +1103,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           E::unpack(raw, x);
           unsigned in = 0;
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) in |= (in_bins(x[e] - f.base) ? 1u : 0u) << e;
+          for (int e = 0; e < kVec; ++e) in |= (x[e] >= from && x[e] <= to ? 1u : 0u) << e;
           gather(in, i0, count);
         });
         gather_rest(count);
@@ -1149,14 +1134,14 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         base = S->border_w;
       }
       auto more_kept = [&](float x, int index, bool have) {
-        if (have && short_key(x, index) >= digits) mine += weight(S, f, x);
+        if (have && in_bins(x) && short_key(x, index) >= digits) mine += weight(S, f, x);
       };
       pass(kNear, [&](const uint4& raw, int i0) {           // the weights kept of the bins
         float x[kVec];
         E::unpack(raw, x);
         unsigned in = 0;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) in |= (in_bins(x[e] - f.base) ? 1u : 0u) << e;
+        for (int e = 0; e < kVec; ++e) in |= (x[e] >= from && x[e] <= to ? 1u : 0u) << e;
         gather(in, i0, more_kept);
       });
       gather_rest(more_kept);
