@@ -33,8 +33,6 @@
 //   are gathered and ranked on top of the exact sums above them.  Bins too full
 //   for that (flat rows, long runs of equal logits) are searched digit by digit,
 //   nine bits of the key a pass.
-#include <type_traits>
-
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
@@ -44,6 +42,7 @@ namespace {
 constexpr int kSmpThreads = 512;
 constexpr int kSmpWarps = kSmpThreads / 32;
 constexpr int kSmpMaxCluster = 16;
+constexpr int kSmpAhead = 6;                // vectors of a lane per noted maximum
 constexpr int kSmpBins = 512;
 constexpr int kSmpList = 512;               // gathered keys of a bin
 constexpr int kSmpMaxGroups = 512;          // groups of lanes whose maxima are ranked
@@ -289,6 +288,7 @@ struct Elem<PCTREE_F32> {
   }
   // the largest of a vector's elements and `m` (NaN if any is)
   using Max = float;
+  static __device__ __forceinline__ Max join(Max a, Max b) { return max_nan(a, b); }
   static __device__ __forceinline__ Max none() { return -INFINITY; }
   static __device__ __forceinline__ Max larger(const uint4& v, Max m) {
     m = max_nan(m, __uint_as_float(v.x), __uint_as_float(v.y));
@@ -329,6 +329,7 @@ struct Elem16 {
     else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
+  static __device__ __forceinline__ Max join(Max a, Max b) { return max2(a, b); }
   static __device__ __forceinline__ Max larger(const uint4& v, Max m) {
     return max2(max2(max2(v.x, v.y), max2(v.z, v.w)), m);
   }
@@ -398,6 +399,11 @@ __device__ __forceinline__ unsigned long long weight(const SampleShared* S, cons
 }
 
 static_assert(kSmpBins == kSmpThreads && kSmpMaxV == 1 << 18, "digits: a bin a thread");
+
+// Maxima a lane of a streamed row notes.
+__host__ __device__ constexpr int notes_of(int n_vec) {
+  return ((n_vec + kSmpWarps - 1) / kSmpWarps + 32 * kSmpAhead - 1) / (32 * kSmpAhead);
+}
 
 template <int DT, bool STREAM>
 __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
@@ -514,41 +520,93 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   const uint4* vec = STREAM ? reinterpret_cast<const uint4*>(src)
                             : reinterpret_cast<const uint4*>(data);
   const int first = e0 - pad;                               // row index of data[0]
-  // fn(vector, row index of its first element) over the lane's vectors; lanes
-  // past the run's end get -inf, so the warp stays together.  Little work per
-  // vector (kFar): several loads, then their work; else the next load ahead of
-  // the work and one copy of it (unrolled heavy passes waited for instructions).
-  constexpr std::true_type kFar{};
-  constexpr std::false_type kNear{};
-  auto pass = [&](auto far, auto&& fn, bool reads = true) { // reads: else the lane gets -inf
+  // fn(vector, row index of its first element) over the lane's vectors, the
+  // next load ahead of the work; lanes past the run's end (and those that do not
+  // read) get -inf, so the warp stays together.
+  auto pass = [&](auto&& fn, bool reads = true) {
     auto load = [&](int v) { return v < v1 && reads ? vec[v] : E::low_vec(); };
-    if constexpr (decltype(far)::value && STREAM) {
-      constexpr int kAhead = 6;
+    uint4 next = load(v0 + lane);
 #pragma unroll 1
-      for (int vb = v0; vb < v1; vb += 32 * kAhead) {
-        uint4 raw[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) raw[i] = load(vb + i * 32 + lane);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fn(raw[i], first + (vb + i * 32 + lane) * kVec);
-      }
-    } else {
-      uint4 next = load(v0 + lane);
-#pragma unroll 1
-      for (int vb = v0; vb < v1; vb += 32) {
-        const uint4 now = next;
-        next = load(vb + 32 + lane);
-        fn(now, first + (vb + lane) * kVec);
-      }
+    for (int vb = v0; vb < v1; vb += 32) {
+      const uint4 now = next;
+      next = load(vb + 32 + lane);
+      fn(now, first + (vb + lane) * kVec);
     }
   };
 
   // ---------------- maximum ----------------
+  // A streamed row's lanes also note the maxima of kSmpAhead vectors each: later
+  // passes for few logits then read only where one is.
   typename E::Max largest = E::none();
-  pass(kFar, [&](const uint4& raw, int) { largest = E::larger(raw, largest); });
+  typename E::Max* noted = reinterpret_cast<typename E::Max*>(data) + tid;
+  if constexpr (STREAM) {
+    int note = 0;
+#pragma unroll 1
+    for (int vb = v0; vb < v1; vb += 32 * kSmpAhead, note += kSmpThreads) {
+      uint4 raw[kSmpAhead];
+#pragma unroll
+      for (int i = 0; i < kSmpAhead; ++i) {
+        const int v = vb + i * 32 + lane;
+        raw[i] = v < v1 ? vec[v] : E::low_vec();
+      }
+      typename E::Max here = E::none();
+#pragma unroll
+      for (int i = 0; i < kSmpAhead; ++i) here = E::larger(raw[i], here);
+      noted[note] = here;
+      largest = E::join(largest, here);
+    }
+  } else {
+    pass([&](const uint4& raw, int) { largest = E::larger(raw, largest); });
+  }
   float m = E::value(largest);
   if (!landed) m = __int_as_float(0x7fc00000);
   const float m1 = m;
+  // pass over at least the vectors with a logit that is wanted (monotone)
+  auto sparse_pass = [&](auto&& wanted, auto&& fn) {
+    if (!__any_sync(kFull, wanted(m1))) return;             // none in this warp's run
+    if constexpr (STREAM) {
+      // places (kSmpAhead vectors of a lane) are listed until 30 are known; then
+      // each lane loads one vector of each of six
+      static_assert(kSmpAhead == 6, "five places a load, six loads");
+      int* list = reinterpret_cast<int*>(data) + notes_of(n_vec) * kSmpThreads + warp * 64;
+      const int of = lane / 6, at = lane - of * 6;          // lanes 30 and 31: none
+      int n = 0;
+      auto read = [&]() {
+        uint4 raw[6];
+        int v[6];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+          const int x = i * 5 + of;
+          const int place = of < 5 && x < n ? list[x] : 0;
+          v[i] = v0 + ((place >> 5) * kSmpAhead + at) * 32 + (place & 31);
+          raw[i] = of < 5 && x < n && v[i] < v1 ? vec[v[i]] : E::low_vec();
+        }
+#pragma unroll
+        for (int i = 0; i < 6; ++i)
+          if (i * 5 < n) fn(raw[i], first + v[i] * kVec);
+      };
+      int note = 0;
+#pragma unroll 1
+      for (int vb = v0; vb < v1; vb += 32 * kSmpAhead, ++note) {
+        const bool hit = wanted(E::value(noted[note * kSmpThreads]));
+        const unsigned who = __ballot_sync(kFull, hit);
+        if (hit) list[n + __popc(who & ((1u << lane) - 1u))] = note * 32 + lane;
+        n += __popc(who);
+        __syncwarp();
+        while (n >= 30) {
+          read();
+          const int rest = list[30 + lane];
+          __syncwarp();
+          list[lane] = rest;
+          __syncwarp();
+          n -= 30;
+        }
+      }
+      if (n > 0) read();
+    } else {
+      pass(fn, wanted(m1));
+    }
+  };
   float mg = m;                                             // of this lane's group
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -584,16 +642,14 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   }
   if (temp == 0.0f) {                                       // the lowest index of the maximum
     int at = 0x7fffffff;
-    if (mw == m) {                                          // in this warp's run
-      pass(kFar, [&](const uint4& raw, int i0) {
-        if (E::value(E::larger(raw, E::none())) != m) return;
-        float x[kVec];
-        E::unpack(raw, x);
+    sparse_pass([&](float x) { return x == m; }, [&](const uint4& raw, int i0) {
+      if (E::value(E::larger(raw, E::none())) != m) return;
+      float x[kVec];
+      E::unpack(raw, x);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (x[e] == m) at = min(at, i0 + e);
-      });
-    }
+      for (int e = 0; e < kVec; ++e)
+        if (x[e] == m) at = min(at, i0 + e);
+    });
     at = __reduce_min_sync(kFull, at);
     int* best = reinterpret_cast<int*>(S->red);
     if (lane == 0) best[warp] = at;
@@ -694,7 +750,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     // (the sum of rounded weights is the sum of w + (w & 1), halved)
     mine = 0;
     unsigned odd = 0;
-    pass(kNear, [&](uint4 raw, int) {
+    pass([&](uint4 raw, int) {
 #pragma unroll 1
       for (int i = 0; i < kVec / 2; ++i) {
         const float2 x = E::next2(raw);
@@ -708,27 +764,25 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     const unsigned long long rough = cluster_total(mine);
     f.fine_from =
         fmaxf(f.cut, f.m + (log2f(static_cast<float>(rough)) - 57.0f) * octave);
-    if (__any_sync(kFull, m1 - f.base >= f.fine_from)) {    // some in this warp's run
-      auto more = [&](float x, int, bool have) {
-        if (!have) return;
-        const float z = x - f.base;
-        unsigned long long w0, w1;
-        light_weights(S, f, z, z, w0, w1);
-        mine += fine_weight(f, z) - w0;
-      };
-      pass(kFar, [&](const uint4& raw, int i0) {
-        unsigned hits = 0;
-        if (E::value(E::larger(raw, E::none())) - f.base >= f.fine_from) {
-          float x[kVec];
-          E::unpack(raw, x);
+    auto more = [&](float x, int, bool have) {
+      if (!have) return;
+      const float z = x - f.base;
+      unsigned long long w0, w1;
+      light_weights(S, f, z, z, w0, w1);
+      mine += fine_weight(f, z) - w0;
+    };
+    auto is_fine = [&](float x) { return x - f.base >= f.fine_from; };
+    sparse_pass(is_fine, [&](const uint4& raw, int i0) {
+      unsigned hits = 0;
+      if (is_fine(E::value(E::larger(raw, E::none())))) {
+        float x[kVec];
+        E::unpack(raw, x);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e)
-            hits |= (x[e] - f.base >= f.fine_from ? 1u : 0u) << e;
-        }
-        gather(hits, i0, more);
-      });
-      gather_rest(more);
-    }
+        for (int e = 0; e < kVec; ++e) hits |= (is_fine(x[e]) ? 1u : 0u) << e;
+      }
+      gather(hits, i0, more);
+    });
+    gather_rest(more);
     if (by_k || by_p) all_w = cluster_total(mine);          // else the draw adds up
   };
   if (all_light) sum_all();
@@ -769,29 +823,28 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     // (top_p needs the weight of all that top_k leaves)
     if (by_m && (group_lanes == 0 || !by_p)) from = fmaxf(from, f.min_z);
     unsigned mine_n = 0;
-    if (__any_sync(kFull, m1 >= from)) {                    // some in this warp's run
-      pass(kFar, [&](const uint4& raw, int i0) {
-        if (E::value(E::larger(raw, E::none())) >= from) {
-          float x[kVec];
-          E::unpack(raw, x);
-          unsigned hits = 0;
+    sparse_pass([&](float x) { return x >= from; }, [&](const uint4& raw, int i0) {
+      if (E::value(E::larger(raw, E::none())) >= from) {
+        float x[kVec];
+        E::unpack(raw, x);
+        unsigned hits = 0;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          hits |= (x[e] >= from && x[e] - f.base >= f.cut ? 1u : 0u) << e;
+        const unsigned n = __popc(hits);
+        if (n != 0) {
+          mine_n += n;
+          unsigned at = atomicAdd(&L->list_n, n);
 #pragma unroll
           for (int e = 0; e < kVec; ++e)
-            hits |= (x[e] >= from && x[e] - f.base >= f.cut ? 1u : 0u) << e;
-          const unsigned n = __popc(hits);
-          if (n != 0) {
-            mine_n += n;
-            unsigned at = atomicAdd(&L->list_n, n);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-              if ((hits >> e) & 1u) {
-                if (at < kSmpCand) L->cand.key[at] = order_key(x[e], i0 + e);
-                ++at;
-              }
-          }
+            if ((hits >> e) & 1u) {
+              if (at < kSmpCand) L->cand.key[at] = order_key(x[e], i0 + e);
+              ++at;
+            }
         }
-      }, m1 >= from);
-    }
+      }
+      __syncwarp();
+    });
     mine_n = __reduce_add_sync(kFull, mine_n);
     if (lane == 0 && mine_n != 0) atomicAdd(&S->local_n, mine_n);
     __syncthreads();
@@ -917,7 +970,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
     const unsigned long long slack = (unit_total >> 18) + a.V / 2 + 4096;
     for (int i = tid; i < 2 * kSmpBins; i += kSmpThreads) (&S->hist[0][0])[i] = 0;
     __syncthreads();
-    pass(kNear, [&](const uint4& raw, int) {
+    pass([&](const uint4& raw, int) {
       float x[kVec];
       E::unpack(raw, x);
 #pragma unroll
@@ -1005,7 +1058,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         }
         __syncwarp();
       };
-      pass(kNear, [&](const uint4& raw, int i0) {
+      pass([&](const uint4& raw, int i0) {
         float x[kVec];
         E::unpack(raw, x);
         unsigned hits = 0;
@@ -1098,7 +1151,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
             if (lane == 0) add(d0, v);
           }
         };
-        pass(kNear, [&](const uint4& raw, int i0) {
+        pass([&](const uint4& raw, int i0) {
           float x[kVec];
           E::unpack(raw, x);
           unsigned in = 0;
@@ -1136,7 +1189,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       auto more_kept = [&](float x, int index, bool have) {
         if (have && in_bins(x) && short_key(x, index) >= digits) mine += weight(S, f, x);
       };
-      pass(kNear, [&](const uint4& raw, int i0) {           // the weights kept of the bins
+      pass([&](const uint4& raw, int i0) {           // the weights kept of the bins
         float x[kVec];
         E::unpack(raw, x);
         unsigned in = 0;
@@ -1192,7 +1245,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   };
   if (!summed) {
     mine = 0;
-    pass(kNear, [&](const uint4& raw, int i0) {
+    pass([&](const uint4& raw, int i0) {
       float x[kVec];
       E::unpack(raw, x);
       unsigned keep = 0;
@@ -1314,6 +1367,8 @@ const void* sample_fn(int dtype, bool streamed) {
              : (streamed ? sample_fn<PCTREE_F16, true>() : sample_fn<PCTREE_F16, false>());
 }
 
+// Bytes of a slice with which two CTAs of a cluster placement share an SM.
+constexpr size_t kSmpSlice = 228 * 1024 / 2 - 1024 - 64 - sizeof(SampleShared);
 constexpr size_t kSampleSmem = sizeof(SampleShared) + (kSmpMaxV / 8 + 8) * 4;
 static_assert(kSampleSmem <= 227 * 1024 && kSampleSmem >= 120 * 1024, "shared memory per CTA");
 
@@ -1390,13 +1445,15 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   size_t bytes = sizeof(SampleShared);
   if (streamed) {
     a.slice = c.V;
-    if (per_sm == 1) bytes = 120 * 1024;                    // keeps a second CTA off the SM
+    bytes += static_cast<size_t>(notes_of(c.V / vec)) * kSmpThreads * 4 + kSmpWarps * 64 * 4;
+    // a size that keeps a second CTA off the SM
+    if (per_sm == 1 && bytes < 120 * 1024) bytes = 120 * 1024;
   } else {
     const int most = c.rows * 16ll <= num_sms && wide_clusters(c.dtype) ? 16 : 8;
     while (ctas < most && row_bytes > ctas * 8192ull) ctas *= 2;
     // fewer where that keeps all rows on the GPU at once, two CTAs an SM
     while (ctas > 1 && static_cast<long long>(c.rows) * ctas > 2 * num_sms &&
-           row_bytes <= ctas / 2 * 78000ull)
+           row_bytes <= ctas / 2 * kSmpSlice)
       ctas /= 2;
     a.slice = ((c.V + ctas - 1) / ctas + vec - 1) / vec * vec;
     ctas = (c.V + a.slice - 1) / a.slice;
