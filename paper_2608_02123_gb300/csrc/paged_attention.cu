@@ -26,6 +26,18 @@
 //               its own running maximum, sum and O: S is read from TMEM once,
 //               masked and scaled, P = 2^(s - m_used) written back over it
 // All waits are bounded (1 s) and end in PCTREE_ERR_TIMEOUT.
+//
+// What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
+//   tokens of 32 requests over up to 16384 slots: HBM, 850 MB in 138, 0.91 of
+//   the measured copy rate;
+//   four prompts of up to 4096 rows: K and V into the SMs, 64 KB a block at ~60
+//   B/ns, 404 in pages of 64 slots or more (1.06 PFLOP/s; the softmax chain of a
+//   block is nearly as long), 482 in pages of 16, whose 24 TMA boxes a block
+//   cost ~30 ns each; loading for every CTA alone 415 and 629;
+//   a token of one request: two launches and one block's chain, 13.4.
+// K a block ahead of V (415 -> 391 before values were checked), one box for both
+// halves of the dims in small pages (pages of 8: 556 -> 491 and, tokens, 253 ->
+// 183), pieces of equal length (a unit a CTA leaves SMs idle at the end).
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 

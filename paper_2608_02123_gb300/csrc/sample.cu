@@ -7,7 +7,9 @@
 //            results meet through distributed shared memory;
 //   stream   (many rows) a row belongs to one CTA, which reads it from memory
 //            in the first pass and from L2 in the others: no cluster barriers,
-//            and as many rows in flight as L2 holds.
+//            and as many rows in flight as L2 holds (4096 rows of 151936 bf16
+//            logits, mixed filters: 2745 us by clusters, 599 by streams when
+//            these came).
 //
 // Weights w = exp((z - max) / T) are summed as integers in units of 2^-45 of
 // the largest weight, so sums are exact and in any order the same.  A token is
@@ -33,6 +35,13 @@
 //   are gathered and ranked on top of the exact sums above them.  Bins too full
 //   for that (flat rows, long runs of equal logits) are searched digit by digit,
 //   nine bits of the key a pass.
+//
+// What bounds it (one GB300, us, 4096 streamed rows of 151936 bf16 logits; one
+// read of them at the measured copy rate is 184): rows with top-k 50 220 and with
+// min-p 209, HBM; plain ones 645, of which the light weights take 400, some 13
+// integer instructions a logit at half rate; top-p 0.95 alone 1180, the sum,
+// then the bins' atomics and the weights of what is kept.  A single row of f32
+// logits takes 28, a chain of passes and barriers of 16 CTAs.
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
@@ -1431,15 +1440,19 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   if (st != PCTREE_OK) return st;
   const int vec = 16 / el;
   const size_t row_bytes = static_cast<size_t>(c.V) * el;
-  // streamed: whole 16-byte vectors, a row for every CTA place of the GPU, and
-  // (two CTAs an SM, or one) the rows in flight in L2
+  // streamed: whole 16-byte vectors, (two CTAs an SM, or one) the rows in flight
+  // in L2, and rows for 3/5 of the SMs (us, clusters / streams, bf16 logits,
+  // plain | top-p 0.95 | top-k 50: 64 rows of 151936 46 / 57 | 87 / 170 | 29 / 26,
+  // 96 rows 58 / 58 | 126 / 165 | 36 / 29, 152 rows 79 / 58 | 170 / 171 | 44 / 29;
+  // 64 rows of 65536 32 / 38 | 51 / 65 | 26 / 25, 96 rows 41 / 35 | 68 / 68 | 29 /
+  // 23; f32 logits and shorter rows cross there too)
   const bool aligned = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && c.V % vec == 0 &&
                        (c.row_stride * el) % 16 == 0;
   const int per_sm = row_bytes * 2 * num_sms <= kStreamBytes ? 2 : 1;
-  const bool streamed = aligned && row_bytes * num_sms <= kStreamBytes &&
-                        c.rows >= num_sms * per_sm;
+  const bool streamed =
+      aligned && row_bytes * num_sms <= kStreamBytes && c.rows * 5ll >= num_sms * 3ll;
   // cluster: slices of at least 8 KB, up to eight of them, 16 while the SMs
-  // have room
+  // have room (one row of 151936 f32: 35.8 us by eight, 29.9 by 16)
   int ctas = 1;
   SampleArgs a{};
   size_t bytes = sizeof(SampleShared);
@@ -1451,7 +1464,8 @@ pctree_status pctree_sample(const pctree_sample_config* cfg, const void* logits,
   } else {
     const int most = c.rows * 16ll <= num_sms && wide_clusters(c.dtype) ? 16 : 8;
     while (ctas < most && row_bytes > ctas * 8192ull) ctas *= 2;
-    // fewer where that keeps all rows on the GPU at once, two CTAs an SM
+    // fewer where that keeps all rows on the GPU at once, two CTAs an SM (61
+    // rows of 32003 f16 logits: 20 us by eight, 11.3 by four)
     while (ctas > 1 && static_cast<long long>(c.rows) * ctas > 2 * num_sms &&
            row_bytes <= ctas / 2 * kSmpSlice)
       ctas /= 2;

@@ -330,8 +330,7 @@ def test_flat_rows(P, rows, dtype):
 
 def test_top_p_needs_no_bisection(P):
     """Rows whose nucleus holds thousands of tokens take about as long as a few
-    passes over them, not as the 64 of the bisection that only long runs of
-    equal logits need."""
+    passes over them, not as one for every bit of a key."""
     z, u = draw(64, 151936, "f32", seed=12)
 
     def ms(**params):
