@@ -28,7 +28,7 @@
 // All waits are bounded (1 s) and end in PCTREE_ERR_TIMEOUT.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
-//   tokens of 32 requests over up to 16384 slots: HBM, 850 MB in 138, 0.91 of
+//   tokens of 32 requests over up to 8192 slots: HBM, 854 MB in 138, 0.91 of
 //   the measured copy rate;
 //   four prompts of up to 4096 rows: K and V into the SMs, 64 KB a block at ~60
 //   B/ns, 404 in pages of 64 slots or more (1.06 PFLOP/s; the softmax chain of a
