@@ -328,6 +328,27 @@ def test_flat_rows(P, rows, dtype):
     np.testing.assert_array_equal(got, want(z, u, group=2, **params))
 
 
+@pytest.mark.parametrize("rows", [12, 312])
+def test_flat_rows_far_from_zero(P, rows):
+    """Long runs of equal logits at offsets whose floats are far apart."""
+    V = 4096
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    z = torch.randint(0, 3, (rows, V), generator=g, device="cuda").float()
+    offset = torch.tensor([0.0, 1e4, -3e4, 1e30, -1e30, 5e-39], device="cuda")
+    step = torch.tensor([1e-3, 0.25, 0.0078125, 1e29, 1e24, 1e-40], device="cuda")
+    i = torch.arange(rows, device="cuda") % 6
+    z = z * step[i][:, None] + offset[i][:, None]
+    u = torch.rand(rows, generator=g, device="cuda")
+    n = rows // 2
+    params = dict(temperature=np.array([1.0, 1e6, 0.01])[np.arange(n) // 3 % 3],
+                  top_p=np.array([0.5, 0.9])[np.arange(n) % 2],
+                  top_k=np.array([0, 2500, 0, 0])[np.arange(n) // 2 % 4])
+    got, st = run(P, z, u, group=2, **params)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, group=2, **params))
+
+
 def test_top_p_needs_no_bisection(P):
     """Rows whose nucleus holds thousands of tokens take about as long as a few
     passes over them, not as one for every bit of a key."""
