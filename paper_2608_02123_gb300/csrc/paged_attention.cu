@@ -285,26 +285,36 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   if (warp == 1) tmem_alloc(&T->tmem_base, kTmemCols);
   pdl_launch_dependents();
   pdl_wait();
-  // the requests, then the work of each, a warp each
+  // the requests and the work of each: a thread each, but a warp where there are
+  // several tiles
   for (int r = threadIdx.x; r < a.rows.batch; r += kThreads) {
-    const int start = a.rows.row_start[r], n = a.rows.n_rows[r], prefix = a.rows.prefix_len[r];
-    const bool good = kv_request_ok(a.rows, start, n, prefix);
-    if (!good && blockIdx.x == 0) report(a.status, PCTREE_ERR_INVALID_ARG);
+    const int start = a.rows.row_start[r], prefix = a.rows.prefix_len[r];
+    int n = a.rows.n_rows[r];
+    if (!kv_request_ok(a.rows, start, n, prefix)) {
+      if (blockIdx.x == 0) report(a.status, PCTREE_ERR_INVALID_ARG);
+      n = 0;
+    }
     T->start[r] = start;
-    T->n[r] = good ? n : 0;
+    T->n[r] = n;
     T->prefix[r] = prefix;
+    if (n <= unit_rows) T->upto[r] = n > 0 ? (blocks_of(a, prefix + n) + kUnitCharge) * a.Hkv : 0;
   }
   __syncthreads();
-  for (int r = warp; r < a.rows.batch; r += kThreads / 32) {
-    const int n = T->n[r], prefix = T->prefix[r];
-    unsigned w = 0;
-    for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
-      w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
-    if (n > unit_rows) {
+  constexpr int kWarps = kThreads / 32;
+  for (int r0 = warp; r0 < a.rows.batch; r0 += kThreads) {   // every kWarps-th is this warp's
+    const int mine = r0 + lane * kWarps;
+    unsigned several =
+        __ballot_sync(kFull, mine < a.rows.batch && T->n[min(mine, a.rows.batch - 1)] > unit_rows);
+    for (; several != 0; several &= several - 1) {
+      const int r = r0 + (__ffs(several) - 1) * kWarps;
+      const int n = T->n[r], prefix = T->prefix[r];
+      unsigned w = 0;
+      for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
+        w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
+      if (lane == 0) T->upto[r] = w * a.Hkv;
     }
-    if (lane == 0) T->upto[r] = w * a.Hkv;
   }
   __syncthreads();
   if (warp == 0) {
