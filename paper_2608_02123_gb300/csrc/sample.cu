@@ -948,13 +948,17 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
   }
 
   // ---------------- selection by bins ----------------
-  if (!all_light) {                                         // binning needs the total
+  const bool no_total = by_k && !by_p && top_k <= a.V / 8;
+  if (!all_light) {
     make_table();
     __syncthreads();
-    sum_all();
+    // a count needs no total; the fine weights of a few kept logits cost less
+    // than the light ones of all
+    if (no_total) f.fine_from = f.cut;
+    else sum_all();
   }
   unsigned long long border = 0;                            // keep keys >= border
-  bool summed = true;                                       // `mine` is of what is kept
+  bool summed = !no_total;                                  // `mine` is of what is kept
   if (by_k || by_p) {
     // top-p alone: as many octaves as tokens below them cannot reach half of
     // 1 - top_p of the weight, were all of them that heavy
@@ -987,7 +991,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
         const float below = m - x[e];
         const unsigned b = __float_as_uint(place(below)) - 0x4b000000u;
         if (b < kSmpBins) {
-          atomicAdd(&S->hist[1][b], __float2uint_rn(ex2_approx(fmaf(below, -scale2, log_unit))));
+          if (by_p)
+            atomicAdd(&S->hist[1][b], __float2uint_rn(ex2_approx(fmaf(below, -scale2, log_unit))));
           if (by_k) atomicAdd(&S->hist[0][b], 1u);
         }
       }
@@ -1222,6 +1227,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       find_bins(static_cast<unsigned long long>(top_k), false, 0);
       if (S->bin1 >= 0) {                                   // else fewer have a weight
         resolve(static_cast<unsigned long long>(top_k), false);
+        summed = true;
         border = S->border;
         all_w = S->border_w;
       }
