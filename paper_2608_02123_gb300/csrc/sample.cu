@@ -39,7 +39,7 @@
 // What bounds it (one GB300, us, 4096 streamed rows of 151936 bf16 logits; one
 // read of them at the measured copy rate is 184): rows with top-k 50 220 and with
 // min-p 209, HBM; plain ones 645, of which the light weights take 400, some 13
-// integer instructions a logit at half rate; top-p 0.95 alone 1180, the sum,
+// integer instructions a logit at half rate; top-p 0.95 alone 1240, the sum,
 // then the bins' atomics and the weights of what is kept.  A single row of f32
 // logits takes 28, a chain of passes and barriers of 16 CTAs.
 #include "kv_rows.cuh"
