@@ -269,6 +269,46 @@ def test_no_rows_at_all(P):
     assert (c.out == 9).all()
 
 
+@pytest.mark.parametrize("page", [0, 16])
+def test_as_many_requests_as_there_may_be(P, page):
+    """1024 requests: none, one and several tiles of rows in any order."""
+    rng = np.random.default_rng(3)
+    rows = rng.choice([0, 1, 1, 1, 2, 5], 1024)
+    rows[[0, 15, 16, 511, 512, 700, 1023]] = [70, 0, 33, 129, 40, 1, 65]
+    prefix = rng.integers(0, 40, 1024)
+    prefix[[3, 600]] = [300, 129]
+    c = Call(P, Batch(rows.tolist(), prefix.tolist(), page), 4, 1, 64)
+    assert c.run(P) == 0
+    c.check()
+
+
+def test_requests_that_share_the_pages_of_a_prefix(P):
+    b = Batch([1, 40, 3], [100, 130, 96], 16)
+    b.table[1, :6] = b.table[0, :6]
+    b.table[2, :6] = b.table[0, :6]
+    c = Call(P, b, 8, 2, 128)
+    assert c.run(P) == 0
+    c.check()
+
+
+def test_two_calls_at_once(P):
+    """On two streams, each with a workspace of its own: single tokens beside
+    prompts in pairs and in clusters of four."""
+    calls = [Call(P, Batch([1] * 20, [int(x) for x in range(5, 1005, 50)], 64), 16, 4, 128),
+             Call(P, Batch([205, 300], [40, 7], 16, seed=1), 16, 2, 128, seed=1),
+             Call(P, Batch([300, 90], [0, 333], 64, seed=2), 16, 2, 64, "f16", seed=2)]
+    want = [c.want() for c in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s in zip(calls, streams):
+            P.pctree_paged_attention(c.cfg, **c.args(), stream=s)
+    torch.cuda.synchronize()
+    for c, w in zip(calls, want):
+        assert int(c.status.item()) == 0
+        c.check(w)
+
+
 def test_streams_and_graphs(P):
     """On another stream, and replayed from two graphs that share a workspace
     one after the other."""

@@ -242,6 +242,28 @@ def test_stream_and_graph(P):
     np.testing.assert_array_equal(tokens.cpu().numpy(), ref)
 
 
+def test_two_calls_at_once(P):
+    """On two streams: rows in clusters beside streamed rows."""
+    sets = [(3, 151936, "f32", dict(top_p=0.95)), (320, 32000, "bf16", dict(top_k=50)),
+            (5, 9001, "f16", {})]
+    made = []
+    for i, (rows, V, dtype, params) in enumerate(sets):
+        z, u = draw(rows, V, dtype, seed=40 + i)
+        dev = {k: torch.full((rows,), v, device="cuda",
+                             dtype=torch.int32 if k == "top_k" else torch.float32)
+               for k, v in params.items()}
+        made.append((P.sample_config(rows, V, dtype=z.dtype), z, u,
+                     torch.empty(rows, dtype=torch.int32, device="cuda"), dev,
+                     want(z, u, **params), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for cfg, z, u, tokens, dev, _, stream in made:
+            P.pctree_sample(cfg, z, u, tokens, stream=stream, **dev)
+    torch.cuda.synchronize()
+    for _, _, _, tokens, _, ref, _ in made:
+        np.testing.assert_array_equal(tokens.cpu().numpy(), ref)
+
+
 def mixed_params(repeat=1):
     """One parameter set per group: every filter above."""
     sets = [FILTERS[n] for n in sorted(FILTERS)] * repeat
