@@ -222,6 +222,17 @@ def test_largest_vocabulary(P):
         np.testing.assert_array_equal(got, want(z, u, **params))
 
 
+@pytest.mark.parametrize("V,dtype", [(1 << 18, "f16"), (1 << 18, "bf16"), (179200, "f32")])
+def test_largest_streamed_vocabularies(P, V, dtype):
+    """The longest rows that still belong to one CTA each, every filter."""
+    params = mixed_params()
+    n = len(params["top_k"])
+    z, u = draw(6 * n, V, dtype, seed=21)
+    got, st = run(P, z, u, group=6, **params)
+    assert st == 0
+    np.testing.assert_array_equal(got, want(z, u, group=6, **params))
+
+
 def test_stream_and_graph(P):
     z, u = draw(9, 9001, "bf16", seed=6)
     ref = want(z, u, top_k=20)
