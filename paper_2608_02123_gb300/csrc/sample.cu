@@ -123,6 +123,7 @@ struct alignas(16) SampleShared {
   int bin0, bin1;                           // the bins a target can fall in (-1: past all)
   unsigned long long border, border_w;      // K* and the weight of its head
   int found;
+  unsigned long long kept_w[kSmpWarps];     // of the list, by the warps of their runs
   unsigned list_n, local_n;
   int run;                                  // the warp whose run holds the token (-1: none)
   unsigned long long run_before;            // the weight before that run
@@ -138,6 +139,7 @@ struct alignas(16) SampleShared {
         unsigned hist[2][kSmpBins];         // count, weight in 2^-32 of the total
         struct {
           unsigned long long key[kSmpList], w[kSmpList];
+          unsigned char owner[kSmpList];    // the warp, of all CTAs'
         } list;
       };
     };
@@ -1044,6 +1046,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           R->found = 0;
         }
       }
+      if (tid < kSmpWarps) S->kept_w[tid] = 0;
       csync<STREAM>();
     };
     // K* of `target` (a count, or an exact weight) and the weight of its head,
@@ -1068,6 +1071,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
           if (at < kSmpList) {
             L->list.key[at] = order_key(x, index);
             L->list.w[at] = weight(S, f, x);
+            L->list.owner[at] = static_cast<unsigned char>(rank * kSmpWarps + warp);
           }
         }
         __syncwarp();
@@ -1085,35 +1089,46 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(SampleArgs a) {
       above_w = cluster_total(above_w);
       const unsigned long long above_n = by_weight ? 0 : cluster_total(above);
       const unsigned n = S->list_n;                         // (the leader's counts)
-      if (rank == 0 && n <= kSmpList && tid < n) {
-        const unsigned long long key = S->list.key[tid], own = S->list.w[tid];
-        unsigned long long hn = above_n, hw = above_w;      // up to and with this key
-        for (unsigned i = 0; i < n; ++i)
-          if (S->list.key[i] >= key) {
-            ++hn;
-            hw += S->list.w[i];
-          }
-        if (by_weight ? hw >= target && hw - own < target : hn == target) {
+      if (rank == 0 && n <= kSmpList) {
+        // a power of two of threads per key
+        int split = 1;
+        while (split < 32 && n * split * 2 <= kSmpThreads) split *= 2;
+        const unsigned k = tid / split;
+        const unsigned long long key = k < n ? S->list.key[k] : ~0ull;
+        const unsigned long long own = k < n ? S->list.w[k] : 0ull;
+        unsigned long long hn = 0, hw = 0;                  // up to and with this key
+        if (k < n)
+          for (unsigned i = tid & (split - 1); i < n; i += split)
+            if (S->list.key[i] >= key) {
+              ++hn;
+              hw += S->list.w[i];
+            }
+        for (int o = 1; o < split; o <<= 1) {
+          hn += __shfl_xor_sync(kFull, hn, o);
+          hw += __shfl_xor_sync(kFull, hw, o);
+        }
+        hn += above_n;
+        hw += above_w;
+        if ((tid & (split - 1)) == 0 && k < n &&
+            (by_weight ? hw >= target && hw - own < target : hn == target)) {
           for (int r = 0; r < n_cta; ++r) {
             SampleShared* R = cluster_ptr<STREAM>(S, r);
             R->border = key;
             R->border_w = hw;
-            R->found = static_cast<int>(n);
+            R->found = 1;
           }
+        }
+        __syncthreads();
+        // the weights kept of the list, to the warps whose runs they are of
+        if (S->found != 0 && tid < n && S->list.key[tid] >= S->border) {
+          const int owner = S->list.owner[tid];
+          atomicAdd(&cluster_ptr<STREAM>(S, owner / kSmpWarps)->kept_w[owner % kSmpWarps],
+                    S->list.w[tid]);
         }
       }
       csync<STREAM>();
       if (S->found != 0) {
-        // this warp's share of the bins' kept keys
-        const unsigned long long least = S->border;
-        for (int i = lane; i < S->found; i += 32) {
-          const unsigned long long key = L->list.key[i];
-          // (a run's vectors reach past the slice's ends)
-          const int at = static_cast<int>(0xffffffffu - static_cast<unsigned>(key));
-          if (key >= least && at >= max(e0, first + v0 * kVec) &&
-              at < min(e0 + n_el, first + v1 * kVec))
-            mine += L->list.w[i];
-        }
+        if (lane == 0) mine += S->kept_w[warp];
         return;
       }
       // Too many keys in the bins (a flat row, or long runs of equal logits): K*
