@@ -41,7 +41,7 @@
 // min-p 209, HBM; plain ones 645, of which the light weights take 400, some 13
 // integer instructions a logit at half rate; top-p 0.95 alone 1240, the sum,
 // then the bins' atomics and the weights of what is kept.  A single row of f32
-// logits takes 28, a chain of passes and barriers of 16 CTAs.
+// logits takes 26, a chain of passes and barriers of 16 CTAs.
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
