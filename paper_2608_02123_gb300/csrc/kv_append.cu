@@ -362,11 +362,12 @@ pctree_status pctree_kv_append(const pctree_append_config* cfg, const void* q, c
   a.interleaved = c.interleaved;
   a.eps = c.eps;
   a.scale = c.rope_scale;
-  // runs of heads: as many warps as the SMs hold while rows are few, whole
-  // rows (one set of sines and cosines) once there are enough of them
+  // runs of heads: all that the SMs' warps take at once while rows are few (512
+  // rows of 56 heads: 7.1 us in four runs a row, 8.8 in five, which need a second
+  // round), whole rows (one set of sines and cosines) once there are enough
   const int heads = c.Hq + 2 * c.Hkv, groups = 512 / c.D;
   const long long warps = static_cast<long long>(num_sms) * kAppendWarps * kAppendCtas;
-  long long parts = (warps + c.total_rows - 1) / c.total_rows;
+  long long parts = warps > c.total_rows ? warps / c.total_rows : 1;
   const int most = (heads + groups - 1) / groups;
   if (parts > most) parts = most;
   a.heads_per_part = (heads + static_cast<int>(parts) - 1) / static_cast<int>(parts);
