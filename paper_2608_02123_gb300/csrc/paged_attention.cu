@@ -13,8 +13,8 @@
 // in order.
 //
 //   warp 0      TMA producer, all lanes: the tile's Q (two buffers), then K and
-//               V blocks (128-byte swizzle, 64 dims a half), K a block ahead,
-//               into a ring; a lane issues the copies of one page
+//               V blocks (128-byte swizzle, 64 dims a half) into a ring; a lane
+//               issues the copies of one page
 //   warp 1      S issuer: S_b = Q K_b^T (tcgen05.mma, M = N = 128) into one of
 //               two TMEM buffers
 //   warp 2      PV issuer: O_h += P_b V_b over each half h of the block's keys
@@ -30,14 +30,15 @@
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
 //   tokens of 32 requests over up to 8192 slots: HBM, 854 MB in 138, 0.91 of
 //   the measured copy rate;
-//   four prompts of up to 4096 rows: K and V into the SMs, 64 KB a block at ~60
-//   B/ns, 404 in pages of 64 slots or more (1.06 PFLOP/s; the softmax chain of a
-//   block is nearly as long), 482 in pages of 16, whose 24 TMA boxes a block
-//   cost ~30 ns each; loading for every CTA alone 415 and 629;
+//   four prompts of up to 4096 rows: K and V into the SMs, 64 KB a block for
+//   every tile, 450 in pages of 64 (0.95 PFLOP/s), 480 of 32, 588 of 16, whose
+//   24 TMA boxes a block cost ~30 ns each, 666 of 8;
 //   a token of one request: two launches and one block's chain, 13.4.
-// K a block ahead of V (415 -> 391 before values were checked), one box for both
-// halves of the dims in small pages (pages of 8: 556 -> 491 and, tokens, 253 ->
-// 183), pieces of equal length (a unit a CTA leaves SMs idle at the end).
+// K and V in turn (K a block ahead: 471 in pages of 64, 603 of 16), one box for
+// both halves of the dims in small pages (pages of 8: 253 -> 183 for tokens),
+// pieces of equal length (a unit a CTA leaves SMs idle at the end).  Every CTA
+// loads for itself: copies that multicast a block to the tiles of a cluster
+// would halve those bytes, but the library is also that of runs on several GPUs.
 #include "kv_rows.cuh"
 #include "sm103_ptx.cuh"
 
@@ -86,7 +87,6 @@ struct PagedArgs {
   // halves of the dims.  A group of V is at least 8 keys, of K 8 or all (the
   // 8-key steps of an MMA operand are equally far apart).
   int k_group, v_group;
-  int join_step;          // CTAs from one piece of a unit to the next
   float scale_log2;
 };
 
@@ -118,8 +118,8 @@ __device__ __forceinline__ uint32_t bad_entry(uint4& v, int key, int place) {
 }
 
 // Places of the g-th block's K and V in the ring's sequence.
-__device__ __forceinline__ int k_place(int g) { return g == 0 ? 0 : 2 * g - 1; }
-__device__ __forceinline__ int v_place(int g) { return 2 * g + 2; }
+__device__ __forceinline__ int k_place(int g) { return 2 * g; }
+__device__ __forceinline__ int v_place(int g) { return 2 * g + 1; }
 
 struct Tail {
   uint64_t q_full[2], q_empty[2];
@@ -224,7 +224,7 @@ __device__ __noinline__ void clean_v(uint8_t* v, Tail* T, int parity, int thread
   }
 }
 
-template <int D, bool F16, int CTAS>
+template <int D, bool F16>
 __global__ void __maxnreg__(112)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k,
@@ -239,16 +239,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   Tail* T = reinterpret_cast<Tail*>(skv + kSlots * kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = a.G * a.npt;                       // rows of a tile
-  const int rank = CTAS > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  constexpr uint16_t kAll = (1 << CTAS) - 1;       // the CTAs that share a block's loads
-  const int unit_rows = CTAS * a.npt;              // a tile for each of them
   volatile int* abort_v = &T->abort;
 
   // ---------------- set-up ----------------
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(&T->kv_full[s], 1);
-      mbar_init(&T->kv_empty[s], CTAS);          // the MMAs of every CTA that got the block
+      mbar_init(&T->kv_empty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&T->q_full[s], 1);
@@ -297,20 +294,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     T->start[r] = start;
     T->n[r] = n;
     T->prefix[r] = prefix;
-    if (n <= unit_rows) T->upto[r] = n > 0 ? (blocks_of(a, prefix + n) + kUnitCharge) * a.Hkv : 0;
+    if (n <= a.npt) T->upto[r] = n > 0 ? (blocks_of(a, prefix + n) + kUnitCharge) * a.Hkv : 0;
   }
   __syncthreads();
   constexpr int kWarps = kThreads / 32;
   for (int r0 = warp; r0 < a.rows.batch; r0 += kThreads) {   // every kWarps-th is this warp's
     const int mine = r0 + lane * kWarps;
     unsigned several =
-        __ballot_sync(kFull, mine < a.rows.batch && T->n[min(mine, a.rows.batch - 1)] > unit_rows);
+        __ballot_sync(kFull, mine < a.rows.batch && T->n[min(mine, a.rows.batch - 1)] > a.npt);
     for (; several != 0; several &= several - 1) {
       const int r = r0 + (__ffs(several) - 1) * kWarps;
       const int n = T->n[r], prefix = T->prefix[r];
       unsigned w = 0;
-      for (int j = lane * unit_rows; j < n; j += 32 * unit_rows)
-        w += blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge;
+      for (int j = lane * a.npt; j < n; j += 32 * a.npt)
+        w += blocks_of(a, prefix + min(n, j + a.npt)) + kUnitCharge;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
       if (lane == 0) T->upto[r] = w * a.Hkv;
@@ -334,7 +331,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  if constexpr (CTAS > 1) cluster_sync();          // all CTAs' barriers are initialised
   const uint32_t tmem = T->tmem_base;
 
   auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
@@ -362,21 +358,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
 
   if (warp == 0) {
     // ---------------- TMA producer ----------------
-    // K runs a block ahead of V, in the order the MMAs free them: K_0 K_1 V_0
-    // K_2 V_1 ..., place k_place(g) and v_place(g) of the ring's sequence.
+    // K_0 V_0 K_1 V_1 ..., place k_place(g) and v_place(g) of the ring's sequence
     struct Box {
       int page, off, boxes, kvh;                   // this lane's box of a block
     };
     int g = 0, q = 0, k = 0, b = 0;                // blocks, Q tiles, items fetched, block
-    bool ok = true, more = true;
+    bool ok = true;
     Item it;
     it.b1 = 0;
     auto next_block = [&](Box& x) {                // false: no more, or not ok
       if (b >= it.b1) {
-        if (!(ok = fetch_warp(k++, it)) || it.nblk == 0) return more = false;
+        if (!(ok = fetch_warp(k++, it)) || it.nblk == 0) return false;
         b = it.b0;
         const int qb = q & 1;
-        if (!(ok = wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1))) return more = false;
+        if (!(ok = wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1))) return false;
         if (lane == 0) {
           mbar_arrive_expect_tx(&T->q_full[qb], static_cast<uint32_t>(kHalves * R) * 128u);
           for (int h = 0; h < kHalves; ++h)
@@ -415,69 +410,42 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         mbar_arrive_expect_tx(&T->kv_full[slot],
                               static_cast<uint32_t>(kHalves * x.boxes * a.box_rows) * 128u);
       __syncwarp();
-      // a cluster's CTAs take the boxes in turn, each for all of them
-      if (lane < x.boxes && (lane & (CTAS - 1)) == rank) {
+      if (lane < x.boxes) {
         if (both) {
-          if constexpr (CTAS > 1)
-            tma_load_5d_multicast(dst, map, &T->kv_full[slot], 0, x.off, 0, x.kvh, x.page, kAll);
-          else
-            tma_load_5d(dst, map, &T->kv_full[slot], 0, x.off, 0, x.kvh, x.page);
+          tma_load_5d(dst, map, &T->kv_full[slot], 0, x.off, 0, x.kvh, x.page);
         } else {
 #pragma unroll
-          for (int h = 0; h < kHalves; ++h) {
-            if constexpr (CTAS > 1)
-              tma_load_5d_multicast(dst + h * kHalfBytes, map, &T->kv_full[slot], 0, x.off, h,
-                                    x.kvh, x.page, kAll);
-            else
-              tma_load_5d(dst + h * kHalfBytes, map, &T->kv_full[slot], 0, x.off, h, x.kvh,
-                          x.page);
-          }
+          for (int h = 0; h < kHalves; ++h)
+            tma_load_5d(dst + h * kHalfBytes, map, &T->kv_full[slot], 0, x.off, h, x.kvh, x.page);
         }
       }
     };
-    Box cur, next;
+    Box cur;
     int k_issued = 0, v_issued = 0;
-    if (next_block(cur)) {
-      load(&tm_k, cur, k_place(0));
-      k_issued = 1;
-      for (; ok; ++g) {
-        const bool has = next_block(next);
-        if (!ok) break;
-        if (has) {
-          load(&tm_k, next, k_place(g + 1));
-          if (!ok) break;
-          ++k_issued;
-        }
-        load(&tm_v, cur, v_place(g));
-        if (!ok) break;
-        ++v_issued;
-        if (!has) break;
-        cur = next;
-      }
+    for (; ok && next_block(cur); ++g) {
+      load(&tm_k, cur, k_place(g));
+      if (!ok) break;
+      ++k_issued;
+      load(&tm_v, cur, v_place(g));
+      if (!ok) break;
+      ++v_issued;
     }
     __syncwarp();
     if (lane == 0) {
       if (!ok) give_up();
       // copies still in flight land before the CTA may exit
       volatile int never = 0;
-      auto drain = [&](uint64_t* bars) {           // each slot's last place
-        for (int slot = 0; slot < kSlots; ++slot) {
-          int last = -1;
-          for (int x = max(0, k_issued - kSlots); x < k_issued; ++x)
-            if (k_place(x) % kSlots == slot) last = max(last, k_place(x));
-          for (int x = max(0, v_issued - kSlots); x < v_issued; ++x)
-            if (v_place(x) % kSlots == slot) last = max(last, v_place(x));
-          if (last >= 0)
-            (void)mbar_wait_bounded(&bars[slot], (last / kSlots) & 1, &never, kLimitNs);
-        }
-      };
-      drain(T->kv_full);
+      for (int slot = 0; slot < kSlots; ++slot) {  // each slot's last place
+        int last = -1;
+        for (int x = max(0, k_issued - kSlots); x < k_issued; ++x)
+          if (k_place(x) % kSlots == slot) last = max(last, k_place(x));
+        for (int x = max(0, v_issued - kSlots); x < v_issued; ++x)
+          if (v_place(x) % kSlots == slot) last = max(last, v_place(x));
+        if (last >= 0)
+          (void)mbar_wait_bounded(&T->kv_full[slot], (last / kSlots) & 1, &never, kLimitNs);
+      }
       for (int x = q > 2 ? q - 2 : 0; x < q; ++x)
         (void)mbar_wait_bounded(&T->q_full[x & 1], (x >> 1) & 1, &never, kLimitNs);
-      // and so do the other CTAs' arrivals
-      if constexpr (CTAS > 1) {
-        if (ok) drain(T->kv_empty);
-      }
     }
   } else if (warp == 1 && lane == 0) {
     // ---------------- S issuer ----------------
@@ -511,8 +479,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
           tc_mma_bf16(tmem + sb * kBK, qd + q_off, kd + k_off, idS, kk > 0 ? 1u : 0u);
         }
         tc_commit(&T->s_full[sb]);
-        if constexpr (CTAS > 1) tc_commit_multicast(&T->kv_empty[slot], kAll);
-        else tc_commit(&T->kv_empty[slot]);
+        tc_commit(&T->kv_empty[slot]);
       }
       tc_commit(&T->q_empty[qb]);
     }
@@ -552,8 +519,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         tc_commit(&T->p_empty[sb]);
         if (b + 1 == it.b1) tc_commit(&T->o_full);
-        if constexpr (CTAS > 1) tc_commit_multicast(&T->kv_empty[slot], kAll);
-        else tc_commit(&T->kv_empty[slot]);
+        tc_commit(&T->kv_empty[slot]);
       }
     }
     if (!ok) give_up();
@@ -563,7 +529,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   } else if (warp == 3) {
     // ---------------- planner ----------------
     const unsigned total = T->upto[a.rows.batch - 1];
-    const unsigned places = gridDim.x / CTAS, place = blockIdx.x / CTAS;
+    const unsigned places = gridDim.x, place = blockIdx.x;
     const unsigned stretch = max((total + places - 1) / places, static_cast<unsigned>(kMinStretch));
     // (place * stretch is at most total + places * kMinStretch)
     unsigned x = place * stretch;
@@ -602,8 +568,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       kvh = static_cast<int>(in / per_head);
       in -= kvh * per_head;
       for (;;) {
-        const int j = (tile + lane) * unit_rows;
-        const unsigned cost = j < n ? blocks_of(a, prefix + min(n, j + unit_rows)) + kUnitCharge : 0;
+        const int j = (tile + lane) * a.npt;
+        const unsigned cost = j < n ? blocks_of(a, prefix + min(n, j + a.npt)) + kUnitCharge : 0;
         unsigned c = cost;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -621,16 +587,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         tile += 32;
       }
       while (ok && x < x_end) {
-        // this CTA's tile of the unit; the keys are those of the whole unit
-        const int j0 = tile * unit_rows + rank * a.npt, j1 = min(n, j0 + a.npt);
+        const int j0 = tile * a.npt;
         Item it;
         it.r = r;
         it.kvh = kvh;
         it.row0 = start + j0;
-        it.n_rows = max(0, j1 - j0);
+        it.n_rows = min(n - j0, a.npt);
         it.j0 = j0;
         it.prefix = prefix;
-        it.key_end = prefix + min(n, (tile + 1) * unit_rows);
+        it.key_end = prefix + min(n, j0 + a.npt);
         it.nblk = blocks_of(a, it.key_end);
         const unsigned left = it.nblk + kUnitCharge - in;
         const unsigned take = min(left, x_end - x);
@@ -649,7 +614,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         x += take;
         in = 0;
         ++tile;
-        if (x < x_end && tile * unit_rows >= n) {
+        if (x < x_end && tile * a.npt >= n) {
           tile = 0;
           if (++kvh == a.Hkv) {
             kvh = 0;
@@ -910,11 +875,6 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   __syncthreads();
   tc_fence_after_sync();
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  if constexpr (CTAS > 1) {
-    // the other CTAs' copies and commits no longer reach this one's memory
-    __syncwarp();
-    cluster_sync();
-  }
 }
 
 // Joins the pieces of the units that end in another CTA than they began in: a
@@ -947,7 +907,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(PagedArgs a
         const bool in = s0 + u < j.pieces;
         // the first piece is its CTA's last, every other one its CTA's first
         const size_t part =
-            static_cast<size_t>(c0 + (s0 + u) * a.join_step) * 2 + (s0 + u == 0 ? 1 : 0);
+            static_cast<size_t>(c0 + s0 + u) * 2 + (s0 + u == 0 ? 1 : 0);
         w[u] = in ? a.part_ml[part * 128 + row] : make_float2(-INFINITY, 0.0f);
         v[u] = in ? po[(part * kQuads + quad) * 128 + row] : acc;
       }
@@ -1035,27 +995,7 @@ PagedWs paged_ws(const pctree_paged_attn_config& c) {
   return w;
 }
 
-// CTAs of a grid of clusters that are on the GPU together (at most kMaxCtas);
-// asked once per device.
-template <int CTAS>
-int resident_ctas(const void* fn, const cudaLaunchConfig_t& lc, int num_sms) {
-  const int most = num_sms < kMaxCtas ? num_sms : kMaxCtas;
-  if (CTAS == 1) return most;
-  static std::mutex mu;
-  static int known[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return CTAS;
-  std::lock_guard<std::mutex> lk(mu);
-  if (known[dev] == 0) {
-    int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, fn, &lc) != cudaSuccess || clusters < 1)
-      clusters = 1;
-    known[dev] = clusters * CTAS < most ? clusters * CTAS : most / CTAS * CTAS;
-  }
-  return known[dev];
-}
-
-template <int D, bool F16, int CTAS>
+template <int D, bool F16>
 pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                            const CUtensorMap& tm_v, const PagedArgs& a, int num_sms,
                            cudaStream_t stream) {
@@ -1063,41 +1003,26 @@ pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
       (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
   static SmemLimit limit;
-  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16, CTAS>);
+  const void* fn = reinterpret_cast<const void*>(paged_attn_kernel<D, F16>);
   if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = CTAS;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(static_cast<unsigned>(kMaxCtas / CTAS * CTAS));
+  const unsigned ctas = static_cast<unsigned>(num_sms < kMaxCtas ? num_sms : kMaxCtas);
+  lc.gridDim = dim3(ctas);
   lc.blockDim = dim3(kThreads);
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
   lc.attrs = attr;
-  lc.numAttrs = CTAS > 1 ? 2 : 1;
-  const int ctas = resident_ctas<CTAS>(fn, lc, num_sms);
-  lc.gridDim = dim3(static_cast<unsigned>(ctas));
-  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16, CTAS>, tm_q, tm_k, tm_v, a) != cudaSuccess)
-    return PCTREE_ERR_CUDA;
   lc.numAttrs = 1;
-  lc.gridDim = dim3(static_cast<unsigned>(ctas), kJoinCtas);
+  if (cudaLaunchKernelEx(&lc, paged_attn_kernel<D, F16>, tm_q, tm_k, tm_v, a) != cudaSuccess)
+    return PCTREE_ERR_CUDA;
+  lc.gridDim = dim3(ctas, kJoinCtas);
   lc.blockDim = dim3(kJoinThreads);
   lc.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&lc, paged_join_kernel<D, F16>, a) == cudaSuccess ? PCTREE_OK
                                                                              : PCTREE_ERR_CUDA;
-}
-
-template <int D, bool F16>
-pctree_status paged_launch(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
-                           const CUtensorMap& tm_v, const PagedArgs& a, int num_sms,
-                           cudaStream_t stream) {
-  return a.join_step == 4   ? paged_launch<D, F16, 4>(tm_q, tm_k, tm_v, a, num_sms, stream)
-         : a.join_step == 2 ? paged_launch<D, F16, 2>(tm_q, tm_k, tm_v, a, num_sms, stream)
-                            : paged_launch<D, F16, 1>(tm_q, tm_k, tm_v, a, num_sms, stream);
 }
 
 }  // namespace
@@ -1156,16 +1081,7 @@ pctree_status pctree_paged_attention(const pctree_paged_attn_config* cfg, const 
   a.npt = rows_per_tile(c);
   a.packed = packed_pages(c.page_size);
   a.page_blocks = (c.page_size + kBK - 1) / kBK;
-  // Requests of more than a tile of rows, on average: the CTAs of a cluster take
-  // tiles of a head side by side, and each loads a share of the keys for all.
-  // Four of them where pages are small and requests have tiles enough.
-  const long long tiles = c.total_rows / (static_cast<long long>(c.batch) * a.npt);
-  // (us, four prompts of up to 4096 rows, two / four: pages of 8 674 / 556,
-  // 16 513 / 479, 32 425 / 430; 36 clusters of four fit, 144 of 152 SMs.)
-  a.join_step = num_sms < 4 || c.total_rows <= static_cast<long long>(c.batch) * a.npt ? 1
-                : c.page_size <= 16 && tiles >= 6 ? 4 : 2;
-  const int most = kBK / a.join_step;              // so that every CTA has boxes to load
-  a.box_rows = c.page_size < most ? c.page_size : most;
+  a.box_rows = c.page_size < kBK ? c.page_size : kBK;
   a.v_group = a.packed != 0 && a.box_rows < kBK ? a.box_rows : kBK;
   a.k_group = a.v_group == 8 ? 8 : kBK;
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);

@@ -134,8 +134,7 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map,
       : "memory");
 }
 
-// 5-D box loads; multicast: into the shared memory of every CTA of `mask` (bits are
-// cluster ranks), each completing on the barrier at the same place of its own.
+// 5-D box load; same rules as tma_load_2d.
 __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, uint64_t* bar,
                                             int32_t x, int32_t y, int32_t z, int32_t w,
                                             int32_t v) {
@@ -144,17 +143,6 @@ __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, u
       "bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w),
       "r"(v)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_5d_multicast(void* dst, const CUtensorMap* map,
-                                                      uint64_t* bar, int32_t x, int32_t y,
-                                                      int32_t z, int32_t w, int32_t v,
-                                                      uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::"
-      "bytes.multicast::cluster [%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w),
-      "r"(v), "h"(mask)
       : "memory");
 }
 
@@ -372,16 +360,6 @@ __device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
       "[%0], %1;" ::"r"(smem_u32(bar)),
       "h"(static_cast<uint16_t>(3))
-      : "memory");
-}
-
-// tc_commit that arrives on the barrier at this place in every CTA of `mask`
-// (bits are cluster ranks), for MMAs of this CTA alone.
-__device__ __forceinline__ void tc_commit_multicast(uint64_t* bar, uint16_t mask) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
-      "[%0], %1;" ::"r"(smem_u32(bar)),
-      "h"(mask)
       : "memory");
 }
 
