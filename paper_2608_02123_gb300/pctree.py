@@ -797,11 +797,12 @@ class Drafter:
         node (uniform [batch][N]) and the parameters [batch] of pctree_sample:
         the committed tokens and the bonus are samples of the target.  Rows
         past a tree's nodes are not read; the sampled tokens are in
-        ``self.target``."""
+        ``self.target``.  A row without a token (-1, and so perhaps the bonus)
+        sets ``status``, by default the round's, which check_status reads."""
         cfg = self.cfg
         sc = sample_config(cfg.batch * cfg.N, logits.shape[-1], cfg.N, logits.dtype)
         pctree_sample(sc, logits, uniform, self.target, temperature, top_k, top_p, min_p,
-                      self.tree.n_nodes, status, stream)
+                      self.tree.n_nodes, self.tree.status if status is None else status, stream)
         return self.accept(self.target, stream)
 
     def check_status(self) -> None:
