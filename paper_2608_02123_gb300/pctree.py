@@ -480,10 +480,65 @@ def _device_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
     return _stream_ptr(stream)
 
 
-def _flat(t: Optional[torch.Tensor], dt, n: int, device: int) -> bool:
-    """None, or a contiguous tensor of type dt and at least n elements there."""
-    return t is None or (t.dtype is dt and t.numel() >= n and t.get_device() == device
-                         and t.is_contiguous())
+def _trim(shape):
+    """Without leading dimensions of one entry."""
+    lead = 0
+    while lead < len(shape) - 1 and shape[lead] == 1:
+        lead += 1
+    return shape[lead:]
+
+
+def _whole(shape, *rows: int) -> bool:
+    """Whether a contiguous tensor of this shape is flat, or one of whole rows:
+    the product of some of its last dimensions is one of ``rows`` elements."""
+    shape = _trim(shape)
+    n = 1
+    for d in reversed(shape[1:]):
+        n *= d
+        if n in rows:
+            return True
+    return len(shape) <= 1
+
+
+def _flat(t: Optional[torch.Tensor], dt, n: int, device: int, row: int = 1) -> bool:
+    """None, or a contiguous tensor of type dt there, of n elements, or of more
+    of them in a row or in whole rows of `row` (in rows of another length the
+    call would not find the second row where it is)."""
+    if t is None:
+        return True
+    if not (t.dtype is dt and t.get_device() == device and t.is_contiguous()):
+        return False
+    have = t.numel()
+    return have == n or (have > n and _whole(t.shape, row))
+
+
+def _table(t: Optional[torch.Tensor], batch: int, max_pages: int, device: int) -> bool:
+    """None, or page numbers [batch][max_pages] there (flat, or more rows)."""
+    if t is None:
+        return True
+    if not (t.dtype is torch.int32 and t.get_device() == device and t.is_contiguous()):
+        return False
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == max_pages:
+        return shape[0] >= batch
+    return t.numel() >= batch * max_pages and _whole(shape, max_pages)
+
+
+def _cache(t: torch.Tensor, dt, pages: int, page: int, slot: int, D: int, device: int) -> bool:
+    """[n_pages][page_size][Hkv][D] there, or more pages, where a page has `page`
+    and a slot `slot` elements; [places][Hkv][D] and other groupings of the same
+    memory are welcome."""
+    if not (t.dtype is dt and t.get_device() == device and t.is_contiguous()):
+        return False
+    shape = t.shape
+    if len(shape) == 4 and shape[1] * shape[2] * shape[3] == page:
+        return shape[0] >= pages
+    if t.numel() < pages * page:
+        return False
+    dims = len(_trim(shape))
+    if dims > 3 and pages > 1:                       # (of one page, only its start is used)
+        return _whole(shape, page)
+    return _whole(shape, page, slot, D) if dims < 3 else _whole(shape, page, slot)
 
 
 def _rows(t: torch.Tensor, dt, rows: int, heads: int, D: int, stride: int,
@@ -505,8 +560,21 @@ def _refuse(where: str, device: int, checks) -> None:
                              f"cuda:{device}")
 
 
-def _flat_check(name, t, dt, n, device):
-    return name, _flat(t, dt, n, device), f"a contiguous {dt} tensor of at least {n} elements"
+def _flat_check(name, t, dt, n, device, row=1):
+    return (name, _flat(t, dt, n, device, row),
+            f"a contiguous {dt} tensor of at least {n} elements"
+            + (f", in rows of {row}" if row > 1 else ""))
+
+
+def _table_check(t, batch, max_pages, device):
+    return ("page_table", _table(t, batch, max_pages, device),
+            f"a contiguous torch.int32 tensor [{batch}][{max_pages}] (max_pages of the config)")
+
+
+def _cache_check(name, t, dt, cfg, device):
+    slot = cfg.Hkv * cfg.D
+    return (name, _cache(t, dt, cfg.n_pages, cfg.page_size * slot, slot, cfg.D, device),
+            f"a contiguous {dt} tensor [{cfg.n_pages}][{cfg.page_size}][{cfg.Hkv}][{cfg.D}]")
 
 
 def _rows_check(name, t, dt, rows, heads, D, stride, device):
@@ -549,30 +617,32 @@ def pctree_kv_append(cfg: AppendConfig, q: Optional[torch.Tensor], k: torch.Tens
     dev = _device_index()
     dt = _TORCH_TYPE.get(cfg.dtype)
     n, D, Hq, Hkv, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.Hkv, cfg.batch, torch.int32
-    slots = cfg.n_pages * cfg.page_size * Hkv * D
+    pages, slot = cfg.n_pages, Hkv * D
+    page = cfg.page_size * slot
     if not ((Hq == 0 or (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
-                         and _flat(q_out, dt, n * Hq * D, dev)))
+                         and _flat(q_out, dt, n * Hq * D, dev, Hq * D)))
             and _rows(k, dt, n, Hkv, D, cfg.k_stride, dev)
             and _rows(v, dt, n, Hkv, D, cfg.v_stride, dev)
-            and _flat(k_cache, dt, slots, dev) and _flat(v_cache, dt, slots, dev)
+            and _cache(k_cache, dt, pages, page, slot, D, dev)
+            and _cache(v_cache, dt, pages, page, slot, D, dev)
             and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
             and _flat(prefix_len, i32, batch, dev)
-            and _flat(page_table, i32, batch * cfg.max_pages, dev)
+            and _table(page_table, batch, cfg.max_pages, dev)
             and _flat(positions, i32, n, dev)
             and _flat(inv_freq, torch.float64, cfg.rotary_dim // 2, dev)
             and _flat(q_weight, dt, D, dev) and _flat(k_weight, dt, D, dev)
             and _flat(status, i32, 1, dev)):
         _refuse("pctree_kv_append", dev, [
             *([_rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
-               _flat_check("q_out", q_out, dt, n * Hq * D, dev)] if Hq else []),
+               _flat_check("q_out", q_out, dt, n * Hq * D, dev, Hq * D)] if Hq else []),
             _rows_check("k", k, dt, n, Hkv, D, cfg.k_stride, dev),
             _rows_check("v", v, dt, n, Hkv, D, cfg.v_stride, dev),
-            _flat_check("k_cache", k_cache, dt, slots, dev),
-            _flat_check("v_cache", v_cache, dt, slots, dev),
+            _cache_check("k_cache", k_cache, dt, cfg, dev),
+            _cache_check("v_cache", v_cache, dt, cfg, dev),
             _flat_check("row_start", row_start, i32, batch, dev),
             _flat_check("n_rows", n_rows, i32, batch, dev),
             _flat_check("prefix_len", prefix_len, i32, batch, dev),
-            _flat_check("page_table", page_table, i32, batch * cfg.max_pages, dev),
+            _table_check(page_table, batch, cfg.max_pages, dev),
             _flat_check("positions", positions, i32, n, dev),
             _flat_check("inv_freq", inv_freq, torch.float64, cfg.rotary_dim // 2, dev),
             _flat_check("q_weight", q_weight, dt, D, dev),
@@ -616,23 +686,26 @@ def pctree_paged_attention(cfg: PagedAttnConfig, q: torch.Tensor, k_cache: torch
     dev = _device_index()
     dt = _TORCH_TYPE.get(cfg.dtype)
     n, D, Hq, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.batch, torch.int32
-    slots = cfg.n_pages * cfg.page_size * cfg.Hkv * D
-    if not (_rows(q, dt, n, Hq, D, cfg.q_stride, dev) and _flat(out, dt, n * Hq * D, dev)
-            and _flat(k_cache, dt, slots, dev) and _flat(v_cache, dt, slots, dev)
+    pages, slot = cfg.n_pages, cfg.Hkv * D
+    page = cfg.page_size * slot
+    if not (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
+            and _flat(out, dt, n * Hq * D, dev, Hq * D)
+            and _cache(k_cache, dt, pages, page, slot, D, dev)
+            and _cache(v_cache, dt, pages, page, slot, D, dev)
             and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
             and _flat(prefix_len, i32, batch, dev)
-            and _flat(page_table, i32, batch * cfg.max_pages, dev)
-            and _flat(workspace, torch.uint8, 0, dev) and _flat(status, i32, 1, dev)):
+            and _table(page_table, batch, cfg.max_pages, dev)
+            and _flat(workspace, torch.uint8, workspace.numel(), dev) and _flat(status, i32, 1, dev)):
         _refuse("pctree_paged_attention", dev, [
             _rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
-            _flat_check("out", out, dt, n * Hq * D, dev),
-            _flat_check("k_cache", k_cache, dt, slots, dev),
-            _flat_check("v_cache", v_cache, dt, slots, dev),
+            _flat_check("out", out, dt, n * Hq * D, dev, Hq * D),
+            _cache_check("k_cache", k_cache, dt, cfg, dev),
+            _cache_check("v_cache", v_cache, dt, cfg, dev),
             _flat_check("row_start", row_start, i32, batch, dev),
             _flat_check("n_rows", n_rows, i32, batch, dev),
             _flat_check("prefix_len", prefix_len, i32, batch, dev),
-            _flat_check("page_table", page_table, i32, batch * cfg.max_pages, dev),
-            _flat_check("workspace", workspace, torch.uint8, 0, dev),
+            _table_check(page_table, batch, cfg.max_pages, dev),
+            _flat_check("workspace", workspace, torch.uint8, workspace.numel(), dev),
             _flat_check("status", status, i32, 1, dev)])
     rc = LIB.pctree_paged_attention(
         ctypes.byref(cfg), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
@@ -649,14 +722,23 @@ def sample_config(rows: int, V: int, group: int = 1, dtype: torch.dtype = torch.
     return SampleConfig(rows, V, group, _DTYPES[dtype], V if row_stride is None else row_stride)
 
 
-def _logit_rows(t: torch.Tensor, dt, rows: int, V: int, stride: int, device: int) -> bool:
-    """[rows][V] there, rows `stride` apart, or a dense tensor of that many
-    rows of V."""
+def _logit_rows(t: torch.Tensor, dt, rows: int, V: int, group: int, stride: int,
+                device: int) -> bool:
+    """[rows][V] there, rows `stride` apart, under any leading dimensions; more
+    rows than that only in whole groups."""
     if t.dtype is not dt or t.get_device() != device or t.dim() < 1 or t.shape[-1] != V:
         return False
-    if t.dim() == 2 and t.shape[0] >= rows:
-        return (V == 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) == stride)
-    return t.is_contiguous() and t.numel() >= rows * V and (rows <= 1 or stride == V)
+    if V > 1 and t.stride(-1) != 1:
+        return False
+    have, lead, whole = 1, stride, t.dim() <= 2
+    for i in range(t.dim() - 2, -1, -1):
+        n = t.shape[i]
+        if n != 1 and t.stride(i) != lead and rows > 1:
+            return False
+        lead *= n
+        have *= n
+        whole = whole or (i > 0 and have == group)
+    return have >= rows and (have == rows or whole)
 
 
 def pctree_sample(cfg: SampleConfig, logits: torch.Tensor, uniform: torch.Tensor,
@@ -673,16 +755,16 @@ def pctree_sample(cfg: SampleConfig, logits: torch.Tensor, uniform: torch.Tensor
     dt = _TORCH_TYPE.get(cfg.dtype)
     rows, V, group, f32, i32 = cfg.rows, cfg.V, cfg.group, torch.float32, torch.int32
     groups = rows if group == 1 else -(-rows // group) if group > 0 else 0
-    if not (_logit_rows(logits, dt, rows, V, cfg.row_stride, dev)
-            and _flat(uniform, f32, rows, dev) and _flat(tokens, i32, rows, dev)
+    if not (_logit_rows(logits, dt, rows, V, group, cfg.row_stride, dev)
+            and _flat(uniform, f32, rows, dev, group) and _flat(tokens, i32, rows, dev, group)
             and _flat(temperature, f32, groups, dev) and _flat(top_k, i32, groups, dev)
             and _flat(top_p, f32, groups, dev) and _flat(min_p, f32, groups, dev)
             and _flat(n_rows, i32, groups, dev) and _flat(status, i32, 1, dev)):
         _refuse("pctree_sample", dev, [
-            ("logits", _logit_rows(logits, dt, rows, V, cfg.row_stride, dev),
+            ("logits", _logit_rows(logits, dt, rows, V, group, cfg.row_stride, dev),
              f"a {dt} tensor [{rows}][{V}], {cfg.row_stride} elements from row to row"),
-            _flat_check("uniform", uniform, f32, rows, dev),
-            _flat_check("tokens", tokens, i32, rows, dev),
+            _flat_check("uniform", uniform, f32, rows, dev, group),
+            _flat_check("tokens", tokens, i32, rows, dev, group),
             _flat_check("temperature", temperature, f32, groups, dev),
             _flat_check("top_k", top_k, i32, groups, dev),
             _flat_check("top_p", top_p, f32, groups, dev),
