@@ -722,6 +722,15 @@ def sample_config(rows: int, V: int, group: int = 1, dtype: torch.dtype = torch.
     return SampleConfig(rows, V, group, _DTYPES[dtype], V if row_stride is None else row_stride)
 
 
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements from row to row of [...][V]: of the last dimension before V that
+    has more than one entry."""
+    for i in range(t.dim() - 2, -1, -1):
+        if t.shape[i] != 1:
+            return t.stride(i)
+    return t.shape[-1] if t.dim() else 0
+
+
 def _logit_rows(t: torch.Tensor, dt, rows: int, V: int, group: int, stride: int,
                 device: int) -> bool:
     """[rows][V] there, rows `stride` apart, under any leading dimensions; more
@@ -875,14 +884,16 @@ class Drafter:
     def sample_accept(self, logits, uniform, temperature=None, top_k=None, top_p=None,
                       min_p=None, status=None, stream=None):
         """Acceptance against tokens sampled from the target's logits
-        [batch][N][V] of the tree's nodes, with one random number in [0, 1) per
+        [batch][N][V] of the tree's nodes (rows one stride apart, so a padded
+        vocabulary's logits[..., :V] too), with one random number in [0, 1) per
         node (uniform [batch][N]) and the parameters [batch] of pctree_sample:
         the committed tokens and the bonus are samples of the target.  Rows
         past a tree's nodes are not read; the sampled tokens are in
         ``self.target``.  A row without a token (-1, and so perhaps the bonus)
         sets ``status``, by default the round's, which check_status reads."""
         cfg = self.cfg
-        sc = sample_config(cfg.batch * cfg.N, logits.shape[-1], cfg.N, logits.dtype)
+        sc = sample_config(cfg.batch * cfg.N, logits.shape[-1], cfg.N, logits.dtype,
+                           _row_stride(logits))
         pctree_sample(sc, logits, uniform, self.target, temperature, top_k, top_p, min_p,
                       self.tree.n_nodes, self.tree.status if status is None else status, stream)
         return self.accept(self.target, stream)

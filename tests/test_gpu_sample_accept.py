@@ -51,3 +51,18 @@ def test_a_status_of_the_callers_takes_the_error(drafted):
     dr.sample_accept(logits, u, status=own)
     assert int(own.item()) == -5
     dr.check_status()
+
+
+def test_padded_vocabularies(drafted):
+    """logits[..., :V] of a wider tensor: the same tokens, padding never drawn."""
+    P, dr, logits, u = drafted
+    want = [t.clone() for t in dr.sample_accept(logits, u)] + [dr.target.clone()]
+    R, N, V = logits.shape
+    wide = torch.full((R, N, V + 72), 50.0, dtype=logits.dtype, device="cuda")
+    wide[..., :V] = logits
+    for padded in (wide[..., :V], wide.view(R * N, V + 72)[:, :V]):
+        dr.target.fill_(-7)
+        got = [*dr.sample_accept(padded, u), dr.target]
+        dr.check_status()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

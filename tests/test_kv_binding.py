@@ -156,3 +156,18 @@ def test_random_numbers_and_tokens(P):
         sample(P, z, top_p=zeros(*shape, dtype=F32))
     with pytest.raises(ValueError, match="top_p"):
         sample(P, z, top_p=zeros(2, 2, dtype=F32))
+
+
+def test_sample_accept_takes_logits_as_they_lie(P, monkeypatch):
+    """Rows further apart than V, at N = 1 and 1 request as well."""
+    seen = []
+    monkeypatch.setattr(P, "pctree_sample", lambda cfg, *a: seen.append(cfg.row_stride))
+    for batch, N in ((2, 3), (2, 1), (1, 3), (1, 1)):
+        dr = P.Drafter.__new__(P.Drafter)
+        dr.cfg = P.make_config(40, 64, 3, 2, N, batch)
+        dr.target, dr.tree = None, type("T", (), {"n_nodes": None, "status": None})
+        dr.accept = lambda target, stream: None
+        for width in (40, 48):
+            dr.sample_accept(zeros(batch, N, width, dtype=F32)[..., :40], None)
+            want = width if batch * N > 1 else 40
+            assert seen.pop() == want
