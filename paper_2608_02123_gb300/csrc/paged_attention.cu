@@ -704,11 +704,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
             }
           }
           if (n_bad > kMaxBad && T->bad_first[k & 1][quad] <= seen) nan = 0xffffffffu;
-          nan |= pos & neg;
+          // (added: y may be NaN or the opposite infinity already)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            if ((pos >> i) & 1u) y[i] = INFINITY;
-            if ((neg >> i) & 1u) y[i] = -INFINITY;
+            if ((pos >> i) & 1u) y[i] += INFINITY;
+            if ((neg >> i) & 1u) y[i] -= INFINITY;
             if ((nan >> i) & 1u) y[i] = __int_as_float(0x7fc00000);
           }
           __syncwarp();

@@ -1,0 +1,69 @@
+"""pctree_paged_attention where scores or values are not finite in more than one
+way at a time: what the formula gives in float64, NaN and infinities included.
+
+Tolerances of the finite elements are those of test_gpu_paged_attention.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+from tests.kv_util import Batch, f64, half_step
+from tests.test_gpu_paged_attention import Call
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def P():
+    from paper_2608_02123_gb300 import pctree
+    return pctree
+
+
+def put(c, cache, r, slot, head, dim, value):
+    at = int(c.b.places(r, slot, slot + 1)[0])
+    cache[at, head, dim] = value
+
+
+def compare(c):
+    b = c.b
+    with np.errstate(invalid="ignore"):
+        want, size = c.want()
+    used = b.used_rows()
+    got, want, size = f64(c.out[1:-1])[used], want[used], size[used]
+    np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+    np.testing.assert_array_equal(np.isposinf(got), np.isposinf(want))
+    np.testing.assert_array_equal(np.isneginf(got), np.isneginf(want))
+    fin = np.isfinite(want)
+    u = half_step(c.dt)
+    tol = (u + 5e-4) * size[fin] + u * np.abs(want[fin])
+    if c.dt is torch.float16:
+        tol += float(max(b.prefix + b.rows)) * 2.0 ** -25 * 6
+    assert (np.abs(got[fin] - want[fin]) <= tol).all()
+    return want
+
+
+# whole units, and units cut into pieces that are joined
+PREFIXES = {"whole": [200, 30], "pieces": [9000, 2500]}
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "f16")])
+@pytest.mark.parametrize("name", sorted(PREFIXES))
+def test_infinite_values_of_new_rows_do_not_hide_what_came_before(P, name, D, dtype):
+    """A new row's infinite value, in a row that is NaN already (a NaN score) or
+    holds the opposite infinity (a value of the prefix)."""
+    prefix = PREFIXES[name]
+    c = Call(P, Batch([12, 5], prefix, 64), 8, 2, D, dtype)
+    T = prefix[0]
+    put(c, c.k, 0, T + 3, 0, 7, NAN)              # rows from 3 on of head 0: NaN
+    put(c, c.v, 0, T + 5, 0, 11, INF)             # and from 5 on also an infinite value
+    put(c, c.v, 0, T + 6, 0, 12, -INF)
+    put(c, c.v, 0, 17, 1, 20, -INF)               # seen by every row of head 1
+    put(c, c.v, 0, T + 4, 1, 20, INF)             # opposite: NaN from row 4 on
+    put(c, c.v, 0, 18, 1, 33, INF)
+    put(c, c.v, 0, T + 4, 1, 33, INF)             # the same sign: stays infinite
+    assert c.run(P) == 0
+    want = compare(c)
+    assert np.isnan(want[5:12, :4, 11]).all() and np.isnan(want[4:12, 4:, 20]).all()
+    assert np.isneginf(want[:4, 4:, 20]).all() and np.isposinf(want[:12, 4:, 33]).all()
