@@ -664,12 +664,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       float f1 = l1 != 0.0f ? exp2f(m1 - m) : 0.0f;
       const float l = l0 * f0 + l1 * f1;
       const uint32_t o_col = lane_base + kOCol;
-      if (whole && l != 0.0f) {
+      if (whole) {                                 // (no finite score, l = 0: NaN)
         const float inv = 1.0f / l;
         f0 *= inv;
         f1 *= inv;
       }
-      const uint32_t keep = l != 0.0f ? 0xffffffffu : 0u;
       const bool in_tile = t / a.G < it.n_rows && t < R;
       if (!whole && in_tile)
         a.part_ml[part * 128 + t] = make_float2(l != 0.0f ? m : -INFINITY, l);
@@ -735,7 +734,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         for (int q = 0; q < 4; ++q) {
           uint32_t w[4];
 #pragma unroll
-          for (int h = 0; h < 4; ++h) w[h] = pack16<F16>(y[q * 8 + 2 * h], y[q * 8 + 2 * h + 1]) & keep;
+          for (int h = 0; h < 4; ++h) w[h] = pack16<F16>(y[q * 8 + 2 * h], y[q * 8 + 2 * h + 1]);
           *reinterpret_cast<uint4*>(stg + lane * 64 + ((q ^ (lane >> 1)) & 3) * 16) =
               make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -934,7 +933,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(PagedArgs a
         }
       }
     }
-    const float inv = lsum != 0.0f ? 1.0f / lsum : 0.0f;
+    const float inv = 1.0f / lsum;               // (no finite score, lsum = 0: NaN)
     uint16_t* orow =
         a.out + ((static_cast<size_t>(j.row0) + nl) * a.Hq + j.kvh * a.G + g) * D + quad * 4;
     *reinterpret_cast<uint2*>(orow) = make_uint2(pack16<F16>(acc.x * inv, acc.y * inv),

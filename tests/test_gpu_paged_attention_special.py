@@ -67,3 +67,24 @@ def test_infinite_values_of_new_rows_do_not_hide_what_came_before(P, name, D, dt
     want = compare(c)
     assert np.isnan(want[5:12, :4, 11]).all() and np.isnan(want[4:12, 4:, 20]).all()
     assert np.isneginf(want[:4, 4:, 20]).all() and np.isposinf(want[:12, 4:, 33]).all()
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "f16")])
+def test_rows_whose_scores_are_all_minus_infinity(P, D, dtype):
+    """Such a row has no softmax: NaN.  With one finite score among them it is
+    that key's value."""
+    c = Call(P, Batch([1, 3, 1, 2], [0, 0, 9000, 130], 64), 8, 2, D, dtype)
+    c.q[..., 5] = 1.0
+    b = c.b
+
+    def sink(r, first, last):
+        at = torch.from_numpy(b.places(r, first, last)).cuda()
+        c.k[at, :, 5] = -INF
+
+    sink(0, 0, 1)                                 # the only key
+    sink(1, 0, 1)                                 # the first row's only key
+    sink(2, 0, 9001)                              # every key, over many CTAs
+    sink(3, 0, 130)                               # all but the rows' own
+    assert c.run(P) == 0
+    want = compare(c)
+    assert np.isnan(want[[0, 1, 4]]).all() and np.isfinite(want[[2, 3, 5, 6]]).all()
