@@ -25,7 +25,8 @@
 //   warps 8..15 softmax, two threads per tile row, 64 keys of a block each with
 //               its own running maximum, sum and O: S is read from TMEM once,
 //               masked and scaled, P = 2^(s - m_used) written back over it
-// All waits are bounded (1 s) and end in PCTREE_ERR_TIMEOUT.
+// All waits are bounded (1 s; those for a whole piece 1 s without a block) and end
+// in PCTREE_ERR_TIMEOUT.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
 //   tokens of 32 requests over up to 8192 slots: HBM, 854 MB in 138, 0.91 of
@@ -130,6 +131,7 @@ struct Tail {
   uint64_t done;
   uint32_t tmem_base;
   int abort;
+  int blocks;                                // multiplied so far (see wwait_long)
   Item item[kItemRing];
   float row_l[2][128], row_m[2][128];
   // Non-finite values at keys that only some rows of the piece's tile see, by
@@ -262,6 +264,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     mbar_init(&T->o_empty, 4);
     mbar_init(&T->done, 2);
     T->abort = 0;
+    T->blocks = 0;
     for (int i = 0; i < 8; ++i) {
       T->bad_n[i >> 2][i & 3] = 0;
       T->bad_first[i >> 2][i & 3] = kBK;
@@ -335,6 +338,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
 
   auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
     return __all_sync(kFull, mbar_wait_bounded(bar, parity, abort_v, kLimitNs));
+  };
+  // a wait that lasts as long as pieces do: over once no block has been multiplied
+  // for the limit
+  auto wwait_long = [&](uint64_t* bar, uint32_t parity) -> bool {
+    volatile int* blocks = &T->blocks;
+    for (;;) {
+      const int before = *blocks;
+      if (wwait(bar, parity)) return true;
+      if (__any_sync(kFull, *abort_v != 0) || __all_sync(kFull, *blocks == before)) return false;
+    }
   };
   auto give_up = [&]() {
     *abort_v = 1;
@@ -498,6 +511,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
 #pragma unroll
     for (int kk = 0; kk < kBK / 16; ++kk) v_off[kk] = v_place_of(16 * kk, a.v_group, kHalves) >> 4;
     bool ok = true;
+    volatile int* blocks = &T->blocks;
     Item it;
     for (int k = 0; ok; ++k) {
       if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
@@ -519,6 +533,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         tc_commit(&T->p_empty[sb]);
         if (b + 1 == it.b1) tc_commit(&T->o_full);
+        *blocks = g + 1;
         tc_commit(&T->kv_empty[slot]);
       }
     }
@@ -539,7 +554,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     bool ok = true;
     auto post = [&](const Item& it) {              // lane 0 writes the k-th piece
       const int s = k % kItemRing;
-      if (!(ok = wwait(&T->item_empty[s], ((k / kItemRing) & 1) ^ 1))) return;
+      if (!(ok = wwait_long(&T->item_empty[s], ((k / kItemRing) & 1) ^ 1))) return;
       if (lane == 0) {
         T->item[s] = it;
         mbar_arrive(&T->item_full[s]);
@@ -649,7 +664,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
     Item it;
     for (int k = 0;; ++k) {
       if (!(ok = fetch_warp(k, it)) || it.nblk == 0) break;
-      if (!(ok = wwait(&T->o_full, k & 1))) break;
+      if (!(ok = wwait_long(&T->o_full, k & 1))) break;
       tc_fence_after_sync();
       uint16_t* oitem = a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G) * D;
       const bool whole = it.b0 == 0 && it.b1 == it.nblk;
