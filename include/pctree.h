@@ -523,7 +523,9 @@ pctree_paged_attention_workspace_bytes(const pctree_paged_attn_config* cfg);
  *                   A bad page number (see above) stands for a page of zeros.
  *   workspace       not used concurrently by another call
  *   status          one device int32 or NULL; written only on an error
- *                   (PCTREE_ERR_TIMEOUT if a bounded wait ran out)
+ *                   (PCTREE_ERR_TIMEOUT if a bounded wait ran out,
+ *                   PCTREE_ERR_INVALID_ARG with nothing of out written if the
+ *                   requests have more rows together than total_rows)
  * Any page_size >= 1 works; 8, 16, 32, 64 and multiples of 128 fill the
  * kernel's blocks of 128 keys.
  * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED /

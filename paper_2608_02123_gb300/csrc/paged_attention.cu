@@ -319,9 +319,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
   __syncthreads();
   if (warp == 0) {
     unsigned base = 0;
+    long long n_all = 0;
     for (int r0 = 0; r0 < a.rows.batch; r0 += 32) {
       const int r = r0 + lane;
       unsigned w = r < a.rows.batch ? T->upto[r] : 0;
+      n_all += r < a.rows.batch ? T->n[r] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const unsigned p = __shfl_up_sync(kFull, w, o);
@@ -329,6 +331,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       }
       if (r < a.rows.batch) T->upto[r] = base + w;
       base += __shfl_sync(kFull, w, 31);
+    }
+    // More rows than there are: requests overlap, and their work may be more than
+    // the host has checked.  Nothing is done.
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n_all += __shfl_xor_sync(kFull, n_all, o);
+    if (n_all > a.rows.total_rows) {
+      for (int r = lane; r < a.rows.batch; r += 32) T->upto[r] = 0;
+      if (blockIdx.x == 0 && lane == 0) report(a.status, PCTREE_ERR_INVALID_ARG);
     }
   }
   tc_fence_before_sync();

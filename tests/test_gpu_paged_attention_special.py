@@ -88,3 +88,17 @@ def test_rows_whose_scores_are_all_minus_infinity(P, D, dtype):
     assert c.run(P) == 0
     want = compare(c)
     assert np.isnan(want[[0, 1, 4]]).all() and np.isfinite(want[[2, 3, 5, 6]]).all()
+
+
+def test_requests_that_claim_the_same_rows(P):
+    """More rows together than there are: an error, and nothing is written."""
+    c = Call(P, Batch([30, 7, 1], [100, 20, 0], 16), 4, 2, 64)
+    c.dev["row_start"].zero_()
+    c.dev["n_rows"].copy_(torch.tensor([38, 7, 1]))
+    c.dev["prefix_len"].copy_(torch.tensor([80, 20, 0]))
+    assert c.run(P) == -1
+    assert (c.out == 9).all()
+    b = Batch([30, 7, 1], [100, 20, 0], 16)          # and as many as there are
+    c = Call(P, b, 4, 2, 64)
+    assert c.run(P) == 0
+    c.check()
