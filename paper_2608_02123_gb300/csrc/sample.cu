@@ -20,7 +20,7 @@
 //   light  2^(n/128) from a table in 31-bit fixed point, times 1 + s, s the
 //          rest of at most 1/256 octave by a cubic: relative error 2^-30.5,
 //          independent from token to token;
-//   fine   the same with every term carried as a float pair: 2^-41.
+//   fine   the same with every term carried as a float pair: 2^-39.5.
 // Tokens above 2^-12 of the total use the fine form (there are at most 4096);
 // the errors of the light ones then add up to at most 2^-36.5 of the total.
 //
@@ -242,12 +242,12 @@ __device__ __noinline__ unsigned long long fine_weight(const RowFacts& f, float 
   const int n = static_cast<int>(kf) - f.k;
   const int j = n & 127;
   const float th = kPow2.hi[j], tl = kPow2.lo[j];
-  // th + q + rest in units of 2^-45: th's bits, q in units of 2^-30 and what is
-  // left
+  // (th + tl)(1 + yh + sl) = th + q + rest in units of 2^-45: th's bits, q in units
+  // of 2^-30 and what is left (tl yh is up to 2^-32.7; tl sl is below 2^-42)
   const float q = th * yh;
   const int qi = __float2int_rn(q * 1073741824.0f);
   const float rest = fmaf(static_cast<float>(qi), -1.0f / 1073741824.0f, q) +
-                     (fmaf(th, yh, -q) + fmaf(th, sl, tl));
+                     (fmaf(th, yh, -q) + fmaf(th, sl, fmaf(tl, yh, tl)));
   const long long w =
       (static_cast<long long>((__float_as_uint(th) & 0x7fffffu) | 0x800000u) << 22) +
       (static_cast<long long>(qi) << 15) + __float2int_rn(rest * 35184372088832.0f);
