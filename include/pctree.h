@@ -552,9 +552,13 @@ PCTREE_API pctree_status pctree_paged_attention(
  *   min-p    keeps those with w_i >= min_p (0: all)
  *   token    the first kept i, by ascending index, whose kept w_0 + .. + w_i
  *            exceed u times the sum of all kept w.
- * Temperature 0: the first of the order.  The sums are exact integers of
- * weights good to 2^-32 and 2^-44 of the largest, so that a token does not
- * depend on the order of summation or the launch.
+ * Temperature 0: the first of the order.  The sums are exact integers, so that
+ * a token does not depend on the order of summation or the launch.  A weight is
+ * good to 2^-39 of itself if it is more than 2^-12 of the sum, else to 2^-29
+ * (and both to 2^-45 of the largest): a random number within 2^-30 of a border
+ * between two tokens (of the sum; 2^-35 where thousands of tokens do not share
+ * a few values) may give the neighbour, and so may a top_p that close to the
+ * share of a head.
  */
 typedef struct {
   int32_t rows;          /* rows of logits                                   */

@@ -60,3 +60,27 @@ def test_two_tokens(P, form):
     elif form == "min_p":
         params["min_p"] = np.full(len(u), 1e-12, np.float32)
     np.testing.assert_array_equal(sample(P, torch.from_numpy(z).cuda(), u, **params), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("streamed", [False, True])
+def test_thousands_of_equal_tokens(P, dtype, streamed):
+    """Rows of two values, all of them light: weights good to 2^-29.4, the same
+    error for equal logits, so a border moves by up to 2^-30.4."""
+    V = 16384 if streamed else 16383
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    rng = np.random.default_rng(7)
+    n = 1 << 17
+    z = torch.from_numpy(rng.uniform(-1, 1, (n, 2)).astype(np.float32)).to(dt).float().numpy()
+    T = rng.uniform(0.8, 3, n).astype(np.float32)
+    first = rng.integers(6000, V - 6000, n)      # tokens of the first value
+    w = np.exp((z[:, 1].astype(L) - z[:, 0]) / T)
+    F = first / (first + (V - first) * w)
+    u, at = near(F, 2.0 ** -30.3, 2.0 ** -28.5)
+    u, at = u[:400], at[:400]
+    assert len(u) == 400
+    rows = torch.from_numpy(z[at]).cuda().to(dt)
+    low = torch.arange(V, device="cuda") < torch.from_numpy(first[at]).cuda()[:, None]
+    rows = torch.where(low, rows[:, :1], rows[:, 1:])
+    want = first[at] - (u.astype(L) < F[at])
+    np.testing.assert_array_equal(sample(P, rows, u, temperature=T[at]), want)
