@@ -1430,14 +1430,17 @@ bool wide_clusters(int dtype) {
     lc.attrs = attr;
     lc.numAttrs = 1;
     int clusters = 0;
-    const bool fits =
+    const bool asked =
         cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(kSampleSmem)) == cudaSuccess &&
         cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) ==
             cudaSuccess &&
-        cudaOccupancyMaxActiveClusters(&clusters, fn, &lc) == cudaSuccess && clusters > 0;
-    if (!fits) (void)cudaGetLastError();
-    k = fits ? 1 : -1;
+        cudaOccupancyMaxActiveClusters(&clusters, fn, &lc) == cudaSuccess;
+    if (!asked) {                                // no answer to keep
+      (void)cudaGetLastError();
+      return false;
+    }
+    k = clusters > 0 ? 1 : -1;
   }
   return k > 0;
 }
