@@ -226,6 +226,31 @@ __device__ __noinline__ void clean_v(uint8_t* v, Tail* T, int parity, int thread
   }
 }
 
+// Scores (in log2 units) whose floats are half an octave apart: from here on the
+// softmax's fused product would differ from its reference, a rounded product, by
+// powers of two that P's type does not hold.
+constexpr float kWideScore = 4194304.0f;
+
+// The 64 scores of a block half at TMEM columns s_col .. (those from `seen` on are
+// -inf) become what, times sc, is the rounded score less the reference.  (Not
+// inline: in the loop it cost prompts 6 %.)
+__device__ __noinline__ void wide_scores(uint32_t s_col, float sc, float mref, int seen) {
+  const float inv = 1.0f / sc;
+#pragma unroll 1
+  for (int c = 0; c < 64; c += 8) {
+    uint32_t y[8];
+    tmem_ld_32x32b_x8(s_col + c, y);
+    tmem_ld_wait();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float x = c + k < seen ? __uint_as_float(y[k]) : -INFINITY;
+      y[k] = __float_as_uint((__fmul_rn(x, sc) - mref) * inv);
+    }
+    tmem_st_x8(s_col + c, y);
+  }
+  tmem_st_wait();
+}
+
 template <int D, bool F16>
 __global__ void __maxnreg__(112)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
@@ -792,6 +817,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
       // keys this row sees: slots below `end`
       const int end = min(it.key_end, it.prefix + it.j0 + nl + 1);
       float m_used = -INFINITY, l_sum = 0.0f;
+      float over = -INFINITY;                      // a maximum above it needs a look
       for (int b = it.b0; b < it.b1; ++b, ++g) {
         const int sb = g & 1;
         int cap;
@@ -821,7 +847,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
         for (int k2 = 8; k2 < 64; ++k2) m8[k2 & 7] = fmaxf(m8[k2 & 7], x[k2]);
         const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
                          fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * sc;
-        if (__any_sync(kFull, mx > m_used + 8.0f)) {
+        bool shifted = false;
+        if (__any_sync(kFull, mx > over)) {
           const bool mine = mx > m_used + 8.0f;
           const float alpha = mine ? ex2_approx(m_used - mx) : 1.0f;
           if (b > it.b0) {
@@ -843,8 +870,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
             l_sum *= alpha;
             m_used = mx;
           }
+          const bool wide = fabsf(m_used) > kWideScore && m_used > -INFINITY;
+          over = wide ? -INFINITY : m_used + 8.0f;
+          shifted = __any_sync(kFull, wide);
+          if (shifted) {
+            wide_scores(s_col, sc, m_used == -INFINITY ? 0.0f : m_used, seen);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              tmem_ld_32x32b_x32(s_col + c * 32,
+                                 *reinterpret_cast<uint32_t(*)[32]>(
+                                     reinterpret_cast<uint32_t*>(x) + c * 32));
+            tmem_ld_wait();
+          }
         }
-        const float mref = m_used == -INFINITY ? 0.0f : m_used;
+        const float mref = shifted || m_used == -INFINITY ? 0.0f : m_used;
         const uint64_t sc2 = pack2(sc, sc), nm2 = pack2(-mref, -mref);
         uint64_t ls[4] = {0, 0, 0, 0};
 #pragma unroll

@@ -102,3 +102,42 @@ def test_requests_that_claim_the_same_rows(P):
     c = Call(P, b, 4, 2, 64)
     assert c.run(P) == 0
     c.check()
+
+
+@pytest.mark.parametrize("D,dtype,power", [(64, "bf16", 30), (64, "bf16", 58), (128, "bf16", 40),
+                                           (64, "f16", 27), (128, "f16", 27)])
+@pytest.mark.parametrize("name", sorted(PREFIXES))
+def test_scores_too_large_for_fractions(P, name, D, dtype, power):
+    """Scores whose floats are whole numbers apart (2^power and more): the largest
+    takes all, exactly."""
+    prefix = PREFIXES[name]
+    b = Batch([12, 5], prefix, 64)
+    c = Call(P, b, 8, 2, D, dtype, garbage=False)
+    # one product a score, four times or D times the same: exact in float32
+    n = 4 if dtype == "bf16" else D
+    c.q.zero_()
+    c.k.zero_()
+    half = power // 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(power)
+    steps = torch.randint(-128, 128, c.k.shape[:2], generator=g, device="cuda")
+    if half > 14:                                # float16 ends at 2^16
+        c.q[..., :n] = 2.0 ** (power - half)
+        c.k[..., :n] = ((1 + steps / 128.0) * 2.0 ** half)[..., None].to(c.dt)
+    else:
+        c.q[..., :n] = 2.0 ** 14
+        c.k[..., :n] = ((1 + steps / 128.0) * 2.0 ** (power - 14))[..., None].to(c.dt)
+    # a largest one early in the prefix, one among the new rows
+    for r in range(2):
+        at = int(b.places(r, 9, 10)[0])
+        c.k[at, :, :n] = 2.25 * 2.0 ** (half if half > 14 else power - 14)
+        at = int(b.places(r, prefix[r] + 3, prefix[r] + 4)[0])
+        c.k[at, :, :n] = 2.5 * 2.0 ** (half if half > 14 else power - 14)
+    assert c.run(P) == 0
+    got, v = c.out[1:-1], c.v
+    for r in range(2):
+        for j in range(int(b.rows[r])):
+            at = int(b.places(r, 9, 10)[0] if j < 3 else b.places(r, prefix[r] + 3,
+                                                                  prefix[r] + 4)[0])
+            want = v[at].repeat_interleave(4, 0)
+            assert torch.equal(got[int(b.start[r]) + j], want), (r, j)
