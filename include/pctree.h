@@ -466,7 +466,8 @@ typedef struct {
  *   q_weight,
  *   k_weight        [D] in dtype, 16-byte aligned, or NULL: no norm
  *   inv_freq        [rotary_dim / 2] double (device): radians per position;
- *                   NULL only if rotary_dim = 0
+ *                   NULL only if rotary_dim = 0.  One that is not finite counts
+ *                   as 0 and sets the status to PCTREE_ERR_INVALID_ARG.
  *   positions       [total_rows] int32, or NULL: the slot, prefix_len + j.
  *                   For trees the position_ids of pctree_draft (depth + T).
  *   row_start, n_rows, prefix_len   [batch] int32 (device)

@@ -74,7 +74,11 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) kv_append_kernel(
     sh.weight[i < D ? 0 : 1][d] = w != nullptr ? unpack16<F16>(w[d]).x : 1.0f;
   }
   for (int i = threadIdx.x; i < half; i += kAppendThreads) {
-    const double t = a.inv_freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
+    double t = a.inv_freq[i] * 0.15915494309189533577;   // 1 / (2 pi)
+    if (!(fabs(t) < INFINITY)) {
+      t = 0.0;
+      if (blockIdx.x == 0 && a.status != nullptr) atomicCAS(a.status, 0, PCTREE_ERR_INVALID_ARG);
+    }
     // the fraction in [-0.5, 0.5] as a signed 64-bit integer, twice over
     sh.turn[i] =
         static_cast<unsigned long long>(__double2ll_rn((t - rint(t)) * 9223372036854775808.0)) << 1;
