@@ -422,7 +422,8 @@ PCTREE_API pctree_status pctree_tree_attention(
  * s % page_size of page page_table[r][s / page_size], page_table
  * [batch][max_pages] int32.  page_table NULL: request r's only page is page r
  * (n_pages >= batch, max_pages = 1), which is the contiguous layout of
- * pctree_tree_attention with max_slots = page_size.
+ * pctree_tree_attention with max_slots = page_size.  Trees need that layout:
+ * pctree_tree_attention and pctree_compact know no pages.
  *
  * A request with n_rows[r] < 0, prefix_len[r] < 0, rows outside
  * 0 .. total_rows - 1 or slots past max_pages * page_size is left out
@@ -469,7 +470,8 @@ typedef struct {
  *                   NULL only if rotary_dim = 0.  One that is not finite counts
  *                   as 0 and sets the status to PCTREE_ERR_INVALID_ARG.
  *   positions       [total_rows] int32, or NULL: the slot, prefix_len + j.
- *                   For trees the position_ids of pctree_draft (depth + T).
+ *                   For trees depth + T of each request (the position_ids of
+ *                   pctree_draft where every T is its pos_offset).
  *   row_start, n_rows, prefix_len   [batch] int32 (device)
  *   page_table      [batch][max_pages] int32 (device) or NULL
  *   status          one device int32 or NULL; written only on an error.  A row
@@ -494,12 +496,13 @@ PCTREE_API pctree_status pctree_kv_append(
  * rows (behind a prefix of earlier chunks or none), a drafted chain (k = 1)
  * is verified as the rows behind its root.  Keys and values of the rows are
  * in the cache before the call (pctree_kv_append).  Slots past the last row
- * are never used (their values may be anything).  A NaN or infinite score or
- * value reaches the rows that see it and no others (where one tile's new rows,
- * at most 128 / G, hold non-finite values in more than 64 groups of 8 dims of
- * a head, every dim of the rows that see the first of them is NaN).  Scores,
- * row maxima and sums and the output's accumulation are float32; probabilities
- * are rounded to dtype for the product with the values.
+ * are never used (their values may be anything).  A row without a finite score
+ * is NaN.  A NaN or infinite score or value reaches the rows that see it and no
+ * others (where one tile's new rows, at most 128 / G, hold non-finite values in
+ * more than 64 groups of 8 dims of a head, every dim of the rows that see the
+ * first of them is NaN).  Scores, row maxima and sums and the output's
+ * accumulation are float32; probabilities are rounded to dtype for the product
+ * with the values.
  */
 typedef struct {
   int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
@@ -528,7 +531,8 @@ pctree_paged_attention_workspace_bytes(const pctree_paged_attn_config* cfg);
  *                   PCTREE_ERR_INVALID_ARG with nothing of out written if the
  *                   requests have more rows together than total_rows)
  * Any page_size >= 1 works; 8, 16, 32, 64 and multiples of 128 fill the
- * kernel's blocks of 128 keys.
+ * kernel's blocks of 128 keys, others have a block a page (or part of one) and
+ * take as much longer.
  * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED /
  * PCTREE_ERR_WORKSPACE for bad arguments (nothing enqueued) and
  * PCTREE_ERR_CUDA if the launch fails.

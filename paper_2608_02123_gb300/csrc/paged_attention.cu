@@ -29,13 +29,13 @@
 // in PCTREE_ERR_TIMEOUT.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
-//   tokens of 32 requests over up to 8192 slots: HBM, 854 MB in 138, 0.91 of
+//   tokens of 32 requests over up to 8192 slots: HBM, 854 MB in 141, 0.89 of
 //   the measured copy rate;
 //   four prompts of up to 4096 rows: K and V into the SMs, 64 KB a block for
-//   every tile, 450 in pages of 64 (0.95 PFLOP/s), 480 of 32, 588 of 16, whose
-//   24 TMA boxes a block cost ~30 ns each, 666 of 8;
-//   a token of one request: two launches and one block's chain, 13.4.
-// K and V in turn (K a block ahead: 471 in pages of 64, 603 of 16), one box for
+//   every tile, 458 in pages of 64 (0.93 PFLOP/s), 485 of 32, 591 of 16, whose
+//   24 TMA boxes a block cost ~30 ns each, 668 of 8;
+//   a token of one request: two launches and one block's chain, 14.4.
+// K and V in turn (K a block ahead: 450 -> 471 in pages of 64, 588 -> 603 of 16), one box for
 // both halves of the dims in small pages (pages of 8: 253 -> 183 for tokens),
 // pieces of equal length (a unit a CTA leaves SMs idle at the end).  Every CTA
 // loads for itself: copies that multicast a block to the tiles of a cluster
