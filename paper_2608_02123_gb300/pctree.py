@@ -562,8 +562,8 @@ def _refuse(where: str, device: int, checks) -> None:
 
 def _flat_check(name, t, dt, n, device, row=1):
     return (name, _flat(t, dt, n, device, row),
-            f"a contiguous {dt} tensor of at least {n} elements"
-            + (f", in rows of {row}" if row > 1 else ""))
+            f"a contiguous {dt} tensor of {n} elements (or more, in one dimension"
+            + (f" or rows of {row})" if row > 1 else ")"))
 
 
 def _table_check(t, batch, max_pages, device):

@@ -106,7 +106,7 @@ def test_one_request_in_a_longer_contiguous_cache(P):
 
 def test_positions_of_trees(P):
     append(P, positions=zeros(2, 3, dtype=I32))
-    with pytest.raises(ValueError, match="positions"):
+    with pytest.raises(ValueError, match="positions must be a contiguous .* of 6 elements"):
         append(P, positions=zeros(2, 4, dtype=I32))          # rows 4 apart, not 3
 
 
