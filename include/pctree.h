@@ -544,6 +544,168 @@ PCTREE_API pctree_status pctree_paged_attention(
     void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
+ * The cache in 8 bits.  k_cache and v_cache hold e4m3 codes, a byte each, in the
+ * places of a 16-bit cache ([n_pages][page_size][Hkv][D], dense; slots, pages and
+ * requests as above).  `scale_block` consecutive slots of a page (1, 2, 4 .. 128;
+ * a page's last block may be shorter) share a power-of-two scale per KV head:
+ *   value = code * 2^(byte - 127),  byte of k_scale / v_scale
+ *   [n_pages][ceil(page_size / scale_block)][Hkv], one byte each (e8m0),
+ *   its exponent byte - 127 in -15 .. 7.
+ * So magnitudes from 2^-24 to 57344 are held, to 2^-4 of themselves where the
+ * block's largest is less than 2^15 times as large; a power of two as the scale
+ * costs a floating code no precision, makes every value exact in float16, and a
+ * block whose scale grows rounds no code again but subnormal ones.  Code 0x7f /
+ * 0xff is NaN.
+ */
+
+/*
+ * pctree_kv_append into a cache in 8 bits: the same norms and rotation (queries
+ * go to q_out in dtype), keys and values to codes:
+ *   e    = the smallest exponent in -15 .. 7 with max |x'| <= 448 * 2^e, the
+ *          maximum over the block's new slots and the head's dims; not below the
+ *          block's own, if the block holds earlier slots of the request (those
+ *          below prefix_len), whose codes are then brought to the new scale
+ *   code = x' * 2^-e, rounded to nearest even; past 448 it is 448.
+ * Arithmetic before that is float32.  A key or value that is not finite gets the
+ * code 0x7f, is left out of the maximum and sets the status to
+ * PCTREE_ERR_NONFINITE.  The slots of a block that one call appends to belong to
+ * one request (blocks of pages that requests share are full).
+ */
+typedef struct {
+  int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
+  int32_t total_rows;    /* rows of q, k, v, q_out and positions             */
+  int32_t Hq, Hkv, D;    /* Hq may be 0 (keys and values only); D 64, 128    */
+  int32_t page_size, n_pages, max_pages;
+  int32_t scale_block;   /* slots that share a scale: a power of two, 1 .. 128 */
+  int32_t dtype;         /* PCTREE_BF16 or PCTREE_F16, of q, k, v, q_out and
+                            the weights                                      */
+  int32_t rotary_dim;    /* as in pctree_append_config, all that follow      */
+  int32_t interleaved;
+  int64_t q_stride, k_stride, v_stride;
+  float eps;
+  float rope_scale;
+} pctree_kv8_append_config;
+
+/*
+ * Arguments, alignments, refusals and the status as in pctree_kv_append, with
+ * k_scale and v_scale behind the caches (any alignment).  If the requests have
+ * more rows together than total_rows, nothing is written where scale_block > 1
+ * (PCTREE_ERR_INVALID_ARG).  No workspace.  Memory bound: rows are read from
+ * memory once and written once.
+ */
+PCTREE_API pctree_status pctree_kv8_append(
+    const pctree_kv8_append_config* cfg, const void* q, const void* k, const void* v,
+    const void* q_weight, const void* k_weight, const double* inv_freq,
+    const int32_t* positions, const int32_t* row_start, const int32_t* n_rows,
+    const int32_t* prefix_len, const int32_t* page_table, void* k_cache,
+    void* v_cache, void* k_scale, void* v_scale, void* q_out, int32_t* status,
+    void* stream);
+
+/*
+ * Attention of new rows over a cache in 8 bits that holds them and their prefix:
+ * pctree_paged_attention's formula and rows with K and V as above, and, with
+ * `parent`, packed trees as in pctree_tree_attention: row j of request r sees the
+ * slots 0 .. prefix_len[r] - 1 and prefix_len[r] + m for the m on the path from j
+ * to its root (j included).  Both forms take paged and contiguous caches.
+ *
+ * Slots no row of the request sees are never used.  A row without a finite score
+ * is NaN.  A NaN code reaches the rows that see its slot (a key's every dim, a
+ * value's own dim; where one tile's new rows, at most 128 / G, hold NaN values in
+ * more than 64 groups of 16 dims of a head, every dim of the rows that see the
+ * first of them) and no others.  Scores, row maxima and sums and the output's
+ * accumulation are float32; what else is rounded before the end is stated at the
+ * kernels and stays below half a step of float16 for each probability.
+ */
+typedef struct {
+  int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
+  int32_t total_rows;    /* rows of q, out and parent                        */
+  int32_t Hq, Hkv, D;    /* Hq a multiple of Hkv, Hq / Hkv <= 128; D 64, 128 */
+  int32_t page_size, n_pages, max_pages;
+  int32_t scale_block;   /* slots that share a scale: a power of two, 1 .. 128 */
+  int32_t dtype;         /* PCTREE_BF16 or PCTREE_F16, of q and out          */
+  int64_t q_stride;      /* elements from row to row of q, a multiple of 8,
+                            at least Hq * D                                  */
+  float scale;           /* softmax scale, e.g. 1/sqrt(D), > 0               */
+} pctree_kv8_attn_config;
+
+/* Workspace bytes pctree_kv8_attention needs on any GPU of this kind; 0 for a
+ * bad config.  256-byte aligned, any prior content. */
+PCTREE_API size_t
+pctree_kv8_attention_workspace_bytes(const pctree_kv8_attn_config* cfg);
+
+/*
+ *   q               [total_rows] rows of [Hq][D], 16-byte aligned
+ *   out             [total_rows][Hq][D], 16-byte aligned, not overlapping q
+ *   k_cache, v_cache   codes, 16-byte aligned; k_scale, v_scale: their scales.
+ *                   A scale outside its range counts as the nearest one in it
+ *                   and sets the status to PCTREE_ERR_INVALID_ARG.
+ *   page_table      [batch][max_pages] int32 or NULL.  A bad page number stands
+ *                   for a page of zeros (status PCTREE_ERR_INVALID_ARG).
+ *   parent          [total_rows] int32 or NULL: a row's parent, counted from its
+ *                   request's first row, smaller than its own number; -1 for a
+ *                   root (several are allowed).  Another value counts as -1 and
+ *                   sets the status to PCTREE_ERR_INVALID_ARG, and so does a
+ *                   request with more than PCTREE_ATTN_MAX_N rows, which is left
+ *                   out.
+ *   workspace       not used concurrently by another call
+ *   status          one device int32 or NULL; written only on an error (as in
+ *                   pctree_paged_attention, and the above)
+ * Any page_size >= 1 works at the same speed.
+ * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED /
+ * PCTREE_ERR_WORKSPACE for bad arguments (nothing enqueued) and
+ * PCTREE_ERR_CUDA if the launch fails.
+ */
+PCTREE_API pctree_status pctree_kv8_attention(
+    const pctree_kv8_attn_config* cfg, const void* q, const void* k_cache,
+    const void* v_cache, const void* k_scale, const void* v_scale,
+    const int32_t* row_start, const int32_t* n_rows, const int32_t* prefix_len,
+    const int32_t* page_table, const int32_t* parent, void* out, void* workspace,
+    size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * pctree_compact for caches in 8 bits, paged or contiguous, all layers in one
+ * call: for the accepted nodes a = accepted_idx[r][0 .. L], L = accepted_len[r],
+ * and T = prefix_len[r],
+ *   slot T + j  <-  slot T + a[j]     (j = 0 .. L, keys and values, in place).
+ * A block that holds slots T .. T + L gets the largest scale of the rows that it
+ * then holds (slots below T of the request included), and codes of a smaller one
+ * are brought to it.  Slots past T + L in those blocks have no defined value
+ * afterwards; all others keep theirs.  Hidden states: pctree_compact with layers
+ * = planes = 0.
+ */
+typedef struct {
+  int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
+  int32_t B;             /* accepted_idx rows hold B + 1 ints                */
+  int32_t N;             /* packed tree size: T + N slots exist              */
+  int32_t layers;
+  int32_t Hkv, D;        /* D 64, 128                                        */
+  int32_t page_size, n_pages, max_pages;
+  int32_t scale_block;   /* slots that share a scale: a power of two, 1 .. 128 */
+  int64_t cache_layer_stride;  /* bytes from layer to layer of k_cache and
+                            v_cache, a multiple of 16, and of k_scale and    */
+  int64_t scale_layer_stride;  /* v_scale; at least a layer's (unused if
+                            layers = 1)                                      */
+} pctree_kv8_compact_config;
+
+/*
+ *   accepted_idx, accepted_len, prefix_len   as in pctree_compact
+ *   page_table      [batch][max_pages] int32 (device) or NULL, of all layers
+ *   k_cache, v_cache   [layers] caches, 16-byte aligned; k_scale, v_scale
+ *   status          one device int32 or NULL.  A request whose accepted path is
+ *                   not one pctree_accept can return, with T < 0 or T + N >
+ *                   max_pages * page_size, or with a bad page among those of its
+ *                   rows, is left untouched and sets it to
+ *                   PCTREE_ERR_INVALID_ARG; otherwise it is not written.
+ * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED for bad arguments
+ * (nothing enqueued) and PCTREE_ERR_CUDA if the launch fails.  No workspace.
+ */
+PCTREE_API pctree_status pctree_kv8_compact(
+    const pctree_kv8_compact_config* cfg, const int32_t* accepted_idx,
+    const int32_t* accepted_len, const int32_t* prefix_len,
+    const int32_t* page_table, void* k_cache, void* v_cache, void* k_scale,
+    void* v_scale, int32_t* status, void* stream);
+
+/*
  * The target's tokens from its logits and one given random number a row, the
  * `target_tokens` of pctree_accept.  (Accepting the drafted child that equals
  * the token sampled at its parent keeps the target's distribution: every

@@ -1,0 +1,1000 @@
+// pctree_kv8_attention: grouped-query attention of new rows of several requests
+// (tokens, chains, packed trees, prompts) over a paged or contiguous cache of
+// 8-bit codes with a power-of-two scale per block of slots and head.
+//
+// Units, pieces and joins are kv_pieces.cuh's: a tile's rows are (row, query head
+// of the group) pairs, R = G * npt <= 128, and its keys come in blocks of 128
+// consecutive slots, gathered slot by slot, so pages of any size fill a block.
+//
+//   warp 0        planner: the CTA's pieces, in order, up to kItemRing ahead
+//   warp 1        S issuer: S_b = Q K_b^T (tcgen05.mma, M = N = 128) into one of
+//                 two TMEM buffers
+//   warp 2        PV issuer: O_h += P_b V_b over each half h of the block's keys
+//                 (P read from TMEM)
+//   warps 4..7    a tile's Q (two buffers) and its rows' ancestors, two pieces
+//                 ahead; the two O of a finished piece, combined, to rows of out
+//                 or the piece's partial, while the softmax goes on
+//   warps 8..15   softmax, two threads per tile row, 64 keys of a block each with
+//                 its own running maximum, sum and O
+//   warps 16..19  K, and warps 20..23 V: codes to registers a block ahead (and
+//                 page numbers two), to float16 in shared memory (128-byte
+//                 swizzle, 64 dims a half), two blocks of each
+// All waits are bounded (1 s; those for a whole piece 1 s without a block) and end
+// in PCTREE_ERR_TIMEOUT.
+//
+// Numbers: code * 2^e is exact in float16 for every exponent of the format, so the
+// products' K and V are the cache's values.  A bfloat16 row of Q is multiplied by
+// a power of two that brings its largest element to 2^14 .. 2^15, which float16
+// holds to 2^-39 of the largest; the power goes into the row's softmax scale.  P is
+// 2^7 times the probability relative to the row's running maximum, in float16 (11
+// bits; down to 2^-31 of the maximum): far keys of a long context that are each
+// small against the first are not lost.  Row sums add the unrounded values.
+#include "kv8.cuh"
+#include "kv_pieces.cuh"
+
+namespace pct {
+namespace {
+
+constexpr int kBK = 128;                     // keys per block
+constexpr int kHalfBytes = 128 * 128;        // 128 rows x 64 halves
+constexpr uint64_t kLimitNs = 1000000000ull;
+constexpr int kThreads = 768;
+constexpr int kSlots = 4;                    // K and V blocks in the ring, in turn
+constexpr int kItemRing = 4;
+constexpr int kMaxBad = 64;                  // groups of 16 values of V told apart
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kOCol = 2 * kBK;
+constexpr float kPBits = 7.0f;               // P is 2^7 times what it is relative to
+
+struct Kv8AttnArgs {
+  Units units;
+  Kv8Blocks blocks;
+  const uint16_t* q;
+  const uint8_t* cache[2];                   // keys, values
+  const uint8_t* scale[2];
+  const int32_t* parent;                     // NULL: causal
+  uint16_t* out;
+  float* part_o;                             // as in JoinArgs
+  float2* part_ml;
+  PieceJoin* join;
+  int32_t* status;
+  long long q_stride;
+  int Hq, G;
+  float scale_log2;
+};
+
+struct Tail {
+  uint64_t q_full[2], q_empty[2];
+  uint64_t kv_full[kSlots], kv_empty[kSlots];
+  uint64_t s_full[2], p_full[2], p_empty[2];
+  uint64_t o_full, o_empty;
+  uint64_t item_full[kItemRing], item_empty[kItemRing];
+  uint64_t done, out_sync;
+  uint32_t tmem_base;
+  int abort;
+  int blocks;                                // multiplied so far (see wwait_long)
+  Piece item[kItemRing];
+  float row_l[2][128], row_m[2][128];
+  float row_scale[2][128];                   // of Q's rows, by Q buffer (log2 units)
+  // NaN values at keys that only some rows of the piece's tile see, by place in the
+  // item ring: 16 bits of a group of dims, the group << 16, the key (counted from
+  // the first that not every row sees) << 20; their number and the first such key.
+  int bad_n[kItemRing], bad_first[kItemRing];
+  uint32_t bad[kItemRing][kMaxBad];
+  int16_t par[PCTREE_ATTN_MAX_N];
+  uint32_t path[2][128][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by Q buffer
+  alignas(16) uint8_t stage[4][32 * 32];
+  unsigned upto[PCTREE_KV_MAX_BATCH];        // work of requests 0 .. r
+};
+
+__device__ __forceinline__ void report(int32_t* status, int code) {
+  if (status != nullptr) atomicCAS(status, 0, code);
+}
+
+template <int N>
+__device__ __forceinline__ void set_registers_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void set_registers_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15])
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem] (see tc_mma_bf16): A's 16 K elements are 8
+// columns of 16-bit pairs.
+__device__ __forceinline__ void tc_mma_tmem_a(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor with float16 operands.
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
+  return idesc_bf16_f32(M, N) & ~((1u << 7) | (1u << 10));
+}
+
+__device__ __forceinline__ uint4 load16(const uint8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+// Two float16 values times a float16 pair.
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// 2^e in both halves of a word, e in -15 .. 7.
+__device__ __forceinline__ uint32_t half2_exp(int e) {
+  const uint32_t h = e >= -14 ? static_cast<uint32_t>(e + 15) << 10 : 0x200u;
+  return h * 0x10001u;
+}
+
+// The bytes of a word that are the code NaN, as 0xff each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (top >> 7) * 0xffu;
+}
+
+// Scores (in log2 units) whose floats are half an octave apart: from here on the
+// softmax's fused product would differ from its reference, a rounded product, by
+// powers of two that P's type does not hold.
+constexpr float kWideScore = 4194304.0f;
+
+// The 64 scores of a block half at TMEM columns s_col .. (those not in `see` are
+// -inf) become what, times sc, is the rounded score less the reference.
+__device__ __noinline__ void wide_scores(uint32_t s_col, float sc, float mref, uint64_t see) {
+  const float inv = 1.0f / sc;
+#pragma unroll 1
+  for (int c = 0; c < 64; c += 8) {
+    uint32_t y[8];
+    tmem_ld_32x32b_x8(s_col + c, y);
+    tmem_ld_wait();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float x = (see >> (c + k)) & 1 ? __uint_as_float(y[k]) : -INFINITY;
+      y[k] = __float_as_uint((__fmul_rn(x, sc) - mref) * inv);
+    }
+    tmem_st_x8(s_col + c, y);
+  }
+  tmem_st_wait();
+}
+
+// A block of a piece, for the warps that bring K or V.
+struct Block {
+  int r, kvh, key0, key_end, all, ring;      // keys below `all` are seen by every row
+};
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
+  constexpr int kHalves = D / 64;
+  constexpr int kTileBytes = kHalves * kHalfBytes;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sq = sm;                                // Q buffer of the k-th piece: k & 1
+  uint8_t* skv = sm + 2 * kTileBytes;              // ring
+  Tail* T = reinterpret_cast<Tail*>(skv + kSlots * kTileBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int R = a.G * a.units.npt;                 // rows of a tile
+  volatile int* abort_v = &T->abort;
+
+  // ---------------- set-up ----------------
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&T->kv_full[s], 4);
+      mbar_init(&T->kv_empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&T->q_full[s], 4);
+      mbar_init(&T->q_empty[s], 1);
+      mbar_init(&T->s_full[s], 1);
+      mbar_init(&T->p_full[s], 8);
+      mbar_init(&T->p_empty[s], 1);
+    }
+    for (int s = 0; s < kItemRing; ++s) {
+      mbar_init(&T->item_full[s], 1);
+      mbar_init(&T->item_empty[s], 2 + 4 + 8 + 8);
+    }
+    mbar_init(&T->o_full, 1 + 8);
+    mbar_init(&T->o_empty, 4);
+    mbar_init(&T->done, 2);
+    mbar_init(&T->out_sync, 4);
+    T->abort = 0;
+    T->blocks = 0;
+    fence_barrier_init();
+  }
+  // rows R..127 of the Q buffers are never written: zero them once
+  const int zq = (128 - R) * 8;
+  for (int i = threadIdx.x; i < 2 * kHalves * zq; i += kThreads) {
+    const int h = i / zq, rem = i - h * zq;
+    *reinterpret_cast<uint4*>(sq + h * kHalfBytes + (R + rem / 8) * 128 + (rem % 8) * 16) =
+        make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async_smem();
+  if (warp == 1) tmem_alloc(&T->tmem_base, kTmemCols);
+  pdl_launch_dependents();
+  pdl_wait();
+  count_work<kThreads>(a.units, T->upto, [&](int code) {
+    if (blockIdx.x == 0) report(a.status, code);
+  });
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = T->tmem_base;
+
+  auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
+    return __all_sync(kFull, mbar_wait_bounded(bar, parity, abort_v, kLimitNs));
+  };
+  // a wait that lasts as long as pieces do: over once no block has been multiplied
+  // for the limit
+  auto wwait_long = [&](uint64_t* bar, uint32_t parity) -> bool {
+    volatile int* blocks = &T->blocks;
+    for (;;) {
+      const int before = *blocks;
+      if (wwait(bar, parity)) return true;
+      if (__any_sync(kFull, *abort_v != 0) || __all_sync(kFull, *blocks == before)) return false;
+    }
+  };
+  auto give_up = [&]() {
+    *abort_v = 1;
+    report(a.status, PCTREE_ERR_TIMEOUT);
+  };
+  auto fetch_one = [&](int k, Piece& it) -> bool {
+    const int s = k % kItemRing;
+    if (!mbar_wait_bounded(&T->item_full[s], (k / kItemRing) & 1, abort_v, kLimitNs)) return false;
+    it = T->item[s];
+    mbar_arrive(&T->item_empty[s]);
+    return true;
+  };
+  // (peek leaves the place taken)
+  auto peek_warp = [&](int k, Piece& it) -> bool {
+    const int s = k % kItemRing;
+    if (!wwait_long(&T->item_full[s], (k / kItemRing) & 1)) return false;
+    it = T->item[s];
+    return true;
+  };
+  auto release_warp = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&T->item_empty[k % kItemRing]);
+  };
+
+  if (warp < 4) {
+    set_registers_down<48>();
+    if (warp == 1 && lane == 0) {
+      // ---------------- S issuer ----------------
+      constexpr uint32_t idS = idesc_f16(128, kBK);
+      int q = 0, g = 0;
+      const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
+      const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
+      bool ok = true;
+      Piece it;
+      for (int k = 0; ok; ++k) {
+        if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
+        const int qb = q & 1;
+        if (!(ok = mbar_wait_bounded(&T->q_full[qb], (q >> 1) & 1, abort_v, kLimitNs))) break;
+        ++q;
+        const uint64_t qd = q_desc + qb * (kTileBytes >> 4);
+        for (int b = it.b0; b < it.b1; ++b, ++g) {
+          const int sb = g & 1, slot = (2 * g) % kSlots;
+          ok = mbar_wait_bounded(&T->kv_full[slot], (2 * g / kSlots) & 1, abort_v, kLimitNs) &&
+               mbar_wait_bounded(&T->p_empty[sb], ((g >> 1) & 1) ^ 1, abort_v, kLimitNs);
+          if (!ok) break;
+          const uint64_t kd = k_desc + slot * (kTileBytes >> 4);
+          tc_fence_after_sync();
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const int off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+            tc_mma_bf16(tmem + sb * kBK, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
+          }
+          tc_commit(&T->s_full[sb]);
+          tc_commit(&T->kv_empty[slot]);
+        }
+        tc_commit(&T->q_empty[qb]);
+      }
+      if (!ok) give_up();
+      tc_commit(&T->done);
+      volatile int never = 0;
+      (void)mbar_wait_bounded(&T->done, 0, &never, kLimitNs);
+    } else if (warp == 2 && lane == 0) {
+      // ---------------- PV issuer ----------------
+      constexpr uint32_t idO = idesc_f16(128, D) | (1u << 16);   // B MN-major
+      int g = 0;
+      const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), kHalfBytes, 1024);
+      bool ok = true;
+      volatile int* blocks = &T->blocks;
+      Piece it;
+      for (int k = 0; ok; ++k) {
+        if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
+        for (int b = it.b0; b < it.b1; ++b, ++g) {
+          const int sb = g & 1, slot = (2 * g + 1) % kSlots;
+          ok = mbar_wait_bounded(&T->kv_full[slot], ((2 * g + 1) / kSlots) & 1, abort_v,
+                                 kLimitNs) &&
+               mbar_wait_bounded(&T->p_full[sb], (g >> 1) & 1, abort_v, kLimitNs) &&
+               (b > it.b0 ||                       // the last piece's O has been read
+                mbar_wait_bounded(&T->o_empty, (k & 1) ^ 1, abort_v, kLimitNs));
+          if (!ok) break;
+          const uint64_t vd = v_desc + slot * (kTileBytes >> 4);
+          tc_fence_after_sync();
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk) {
+            const int h = kk >> 2;
+            tc_mma_tmem_a(tmem + kOCol + h * D, tmem + sb * kBK + h * 64 + (kk & 3) * 8,
+                          vd + ((16 * kk * 128) >> 4), idO,
+                          (b > it.b0 || (kk & 3) > 0) ? 1u : 0u);
+          }
+          tc_commit(&T->p_empty[sb]);
+          if (b + 1 == it.b1) tc_commit(&T->o_full);
+          *blocks = g + 1;
+          tc_commit(&T->kv_empty[slot]);
+        }
+      }
+      if (!ok) give_up();
+      tc_commit(&T->done);
+      volatile int never = 0;
+      (void)mbar_wait_bounded(&T->done, 0, &never, kLimitNs);
+    } else if (warp == 0) {
+      // ---------------- planner ----------------
+      int k = 0;
+      auto post = [&](const Piece& it) -> bool {   // lane 0 writes the k-th piece
+        const int s = k % kItemRing;
+        if (!wwait_long(&T->item_empty[s], ((k / kItemRing) & 1) ^ 1)) return false;
+        if (lane == 0) {
+          T->bad_n[s] = 0;
+          T->bad_first[s] = PCTREE_ATTN_MAX_N;
+          T->item[s] = it;
+          mbar_arrive(&T->item_full[s]);
+        }
+        __syncwarp();
+        ++k;
+        return true;
+      };
+      PieceJoin join;
+      bool ok = plan_pieces(a.units, T->upto, join, post);
+      if (lane == 0) a.join[blockIdx.x] = join;
+      if (ok) {
+        Piece end = {};
+        ok = post(end);
+      }
+      if (!ok && lane == 0) give_up();
+    }
+  } else if (warp < 8) {
+    // ---------------- Q in, O out: one thread per tile row ----------------
+    set_registers_down<72>();
+    const int quad = warp & 3;
+    const int t = quad * 32 + lane;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    uint8_t* stg = T->stage[quad];
+    // the rows this lane stores (16 i + lane / 2 of the warp's 32, half lane % 2 of
+    // 16 dims): their places in the tile
+    int out_nl[2], out_off[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int ti = quad * 32 + 16 * i + (lane >> 1), ni = ti / a.G;
+      out_nl[i] = ti < R ? ni : 0x7fffffff;
+      out_off[i] = (ni * a.Hq + ti - ni * a.G) * D + (lane & 1) * 8;
+    }
+    const int nl = t / a.G;
+    // a barrier of these four warps that gives up as other waits do
+    int syncs = 0;
+    auto together = [&]() -> bool {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&T->out_sync);
+      return wwait(&T->out_sync, syncs++ & 1);
+    };
+    // the q-th piece's tile into buffer q & 1; false: given up
+    auto bring_q = [&](int q, const Piece& it) -> bool {
+      const int qb = q & 1;
+      if (!wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1)) return false;
+      uint8_t* tile = sq + qb * kTileBytes;
+      constexpr int kLanes = D / 8;                // lanes of a row
+      constexpr int kRows = 128 / kLanes;          // rows at a time
+      const int c = t % kLanes;
+      constexpr int kDeep = 8;
+#pragma unroll 1
+      for (int r0 = t / kLanes; r0 - t / kLanes < R; r0 += kDeep * kRows) {
+        uint4 x[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+          const int row = r0 + u * kRows, n = row / a.G;
+          x[u] = make_uint4(0, 0, 0, 0);
+          if (row < R && n < it.n_rows)
+            x[u] = *reinterpret_cast<const uint4*>(
+                a.q + (it.row0 + n) * a.q_stride + (it.kvh * a.G + row - n * a.G) * D + c * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+          const int row = r0 + u * kRows;
+          uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+          float sc = a.scale_log2;
+          if constexpr (!F16) {
+            float2 f[4];
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f[i] = unpack16<false>(w[i]);
+              top = fmaxf(top, fmaxf(fabsf(f[i].x), fabsf(f[i].y)));
+            }
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1)
+              top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+            // (a row with an infinity is NaN in the end, whatever its others are)
+            const int e =
+                max(-100, min(126, static_cast<int>(__float_as_uint(top) >> 23) - 127)) - 14;
+            const float by = exp2_of(-e);
+            sc *= exp2_of(e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack16<true>(f[i].x * by, f[i].y * by);
+          }
+          if (row < R) {
+            *reinterpret_cast<uint4*>(tile + (c >> 3) * kHalfBytes + row * 128 +
+                                      (((c & 7) ^ (row & 7)) * 16)) =
+                make_uint4(w[0], w[1], w[2], w[3]);
+            if (c == 0) T->row_scale[qb][row] = sc;
+          }
+        }
+      }
+      if (a.parent != nullptr) {
+        // ancestors of the tile's rows, from the parents of the request's first rows
+        const int n = it.j0 + it.n_rows;
+        const int32_t* parent = a.parent + it.row0 - it.j0;
+        if (!together()) return false;
+        for (int i = t; i < n; i += 128) {
+          int p = parent[i];
+          if (p < -1 || p >= i) {                  // parents precede children
+            report(a.status, PCTREE_ERR_INVALID_ARG);
+            p = -1;
+          }
+          T->par[i] = static_cast<int16_t>(p);
+        }
+        if (!together()) return false;
+        if (t < it.n_rows) {
+          uint32_t* path = T->path[qb][t];
+          for (int i = 0; i < PCTREE_ATTN_MAX_N / 32; ++i) path[i] = 0;
+          for (int m = it.j0 + t; m >= 0; m = T->par[m]) path[m >> 5] |= 1u << (m & 31);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&T->q_full[qb]);
+      return true;
+    };
+    bool ok = true, more = true;
+    Piece it, next;
+    int q = 0;                                     // tiles brought
+    for (; ok && more && q < 2; ++q) {
+      if (!(ok = peek_warp(q, next))) break;
+      more = next.nblk != 0;
+      if (!more) break;
+      ok = bring_q(q, next);
+    }
+    for (int k = 0; ok; ++k) {
+      if (!(ok = peek_warp(k, it)) || it.nblk == 0) break;
+      if (!(ok = wwait_long(&T->o_full, k & 1))) break;
+      tc_fence_after_sync();
+      uint16_t* oitem = a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G) * D;
+      const bool whole = it.b0 == 0 && it.b1 == it.nblk;
+      const int ring = k % kItemRing, n_bad = T->bad_n[ring];
+      const size_t part = static_cast<size_t>(blockIdx.x) * 2 + (it.b0 == 0 ? 1 : 0);
+      // the halves' sums and O relative to the larger of their references
+      const float l0 = T->row_l[0][t], l1 = T->row_l[1][t];
+      const float m0 = l0 != 0.0f ? T->row_m[0][t] : -INFINITY;
+      const float m1 = l1 != 0.0f ? T->row_m[1][t] : -INFINITY;
+      const float m = fmaxf(m0, m1);
+      float f0 = l0 != 0.0f ? exp2f(m0 - m) : 0.0f;
+      float f1 = l1 != 0.0f ? exp2f(m1 - m) : 0.0f;
+      const float l = l0 * f0 + l1 * f1;
+      const uint32_t o_col = lane_base + kOCol;
+      if (whole) {                                 // (no finite score, l = 0: NaN)
+        const float inv = 1.0f / l;
+        f0 *= inv;
+        f1 *= inv;
+      }
+      const bool in_tile = nl < it.n_rows && t < R;
+      if (!whole && in_tile)
+        a.part_ml[part * 128 + t] = make_float2(l != 0.0f ? m : -INFINITY, l);
+#pragma unroll 1
+      for (int c = 0; c < D / 16; ++c) {
+        float y[16];
+        {
+          uint32_t y0[16], y1[16];
+          tmem_ld_32x32b_x16(o_col + c * 16, y0);
+          tmem_ld_32x32b_x16(o_col + D + c * 16, y1);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const uint64_t a0 = pack2(__uint_as_float(y0[i]), __uint_as_float(y0[i + 1]));
+            const uint64_t a1 = pack2(__uint_as_float(y1[i]), __uint_as_float(y1[i + 1]));
+            unpack2(fma2(a0, pack2(f0, f0), mul2(a1, pack2(f1, f1))), y[i], y[i + 1]);
+          }
+        }
+        if (n_bad != 0) {
+          // NaN values that were taken out of V reach the rows that see their keys
+          auto sees = [&](int key) {
+            return a.parent == nullptr
+                       ? key < nl
+                       : nl < 128 && ((T->path[k & 1][nl][key >> 5] >> (key & 31)) & 1) != 0;
+          };
+          uint32_t nan = 0;
+          for (int i = 0; i < min(n_bad, kMaxBad); ++i) {
+            const uint32_t e = T->bad[ring][i];
+            if (static_cast<int>((e >> 16) & 15) == c && sees(e >> 20)) nan |= e & 0xffffu;
+          }
+          if (n_bad > kMaxBad && sees(T->bad_first[ring])) nan = 0xffffu;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if ((nan >> i) & 1u) y[i] = __int_as_float(0x7fc00000);
+          __syncwarp();
+        }
+        if (c == D / 16 - 1) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&T->o_empty);
+        }
+        if (!whole) {
+          float4* po = reinterpret_cast<float4*>(a.part_o) + part * (D / 4) * 128 + c * 4 * 128 + t;
+          if (in_tile) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              po[i * 128] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int h = 0; h < 4; ++h) w[h] = pack16<F16>(y[i * 8 + 2 * h], y[i * 8 + 2 * h + 1]);
+          *reinterpret_cast<uint4*>(stg + lane * 32 + ((i ^ (lane >> 2)) & 1) * 16) =
+              make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = 16 * i + (lane >> 1);
+          const uint4 v = *reinterpret_cast<const uint4*>(
+              stg + row * 32 + (((lane & 1) ^ (row >> 2)) & 1) * 16);
+          if (out_nl[i] < it.n_rows) *reinterpret_cast<uint4*>(oitem + out_off[i] + c * 16) = v;
+        }
+        __syncwarp();
+      }
+      // (a piece's ancestors are read up to here: its Q buffer is refilled after)
+      if (!(ok = together())) break;
+      release_warp(k);
+      if (more) {
+        if (!(ok = peek_warp(q, next))) break;
+        more = next.nblk != 0;
+        if (more) ok = bring_q(q++, next);
+      }
+    }
+    if (!ok && lane == 0) give_up();
+  } else if (warp < 16) {
+    // ---------------- softmax, two threads per tile row ----------------
+    set_registers_up<112>();
+    const int half = (warp - 8) >> 2;
+    const int quad = warp & 3;
+    const int t = quad * 32 + lane;
+    const int nl = t / a.G;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const uint32_t o_col = lane_base + kOCol + half * D;
+    int g = 0;
+    bool ok = true;
+    Piece it;
+    for (int k = 0; ok; ++k) {
+      if (!(ok = peek_warp(k, it))) break;
+      release_warp(k);
+      if (it.nblk == 0) break;
+      if (!(ok = wwait(&T->q_full[k & 1], (k >> 1) & 1))) break;
+      const float sc = t < R ? T->row_scale[k & 1][t] : a.scale_log2;
+      // keys this row sees: slots below `end`, and of those from the prefix on (in
+      // a tree) its ancestors
+      const int end = min(it.key_end, it.prefix + it.j0 + nl + 1);
+      float m_used = -INFINITY, l_sum = 0.0f;
+      float over = -INFINITY;                      // a maximum above it needs a look
+      for (int b = it.b0; b < it.b1; ++b, ++g) {
+        const int sb = g & 1;
+        const int key0 = b * kBK + half * 64;
+        // this half's keys that the row sees
+        const int seen = end - key0;
+        uint64_t see = seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1;
+        if (a.parent != nullptr && key0 + 64 > it.prefix && see != 0) {
+          const int node = key0 - it.prefix;       // > -64: the first key's place in the tree
+          const uint32_t* path = T->path[k & 1][min(nl, 127)];
+          auto word = [&](int i) -> uint64_t {
+            return i >= 0 && i < PCTREE_ATTN_MAX_N / 32 ? path[i] : 0u;
+          };
+          const int w0 = node >> 5, sh = node & 31;
+          const uint64_t lo = word(w0) | word(w0 + 1) << 32, hi = word(w0 + 2);
+          uint64_t anc = sh == 0 ? lo : lo >> sh | hi << (64 - sh);
+          if (node < 0) anc |= (1ull << -node) - 1;   // slots of the prefix
+          see &= anc;
+        }
+        if (!(ok = wwait(&T->s_full[sb], (g >> 1) & 1))) break;
+        tc_fence_after_sync();
+        const uint32_t s_col = lane_base + sb * kBK + half * 64;
+        float x[64];
+        {
+          uint32_t* xu = reinterpret_cast<uint32_t*>(x);
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            tmem_ld_32x32b_x32(s_col + c * 32,
+                               *reinterpret_cast<uint32_t(*)[32]>(xu + c * 32));
+          tmem_ld_wait();
+        }
+        // keys the row may not see become -inf
+        if (__any_sync(kFull, see != ~0ull)) {
+          const uint32_t s0 = static_cast<uint32_t>(see), s1 = static_cast<uint32_t>(see >> 32);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            x[i] = (s0 >> i) & 1u ? x[i] : -INFINITY;
+            x[32 + i] = (s1 >> i) & 1u ? x[32 + i] : -INFINITY;
+          }
+        }
+        float m8[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) m8[u] = x[u];
+#pragma unroll
+        for (int k2 = 8; k2 < 64; ++k2) m8[k2 & 7] = fmaxf(m8[k2 & 7], x[k2]);
+        const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
+                         fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * sc;
+        bool shifted = false;
+        if (__any_sync(kFull, mx > over)) {
+          const bool mine = mx > m_used + 8.0f;
+          const float alpha = mine ? ex2_approx(m_used - mx) : 1.0f;
+          if (b > it.b0) {
+            if (!(ok = wwait(&T->p_empty[(g - 1) & 1], ((g - 1) >> 1) & 1))) break;
+            tc_fence_after_sync();
+#pragma unroll 2
+            for (int c = 0; c < D / 8; ++c) {
+              uint32_t y[8];
+              tmem_ld_32x32b_x8(o_col + c * 8, y);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k2 = 0; k2 < 8; ++k2)
+                y[k2] = __float_as_uint(__uint_as_float(y[k2]) * alpha);
+              tmem_st_x8(o_col + c * 8, y);
+            }
+            tmem_st_wait();
+          }
+          if (mine) {
+            l_sum *= alpha;
+            m_used = mx;
+          }
+          const bool wide = fabsf(m_used) > kWideScore && m_used > -INFINITY;
+          over = wide ? -INFINITY : m_used + 8.0f;
+          shifted = __any_sync(kFull, wide);
+          if (shifted) {
+            wide_scores(s_col, sc, m_used == -INFINITY ? 0.0f : m_used, see);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              tmem_ld_32x32b_x32(s_col + c * 32,
+                                 *reinterpret_cast<uint32_t(*)[32]>(
+                                     reinterpret_cast<uint32_t*>(x) + c * 32));
+            tmem_ld_wait();
+          }
+        }
+        const float mref = (shifted || m_used == -INFINITY ? 0.0f : m_used) - kPBits;
+        const uint64_t sc2 = pack2(sc, sc), nm2 = pack2(-mref, -mref);
+        uint64_t ls[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int h = 0; h < 16; ++h) {
+            float e0, e1;
+            unpack2(fma2(pack2(x[c * 32 + 2 * h], x[c * 32 + 2 * h + 1]), sc2, nm2), e0, e1);
+            const float p0 = ex2_approx(e0), p1 = ex2_approx(e1);
+            ls[h & 3] = add2(ls[h & 3], pack2(p0, p1));
+            pk[h] = pack16<true>(p0, p1);
+          }
+          tmem_st_x16(s_col + c * 16, pk);
+        }
+        tmem_st_wait();
+        {
+          float s0, s1;
+          unpack2(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), s0, s1);
+          l_sum += s0 + s1;
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&T->p_full[sb]);
+      }
+      if (!ok) break;
+      if (!(ok = wwait(&T->o_empty, (k & 1) ^ 1))) break;
+      T->row_l[half][t] = l_sum;
+      T->row_m[half][t] = m_used;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&T->o_full);
+    }
+    if (!ok && lane == 0) give_up();
+  } else {
+    // ---------------- K or V: codes to float16 ----------------
+    set_registers_down<64>();
+    const int is_v = (warp - 16) >> 2, wq = warp & 3;
+    const uint8_t* cache = a.cache[is_v];
+    const uint8_t* scale = a.scale[is_v];
+    constexpr int kRows = 128 / (D / 16) ;         // rows the four warps bring at a time
+    constexpr int kU = kBK / kRows;                // rows a thread brings of a block
+    // 16 bytes of a row a lane; eight neighbouring lanes have four groups of one
+    // half of two neighbouring rows, whose 16-byte places in the swizzled tile are
+    // all different
+    const int c4 = lane & 3;                       // group of 16 dims in its half
+    const int half = kHalves == 2 ? (lane >> 3) & 1 : 0;
+    const int row_in = wq * (kRows / 4) + ((lane >> 2) & 1) +
+                       2 * (kHalves == 2 ? lane >> 4 : lane >> 3);
+    const int dim0 = half * 64 + c4 * 16;
+    const int p_size = a.units.rows.page_size;
+    uint8_t* ring = skv + is_v * kTileBytes + half * kHalfBytes;
+    uint4 raw[kU];                                 // codes of the next block
+    int sc[kU];                                    // their scales' bytes
+    int page[kU];                                  // pages of the block after it
+    Piece it;
+    int k = 0, b = 0, left = 0;                    // pieces fetched; block, blocks left of it
+    bool ok = true;
+    auto next_block = [&](Block& x) {              // no keys: no more
+      x = Block{};
+      if (left == 0) {
+        if (k < 0 || !ok) return;
+        if (!(ok = peek_warp(k, it))) return;
+        release_warp(k);
+        if (it.nblk == 0) {
+          k = -1;
+          return;
+        }
+        ++k;
+        b = it.b0;
+        left = it.b1 - it.b0;
+      }
+      x.r = it.r;
+      x.kvh = it.kvh;
+      x.key0 = b * kBK;
+      x.key_end = it.key_end;
+      x.all = a.parent != nullptr ? it.prefix : it.prefix + it.j0 + 1;
+      x.ring = (k - 1) % kItemRing;
+      ++b;
+      --left;
+    };
+    auto find_page = [&](const Block& x, int u) {
+      const int key = x.key0 + u * kRows + row_in;
+      page[u] = key < x.key_end ? kv_page(a.units.rows, x.r, div_by(key, a.blocks.page)) : -2;
+    };
+    auto load = [&](const Block& x, int u) {
+      raw[u] = make_uint4(0, 0, 0, 0);
+      sc[u] = kExpBias;
+      if (page[u] >= 0) {
+        const int key = x.key0 + u * kRows + row_in;
+        const int off = key - div_by(key, a.blocks.page) * p_size;
+        const long long slot = static_cast<long long>(page[u]) * p_size + off;
+        const long long at =
+            static_cast<long long>(page[u]) * a.blocks.per_page + (off >> a.blocks.shift);
+        raw[u] = load16(cache + (slot * a.units.Hkv + x.kvh) * D + dim0);
+        sc[u] = __ldg(scale + at * a.units.Hkv + x.kvh);
+      } else if (page[u] == -1) {
+        report(a.status, PCTREE_ERR_INVALID_ARG);
+      }
+    };
+    Block cur, nxt, then;
+    next_block(cur);
+    next_block(nxt);
+    if (cur.key_end > 0) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) find_page(cur, u);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) load(cur, u);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) find_page(nxt, u);
+    }
+    for (int g = 0; ok && cur.key_end > 0; ++g) {
+      next_block(then);
+      if (!ok) break;
+      const int place = 2 * g + is_v, slot = place % kSlots;
+      if (!(ok = wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1))) break;
+      uint8_t* tile = ring + (slot - is_v) * kTileBytes;
+      const bool some = is_v != 0 && cur.key0 + kBK > cur.all;   // keys that not all rows see
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int row = u * kRows + row_in;
+        uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+        if (some && cur.key0 + row >= cur.all) {
+          uint32_t bits = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t nan = nan_bytes(w[i]);
+            w[i] &= ~nan;
+            bits |= (((nan & 0x08040201u) * 0x01010101u) >> 24 & 15u) << (4 * i);
+          }
+          if (bits != 0) {
+            const int key = cur.key0 + row - cur.all;
+            atomicMin(&T->bad_first[cur.ring], key);
+            const int n = atomicAdd(&T->bad_n[cur.ring], 1);
+            if (n < kMaxBad)
+              T->bad[cur.ring][n] = bits | static_cast<uint32_t>(dim0 / 16) << 16 |
+                                    static_cast<uint32_t>(key) << 20;
+          }
+        }
+        if (!scale_ok(sc[u])) report(a.status, PCTREE_ERR_INVALID_ARG);
+        const uint32_t by = half2_exp(scale_exp(sc[u]));
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[2 * i] = mul_h2(halves2(w[i]), by);
+          h[2 * i + 1] = mul_h2(halves2(w[i] >> 16), by);
+        }
+        load(nxt, u);
+        uint8_t* dst = tile + row * 128;
+        *reinterpret_cast<uint4*>(dst + (((2 * c4) ^ (row & 7)) * 16)) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(dst + (((2 * c4 + 1) ^ (row & 7)) * 16)) =
+            make_uint4(h[4], h[5], h[6], h[7]);
+        find_page(then, u);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&T->kv_full[slot]);
+      cur = nxt;
+      nxt = then;
+    }
+    if (!ok && lane == 0) give_up();
+  }
+  // ---------------- teardown ----------------
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (warp == 1) tmem_dealloc(tmem, kTmemCols);
+}
+
+// Rows per tile: one where requests have one row each, on average (a tile's
+// rows are multiplied whether or not they are the request's), else as many as fit.
+int rows_per_tile(const pctree_kv8_attn_config& c) {
+  const int fit = 128 / (c.Hq / c.Hkv);
+  return c.total_rows <= c.batch ? 1 : fit < c.total_rows ? fit : c.total_rows;
+}
+
+// Whether the planner can count the most work a configuration can have in 32
+// bits.
+bool work_ok(const pctree_kv8_attn_config& c) {
+  const long long units = c.total_rows / rows_per_tile(c) + 1ll + c.batch;
+  const long long blocks =
+      (static_cast<long long>(c.max_pages) * c.page_size + kBK - 1) / kBK + kUnitCharge;
+  return units * blocks < (1ll << 32) / c.Hkv - 1024;
+}
+
+pctree_status attn8_check(const pctree_kv8_attn_config* c) {
+  if (c == nullptr) return PCTREE_ERR_INVALID_ARG;
+  if (c->Hq < 1 || c->D < 1 || !(c->scale > 0.0f) || !(c->scale < 1e30f))
+    return PCTREE_ERR_INVALID_ARG;
+  const pctree_status st = kv_check(c->batch, c->total_rows, c->Hkv, c->page_size, c->n_pages,
+                                    c->max_pages, c->dtype);
+  if (st != PCTREE_OK) return st;
+  if (!kv8_block_ok(c->scale_block) || c->Hq % c->Hkv != 0 || c->q_stride % 8 != 0 ||
+      c->q_stride < static_cast<int64_t>(c->Hq) * c->D)
+    return PCTREE_ERR_INVALID_ARG;
+  if ((c->D != 64 && c->D != 128) || c->Hq / c->Hkv > 128 || c->q_stride > (1ll << 38) ||
+      !work_ok(*c))
+    return PCTREE_ERR_UNSUPPORTED;
+  return PCTREE_OK;
+}
+
+template <int D, bool F16>
+pctree_status attn8_launch(const Kv8AttnArgs& a, int num_sms, cudaStream_t stream) {
+  constexpr size_t smem =
+      (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;
+  static_assert(smem <= 227 * 1024, "shared memory per CTA");
+  static SmemLimit limit;
+  const void* fn = reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>);
+  if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc = {};
+  const unsigned ctas = static_cast<unsigned>(num_sms < kMaxCtas ? num_sms : kMaxCtas);
+  lc.gridDim = dim3(ctas);
+  lc.blockDim = dim3(kThreads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = stream;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  if (cudaLaunchKernelEx(&lc, kv8_attn_kernel<D, F16>, a) != cudaSuccess) return PCTREE_ERR_CUDA;
+  const JoinArgs j = {a.part_o, a.part_ml, a.join, a.out, a.G, a.Hq};
+  lc.gridDim = dim3(ctas, kJoinCtas);
+  lc.blockDim = dim3(kJoinThreads);
+  lc.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&lc, join_pieces_kernel<D, F16>, j) == cudaSuccess ? PCTREE_OK
+                                                                              : PCTREE_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace pct
+
+extern "C" {
+
+size_t pctree_kv8_attention_workspace_bytes(const pctree_kv8_attn_config* cfg) {
+  if (pct::attn8_check(cfg) != PCTREE_OK) return 0;
+  return pct::piece_ws(cfg->D).total;
+}
+
+pctree_status pctree_kv8_attention(const pctree_kv8_attn_config* cfg, const void* q,
+                                   const void* k_cache, const void* v_cache, const void* k_scale,
+                                   const void* v_scale, const int32_t* row_start,
+                                   const int32_t* n_rows, const int32_t* prefix_len,
+                                   const int32_t* page_table, const int32_t* parent, void* out,
+                                   void* workspace, size_t workspace_bytes, int32_t* status,
+                                   void* stream_ptr) {
+  using namespace pct;
+  NvtxRange range("pctree_kv8_attention");
+  pctree_status st = attn8_check(cfg);
+  if (st != PCTREE_OK) return st;
+  const pctree_kv8_attn_config& c = *cfg;
+  if (q == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr ||
+      v_scale == nullptr || row_start == nullptr || n_rows == nullptr || prefix_len == nullptr ||
+      out == nullptr || !kv_al16(q) || !kv_al16(k_cache) || !kv_al16(v_cache) || !kv_al16(out) ||
+      !kv_table_ok(page_table, c.batch, c.n_pages, c.max_pages))
+    return PCTREE_ERR_INVALID_ARG;
+  {
+    const char* q0 = static_cast<const char*>(q);
+    const char* q1 = q0 + ((c.total_rows - 1) * static_cast<size_t>(c.q_stride) +
+                           static_cast<size_t>(c.Hq) * c.D) * 2;
+    const char* o0 = static_cast<const char*>(out);
+    const char* o1 = o0 + static_cast<size_t>(c.total_rows) * c.Hq * c.D * 2;
+    if (q0 < o1 && o0 < q1) return PCTREE_ERR_INVALID_ARG;   // overlap
+  }
+  const PieceWs w = piece_ws(c.D);
+  if (workspace == nullptr || workspace_bytes < w.total ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+    return PCTREE_ERR_WORKSPACE;
+  int num_sms = 0;
+  st = device_facts(&num_sms);
+  if (st != PCTREE_OK) return st;
+  Kv8AttnArgs a{};
+  a.units = {{row_start, n_rows, prefix_len, page_table, c.batch, c.total_rows, c.page_size,
+              c.n_pages, c.max_pages},
+             c.Hkv, rows_per_tile(c), parent != nullptr ? PCTREE_ATTN_MAX_N : 1 << 30, kBK};
+  a.blocks = kv8_blocks(c.page_size, c.scale_block);
+  a.q = static_cast<const uint16_t*>(q);
+  a.cache[0] = static_cast<const uint8_t*>(k_cache);
+  a.cache[1] = static_cast<const uint8_t*>(v_cache);
+  a.scale[0] = static_cast<const uint8_t*>(k_scale);
+  a.scale[1] = static_cast<const uint8_t*>(v_scale);
+  a.parent = parent;
+  a.out = static_cast<uint16_t*>(out);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.part_o = reinterpret_cast<float*>(ws + w.part_o);
+  a.part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
+  a.join = reinterpret_cast<PieceJoin*>(ws + w.join);
+  a.status = status;
+  a.q_stride = c.q_stride;
+  a.Hq = c.Hq;
+  a.G = c.Hq / c.Hkv;
+  a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+  const bool f16 = c.dtype == PCTREE_F16;
+  if (c.D == 64)
+    return f16 ? attn8_launch<64, true>(a, num_sms, stream)
+               : attn8_launch<64, false>(a, num_sms, stream);
+  return f16 ? attn8_launch<128, true>(a, num_sms, stream)
+             : attn8_launch<128, false>(a, num_sms, stream);
+}
+
+}  // extern "C"

@@ -83,6 +83,32 @@ class PagedAttnConfig(ctypes.Structure):
         ("q_stride", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
+class Kv8AppendConfig(ctypes.Structure):
+    """pctree_kv8_append_config: rows of several requests and their cache in 8 bits."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "total_rows", "Hq", "Hkv", "D", "page_size", "n_pages",
+        "max_pages", "scale_block", "dtype", "rotary_dim", "interleaved")] + [
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64), ("eps", ctypes.c_float),
+        ("rope_scale", ctypes.c_float)]
+
+
+class Kv8AttnConfig(ctypes.Structure):
+    """pctree_kv8_attn_config: one attention layer over a cache in 8 bits."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "total_rows", "Hq", "Hkv", "D", "page_size", "n_pages",
+        "max_pages", "scale_block", "dtype")] + [
+        ("q_stride", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class Kv8CompactConfig(ctypes.Structure):
+    """pctree_kv8_compact_config: all layers of a cache in 8 bits."""
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "batch", "B", "N", "layers", "Hkv", "D", "page_size", "n_pages",
+        "max_pages", "scale_block")] + [
+        ("cache_layer_stride", ctypes.c_int64), ("scale_layer_stride", ctypes.c_int64)]
+
+
 class SampleConfig(ctypes.Structure):
     """pctree_sample_config: rows of logits."""
     _fields_ = [("rows", ctypes.c_int32), ("V", ctypes.c_int32),
@@ -139,6 +165,15 @@ def _load() -> ctypes.CDLL:
     lib.pctree_paged_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.pctree_paged_attention.argtypes = [pp] + [vp] * 9 + [ctypes.c_size_t, vp, vp]
     lib.pctree_paged_attention.restype = ctypes.c_int
+    lib.pctree_kv8_append.argtypes = [ctypes.POINTER(Kv8AppendConfig)] + [vp] * 18
+    lib.pctree_kv8_append.restype = ctypes.c_int
+    p8 = ctypes.POINTER(Kv8AttnConfig)
+    lib.pctree_kv8_attention_workspace_bytes.argtypes = [p8]
+    lib.pctree_kv8_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.pctree_kv8_attention.argtypes = [p8] + [vp] * 12 + [ctypes.c_size_t, vp, vp]
+    lib.pctree_kv8_attention.restype = ctypes.c_int
+    lib.pctree_kv8_compact.argtypes = [ctypes.POINTER(Kv8CompactConfig)] + [vp] * 10
+    lib.pctree_kv8_compact.restype = ctypes.c_int
     lib.pctree_sample.argtypes = [ctypes.POINTER(SampleConfig)] + [vp] * 10
     lib.pctree_sample.restype = ctypes.c_int
     lib.pctree_status_string.argtypes = [ctypes.c_int32]
@@ -714,6 +749,242 @@ def pctree_paged_attention(cfg: PagedAttnConfig, q: torch.Tensor, k_cache: torch
         _device_stream(stream, dev))
     if rc != PCTREE_OK:
         raise PctreeError(rc, "pctree_paged_attention")
+
+
+# The cache in 8 bits: codes are torch.float8_e4m3fn or torch.uint8 tensors,
+# scales torch.float8_e8m0fnu or torch.uint8 (the same bytes).
+_CODE_TYPES = (torch.float8_e4m3fn, torch.uint8)
+_SCALE_TYPES = (torch.float8_e8m0fnu, torch.uint8)
+
+
+def _layers(t: torch.Tensor, layers: int, each: int) -> bool:
+    """Whether `layers` caches of `each` elements lie one behind the other."""
+    n = t.numel()
+    return layers == 1 or n == layers * each or (t.dim() > 1 and t.shape[0] >= layers
+                                                 and n == t.shape[0] * each)
+
+
+def _codes(t: torch.Tensor, cfg, device: int, layers: int = 1) -> bool:
+    """A cache (or `layers` of them, one behind the other) of codes there."""
+    slot = cfg.Hkv * cfg.D
+    page = cfg.page_size * slot
+    return (t.dtype in _CODE_TYPES and _layers(t, layers, cfg.n_pages * page)
+            and _cache(t, t.dtype, cfg.n_pages * layers, page, slot, cfg.D, device))
+
+
+def _scale_page(cfg) -> int:
+    return -(-cfg.page_size // cfg.scale_block) * cfg.Hkv if cfg.scale_block > 0 else 0
+
+
+def _scales(t: torch.Tensor, cfg, device: int, layers: int = 1) -> bool:
+    """The scales of a cache (or of `layers` caches) there: as many as there are,
+    or more in whole pages."""
+    page = _scale_page(cfg)
+    n = cfg.n_pages * layers * page
+    return (t.dtype in _SCALE_TYPES and t.get_device() == device and t.is_contiguous()
+            and _layers(t, layers, cfg.n_pages * page)
+            and (t.numel() == n or (t.numel() > n and _whole(t.shape, page))))
+
+
+def _codes_check(name, t, cfg, device, layers=1):
+    lead = f"[{layers}]" if layers > 1 else ""
+    return (name, _codes(t, cfg, device, layers),
+            f"a contiguous torch.float8_e4m3fn or torch.uint8 tensor {lead}[{cfg.n_pages}]"
+            f"[{cfg.page_size}][{cfg.Hkv}][{cfg.D}]")
+
+
+def _scales_check(name, t, cfg, device, layers=1):
+    lead = f"[{layers}]" if layers > 1 else ""
+    return (name, _scales(t, cfg, device, layers),
+            f"a contiguous torch.float8_e8m0fnu or torch.uint8 tensor {lead}[{cfg.n_pages}]"
+            f"[ceil({cfg.page_size} / {cfg.scale_block})][{cfg.Hkv}]")
+
+
+def kv8_append_config(batch: int, total_rows: int, Hq: int, Hkv: int, D: int,
+                      page_size: int, n_pages: int, max_pages: int = 1, scale_block: int = 1,
+                      dtype: torch.dtype = torch.bfloat16, rotary_dim: Optional[int] = None,
+                      interleaved: bool = False, q_stride: Optional[int] = None,
+                      k_stride: Optional[int] = None, v_stride: Optional[int] = None,
+                      eps: float = 1e-6, rope_scale: float = 1.0) -> Kv8AppendConfig:
+    """append_config for a cache in 8 bits whose blocks of ``scale_block`` slots
+    share a scale per head."""
+    return Kv8AppendConfig(batch, total_rows, Hq, Hkv, D, page_size, n_pages, max_pages,
+                           scale_block, _DTYPES[dtype], D if rotary_dim is None else rotary_dim,
+                           1 if interleaved else 0,
+                           Hq * D if q_stride is None else q_stride,
+                           Hkv * D if k_stride is None else k_stride,
+                           Hkv * D if v_stride is None else v_stride, eps, rope_scale)
+
+
+def pctree_kv8_append(cfg: Kv8AppendConfig, q: Optional[torch.Tensor], k: torch.Tensor,
+                      v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      k_scale: torch.Tensor, v_scale: torch.Tensor,
+                      q_out: Optional[torch.Tensor], row_start: torch.Tensor,
+                      n_rows: torch.Tensor, prefix_len: torch.Tensor,
+                      page_table: Optional[torch.Tensor] = None,
+                      positions: Optional[torch.Tensor] = None,
+                      inv_freq: Optional[torch.Tensor] = None,
+                      q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None,
+                      status: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue pctree_kv_append into a cache in 8 bits (see pctree_kv8_append in
+    include/pctree.h).  Caches are float8_e4m3fn [n_pages][page_size][Hkv][D],
+    scales float8_e8m0fnu [n_pages][ceil(page_size / scale_block)][Hkv] (or
+    uint8 tensors of these shapes)."""
+    dev = _device_index()
+    dt = _TORCH_TYPE.get(cfg.dtype)
+    n, D, Hq, Hkv, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.Hkv, cfg.batch, torch.int32
+    if not ((Hq == 0 or (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
+                         and _flat(q_out, dt, n * Hq * D, dev, Hq * D)))
+            and _rows(k, dt, n, Hkv, D, cfg.k_stride, dev)
+            and _rows(v, dt, n, Hkv, D, cfg.v_stride, dev)
+            and _codes(k_cache, cfg, dev) and _codes(v_cache, cfg, dev)
+            and _scales(k_scale, cfg, dev) and _scales(v_scale, cfg, dev)
+            and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
+            and _flat(prefix_len, i32, batch, dev)
+            and _table(page_table, batch, cfg.max_pages, dev)
+            and _flat(positions, i32, n, dev)
+            and _flat(inv_freq, torch.float64, cfg.rotary_dim // 2, dev)
+            and _flat(q_weight, dt, D, dev) and _flat(k_weight, dt, D, dev)
+            and _flat(status, i32, 1, dev)):
+        _refuse("pctree_kv8_append", dev, [
+            *([_rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
+               _flat_check("q_out", q_out, dt, n * Hq * D, dev, Hq * D)] if Hq else []),
+            _rows_check("k", k, dt, n, Hkv, D, cfg.k_stride, dev),
+            _rows_check("v", v, dt, n, Hkv, D, cfg.v_stride, dev),
+            _codes_check("k_cache", k_cache, cfg, dev),
+            _codes_check("v_cache", v_cache, cfg, dev),
+            _scales_check("k_scale", k_scale, cfg, dev),
+            _scales_check("v_scale", v_scale, cfg, dev),
+            _flat_check("row_start", row_start, i32, batch, dev),
+            _flat_check("n_rows", n_rows, i32, batch, dev),
+            _flat_check("prefix_len", prefix_len, i32, batch, dev),
+            _table_check(page_table, batch, cfg.max_pages, dev),
+            _flat_check("positions", positions, i32, n, dev),
+            _flat_check("inv_freq", inv_freq, torch.float64, cfg.rotary_dim // 2, dev),
+            _flat_check("q_weight", q_weight, dt, D, dev),
+            _flat_check("k_weight", k_weight, dt, D, dev),
+            _flat_check("status", status, i32, 1, dev)])
+    rc = LIB.pctree_kv8_append(
+        ctypes.byref(cfg), _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_weight),
+        _ptr(k_weight), _ptr(inv_freq), _ptr(positions), row_start.data_ptr(),
+        n_rows.data_ptr(), prefix_len.data_ptr(), _ptr(page_table), k_cache.data_ptr(),
+        v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(q_out), _ptr(status),
+        _device_stream(stream, dev))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_kv8_append")
+
+
+def kv8_attn_config(batch: int, total_rows: int, Hq: int, Hkv: int, D: int,
+                    page_size: int, n_pages: int, max_pages: int = 1, scale_block: int = 1,
+                    dtype: torch.dtype = torch.bfloat16, q_stride: Optional[int] = None,
+                    scale: Optional[float] = None) -> Kv8AttnConfig:
+    """``q_stride`` defaults to dense rows, ``scale`` to 1/sqrt(D); the cache's
+    sizes are those of kv8_append_config."""
+    return Kv8AttnConfig(batch, total_rows, Hq, Hkv, D, page_size, n_pages, max_pages,
+                         scale_block, _DTYPES[dtype], Hq * D if q_stride is None else q_stride,
+                         D ** -0.5 if scale is None else scale)
+
+
+def pctree_kv8_attention_workspace_bytes(cfg: Kv8AttnConfig) -> int:
+    return LIB.pctree_kv8_attention_workspace_bytes(ctypes.byref(cfg))
+
+
+def pctree_kv8_attention(cfg: Kv8AttnConfig, q: torch.Tensor, k_cache: torch.Tensor,
+                         v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                         row_start: torch.Tensor, n_rows: torch.Tensor,
+                         prefix_len: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                         page_table: Optional[torch.Tensor] = None,
+                         parent: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue attention of new rows over a cache in 8 bits (see
+    pctree_kv8_attention in include/pctree.h): causal, or with ``parent`` (the
+    trees' [batch][N], row_start = r * N) each row's path to its root."""
+    dev = _device_index()
+    dt = _TORCH_TYPE.get(cfg.dtype)
+    n, D, Hq, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.batch, torch.int32
+    if not (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
+            and _flat(out, dt, n * Hq * D, dev, Hq * D)
+            and _codes(k_cache, cfg, dev) and _codes(v_cache, cfg, dev)
+            and _scales(k_scale, cfg, dev) and _scales(v_scale, cfg, dev)
+            and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
+            and _flat(prefix_len, i32, batch, dev)
+            and _table(page_table, batch, cfg.max_pages, dev) and _flat(parent, i32, n, dev)
+            and _flat(workspace, torch.uint8, workspace.numel(), dev)
+            and _flat(status, i32, 1, dev)):
+        _refuse("pctree_kv8_attention", dev, [
+            _rows_check("q", q, dt, n, Hq, D, cfg.q_stride, dev),
+            _flat_check("out", out, dt, n * Hq * D, dev, Hq * D),
+            _codes_check("k_cache", k_cache, cfg, dev),
+            _codes_check("v_cache", v_cache, cfg, dev),
+            _scales_check("k_scale", k_scale, cfg, dev),
+            _scales_check("v_scale", v_scale, cfg, dev),
+            _flat_check("row_start", row_start, i32, batch, dev),
+            _flat_check("n_rows", n_rows, i32, batch, dev),
+            _flat_check("prefix_len", prefix_len, i32, batch, dev),
+            _table_check(page_table, batch, cfg.max_pages, dev),
+            _flat_check("parent", parent, i32, n, dev),
+            _flat_check("workspace", workspace, torch.uint8, workspace.numel(), dev),
+            _flat_check("status", status, i32, 1, dev)])
+    rc = LIB.pctree_kv8_attention(
+        ctypes.byref(cfg), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+        k_scale.data_ptr(), v_scale.data_ptr(), row_start.data_ptr(), n_rows.data_ptr(),
+        prefix_len.data_ptr(), _ptr(page_table), _ptr(parent), out.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), _ptr(status), _device_stream(stream, dev))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_kv8_attention")
+
+
+def kv8_compact_config(batch: int, B: int, N: int, layers: int, Hkv: int, D: int,
+                       page_size: int, n_pages: int, max_pages: int = 1,
+                       scale_block: int = 1) -> Kv8CompactConfig:
+    """Caches [layers][n_pages][page_size][Hkv][D] and their scales, dense."""
+    cfg = Kv8CompactConfig(batch, B, N, layers, Hkv, D, page_size, n_pages, max_pages,
+                           scale_block, n_pages * page_size * Hkv * D, 0)
+    cfg.scale_layer_stride = n_pages * _scale_page(cfg)
+    return cfg
+
+
+def pctree_kv8_compact(cfg: Kv8CompactConfig, accepted_idx: torch.Tensor,
+                       accepted_len: torch.Tensor, prefix_len: torch.Tensor,
+                       k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                       v_scale: torch.Tensor, page_table: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Enqueue the compaction of all layers of a cache in 8 bits along the
+    accepted paths (see pctree_kv8_compact in include/pctree.h).  Caches and
+    scales are those of kv8_compact_config; layers elsewhere in one allocation
+    need the C call's strides and uint8 views of its bytes."""
+    dev = _device_index()
+    batch, i32 = cfg.batch, torch.int32
+    dense = (cfg.layers == 1
+             or (cfg.cache_layer_stride == cfg.n_pages * cfg.page_size * cfg.Hkv * cfg.D
+                 and cfg.scale_layer_stride == cfg.n_pages * _scale_page(cfg)))
+    if not (dense and _flat(accepted_idx, i32, batch * (cfg.B + 1), dev, cfg.B + 1)
+            and _flat(accepted_len, i32, batch, dev) and _flat(prefix_len, i32, batch, dev)
+            and _codes(k_cache, cfg, dev, cfg.layers) and _codes(v_cache, cfg, dev, cfg.layers)
+            and _scales(k_scale, cfg, dev, cfg.layers)
+            and _scales(v_scale, cfg, dev, cfg.layers)
+            and _table(page_table, batch, cfg.max_pages, dev) and _flat(status, i32, 1, dev)):
+        _refuse("pctree_kv8_compact", dev, [
+            ("cfg", dense, "a config of dense layers"),
+            _flat_check("accepted_idx", accepted_idx, i32, batch * (cfg.B + 1), dev, cfg.B + 1),
+            _flat_check("accepted_len", accepted_len, i32, batch, dev),
+            _flat_check("prefix_len", prefix_len, i32, batch, dev),
+            _codes_check("k_cache", k_cache, cfg, dev, cfg.layers),
+            _codes_check("v_cache", v_cache, cfg, dev, cfg.layers),
+            _scales_check("k_scale", k_scale, cfg, dev, cfg.layers),
+            _scales_check("v_scale", v_scale, cfg, dev, cfg.layers),
+            _table_check(page_table, batch, cfg.max_pages, dev),
+            _flat_check("status", status, i32, 1, dev)])
+    rc = LIB.pctree_kv8_compact(
+        ctypes.byref(cfg), accepted_idx.data_ptr(), accepted_len.data_ptr(),
+        prefix_len.data_ptr(), _ptr(page_table), k_cache.data_ptr(), v_cache.data_ptr(),
+        k_scale.data_ptr(), v_scale.data_ptr(), _ptr(status), _device_stream(stream, dev))
+    if rc != PCTREE_OK:
+        raise PctreeError(rc, "pctree_kv8_compact")
 
 
 def sample_config(rows: int, V: int, group: int = 1, dtype: torch.dtype = torch.float32,
