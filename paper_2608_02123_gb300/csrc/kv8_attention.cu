@@ -11,14 +11,16 @@
 //                 two TMEM buffers
 //   warp 2        PV issuer: O_h += P_b V_b over each half h of the block's keys
 //                 (P read from TMEM)
-//   warps 4..7    a tile's Q (two buffers) and its rows' ancestors, two pieces
-//                 ahead; the two O of a finished piece, combined, to rows of out
-//                 or the piece's partial, while the softmax goes on
+//   warp 3        where the keys of a block lie and what scales they have, up to
+//                 kPlaceRing blocks ahead
+//   warps 4..7    the next tile's Q and its rows' ancestors, once the last S of a
+//                 piece is done; then the two O of the finished piece, combined,
+//                 to rows of out or the piece's partial
 //   warps 8..15   softmax, two threads per tile row, 64 keys of a block each with
 //                 its own running maximum, sum and O
-//   warps 16..19  K, and warps 20..23 V: codes to registers a block ahead (and
-//                 page numbers two), to float16 in shared memory (128-byte
-//                 swizzle, 64 dims a half), two blocks of each
+//   warps 16..19  K, and warps 20..23 V: codes to shared memory a block ahead, 16
+//                 bytes a thread and copy, and to float16 (128-byte swizzle, 64
+//                 dims a half), two blocks of each
 // All waits are bounded (1 s; those for a whole piece 1 s without a block) and end
 // in PCTREE_ERR_TIMEOUT.
 //
@@ -40,7 +42,8 @@ constexpr int kHalfBytes = 128 * 128;        // 128 rows x 64 halves
 constexpr uint64_t kLimitNs = 1000000000ull;
 constexpr int kThreads = 768;
 constexpr int kSlots = 4;                    // K and V blocks in the ring, in turn
-constexpr int kItemRing = 4;
+constexpr int kItemRing = 8;
+constexpr int kPlaceRing = 4;
 constexpr int kMaxBad = 64;                  // groups of 16 values of V told apart
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kOCol = 2 * kBK;
@@ -60,11 +63,23 @@ struct Kv8AttnArgs {
   int32_t* status;
   long long q_stride;
   int Hq, G;
+  FastDiv by_G;
   float scale_log2;
 };
 
+// A block's keys: places (slot * Hkv + head, or kNowhere) and scales (float16, of
+// K and of V).
+constexpr uint32_t kNowhere = 0xffffffffu;
+struct Places {
+  uint32_t at[kBK];
+  uint32_t by[kBK];                          // V's in the upper half
+  int key0, all, ring;                       // keys below `all` are seen by every row
+  int keys;                                  // 0: no more blocks
+};
+
 struct Tail {
-  uint64_t q_full[2], q_empty[2];
+  uint64_t place_full[kPlaceRing], place_empty[kPlaceRing];
+  uint64_t q_full[2], q_empty;               // (full: by piece parity)
   uint64_t kv_full[kSlots], kv_empty[kSlots];
   uint64_t s_full[2], p_full[2], p_empty[2];
   uint64_t o_full, o_empty;
@@ -74,15 +89,16 @@ struct Tail {
   int abort;
   int blocks;                                // multiplied so far (see wwait_long)
   Piece item[kItemRing];
+  Places places[kPlaceRing];
   float row_l[2][128], row_m[2][128];
-  float row_scale[2][128];                   // of Q's rows, by Q buffer (log2 units)
+  float row_scale[2][128];                   // of Q's rows, by piece parity (log2 units)
   // NaN values at keys that only some rows of the piece's tile see, by place in the
   // item ring: 16 bits of a group of dims, the group << 16, the key (counted from
   // the first that not every row sees) << 20; their number and the first such key.
   int bad_n[kItemRing], bad_first[kItemRing];
   uint32_t bad[kItemRing][kMaxBad];
   int16_t par[PCTREE_ATTN_MAX_N];
-  uint32_t path[2][128][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by Q buffer
+  uint32_t path[2][128][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by piece parity
   alignas(16) uint8_t stage[4][32 * 32];
   unsigned upto[PCTREE_KV_MAX_BATCH];        // work of requests 0 .. r
 };
@@ -130,12 +146,18 @@ __host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
   return idesc_bf16_f32(M, N) & ~((1u << 7) | (1u << 10));
 }
 
-__device__ __forceinline__ uint4 load16(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
+// An asynchronous copy of 16 bytes (zeros if not wanted)
+// to shared memory, a group of its own.
+__device__ __forceinline__ void copy16_if(bool wanted, void* dst, const uint8_t* p) {
+  asm volatile(
+      "cp.async.cg.shared.global [%0], [%1], 16, %2;\n cp.async.commit_group;\n" ::"r"(
+          smem_u32(dst)),
+      "l"(p), "r"(wanted ? 16 : 0)
+      : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 // Two float16 values times a float16 pair.
@@ -145,16 +167,35 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// 2^e in both halves of a word, e in -15 .. 7.
-__device__ __forceinline__ uint32_t half2_exp(int e) {
-  const uint32_t h = e >= -14 ? static_cast<uint32_t>(e + 15) << 10 : 0x200u;
-  return h * 0x10001u;
+// 2^e as float16, e in -15 .. 7.
+__device__ __forceinline__ uint16_t half_exp(int e) {
+  return static_cast<uint16_t>(e >= -14 ? (e + 15) << 10 : 0x200);
 }
 
-// The bytes of a word that are the code NaN, as 0xff each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-  return (top >> 7) * 0xffu;
+// Whether a word holds the code NaN (a carry into the byte's top bit).
+__device__ __forceinline__ uint32_t nan_tops(uint32_t w) {
+  return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+__device__ __forceinline__ bool any_nan(const uint4& x) {
+  return (nan_tops(x.x) | nan_tops(x.y) | nan_tops(x.z) | nan_tops(x.w)) != 0;
+}
+
+// Sixteen codes of V with the NaN among them replaced by 0 and noted.
+__device__ __noinline__ uint4 without_nan(uint4 x, Tail* T, int ring, int key, int dim0) {
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t nan = (nan_tops(w[i]) >> 7) * 0xffu;      // 0xff in those bytes
+    w[i] &= ~nan;
+    bits |= (((nan & 0x08040201u) * 0x01010101u) >> 24 & 15u) << (4 * i);
+  }
+  atomicMin(&T->bad_first[ring], key);
+  const int n = atomicAdd(&T->bad_n[ring], 1);
+  if (n < kMaxBad)
+    T->bad[ring][n] =
+        bits | static_cast<uint32_t>(dim0 / 16) << 16 | static_cast<uint32_t>(key) << 20;
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Scores (in log2 units) whose floats are half an octave apart: from here on the
@@ -181,11 +222,6 @@ __device__ __noinline__ void wide_scores(uint32_t s_col, float sc, float mref, u
   tmem_st_wait();
 }
 
-// A block of a piece, for the warps that bring K or V.
-struct Block {
-  int r, kvh, key0, key_end, all, ring;      // keys below `all` are seen by every row
-};
-
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int kHalves = D / 64;
@@ -193,9 +229,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint8_t* sq = sm;                                // Q buffer of the k-th piece: k & 1
-  uint8_t* skv = sm + 2 * kTileBytes;              // ring
-  Tail* T = reinterpret_cast<Tail*>(skv + kSlots * kTileBytes);
+  uint8_t* sq = sm;
+  uint8_t* skv = sq + kTileBytes;                  // ring
+  uint8_t* codes = skv + kSlots * kTileBytes;      // [K, V][row of a thread][128 threads][16]
+  Tail* T = reinterpret_cast<Tail*>(codes + kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = a.G * a.units.npt;                 // rows of a tile
   volatile int* abort_v = &T->abort;
@@ -206,16 +243,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       mbar_init(&T->kv_full[s], 4);
       mbar_init(&T->kv_empty[s], 1);
     }
+    mbar_init(&T->q_empty, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&T->q_full[s], 4);
-      mbar_init(&T->q_empty[s], 1);
       mbar_init(&T->s_full[s], 1);
       mbar_init(&T->p_full[s], 8);
       mbar_init(&T->p_empty[s], 1);
     }
     for (int s = 0; s < kItemRing; ++s) {
       mbar_init(&T->item_full[s], 1);
-      mbar_init(&T->item_empty[s], 2 + 4 + 8 + 8);
+      mbar_init(&T->item_empty[s], 2 + 1 + 4 + 8);
+    }
+    for (int s = 0; s < kPlaceRing; ++s) {
+      mbar_init(&T->place_full[s], 1);
+      mbar_init(&T->place_empty[s], 8);
     }
     mbar_init(&T->o_full, 1 + 8);
     mbar_init(&T->o_empty, 4);
@@ -225,9 +266,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     T->blocks = 0;
     fence_barrier_init();
   }
-  // rows R..127 of the Q buffers are never written: zero them once
+  // rows R..127 of Q are never written: zero them once
   const int zq = (128 - R) * 8;
-  for (int i = threadIdx.x; i < 2 * kHalves * zq; i += kThreads) {
+  for (int i = threadIdx.x; i < kHalves * zq; i += kThreads) {
     const int h = i / zq, rem = i - h * zq;
     *reinterpret_cast<uint4*>(sq + h * kHalfBytes + (R + rem / 8) * 128 + (rem % 8) * 16) =
         make_uint4(0, 0, 0, 0);
@@ -242,8 +283,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem = T->tmem_base;
-
   auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
     return __all_sync(kFull, mbar_wait_bounded(bar, parity, abort_v, kLimitNs));
   };
@@ -282,20 +321,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
 
   if (warp < 4) {
     set_registers_down<48>();
+    const uint32_t tmem = T->tmem_base;
     if (warp == 1 && lane == 0) {
       // ---------------- S issuer ----------------
       constexpr uint32_t idS = idesc_f16(128, kBK);
-      int q = 0, g = 0;
+      int g = 0;
       const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
       const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
       bool ok = true;
       Piece it;
       for (int k = 0; ok; ++k) {
         if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
-        const int qb = q & 1;
-        if (!(ok = mbar_wait_bounded(&T->q_full[qb], (q >> 1) & 1, abort_v, kLimitNs))) break;
-        ++q;
-        const uint64_t qd = q_desc + qb * (kTileBytes >> 4);
+        if (!(ok = mbar_wait_bounded(&T->q_full[k & 1], (k >> 1) & 1, abort_v, kLimitNs))) break;
         for (int b = it.b0; b < it.b1; ++b, ++g) {
           const int sb = g & 1, slot = (2 * g) % kSlots;
           ok = mbar_wait_bounded(&T->kv_full[slot], (2 * g / kSlots) & 1, abort_v, kLimitNs) &&
@@ -306,12 +343,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const int off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-            tc_mma_bf16(tmem + sb * kBK, qd + off, kd + off, idS, kk > 0 ? 1u : 0u);
+            tc_mma_bf16(tmem + sb * kBK, q_desc + off, kd + off, idS, kk > 0 ? 1u : 0u);
           }
           tc_commit(&T->s_full[sb]);
           tc_commit(&T->kv_empty[slot]);
         }
-        tc_commit(&T->q_empty[qb]);
+        tc_commit(&T->q_empty);
       }
       if (!ok) give_up();
       tc_commit(&T->done);
@@ -378,10 +415,118 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         ok = post(end);
       }
       if (!ok && lane == 0) give_up();
+    } else if (warp == 3) {
+      // ---------------- places and scales of the keys ----------------
+      // Four keys a lane.  Page numbers are read a block ahead of their use, and a
+      // block's scales are under way while the block before it is written down.
+      constexpr int kKeys = kBK / 32;
+      const KvRows& rows = a.units.rows;
+      const int Hkv = a.units.Hkv;
+      Piece it;
+      int k = 0, b = 0, left = 0;                  // pieces fetched; block, blocks left of it
+      bool ok = true;
+      struct Block {
+        int r, kvh, key0, key_end, all, ring;
+      };
+      auto next_block = [&](Block& x) {            // no keys: no more
+        x = Block{};
+        if (left == 0) {
+          if (k < 0 || !ok) return;
+          if (!(ok = peek_warp(k, it))) return;
+          release_warp(k);
+          if (it.nblk == 0) {
+            k = -1;
+            return;
+          }
+          ++k;
+          b = it.b0;
+          left = it.b1 - it.b0;
+        }
+        x.r = it.r;
+        x.kvh = it.kvh;
+        x.key0 = b * kBK;
+        x.key_end = it.key_end;
+        x.all = a.parent != nullptr ? it.prefix : it.prefix + it.j0 + 1;
+        x.ring = (k - 1) % kItemRing;
+        ++b;
+        --left;
+      };
+      int page[kKeys];                             // of the block whose scales come next
+      auto find_pages = [&](const Block& x) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+          const int key = x.key0 + i * 32 + lane;
+          page[i] = key < x.key_end ? kv_page(rows, x.r, div_by(key, a.blocks.page)) : -2;
+        }
+      };
+      uint32_t sk[kKeys], sv[kKeys];               // scales' bytes, under way
+      Block cur;
+      next_block(cur);
+      find_pages(cur);
+      for (int g = 0; ok; ++g) {
+        // the g-th block's places (without keys: the end); then the scales of the
+        // block before it, which are there by now
+        const int st = g % kPlaceRing;
+        if (!(ok = wwait(&T->place_empty[st], ((g / kPlaceRing) & 1) ^ 1))) break;
+        uint32_t tk[kKeys], tv[kKeys];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+          uint32_t at = kNowhere;
+          tk[i] = tv[i] = kExpBias;
+          if (page[i] >= 0) {
+            const int key = cur.key0 + i * 32 + lane;
+            const int off = key - div_by(key, a.blocks.page) * rows.page_size;
+            at = (static_cast<uint32_t>(page[i]) * rows.page_size + off) * Hkv + cur.kvh;
+            const long long sc = (static_cast<long long>(page[i]) * a.blocks.per_page +
+                                  (off >> a.blocks.shift)) * Hkv + cur.kvh;
+            tk[i] = __ldg(a.scale[0] + sc);
+            tv[i] = __ldg(a.scale[1] + sc);
+          } else if (page[i] == -1) {
+            report(a.status, PCTREE_ERR_INVALID_ARG);
+          }
+          T->places[st].at[i * 32 + lane] = at;
+        }
+        const bool end = cur.key_end == 0;
+        if (lane == 0) {
+          T->places[st].key0 = cur.key0;
+          T->places[st].all = cur.all;
+          T->places[st].ring = cur.ring;
+          T->places[st].keys = end ? 0 : kBK;
+        }
+        if (!end) {
+          next_block(cur);
+          if (!ok) break;
+          find_pages(cur);
+        }
+        if (g > 0) {
+          Places& p = T->places[(g - 1) % kPlaceRing];
+          bool fine = true;
+#pragma unroll
+          for (int i = 0; i < kKeys; ++i) {
+            p.by[i * 32 + lane] = half_exp(scale_exp(sk[i])) |
+                                  static_cast<uint32_t>(half_exp(scale_exp(sv[i]))) << 16;
+            fine = fine && scale_ok(sk[i]) && scale_ok(sv[i]);
+          }
+          if (!fine) report(a.status, PCTREE_ERR_INVALID_ARG);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&T->place_full[(g - 1) % kPlaceRing]);
+        }
+        if (end) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&T->place_full[st]);
+          break;
+        }
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+          sk[i] = tk[i];
+          sv[i] = tv[i];
+        }
+      }
+      if (!ok && lane == 0) give_up();
     }
   } else if (warp < 8) {
     // ---------------- Q in, O out: one thread per tile row ----------------
-    set_registers_down<72>();
+    const uint32_t tmem = T->tmem_base;
     const int quad = warp & 3;
     const int t = quad * 32 + lane;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
@@ -403,49 +548,50 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (lane == 0) mbar_arrive(&T->out_sync);
       return wwait(&T->out_sync, syncs++ & 1);
     };
-    // the q-th piece's tile into buffer q & 1; false: given up
-    auto bring_q = [&](int q, const Piece& it) -> bool {
-      const int qb = q & 1;
-      if (!wwait(&T->q_empty[qb], ((q >> 1) & 1) ^ 1)) return false;
-      uint8_t* tile = sq + qb * kTileBytes;
+    // the k-th piece's tile; false: given up
+    auto bring_q = [&](int k, const Piece& it) -> bool {
+      const int qb = k & 1;
+      if (!wwait_long(&T->q_empty, (k & 1) ^ 1)) return false;
+      uint8_t* tile = sq;
       constexpr int kLanes = D / 8;                // lanes of a row
       constexpr int kRows = 128 / kLanes;          // rows at a time
       const int c = t % kLanes;
-      constexpr int kDeep = 8;
+      constexpr int kDeep = 4;                     // rows in flight
+      // (few instructions: they come from memory again for every piece)
 #pragma unroll 1
-      for (int r0 = t / kLanes; r0 - t / kLanes < R; r0 += kDeep * kRows) {
+      for (int r0 = t / kLanes; r0 < R + t / kLanes; r0 += kDeep * kRows) {
         uint4 x[kDeep];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
-          const int row = r0 + u * kRows, n = row / a.G;
-          x[u] = make_uint4(0, 0, 0, 0);
-          if (row < R && n < it.n_rows)
-            x[u] = *reinterpret_cast<const uint4*>(
-                a.q + (it.row0 + n) * a.q_stride + (it.kvh * a.G + row - n * a.G) * D + c * 8);
+          // rows that are not there: the last one's load, and zeros below
+          const int row = min(r0 + u * kRows, it.n_rows * a.G - 1), n = div_by(row, a.by_G);
+          x[u] = *reinterpret_cast<const uint4*>(
+              a.q + (it.row0 + n) * a.q_stride + (it.kvh * a.G + row - n * a.G) * D + c * 8);
         }
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
           const int row = r0 + u * kRows;
-          uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+          const uint32_t keep = row < it.n_rows * a.G ? ~0u : 0u;
+          uint32_t w[4] = {x[u].x & keep, x[u].y & keep, x[u].z & keep, x[u].w & keep};
           float sc = a.scale_log2;
           if constexpr (!F16) {
-            float2 f[4];
-            float top = 0.0f;
+            // (magnitudes of bfloat16 are ordered as the integers they are)
+            uint32_t top2 = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              f[i] = unpack16<false>(w[i]);
-              top = fmaxf(top, fmaxf(fabsf(f[i].x), fabsf(f[i].y)));
-            }
+            for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1)
-              top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-            // (a row with an infinity is NaN in the end, whatever its others are)
-            const int e =
-                max(-100, min(126, static_cast<int>(__float_as_uint(top) >> 23) - 127)) - 14;
+              top2 = __vmaxu2(top2, __shfl_xor_sync(kFull, top2, o));
+            const int top = static_cast<int>(max(top2 >> 16, top2 & 0xffffu) >> 7) - 127;
+            // (a row with an infinity or NaN is NaN in the end, whatever its others are)
+            const int e = max(-100, min(126, top)) - 14;
             const float by = exp2_of(-e);
             sc *= exp2_of(e);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack16<true>(f[i].x * by, f[i].y * by);
+            for (int i = 0; i < 4; ++i) {
+              const float2 f = unpack16<false>(w[i]);
+              w[i] = pack16<true>(f.x * by, f.y * by);
+            }
           }
           if (row < R) {
             *reinterpret_cast<uint4*>(tile + (c >> 3) * kHalfBytes + row * 128 +
@@ -480,17 +626,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (lane == 0) mbar_arrive(&T->q_full[qb]);
       return true;
     };
-    bool ok = true, more = true;
-    Piece it, next;
-    int q = 0;                                     // tiles brought
-    for (; ok && more && q < 2; ++q) {
-      if (!(ok = peek_warp(q, next))) break;
-      more = next.nblk != 0;
-      if (!more) break;
-      ok = bring_q(q, next);
-    }
-    for (int k = 0; ok; ++k) {
-      if (!(ok = peek_warp(k, it)) || it.nblk == 0) break;
+    Piece it;
+    bool ok = peek_warp(0, it);
+    if (ok && it.nblk != 0) ok = bring_q(0, it);
+    for (int k = 0; ok && it.nblk != 0; ++k) {
+      Piece next;
+      if (!(ok = peek_warp(k + 1, next))) break;
+      if (next.nblk != 0 && !(ok = bring_q(k + 1, next))) break;
       if (!(ok = wwait_long(&T->o_full, k & 1))) break;
       tc_fence_after_sync();
       uint16_t* oitem = a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G) * D;
@@ -579,19 +721,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         }
         __syncwarp();
       }
-      // (a piece's ancestors are read up to here: its Q buffer is refilled after)
+      // (a piece's ancestors are read up to here: they are replaced after)
       if (!(ok = together())) break;
       release_warp(k);
-      if (more) {
-        if (!(ok = peek_warp(q, next))) break;
-        more = next.nblk != 0;
-        if (more) ok = bring_q(q++, next);
-      }
+      it = next;
     }
     if (!ok && lane == 0) give_up();
   } else if (warp < 16) {
     // ---------------- softmax, two threads per tile row ----------------
-    set_registers_up<112>();
+    set_registers_up<120>();
+    const uint32_t tmem = T->tmem_base;
     const int half = (warp - 8) >> 2;
     const int quad = warp & 3;
     const int t = quad * 32 + lane;
@@ -605,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (!(ok = peek_warp(k, it))) break;
       release_warp(k);
       if (it.nblk == 0) break;
-      if (!(ok = wwait(&T->q_full[k & 1], (k >> 1) & 1))) break;
+      if (!(ok = wwait_long(&T->q_full[k & 1], (k >> 1) & 1))) break;
       const float sc = t < R ? T->row_scale[k & 1][t] : a.scale_log2;
       // keys this row sees: slots below `end`, and of those from the prefix on (in
       // a tree) its ancestors
@@ -634,46 +773,56 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         tc_fence_after_sync();
         const uint32_t s_col = lane_base + sb * kBK + half * 64;
         float x[64];
-        {
+        bool shifted = false;
+        // The scores, and once more if the reference has moved: the rescaling of O
+        // takes their registers.  (Loops, not copies of the code: instructions that
+        // run rarely come from memory.)
+#pragma unroll 1
+        for (bool again = false;; again = true) {
           uint32_t* xu = reinterpret_cast<uint32_t*>(x);
 #pragma unroll
           for (int c = 0; c < 2; ++c)
             tmem_ld_32x32b_x32(s_col + c * 32,
                                *reinterpret_cast<uint32_t(*)[32]>(xu + c * 32));
           tmem_ld_wait();
-        }
-        // keys the row may not see become -inf
-        if (__any_sync(kFull, see != ~0ull)) {
-          const uint32_t s0 = static_cast<uint32_t>(see), s1 = static_cast<uint32_t>(see >> 32);
+          // keys the row may not see become -inf
+          if (__any_sync(kFull, see != ~0ull)) {
+            const uint32_t s0 = static_cast<uint32_t>(see), s1 = static_cast<uint32_t>(see >> 32);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            x[i] = (s0 >> i) & 1u ? x[i] : -INFINITY;
-            x[32 + i] = (s1 >> i) & 1u ? x[32 + i] : -INFINITY;
+            for (int i = 0; i < 32; ++i) {
+              x[i] = (s0 >> i) & 1u ? x[i] : -INFINITY;
+              x[32 + i] = (s1 >> i) & 1u ? x[32 + i] : -INFINITY;
+            }
           }
-        }
-        float m8[8];
+          if (again) break;
+          float m8[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) m8[u] = x[u];
+          for (int u = 0; u < 8; ++u) m8[u] = x[u];
 #pragma unroll
-        for (int k2 = 8; k2 < 64; ++k2) m8[k2 & 7] = fmaxf(m8[k2 & 7], x[k2]);
-        const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
-                         fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * sc;
-        bool shifted = false;
-        if (__any_sync(kFull, mx > over)) {
+          for (int k2 = 8; k2 < 64; ++k2) m8[k2 & 7] = fmaxf(m8[k2 & 7], x[k2]);
+          const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
+                           fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7]))) * sc;
+          if (!__any_sync(kFull, mx > over)) break;
           const bool mine = mx > m_used + 8.0f;
           const float alpha = mine ? ex2_approx(m_used - mx) : 1.0f;
           if (b > it.b0) {
             if (!(ok = wwait(&T->p_empty[(g - 1) & 1], ((g - 1) >> 1) & 1))) break;
             tc_fence_after_sync();
-#pragma unroll 2
-            for (int c = 0; c < D / 8; ++c) {
-              uint32_t y[8];
-              tmem_ld_32x32b_x8(o_col + c * 8, y);
+            const uint64_t alpha2 = pack2(alpha, alpha);
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t y[32];
+              tmem_ld_32x32b_x32(o_col + c, y);
               tmem_ld_wait();
 #pragma unroll
-              for (int k2 = 0; k2 < 8; ++k2)
-                y[k2] = __float_as_uint(__uint_as_float(y[k2]) * alpha);
-              tmem_st_x8(o_col + c * 8, y);
+              for (int k2 = 0; k2 < 32; k2 += 2) {
+                float y0, y1;
+                unpack2(mul2(pack2(__uint_as_float(y[k2]), __uint_as_float(y[k2 + 1])), alpha2),
+                        y0, y1);
+                y[k2] = __float_as_uint(y0);
+                y[k2 + 1] = __float_as_uint(y1);
+              }
+              tmem_st_32x32b_x32(o_col + c, y);
             }
             tmem_st_wait();
           }
@@ -684,16 +833,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
           const bool wide = fabsf(m_used) > kWideScore && m_used > -INFINITY;
           over = wide ? -INFINITY : m_used + 8.0f;
           shifted = __any_sync(kFull, wide);
-          if (shifted) {
-            wide_scores(s_col, sc, m_used == -INFINITY ? 0.0f : m_used, see);
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              tmem_ld_32x32b_x32(s_col + c * 32,
-                                 *reinterpret_cast<uint32_t(*)[32]>(
-                                     reinterpret_cast<uint32_t*>(x) + c * 32));
-            tmem_ld_wait();
-          }
+          if (shifted) wide_scores(s_col, sc, m_used == -INFINITY ? 0.0f : m_used, see);
         }
+        if (!ok) break;
         const float mref = (shifted || m_used == -INFINITY ? 0.0f : m_used) - kPBits;
         const uint64_t sc2 = pack2(sc, sc), nm2 = pack2(-mref, -mref);
         uint64_t ls[4] = {0, 0, 0, 0};
@@ -730,11 +872,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     if (!ok && lane == 0) give_up();
   } else {
     // ---------------- K or V: codes to float16 ----------------
-    set_registers_down<64>();
+    set_registers_down<56>();
     const int is_v = (warp - 16) >> 2, wq = warp & 3;
     const uint8_t* cache = a.cache[is_v];
-    const uint8_t* scale = a.scale[is_v];
-    constexpr int kRows = 128 / (D / 16) ;         // rows the four warps bring at a time
+    constexpr int kRows = 128 / (D / 16);          // rows the four warps bring at a time
     constexpr int kU = kBK / kRows;                // rows a thread brings of a block
     // 16 bytes of a row a lane; eight neighbouring lanes have four groups of one
     // half of two neighbouring rows, whose 16-byte places in the swizzled tile are
@@ -744,117 +885,76 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     const int row_in = wq * (kRows / 4) + ((lane >> 2) & 1) +
                        2 * (kHalves == 2 ? lane >> 4 : lane >> 3);
     const int dim0 = half * 64 + c4 * 16;
-    const int p_size = a.units.rows.page_size;
-    uint8_t* ring = skv + is_v * kTileBytes + half * kHalfBytes;
-    uint4 raw[kU];                                 // codes of the next block
-    int sc[kU];                                    // their scales' bytes
-    int page[kU];                                  // pages of the block after it
-    Piece it;
-    int k = 0, b = 0, left = 0;                    // pieces fetched; block, blocks left of it
-    bool ok = true;
-    auto next_block = [&](Block& x) {              // no keys: no more
-      x = Block{};
-      if (left == 0) {
-        if (k < 0 || !ok) return;
-        if (!(ok = peek_warp(k, it))) return;
-        release_warp(k);
-        if (it.nblk == 0) {
-          k = -1;
-          return;
-        }
-        ++k;
-        b = it.b0;
-        left = it.b1 - it.b0;
-      }
-      x.r = it.r;
-      x.kvh = it.kvh;
-      x.key0 = b * kBK;
-      x.key_end = it.key_end;
-      x.all = a.parent != nullptr ? it.prefix : it.prefix + it.j0 + 1;
-      x.ring = (k - 1) % kItemRing;
-      ++b;
-      --left;
+    // (rows kRows apart are multiples of 8 apart: the same swizzle)
+    uint8_t* mine = skv + is_v * kTileBytes + half * kHalfBytes + row_in * 128;
+    const int lo16 = ((2 * c4) ^ (row_in & 7)) * 16, hi16 = ((2 * c4 + 1) ^ (row_in & 7)) * 16;
+    uint8_t* raw = codes + (is_v * kU * 128 + (threadIdx.x & 127)) * 16;
+    cache += dim0;
+    // (one copy a group of copies)
+    auto load = [&](uint32_t at, int u) {
+      const bool is = at != kNowhere;
+      copy16_if(is, raw + u * 128 * 16, cache + static_cast<size_t>(is ? at : 0) * D);
     };
-    auto find_page = [&](const Block& x, int u) {
-      const int key = x.key0 + u * kRows + row_in;
-      page[u] = key < x.key_end ? kv_page(a.units.rows, x.r, div_by(key, a.blocks.page)) : -2;
-    };
-    auto load = [&](const Block& x, int u) {
-      raw[u] = make_uint4(0, 0, 0, 0);
-      sc[u] = kExpBias;
-      if (page[u] >= 0) {
-        const int key = x.key0 + u * kRows + row_in;
-        const int off = key - div_by(key, a.blocks.page) * p_size;
-        const long long slot = static_cast<long long>(page[u]) * p_size + off;
-        const long long at =
-            static_cast<long long>(page[u]) * a.blocks.per_page + (off >> a.blocks.shift);
-        raw[u] = load16(cache + (slot * a.units.Hkv + x.kvh) * D + dim0);
-        sc[u] = __ldg(scale + at * a.units.Hkv + x.kvh);
-      } else if (page[u] == -1) {
-        report(a.status, PCTREE_ERR_INVALID_ARG);
-      }
-    };
-    Block cur, nxt, then;
-    next_block(cur);
-    next_block(nxt);
-    if (cur.key_end > 0) {
-#pragma unroll
-      for (int u = 0; u < kU; ++u) find_page(cur, u);
-#pragma unroll
-      for (int u = 0; u < kU; ++u) load(cur, u);
-#pragma unroll
-      for (int u = 0; u < kU; ++u) find_page(nxt, u);
+    bool ok = wwait_long(&T->place_full[0], 0), more = ok && T->places[0].keys > 0;
+    if (more) {
+      for (int u = 0; u < kU; ++u) load(T->places[0].at[u * kRows + row_in], u);
     }
-    for (int g = 0; ok && cur.key_end > 0; ++g) {
-      next_block(then);
-      if (!ok) break;
+    for (int g = 0; ok && more; ++g) {
+      const Places& cur = T->places[g % kPlaceRing];
+      const Places& nxt = T->places[(g + 1) % kPlaceRing];
       const int place = 2 * g + is_v, slot = place % kSlots;
-      if (!(ok = wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1))) break;
-      uint8_t* tile = ring + (slot - is_v) * kTileBytes;
+      ok = wwait_long(&T->place_full[(g + 1) % kPlaceRing], ((g + 1) / kPlaceRing) & 1) &&
+           wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1);
+      if (!ok) break;
+      more = nxt.keys > 0;
+      uint8_t* tile = mine + (slot - is_v) * kTileBytes;
       const bool some = is_v != 0 && cur.key0 + kBK > cur.all;   // keys that not all rows see
+#pragma unroll 1
+      for (int u0 = 0; u0 < kU; u0 += 4) {         // (four rows' latencies at once)
+        uint4 x[4];
+        uint32_t by[4], at[4];
+        copies_wait<kU - 4>();
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int row = u * kRows + row_in;
-        uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-        if (some && cur.key0 + row >= cur.all) {
-          uint32_t bits = 0;
+        for (int u = 0; u < 4; ++u) {
+          const int row = (u0 + u) * kRows + row_in;
+          x[u] = *reinterpret_cast<const uint4*>(raw + (u0 + u) * 128 * 16);
+          by[u] = (cur.by[row] >> (16 * is_v) & 0xffffu) * 0x10001u;
+          at[u] = nxt.at[row];                     // (no more: nowhere)
+        }
+        if (some) {
+          // their NaN values are taken out and noted
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int key = cur.key0 + (u0 + u) * kRows + row_in - cur.all;
+            if (key >= 0 && any_nan(x[u])) x[u] = without_nan(x[u], T, cur.ring, key, dim0);
+          }
+        }
+        uint8_t* dst = tile + u0 * kRows * 128;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+          uint32_t h[8];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t nan = nan_bytes(w[i]);
-            w[i] &= ~nan;
-            bits |= (((nan & 0x08040201u) * 0x01010101u) >> 24 & 15u) << (4 * i);
+            h[2 * i] = mul_h2(halves2(w[i]), by[u]);
+            h[2 * i + 1] = mul_h2(halves2(w[i] >> 16), by[u]);
           }
-          if (bits != 0) {
-            const int key = cur.key0 + row - cur.all;
-            atomicMin(&T->bad_first[cur.ring], key);
-            const int n = atomicAdd(&T->bad_n[cur.ring], 1);
-            if (n < kMaxBad)
-              T->bad[cur.ring][n] = bits | static_cast<uint32_t>(dim0 / 16) << 16 |
-                                    static_cast<uint32_t>(key) << 20;
-          }
+          *reinterpret_cast<uint4*>(dst + u * kRows * 128 + lo16) =
+              make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(dst + u * kRows * 128 + hi16) =
+              make_uint4(h[4], h[5], h[6], h[7]);
         }
-        if (!scale_ok(sc[u])) report(a.status, PCTREE_ERR_INVALID_ARG);
-        const uint32_t by = half2_exp(scale_exp(sc[u]));
-        uint32_t h[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[2 * i] = mul_h2(halves2(w[i]), by);
-          h[2 * i + 1] = mul_h2(halves2(w[i] >> 16), by);
-        }
-        load(nxt, u);
-        uint8_t* dst = tile + row * 128;
-        *reinterpret_cast<uint4*>(dst + (((2 * c4) ^ (row & 7)) * 16)) =
-            make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(dst + (((2 * c4 + 1) ^ (row & 7)) * 16)) =
-            make_uint4(h[4], h[5], h[6], h[7]);
-        find_page(then, u);
+        for (int u = 0; u < 4; ++u) load(at[u], u0 + u);
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&T->kv_full[slot]);
-      cur = nxt;
-      nxt = then;
+      if (lane == 0) {
+        mbar_arrive(&T->kv_full[slot]);
+        mbar_arrive(&T->place_empty[g % kPlaceRing]);
+      }
     }
+    copies_wait<0>();                              // copies land before the CTA may exit
     if (!ok && lane == 0) give_up();
   }
   // ---------------- teardown ----------------
@@ -862,7 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  if (warp == 1) tmem_dealloc(tmem, kTmemCols);
+  if (warp == 1) tmem_dealloc(T->tmem_base, kTmemCols);
 }
 
 // Rows per tile: one where requests have one row each, on average (a tile's
@@ -881,6 +981,12 @@ bool work_ok(const pctree_kv8_attn_config& c) {
   return units * blocks < (1ll << 32) / c.Hkv - 1024;
 }
 
+// Whether a 32-bit number tells all heads of all slots apart (a plane of 2^32 heads
+// of 64 codes alone would fill the memory of a GB300).
+bool places_ok(const pctree_kv8_attn_config& c) {
+  return static_cast<long long>(c.n_pages) * c.page_size <= 0xfffffffell / c.Hkv;
+}
+
 pctree_status attn8_check(const pctree_kv8_attn_config* c) {
   if (c == nullptr) return PCTREE_ERR_INVALID_ARG;
   if (c->Hq < 1 || c->D < 1 || !(c->scale > 0.0f) || !(c->scale < 1e30f))
@@ -892,7 +998,7 @@ pctree_status attn8_check(const pctree_kv8_attn_config* c) {
       c->q_stride < static_cast<int64_t>(c->Hq) * c->D)
     return PCTREE_ERR_INVALID_ARG;
   if ((c->D != 64 && c->D != 128) || c->Hq / c->Hkv > 128 || c->q_stride > (1ll << 38) ||
-      !work_ok(*c))
+      !work_ok(*c) || !places_ok(*c))
     return PCTREE_ERR_UNSUPPORTED;
   return PCTREE_OK;
 }
@@ -900,7 +1006,7 @@ pctree_status attn8_check(const pctree_kv8_attn_config* c) {
 template <int D, bool F16>
 pctree_status attn8_launch(const Kv8AttnArgs& a, int num_sms, cudaStream_t stream) {
   constexpr size_t smem =
-      (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;
+      (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;   // Q, K and V, codes
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
   static SmemLimit limit;
   const void* fn = reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>);
@@ -987,6 +1093,7 @@ pctree_status pctree_kv8_attention(const pctree_kv8_attn_config* cfg, const void
   a.q_stride = c.q_stride;
   a.Hq = c.Hq;
   a.G = c.Hq / c.Hkv;
+  a.by_G = fast_div(a.G);
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
   const bool f16 = c.dtype == PCTREE_F16;
