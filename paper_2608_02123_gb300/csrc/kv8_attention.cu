@@ -2,25 +2,25 @@
 // (tokens, chains, packed trees, prompts) over a paged or contiguous cache of
 // 8-bit codes with a power-of-two scale per block of slots and head.
 //
-// Units, pieces and joins are kv_pieces.cuh's: a tile's rows are (row, query head
-// of the group) pairs, R = G * npt <= 128, and its keys come in blocks of 128
-// consecutive slots, gathered slot by slot, so pages of any size fill a block.
+// Units, pieces and joins are kv_pieces.cuh's.  A unit has up to two tiles of rows;
+// a tile's rows are (row, query head of the group) pairs, R = G * tile_rows <= 128.
+// Keys come in blocks of 64 consecutive slots, gathered slot by slot, so pages of
+// any size fill a block, and are brought and widened once for both tiles.
 //
 //   warp 0        planner: the CTA's pieces, in order, up to kItemRing ahead
-//   warp 1        S issuer: S_b = Q K_b^T (tcgen05.mma, M = N = 128) into one of
-//                 two TMEM buffers
-//   warp 2        PV issuer: O_h += P_b V_b over each half h of the block's keys
-//                 (P read from TMEM)
+//   warp 1        S issuer: S = Q K^T (tcgen05.mma, M = 128, N = 64) of each tile
+//                 into one of its two TMEM buffers
+//   warp 2        PV issuer: O += P V of each tile (P read from TMEM)
 //   warp 3        where the keys of a block lie and what scales they have, up to
 //                 kPlaceRing blocks ahead
-//   warps 4..7    the next tile's Q and its rows' ancestors, once the last S of a
-//                 piece is done; then the two O of the finished piece, combined,
-//                 to rows of out or the piece's partial
-//   warps 8..15   softmax, two threads per tile row, 64 keys of a block each with
-//                 its own running maximum, sum and O
-//   warps 16..19  K, and warps 20..23 V: codes to shared memory a block ahead, 16
-//                 bytes a thread and copy, and to float16 (128-byte swizzle, 64
-//                 dims a half), two blocks of each
+//   warps 4..7    the next unit's Q and its rows' ancestors, once the last S of a
+//                 piece is done; then O of the finished piece to rows of out or to
+//                 the piece's partial
+//   warps 8..15   softmax, four warps a tile and a thread a row: S is read from
+//                 TMEM, masked and scaled, P = 2^(s - m_used) written back over it
+//   warps 16..19  K, and warps 20..23 V: codes to shared memory two blocks ahead,
+//                 16 bytes a thread and copy, and to float16 (128-byte swizzle, 64
+//                 dims a half)
 // All waits are bounded (1 s; those for a whole piece 1 s without a block) and end
 // in PCTREE_ERR_TIMEOUT.
 //
@@ -31,41 +31,33 @@
 // 2^7 times the probability relative to the row's running maximum, in float16 (11
 // bits; down to 2^-31 of the maximum): far keys of a long context that are each
 // small against the first are not lost.  Row sums add the unrounded values.
-#include "kv8.cuh"
-#include "kv_pieces.cuh"
+#include <algorithm>
+
+#include "kv8_tokens.cuh"
 
 namespace pct {
 namespace {
 
-constexpr int kBK = 128;                     // keys per block
-constexpr int kHalfBytes = 128 * 128;        // 128 rows x 64 halves
+constexpr int kBK = 64;                      // keys per block
+constexpr int kQHalf = 128 * 128;            // bytes of 128 rows x 64 halves
+constexpr int kKHalf = kBK * 128;            // of a block's
 constexpr uint64_t kLimitNs = 1000000000ull;
 constexpr int kThreads = 768;
-constexpr int kSlots = 4;                    // K and V blocks in the ring, in turn
+constexpr int kSlots = 6;                    // K and V blocks in the ring, in turn
+constexpr int kAhead = 2;                    // blocks of codes under way
 constexpr int kItemRing = 8;
 constexpr int kPlaceRing = 4;
 constexpr int kMaxBad = 64;                  // groups of 16 values of V told apart
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kOCol = 2 * kBK;
+// Registers a thread: of the launch, and what the groups of four warps make of
+// them (their sum must not exceed the launch's).
+constexpr int kRegsLaunch = 80, kRegsIssue = 48, kRegsSoftmax = 112, kRegsConvert = 64;
+static_assert(kRegsLaunch * kThreads <= 65536 &&
+                  kRegsIssue + kRegsLaunch + 2 * kRegsSoftmax + 2 * kRegsConvert <=
+                      kRegsLaunch * (kThreads / 128),
+              "registers");
+constexpr uint32_t kOCol = 4 * kBK;          // S of tile t, buffer b: column (2 t + b) * kBK
 constexpr float kPBits = 7.0f;               // P is 2^7 times what it is relative to
-
-struct Kv8AttnArgs {
-  Units units;
-  Kv8Blocks blocks;
-  const uint16_t* q;
-  const uint8_t* cache[2];                   // keys, values
-  const uint8_t* scale[2];
-  const int32_t* parent;                     // NULL: causal
-  uint16_t* out;
-  float* part_o;                             // as in JoinArgs
-  float2* part_ml;
-  PieceJoin* join;
-  int32_t* status;
-  long long q_stride;
-  int Hq, G;
-  FastDiv by_G;
-  float scale_log2;
-};
 
 // A block's keys: places (slot * Hkv + head, or kNowhere) and scales (float16, of
 // K and of V).
@@ -81,8 +73,8 @@ struct Tail {
   uint64_t place_full[kPlaceRing], place_empty[kPlaceRing];
   uint64_t q_full[2], q_empty;               // (full: by piece parity)
   uint64_t kv_full[kSlots], kv_empty[kSlots];
-  uint64_t s_full[2], p_full[2], p_empty[2];
-  uint64_t o_full, o_empty;
+  uint64_t s_full[2][2], p_full[2][2], p_empty[2][2];      // [tile][buffer]
+  uint64_t o_full[2], o_empty[2];            // [tile]
   uint64_t item_full[kItemRing], item_empty[kItemRing];
   uint64_t done, out_sync;
   uint32_t tmem_base;
@@ -90,22 +82,18 @@ struct Tail {
   int blocks;                                // multiplied so far (see wwait_long)
   Piece item[kItemRing];
   Places places[kPlaceRing];
-  float row_l[2][128], row_m[2][128];
-  float row_scale[2][128];                   // of Q's rows, by piece parity (log2 units)
-  // NaN values at keys that only some rows of the piece's tile see, by place in the
-  // item ring: 16 bits of a group of dims, the group << 16, the key (counted from
-  // the first that not every row sees) << 20; their number and the first such key.
+  float row_l[2][128], row_m[2][128];        // [tile]
+  float row_scale[2][2][128];                // of Q's rows (log2 units), [piece parity][tile]
+  // NaN values at keys that only some rows of the unit see, by place in the item
+  // ring: 16 bits of a group of dims, the group << 16, the key (counted from the
+  // first that not every row sees) << 20; their number and the first such key.
   int bad_n[kItemRing], bad_first[kItemRing];
   uint32_t bad[kItemRing][kMaxBad];
   int16_t par[PCTREE_ATTN_MAX_N];
-  uint32_t path[2][128][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by piece parity
+  uint32_t path[2][256][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by piece parity
   alignas(16) uint8_t stage[4][32 * 32];
   unsigned upto[PCTREE_KV_MAX_BATCH];        // work of requests 0 .. r
 };
-
-__device__ __forceinline__ void report(int32_t* status, int code) {
-  if (status != nullptr) atomicCAS(status, 0, code);
-}
 
 template <int N>
 __device__ __forceinline__ void set_registers_up() {
@@ -146,14 +134,15 @@ __host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
   return idesc_bf16_f32(M, N) & ~((1u << 7) | (1u << 10));
 }
 
-// An asynchronous copy of 16 bytes (zeros if not wanted)
-// to shared memory, a group of its own.
+// An asynchronous copy of 16 bytes (zeros if not wanted) to shared memory.
 __device__ __forceinline__ void copy16_if(bool wanted, void* dst, const uint8_t* p) {
   asm volatile(
-      "cp.async.cg.shared.global [%0], [%1], 16, %2;\n cp.async.commit_group;\n" ::"r"(
-          smem_u32(dst)),
-      "l"(p), "r"(wanted ? 16 : 0)
+      "cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(p),
+      "r"(wanted ? 16 : 0)
       : "memory");
+}
+__device__ __forceinline__ void copies_commit() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
 }
 template <int N>
 __device__ __forceinline__ void copies_wait() {
@@ -222,20 +211,38 @@ __device__ __noinline__ void wide_scores(uint32_t s_col, float sc, float mref, u
   tmem_st_wait();
 }
 
+__device__ __forceinline__ bool wait_one(Tail* T, uint64_t* bar, uint32_t parity) {
+  return mbar_wait_bounded(bar, parity, &T->abort, kLimitNs);
+}
+// By a whole warp; and one that lasts as long as pieces do: over once no block has
+// been multiplied for the limit.
+__device__ __forceinline__ bool wwait(Tail* T, uint64_t* bar, uint32_t parity) {
+  return __all_sync(kFull, wait_one(T, bar, parity));
+}
+__device__ __forceinline__ bool wwait_long(Tail* T, uint64_t* bar, uint32_t parity) {
+  volatile int* blocks = &T->blocks;
+  for (;;) {
+    const int before = *blocks;
+    if (wwait(T, bar, parity)) return true;
+    if (__any_sync(kFull, *static_cast<volatile int*>(&T->abort) != 0) ||
+        __all_sync(kFull, *blocks == before))
+      return false;
+  }
+}
+
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int kHalves = D / 64;
-  constexpr int kTileBytes = kHalves * kHalfBytes;
+  constexpr int kQBytes = kHalves * kQHalf, kKBytes = kHalves * kKHalf;
+  constexpr int kCodeBytes = kBK * D;              // of a block's K or V
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint8_t* sq = sm;
-  uint8_t* skv = sq + kTileBytes;                  // ring
-  uint8_t* codes = skv + kSlots * kTileBytes;      // [K, V][row of a thread][128 threads][16]
-  Tail* T = reinterpret_cast<Tail*>(codes + kTileBytes);
+  uint8_t* sq = sm;                                // [tile]
+  uint8_t* skv = sq + 2 * kQBytes;                 // ring
+  uint8_t* codes = skv + kSlots * kKBytes;         // [K, V][kAhead][row of a thread][128][16]
+  Tail* T = reinterpret_cast<Tail*>(codes + 2 * kAhead * kCodeBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int R = a.G * a.units.npt;                 // rows of a tile
-  volatile int* abort_v = &T->abort;
 
   // ---------------- set-up ----------------
   if (threadIdx.x == 0) {
@@ -246,9 +253,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     mbar_init(&T->q_empty, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&T->q_full[s], 4);
-      mbar_init(&T->s_full[s], 1);
-      mbar_init(&T->p_full[s], 8);
-      mbar_init(&T->p_empty[s], 1);
+      for (int t = 0; t < 2; ++t) {
+        mbar_init(&T->s_full[t][s], 1);
+        mbar_init(&T->p_full[t][s], 4);
+        mbar_init(&T->p_empty[t][s], 1);
+      }
+      mbar_init(&T->o_full[s], 1 + 4);
+      mbar_init(&T->o_empty[s], 4);
     }
     for (int s = 0; s < kItemRing; ++s) {
       mbar_init(&T->item_full[s], 1);
@@ -258,20 +269,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       mbar_init(&T->place_full[s], 1);
       mbar_init(&T->place_empty[s], 8);
     }
-    mbar_init(&T->o_full, 1 + 8);
-    mbar_init(&T->o_empty, 4);
     mbar_init(&T->done, 2);
     mbar_init(&T->out_sync, 4);
     T->abort = 0;
     T->blocks = 0;
     fence_barrier_init();
   }
-  // rows R..127 of Q are never written: zero them once
-  const int zq = (128 - R) * 8;
-  for (int i = threadIdx.x; i < kHalves * zq; i += kThreads) {
-    const int h = i / zq, rem = i - h * zq;
-    *reinterpret_cast<uint4*>(sq + h * kHalfBytes + (R + rem / 8) * 128 + (rem % 8) * 16) =
-        make_uint4(0, 0, 0, 0);
+  // rows past a tile's are never written: zero them once
+  {
+    const int R = a.G * a.tile_rows, zq = (128 - R) * 8;
+    for (int i = threadIdx.x; i < 2 * kHalves * zq; i += kThreads) {
+      const int h = i / zq, rem = i - h * zq;
+      *reinterpret_cast<uint4*>(sq + h * kQHalf + (R + rem / 8) * 128 + (rem % 8) * 16) =
+          make_uint4(0, 0, 0, 0);
+    }
   }
   fence_proxy_async_smem();
   if (warp == 1) tmem_alloc(&T->tmem_base, kTmemCols);
@@ -283,26 +294,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  auto wwait = [&](uint64_t* bar, uint32_t parity) -> bool {
-    return __all_sync(kFull, mbar_wait_bounded(bar, parity, abort_v, kLimitNs));
-  };
-  // a wait that lasts as long as pieces do: over once no block has been multiplied
-  // for the limit
-  auto wwait_long = [&](uint64_t* bar, uint32_t parity) -> bool {
-    volatile int* blocks = &T->blocks;
-    for (;;) {
-      const int before = *blocks;
-      if (wwait(bar, parity)) return true;
-      if (__any_sync(kFull, *abort_v != 0) || __all_sync(kFull, *blocks == before)) return false;
-    }
-  };
+
   auto give_up = [&]() {
-    *abort_v = 1;
+    *static_cast<volatile int*>(&T->abort) = 1;
     report(a.status, PCTREE_ERR_TIMEOUT);
   };
   auto fetch_one = [&](int k, Piece& it) -> bool {
     const int s = k % kItemRing;
-    if (!mbar_wait_bounded(&T->item_full[s], (k / kItemRing) & 1, abort_v, kLimitNs)) return false;
+    if (!wait_one(T, &T->item_full[s], (k / kItemRing) & 1)) return false;
     it = T->item[s];
     mbar_arrive(&T->item_empty[s]);
     return true;
@@ -310,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   // (peek leaves the place taken)
   auto peek_warp = [&](int k, Piece& it) -> bool {
     const int s = k % kItemRing;
-    if (!wwait_long(&T->item_full[s], (k / kItemRing) & 1)) return false;
+    if (!wwait_long(T, &T->item_full[s], (k / kItemRing) & 1)) return false;
     it = T->item[s];
     return true;
   };
@@ -320,32 +319,36 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   };
 
   if (warp < 4) {
-    set_registers_down<48>();
+    set_registers_down<kRegsIssue>();
     const uint32_t tmem = T->tmem_base;
     if (warp == 1 && lane == 0) {
       // ---------------- S issuer ----------------
       constexpr uint32_t idS = idesc_f16(128, kBK);
-      int g = 0;
       const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
       const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
+      int g = 0, gt[2] = {0, 0};                   // blocks, and of each tile
       bool ok = true;
       Piece it;
       for (int k = 0; ok; ++k) {
         if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
-        if (!(ok = mbar_wait_bounded(&T->q_full[k & 1], (k >> 1) & 1, abort_v, kLimitNs))) break;
-        for (int b = it.b0; b < it.b1; ++b, ++g) {
-          const int sb = g & 1, slot = (2 * g) % kSlots;
-          ok = mbar_wait_bounded(&T->kv_full[slot], (2 * g / kSlots) & 1, abort_v, kLimitNs) &&
-               mbar_wait_bounded(&T->p_empty[sb], ((g >> 1) & 1) ^ 1, abort_v, kLimitNs);
-          if (!ok) break;
-          const uint64_t kd = k_desc + slot * (kTileBytes >> 4);
-          tc_fence_after_sync();
+        if (!(ok = wait_one(T, &T->q_full[k & 1], (k >> 1) & 1))) break;
+        const int tiles = it.n_rows > a.tile_rows ? 2 : 1;
+        for (int b = it.b0; ok && b < it.b1; ++b, ++g) {
+          const int slot = (2 * g) % kSlots;
+          if (!(ok = wait_one(T, &T->kv_full[slot], (2 * g / kSlots) & 1))) break;
+          const uint64_t kd = k_desc + slot * (kKBytes >> 4);
+#pragma unroll 1
+          for (int t = 0; t < tiles; ++t) {
+            const int n = t == 0 ? gt[0]++ : gt[1]++, sb = n & 1;
+            if (!(ok = wait_one(T, &T->p_empty[t][sb], ((n >> 1) & 1) ^ 1))) break;
+            tc_fence_after_sync();
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const int off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
-            tc_mma_bf16(tmem + sb * kBK, q_desc + off, kd + off, idS, kk > 0 ? 1u : 0u);
+            for (int kk = 0; kk < D / 16; ++kk)
+              tc_mma_bf16(tmem + (2 * t + sb) * kBK,
+                          q_desc + ((t * kQBytes + (kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
+                          kd + (((kk >> 2) * kKHalf + (kk & 3) * 32) >> 4), idS, kk > 0 ? 1u : 0u);
+            tc_commit(&T->s_full[t][sb]);
           }
-          tc_commit(&T->s_full[sb]);
           tc_commit(&T->kv_empty[slot]);
         }
         tc_commit(&T->q_empty);
@@ -357,32 +360,33 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     } else if (warp == 2 && lane == 0) {
       // ---------------- PV issuer ----------------
       constexpr uint32_t idO = idesc_f16(128, D) | (1u << 16);   // B MN-major
-      int g = 0;
-      const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), kHalfBytes, 1024);
+      const uint64_t v_desc = desc_mnmajor_sw128(smem_u32(skv), kKHalf, 1024);
+      int g = 0, gt[2] = {0, 0}, kt[2] = {0, 0};   // blocks, of each tile; pieces of each
       bool ok = true;
       volatile int* blocks = &T->blocks;
       Piece it;
       for (int k = 0; ok; ++k) {
         if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
-        for (int b = it.b0; b < it.b1; ++b, ++g) {
-          const int sb = g & 1, slot = (2 * g + 1) % kSlots;
-          ok = mbar_wait_bounded(&T->kv_full[slot], ((2 * g + 1) / kSlots) & 1, abort_v,
-                                 kLimitNs) &&
-               mbar_wait_bounded(&T->p_full[sb], (g >> 1) & 1, abort_v, kLimitNs) &&
-               (b > it.b0 ||                       // the last piece's O has been read
-                mbar_wait_bounded(&T->o_empty, (k & 1) ^ 1, abort_v, kLimitNs));
-          if (!ok) break;
-          const uint64_t vd = v_desc + slot * (kTileBytes >> 4);
-          tc_fence_after_sync();
+        const int tiles = it.n_rows > a.tile_rows ? 2 : 1;
+        for (int b = it.b0; ok && b < it.b1; ++b, ++g) {
+          const int slot = (2 * g + 1) % kSlots;
+          if (!(ok = wait_one(T, &T->kv_full[slot], ((2 * g + 1) / kSlots) & 1))) break;
+          const uint64_t vd = v_desc + slot * (kKBytes >> 4);
+#pragma unroll 1
+          for (int t = 0; t < tiles; ++t) {
+            const int n = t == 0 ? gt[0]++ : gt[1]++, sb = n & 1;
+            ok = wait_one(T, &T->p_full[t][sb], (n >> 1) & 1) &&
+                 (b > it.b0 ||                     // the last piece's O has been read
+                  wait_one(T, &T->o_empty[t], ((t == 0 ? kt[0]++ : kt[1]++) & 1) ^ 1));
+            if (!ok) break;
+            tc_fence_after_sync();
 #pragma unroll
-          for (int kk = 0; kk < kBK / 16; ++kk) {
-            const int h = kk >> 2;
-            tc_mma_tmem_a(tmem + kOCol + h * D, tmem + sb * kBK + h * 64 + (kk & 3) * 8,
-                          vd + ((16 * kk * 128) >> 4), idO,
-                          (b > it.b0 || (kk & 3) > 0) ? 1u : 0u);
+            for (int kk = 0; kk < kBK / 16; ++kk)
+              tc_mma_tmem_a(tmem + kOCol + t * D, tmem + (2 * t + sb) * kBK + kk * 8,
+                            vd + ((16 * kk * 128) >> 4), idO, (b > it.b0 || kk > 0) ? 1u : 0u);
+            tc_commit(&T->p_empty[t][sb]);
+            if (b + 1 == it.b1) tc_commit(&T->o_full[t]);
           }
-          tc_commit(&T->p_empty[sb]);
-          if (b + 1 == it.b1) tc_commit(&T->o_full);
           *blocks = g + 1;
           tc_commit(&T->kv_empty[slot]);
         }
@@ -396,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       int k = 0;
       auto post = [&](const Piece& it) -> bool {   // lane 0 writes the k-th piece
         const int s = k % kItemRing;
-        if (!wwait_long(&T->item_empty[s], ((k / kItemRing) & 1) ^ 1)) return false;
+        if (!wwait_long(T, &T->item_empty[s], ((k / kItemRing) & 1) ^ 1)) return false;
         if (lane == 0) {
           T->bad_n[s] = 0;
           T->bad_first[s] = PCTREE_ATTN_MAX_N;
@@ -467,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         // the g-th block's places (without keys: the end); then the scales of the
         // block before it, which are there by now
         const int st = g % kPlaceRing;
-        if (!(ok = wwait(&T->place_empty[st], ((g / kPlaceRing) & 1) ^ 1))) break;
+        if (!(ok = wwait(T, &T->place_empty[st], ((g / kPlaceRing) & 1) ^ 1))) break;
         uint32_t tk[kKeys], tv[kKeys];
 #pragma unroll
         for (int i = 0; i < kKeys; ++i) {
@@ -525,53 +529,51 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (!ok && lane == 0) give_up();
     }
   } else if (warp < 8) {
-    // ---------------- Q in, O out: one thread per tile row ----------------
+    // ---------------- Q in, O out ----------------
     const uint32_t tmem = T->tmem_base;
     const int quad = warp & 3;
     const int t = quad * 32 + lane;
-    const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const int R = a.G * a.tile_rows;
     uint8_t* stg = T->stage[quad];
-    // the rows this lane stores (16 i + lane / 2 of the warp's 32, half lane % 2 of
-    // 16 dims): their places in the tile
-    int out_nl[2], out_off[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int ti = quad * 32 + 16 * i + (lane >> 1), ni = ti / a.G;
-      out_nl[i] = ti < R ? ni : 0x7fffffff;
-      out_off[i] = (ni * a.Hq + ti - ni * a.G) * D + (lane & 1) * 8;
-    }
-    const int nl = t / a.G;
     // a barrier of these four warps that gives up as other waits do
     int syncs = 0;
     auto together = [&]() -> bool {
       __syncwarp();
       if (lane == 0) mbar_arrive(&T->out_sync);
-      return wwait(&T->out_sync, syncs++ & 1);
+      return wwait(T, &T->out_sync, syncs++ & 1);
     };
-    // the k-th piece's tile; false: given up
+    // the k-th piece's tiles; false: given up
     auto bring_q = [&](int k, const Piece& it) -> bool {
       const int qb = k & 1;
-      if (!wwait_long(&T->q_empty, (k & 1) ^ 1)) return false;
-      uint8_t* tile = sq;
       constexpr int kLanes = D / 8;                // lanes of a row
       constexpr int kRows = 128 / kLanes;          // rows at a time
       const int c = t % kLanes;
+      const int rows = it.n_rows * a.G;            // of both tiles, one behind the other
+      const uint16_t* q = a.q + it.row0 * a.q_stride + it.kvh * a.G * D + c * 8;
+      auto place_of = [&](int row) {               // of a row of the unit
+        const int n = div_by(row, a.by_G);
+        return q + n * a.q_stride + (row - n * a.G) * D;
+      };
+      // on their way to L2 while the last S is under way
+      for (int row = t; row < rows; row += 128) {
+        const uint16_t* p = place_of(row) - c * 8;
+        for (int i = 0; i < D; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
+      }
+      if (!wwait_long(T, &T->q_empty, (k & 1) ^ 1)) return false;
       constexpr int kDeep = 4;                     // rows in flight
+      // rows past the last one's are zeros up to the end of their tile
+      const int all = it.n_rows > a.tile_rows ? 2 * R : R;
       // (few instructions: they come from memory again for every piece)
 #pragma unroll 1
-      for (int r0 = t / kLanes; r0 < R + t / kLanes; r0 += kDeep * kRows) {
+      for (int r0 = t / kLanes; r0 < all + t / kLanes; r0 += kDeep * kRows) {
         uint4 x[kDeep];
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-          // rows that are not there: the last one's load, and zeros below
-          const int row = min(r0 + u * kRows, it.n_rows * a.G - 1), n = div_by(row, a.by_G);
-          x[u] = *reinterpret_cast<const uint4*>(
-              a.q + (it.row0 + n) * a.q_stride + (it.kvh * a.G + row - n * a.G) * D + c * 8);
-        }
+        for (int u = 0; u < kDeep; ++u)
+          x[u] = *reinterpret_cast<const uint4*>(place_of(min(r0 + u * kRows, rows - 1)));
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
           const int row = r0 + u * kRows;
-          const uint32_t keep = row < it.n_rows * a.G ? ~0u : 0u;
+          const uint32_t keep = row < rows ? ~0u : 0u;
           uint32_t w[4] = {x[u].x & keep, x[u].y & keep, x[u].z & keep, x[u].w & keep};
           float sc = a.scale_log2;
           if constexpr (!F16) {
@@ -593,16 +595,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
               w[i] = pack16<true>(f.x * by, f.y * by);
             }
           }
-          if (row < R) {
-            *reinterpret_cast<uint4*>(tile + (c >> 3) * kHalfBytes + row * 128 +
-                                      (((c & 7) ^ (row & 7)) * 16)) =
+          if (row < all) {
+            const int tile = row >= R ? 1 : 0, in = row - tile * R;
+            *reinterpret_cast<uint4*>(sq + tile * kQBytes + (c >> 3) * kQHalf + in * 128 +
+                                      (((c & 7) ^ (in & 7)) * 16)) =
                 make_uint4(w[0], w[1], w[2], w[3]);
-            if (c == 0) T->row_scale[qb][row] = sc;
+            if (c == 0) T->row_scale[qb][tile][in] = sc;
           }
         }
       }
       if (a.parent != nullptr) {
-        // ancestors of the tile's rows, from the parents of the request's first rows
+        // ancestors of the unit's rows, from the parents of the request's first rows
         const int n = it.j0 + it.n_rows;
         const int32_t* parent = a.parent + it.row0 - it.j0;
         if (!together()) return false;
@@ -615,10 +618,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
           T->par[i] = static_cast<int16_t>(p);
         }
         if (!together()) return false;
-        if (t < it.n_rows) {
-          uint32_t* path = T->path[qb][t];
+        for (int j = t; j < it.n_rows; j += 128) {
+          uint32_t* path = T->path[qb][j];
           for (int i = 0; i < PCTREE_ATTN_MAX_N / 32; ++i) path[i] = 0;
-          for (int m = it.j0 + t; m >= 0; m = T->par[m]) path[m >> 5] |= 1u << (m & 31);
+          for (int m = it.j0 + j; m >= 0; m = T->par[m]) path[m >> 5] |= 1u << (m & 31);
         }
       }
       fence_proxy_async_smem();
@@ -629,123 +632,126 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     Piece it;
     bool ok = peek_warp(0, it);
     if (ok && it.nblk != 0) ok = bring_q(0, it);
+    int kt[2] = {0, 0};                            // pieces of each tile
     for (int k = 0; ok && it.nblk != 0; ++k) {
       Piece next;
       if (!(ok = peek_warp(k + 1, next))) break;
       if (next.nblk != 0 && !(ok = bring_q(k + 1, next))) break;
-      if (!(ok = wwait_long(&T->o_full, k & 1))) break;
-      tc_fence_after_sync();
-      uint16_t* oitem = a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G) * D;
       const bool whole = it.b0 == 0 && it.b1 == it.nblk;
-      const int ring = k % kItemRing, n_bad = T->bad_n[ring];
+      const int ring = k % kItemRing;
       const size_t part = static_cast<size_t>(blockIdx.x) * 2 + (it.b0 == 0 ? 1 : 0);
-      // the halves' sums and O relative to the larger of their references
-      const float l0 = T->row_l[0][t], l1 = T->row_l[1][t];
-      const float m0 = l0 != 0.0f ? T->row_m[0][t] : -INFINITY;
-      const float m1 = l1 != 0.0f ? T->row_m[1][t] : -INFINITY;
-      const float m = fmaxf(m0, m1);
-      float f0 = l0 != 0.0f ? exp2f(m0 - m) : 0.0f;
-      float f1 = l1 != 0.0f ? exp2f(m1 - m) : 0.0f;
-      const float l = l0 * f0 + l1 * f1;
-      const uint32_t o_col = lane_base + kOCol;
-      if (whole) {                                 // (no finite score, l = 0: NaN)
-        const float inv = 1.0f / l;
-        f0 *= inv;
-        f1 *= inv;
-      }
-      const bool in_tile = nl < it.n_rows && t < R;
-      if (!whole && in_tile)
-        a.part_ml[part * 128 + t] = make_float2(l != 0.0f ? m : -INFINITY, l);
+      const int tiles = it.n_rows > a.tile_rows ? 2 : 1;
 #pragma unroll 1
-      for (int c = 0; c < D / 16; ++c) {
-        float y[16];
-        {
-          uint32_t y0[16], y1[16];
-          tmem_ld_32x32b_x16(o_col + c * 16, y0);
-          tmem_ld_32x32b_x16(o_col + D + c * 16, y1);
+      for (int tile = 0; tile < tiles; ++tile) {
+        if (!(ok = wwait_long(T, &T->o_full[tile], (tile == 0 ? kt[0]++ : kt[1]++) & 1))) break;
+        tc_fence_after_sync();
+        const int n_bad = T->bad_n[ring];
+        const int nl = tile * a.tile_rows + div_by(t, a.by_G);   // row of the unit
+        const int n_end = min(it.n_rows, (tile + 1) * a.tile_rows);
+        // (rows of the next tile lie past this one's R)
+        const bool in_tile = t < R && nl < n_end;
+        const float l = T->row_l[tile][t];
+        const float inv = whole ? 1.0f / l : 1.0f;   // (no finite score, l = 0: NaN)
+        const int slot = tile * R + t;               // of the unit's rows
+        if (!whole && in_tile)
+          a.part_ml[part * kUnitRows + slot] =
+              make_float2(l != 0.0f ? T->row_m[tile][t] : -INFINITY, l);
+        const uint32_t o_col = tmem + (static_cast<uint32_t>(quad * 32) << 16) + kOCol + tile * D;
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t y[16];
+          tmem_ld_32x32b_x16(o_col + c * 16, y);
           tmem_ld_wait();
+          float f[16];
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const uint64_t a0 = pack2(__uint_as_float(y0[i]), __uint_as_float(y0[i + 1]));
-            const uint64_t a1 = pack2(__uint_as_float(y1[i]), __uint_as_float(y1[i + 1]));
-            unpack2(fma2(a0, pack2(f0, f0), mul2(a1, pack2(f1, f1))), y[i], y[i + 1]);
-          }
-        }
-        if (n_bad != 0) {
-          // NaN values that were taken out of V reach the rows that see their keys
-          auto sees = [&](int key) {
-            return a.parent == nullptr
-                       ? key < nl
-                       : nl < 128 && ((T->path[k & 1][nl][key >> 5] >> (key & 31)) & 1) != 0;
-          };
-          uint32_t nan = 0;
-          for (int i = 0; i < min(n_bad, kMaxBad); ++i) {
-            const uint32_t e = T->bad[ring][i];
-            if (static_cast<int>((e >> 16) & 15) == c && sees(e >> 20)) nan |= e & 0xffffu;
-          }
-          if (n_bad > kMaxBad && sees(T->bad_first[ring])) nan = 0xffffu;
+          for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(y[i]) * inv;
+          if (l == 0.0f && !whole) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if ((nan >> i) & 1u) y[i] = __int_as_float(0x7fc00000);
+            for (int i = 0; i < 16; ++i) f[i] = 0.0f;
+          }
+          if (n_bad != 0) {
+            // NaN values that were taken out of V reach the rows that see their keys
+            auto sees = [&](int key) {
+              return a.parent == nullptr
+                         ? key < nl
+                         : ((T->path[k & 1][min(nl, 255)][key >> 5] >> (key & 31)) & 1) != 0;
+            };
+            uint32_t nan = 0;
+            for (int i = 0; i < min(n_bad, kMaxBad); ++i) {
+              const uint32_t e = T->bad[ring][i];
+              if (static_cast<int>((e >> 16) & 15) == c && sees(e >> 20)) nan |= e & 0xffffu;
+            }
+            if (n_bad > kMaxBad && sees(T->bad_first[ring])) nan = 0xffffu;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if ((nan >> i) & 1u) f[i] = __int_as_float(0x7fc00000);
+            __syncwarp();
+          }
+          if (c == D / 16 - 1) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&T->o_empty[tile]);
+          }
+          if (!whole) {
+            float4* po =
+                reinterpret_cast<float4*>(a.part_o) + (part * (D / 4) + c * 4) * kUnitRows + slot;
+            if (in_tile) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                po[i * kUnitRows] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            }
+            continue;
+          }
+          // through shared memory: two neighbouring lanes store a row's 32 bytes
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) w[h] = pack16<F16>(f[i * 8 + 2 * h], f[i * 8 + 2 * h + 1]);
+            *reinterpret_cast<uint4*>(stg + lane * 32 + ((i ^ (lane >> 2)) & 1) * 16) =
+                make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * i + (lane >> 1), ti = quad * 32 + row, ni = div_by(ti, a.by_G);
+            const uint4 v = *reinterpret_cast<const uint4*>(
+                stg + row * 32 + (((lane & 1) ^ (row >> 2)) & 1) * 16);
+            if (ti < R && tile * a.tile_rows + ni < n_end)
+              *reinterpret_cast<uint4*>(
+                  a.out + ((static_cast<size_t>(it.row0) + tile * a.tile_rows + ni) * a.Hq +
+                           it.kvh * a.G + ti - ni * a.G) * D + c * 16 + (lane & 1) * 8) = v;
+          }
           __syncwarp();
         }
-        if (c == D / 16 - 1) {
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&T->o_empty);
-        }
-        if (!whole) {
-          float4* po = reinterpret_cast<float4*>(a.part_o) + part * (D / 4) * 128 + c * 4 * 128 + t;
-          if (in_tile) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              po[i * 128] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-          }
-          continue;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int h = 0; h < 4; ++h) w[h] = pack16<F16>(y[i * 8 + 2 * h], y[i * 8 + 2 * h + 1]);
-          *reinterpret_cast<uint4*>(stg + lane * 32 + ((i ^ (lane >> 2)) & 1) * 16) =
-              make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = 16 * i + (lane >> 1);
-          const uint4 v = *reinterpret_cast<const uint4*>(
-              stg + row * 32 + (((lane & 1) ^ (row >> 2)) & 1) * 16);
-          if (out_nl[i] < it.n_rows) *reinterpret_cast<uint4*>(oitem + out_off[i] + c * 16) = v;
-        }
-        __syncwarp();
       }
       // (a piece's ancestors are read up to here: they are replaced after)
-      if (!(ok = together())) break;
+      if (!ok || !(ok = together())) break;
       release_warp(k);
       it = next;
     }
     if (!ok && lane == 0) give_up();
   } else if (warp < 16) {
-    // ---------------- softmax, two threads per tile row ----------------
-    set_registers_up<120>();
+    // ---------------- softmax, a thread per row of a tile ----------------
+    set_registers_up<kRegsSoftmax>();
     const uint32_t tmem = T->tmem_base;
-    const int half = (warp - 8) >> 2;
+    const int tile = (warp - 8) >> 2;
     const int quad = warp & 3;
     const int t = quad * 32 + lane;
-    const int nl = t / a.G;
+    const int R = a.G * a.tile_rows;
+    const int nl = tile * a.tile_rows + div_by(t, a.by_G);     // row of the unit
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-    const uint32_t o_col = lane_base + kOCol + half * D;
-    int g = 0;
+    const uint32_t o_col = lane_base + kOCol + tile * D;
+    int g = 0, kt = 0;                             // this tile's blocks and pieces
     bool ok = true;
     Piece it;
     for (int k = 0; ok; ++k) {
       if (!(ok = peek_warp(k, it))) break;
       release_warp(k);
       if (it.nblk == 0) break;
-      if (!(ok = wwait_long(&T->q_full[k & 1], (k >> 1) & 1))) break;
-      const float sc = t < R ? T->row_scale[k & 1][t] : a.scale_log2;
+      if (!(ok = wwait_long(T, &T->q_full[k & 1], (k >> 1) & 1))) break;
+      if (it.n_rows <= tile * a.tile_rows) continue;
+      const float sc = t < R ? T->row_scale[k & 1][tile][t] : a.scale_log2;
       // keys this row sees: slots below `end`, and of those from the prefix on (in
       // a tree) its ancestors
       const int end = min(it.key_end, it.prefix + it.j0 + nl + 1);
@@ -753,13 +759,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       float over = -INFINITY;                      // a maximum above it needs a look
       for (int b = it.b0; b < it.b1; ++b, ++g) {
         const int sb = g & 1;
-        const int key0 = b * kBK + half * 64;
-        // this half's keys that the row sees
+        const int key0 = b * kBK;
         const int seen = end - key0;
         uint64_t see = seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1;
         if (a.parent != nullptr && key0 + 64 > it.prefix && see != 0) {
           const int node = key0 - it.prefix;       // > -64: the first key's place in the tree
-          const uint32_t* path = T->path[k & 1][min(nl, 127)];
+          const uint32_t* path = T->path[k & 1][min(nl, 255)];
           auto word = [&](int i) -> uint64_t {
             return i >= 0 && i < PCTREE_ATTN_MAX_N / 32 ? path[i] : 0u;
           };
@@ -769,9 +774,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
           if (node < 0) anc |= (1ull << -node) - 1;   // slots of the prefix
           see &= anc;
         }
-        if (!(ok = wwait(&T->s_full[sb], (g >> 1) & 1))) break;
+        if (!(ok = wwait(T, &T->s_full[tile][sb], (g >> 1) & 1))) break;
         tc_fence_after_sync();
-        const uint32_t s_col = lane_base + sb * kBK + half * 64;
+        const uint32_t s_col = lane_base + (2 * tile + sb) * kBK;
         float x[64];
         bool shifted = false;
         // The scores, and once more if the reference has moved: the rescaling of O
@@ -806,7 +811,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
           const bool mine = mx > m_used + 8.0f;
           const float alpha = mine ? ex2_approx(m_used - mx) : 1.0f;
           if (b > it.b0) {
-            if (!(ok = wwait(&T->p_empty[(g - 1) & 1], ((g - 1) >> 1) & 1))) break;
+            if (!(ok = wwait(T, &T->p_empty[tile][(g - 1) & 1], ((g - 1) >> 1) & 1))) break;
             tc_fence_after_sync();
             const uint64_t alpha2 = pack2(alpha, alpha);
 #pragma unroll 1
@@ -860,19 +865,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&T->p_full[sb]);
+        if (lane == 0) mbar_arrive(&T->p_full[tile][sb]);
       }
       if (!ok) break;
-      if (!(ok = wwait(&T->o_empty, (k & 1) ^ 1))) break;
-      T->row_l[half][t] = l_sum;
-      T->row_m[half][t] = m_used;
+      if (!(ok = wwait(T, &T->o_empty[tile], (kt++ & 1) ^ 1))) break;
+      T->row_l[tile][t] = l_sum;
+      T->row_m[tile][t] = m_used;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&T->o_full);
+      if (lane == 0) mbar_arrive(&T->o_full[tile]);
     }
     if (!ok && lane == 0) give_up();
   } else {
     // ---------------- K or V: codes to float16 ----------------
-    set_registers_down<56>();
+    set_registers_down<kRegsConvert>();
     const int is_v = (warp - 16) >> 2, wq = warp & 3;
     const uint8_t* cache = a.cache[is_v];
     constexpr int kRows = 128 / (D / 16);          // rows the four warps bring at a time
@@ -886,72 +891,90 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
                        2 * (kHalves == 2 ? lane >> 4 : lane >> 3);
     const int dim0 = half * 64 + c4 * 16;
     // (rows kRows apart are multiples of 8 apart: the same swizzle)
-    uint8_t* mine = skv + is_v * kTileBytes + half * kHalfBytes + row_in * 128;
+    uint8_t* mine = skv + half * kKHalf + row_in * 128;
     const int lo16 = ((2 * c4) ^ (row_in & 7)) * 16, hi16 = ((2 * c4 + 1) ^ (row_in & 7)) * 16;
-    uint8_t* raw = codes + (is_v * kU * 128 + (threadIdx.x & 127)) * 16;
+    uint8_t* raw = codes + is_v * kAhead * kCodeBytes + (threadIdx.x & 127) * 16;
     cache += dim0;
-    // (one copy a group of copies)
-    auto load = [&](uint32_t at, int u) {
-      const bool is = at != kNowhere;
-      copy16_if(is, raw + u * 128 * 16, cache + static_cast<size_t>(is ? at : 0) * D);
+    // codes of a block's rows on their way (one group of copies)
+    auto load = [&](const Places& p, uint8_t* dst) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const uint32_t at = p.at[u * kRows + row_in];
+        const bool is = at != kNowhere;
+        copy16_if(is, dst + u * 128 * 16, cache + static_cast<size_t>(is ? at : 0) * D);
+      }
+      copies_commit();
     };
-    bool ok = wwait_long(&T->place_full[0], 0), more = ok && T->places[0].keys > 0;
-    if (more) {
-      for (int u = 0; u < kU; ++u) load(T->places[0].at[u * kRows + row_in], u);
+    // places of the g-th block, if there is one (past the end: an empty group)
+    bool ok = true, more = true;
+    auto ahead = [&](int g) -> bool {
+      if (more) {
+        const int st = g % kPlaceRing;
+        if (!wwait_long(T, &T->place_full[st], (g / kPlaceRing) & 1)) return false;
+        more = T->places[st].keys > 0;
+        if (more) {
+          load(T->places[st], raw + (g % kAhead) * kCodeBytes);
+          return true;
+        }
+      }
+      copies_commit();
+      return true;
+    };
+    int n = 0;                                     // blocks whose codes are under way or here
+    for (; ok && n < kAhead; ++n) {
+      ok = ahead(n);
+      if (!more) break;
     }
-    for (int g = 0; ok && more; ++g) {
+    int total = more ? 1 << 30 : n;
+    if (!more)
+      for (int i = n; i < kAhead; ++i) copies_commit();
+    for (int g = 0; ok && g < total; ++g) {
       const Places& cur = T->places[g % kPlaceRing];
-      const Places& nxt = T->places[(g + 1) % kPlaceRing];
       const int place = 2 * g + is_v, slot = place % kSlots;
-      ok = wwait_long(&T->place_full[(g + 1) % kPlaceRing], ((g + 1) / kPlaceRing) & 1) &&
-           wwait(&T->kv_empty[slot], ((place / kSlots) & 1) ^ 1);
-      if (!ok) break;
-      more = nxt.keys > 0;
-      uint8_t* tile = mine + (slot - is_v) * kTileBytes;
-      const bool some = is_v != 0 && cur.key0 + kBK > cur.all;   // keys that not all rows see
-#pragma unroll 1
-      for (int u0 = 0; u0 < kU; u0 += 4) {         // (four rows' latencies at once)
-        uint4 x[4];
-        uint32_t by[4], at[4];
-        copies_wait<kU - 4>();
+      if (!(ok = wwait(T, &T->kv_empty[slot], ((place / kSlots) & 1) ^ 1))) break;
+      copies_wait<kAhead - 1>();
+      const uint8_t* src = raw + (g % kAhead) * kCodeBytes;
+      uint4 x[kU];
+      uint32_t by[kU];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int row = (u0 + u) * kRows + row_in;
-          x[u] = *reinterpret_cast<const uint4*>(raw + (u0 + u) * 128 * 16);
-          by[u] = (cur.by[row] >> (16 * is_v) & 0xffffu) * 0x10001u;
-          at[u] = nxt.at[row];                     // (no more: nowhere)
+      for (int u = 0; u < kU; ++u) {
+        x[u] = *reinterpret_cast<const uint4*>(src + u * 128 * 16);
+        by[u] = (cur.by[u * kRows + row_in] >> (16 * is_v) & 0xffffu) * 0x10001u;
+      }
+      if (is_v != 0 && cur.key0 + kBK > cur.all) {
+        // keys that not every row sees: their NaN values are taken out and noted
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int key = cur.key0 + u * kRows + row_in - cur.all;
+          if (key >= 0 && any_nan(x[u])) x[u] = without_nan(x[u], T, cur.ring, key, dim0);
         }
-        if (some) {
-          // their NaN values are taken out and noted
+      }
+      uint8_t* dst = mine + slot * kKBytes;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int key = cur.key0 + (u0 + u) * kRows + row_in - cur.all;
-            if (key >= 0 && any_nan(x[u])) x[u] = without_nan(x[u], T, cur.ring, key, dim0);
-          }
+      for (int u = 0; u < kU; ++u) {
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[2 * i] = mul_h2(halves2(w[i]), by[u]);
+          h[2 * i + 1] = mul_h2(halves2(w[i] >> 16), by[u]);
         }
-        uint8_t* dst = tile + u0 * kRows * 128;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-          uint32_t h[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            h[2 * i] = mul_h2(halves2(w[i]), by[u]);
-            h[2 * i + 1] = mul_h2(halves2(w[i] >> 16), by[u]);
-          }
-          *reinterpret_cast<uint4*>(dst + u * kRows * 128 + lo16) =
-              make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(dst + u * kRows * 128 + hi16) =
-              make_uint4(h[4], h[5], h[6], h[7]);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) load(at[u], u0 + u);
+        *reinterpret_cast<uint4*>(dst + u * kRows * 128 + lo16) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(dst + u * kRows * 128 + hi16) =
+            make_uint4(h[4], h[5], h[6], h[7]);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(&T->kv_full[slot]);
         mbar_arrive(&T->place_empty[g % kPlaceRing]);
+      }
+      if (total == 1 << 30) {
+        ok = ahead(g + kAhead);
+        if (!more) total = g + kAhead;
+      } else {
+        copies_commit();
       }
     }
     copies_wait<0>();                              // copies land before the CTA may exit
@@ -965,17 +988,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
   if (warp == 1) tmem_dealloc(T->tmem_base, kTmemCols);
 }
 
-// Rows per tile: one where requests have one row each, on average (a tile's
-// rows are multiplied whether or not they are the request's), else as many as fit.
-int rows_per_tile(const pctree_kv8_attn_config& c) {
-  const int fit = 128 / (c.Hq / c.Hkv);
+// Rows per unit: one where requests have one row each, on average (a tile's rows
+// are multiplied whether or not they are the request's), else as many as fit in two
+// tiles.
+int rows_per_tile(const pctree_kv8_attn_config& c) { return 128 / (c.Hq / c.Hkv); }
+int rows_per_unit(const pctree_kv8_attn_config& c) {
+  const int fit = 2 * rows_per_tile(c);
   return c.total_rows <= c.batch ? 1 : fit < c.total_rows ? fit : c.total_rows;
 }
 
 // Whether the planner can count the most work a configuration can have in 32
 // bits.
 bool work_ok(const pctree_kv8_attn_config& c) {
-  const long long units = c.total_rows / rows_per_tile(c) + 1ll + c.batch;
+  const long long units = c.total_rows / rows_per_unit(c) + 1ll + c.batch;
   const long long blocks =
       (static_cast<long long>(c.max_pages) * c.page_size + kBK - 1) / kBK + kUnitCharge;
   return units * blocks < (1ll << 32) / c.Hkv - 1024;
@@ -1003,26 +1028,36 @@ pctree_status attn8_check(const pctree_kv8_attn_config* c) {
   return PCTREE_OK;
 }
 
+// Whether a tile of one row's heads fits the token kernel.
+bool takes_tokens(const pctree_kv8_attn_config& c) {
+  return rows_per_unit(c) == 1 && c.Hq / c.Hkv <= kTokenHeads;
+}
+
 template <int D, bool F16>
-pctree_status attn8_launch(const Kv8AttnArgs& a, int num_sms, cudaStream_t stream) {
-  constexpr size_t smem =
-      (2 + kSlots) * (D / 64) * static_cast<size_t>(kHalfBytes) + sizeof(Tail) + 1024;   // Q, K and V, codes
+pctree_status attn8_launch(const Kv8AttnArgs& a, bool tokens, int num_sms, cudaStream_t stream) {
+  constexpr size_t smem = (D / 64) * static_cast<size_t>(2 * kQHalf + kSlots * kKHalf) +
+                          2 * kAhead * static_cast<size_t>(kBK) * D + sizeof(Tail) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
-  static SmemLimit limit;
-  const void* fn = reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>);
-  if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t lc = {};
   const unsigned ctas = static_cast<unsigned>(num_sms < kMaxCtas ? num_sms : kMaxCtas);
   lc.gridDim = dim3(ctas);
-  lc.blockDim = dim3(kThreads);
-  lc.dynamicSmemBytes = smem;
   lc.stream = stream;
   lc.attrs = attr;
   lc.numAttrs = 1;
-  if (cudaLaunchKernelEx(&lc, kv8_attn_kernel<D, F16>, a) != cudaSuccess) return PCTREE_ERR_CUDA;
+  if (tokens) {
+    const cudaError_t e = a.G <= 8 ? launch_tokens<D, F16, 1>(lc, a) : launch_tokens<D, F16, 2>(lc, a);
+    if (e != cudaSuccess) return PCTREE_ERR_CUDA;
+  } else {
+    static SmemLimit limit;
+    if (limit.ensure(reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>), smem) != cudaSuccess)
+      return PCTREE_ERR_CUDA;
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = smem;
+    if (cudaLaunchKernelEx(&lc, kv8_attn_kernel<D, F16>, a) != cudaSuccess) return PCTREE_ERR_CUDA;
+  }
   const JoinArgs j = {a.part_o, a.part_ml, a.join, a.out, a.G, a.Hq};
   lc.gridDim = dim3(ctas, kJoinCtas);
   lc.blockDim = dim3(kJoinThreads);
@@ -1076,7 +1111,7 @@ pctree_status pctree_kv8_attention(const pctree_kv8_attn_config* cfg, const void
   Kv8AttnArgs a{};
   a.units = {{row_start, n_rows, prefix_len, page_table, c.batch, c.total_rows, c.page_size,
               c.n_pages, c.max_pages},
-             c.Hkv, rows_per_tile(c), parent != nullptr ? PCTREE_ATTN_MAX_N : 1 << 30, kBK};
+             c.Hkv, rows_per_unit(c), parent != nullptr ? PCTREE_ATTN_MAX_N : 1 << 30, kBK};
   a.blocks = kv8_blocks(c.page_size, c.scale_block);
   a.q = static_cast<const uint16_t*>(q);
   a.cache[0] = static_cast<const uint8_t*>(k_cache);
@@ -1094,14 +1129,16 @@ pctree_status pctree_kv8_attention(const pctree_kv8_attn_config* cfg, const void
   a.Hq = c.Hq;
   a.G = c.Hq / c.Hkv;
   a.by_G = fast_div(a.G);
+  a.tile_rows = std::min(rows_per_tile(c), a.units.npt);
   a.scale_log2 = static_cast<float>(static_cast<double>(c.scale) * 1.4426950408889634);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
-  const bool f16 = c.dtype == PCTREE_F16;
+  const bool f16 = c.dtype == PCTREE_F16, tokens = takes_tokens(c);
+  if (tokens) a.units.block_keys = kTokenBlock;
   if (c.D == 64)
-    return f16 ? attn8_launch<64, true>(a, num_sms, stream)
-               : attn8_launch<64, false>(a, num_sms, stream);
-  return f16 ? attn8_launch<128, true>(a, num_sms, stream)
-             : attn8_launch<128, false>(a, num_sms, stream);
+    return f16 ? attn8_launch<64, true>(a, tokens, num_sms, stream)
+               : attn8_launch<64, false>(a, tokens, num_sms, stream);
+  return f16 ? attn8_launch<128, true>(a, tokens, num_sms, stream)
+             : attn8_launch<128, false>(a, tokens, num_sms, stream);
 }
 
 }  // extern "C"

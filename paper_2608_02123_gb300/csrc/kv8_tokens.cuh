@@ -1,0 +1,370 @@
+// Attention over a cache in 8 bits for requests of one new row: a unit is the G
+// query heads of a row that share a KV head, few against a tile of 128 rows.
+//
+// Every warp works for itself on 16 keys at a time, from registers: with m16n8k16
+// products whose first operand is the cache, S^T = K Q^T has the keys as its rows
+// and the query heads as its (8) columns, and O^T += V^T P^T the dims.  Since the
+// products' inner index may be permuted as long as both sides agree, a lane's
+// share of K is 16 neighbouring dims of a key and of V 16 neighbouring dims of
+// four keys: codes are widened where they were loaded, without shared memory.
+// (tcgen05 would take them from there, widened, for tiles of 128 rows of which G
+// are real: the kernel for many rows takes 245 us for the batch below.)
+//
+// P is relative to the running maximum of score + exponent of the value's scale, so
+// that P V is a product of P with the codes themselves and P fits float16 whatever
+// the scales: 2^7 times, down to 2^-31 of the maximum.  A row's sum adds P 2^-e in
+// float32.
+//
+// A CTA's pieces are kv_pieces.cuh's, planned by every warp alike; a piece's keys
+// are dealt out among its warps, whose (max, sum, O) are added up in order.
+#pragma once
+
+#include "kv8.cuh"
+#include "kv_pieces.cuh"
+
+namespace pct {
+namespace {
+
+struct Kv8AttnArgs {
+  Units units;
+  Kv8Blocks blocks;
+  const uint16_t* q;
+  const uint8_t* cache[2];                   // keys, values
+  const uint8_t* scale[2];
+  const int32_t* parent;                     // NULL: causal
+  uint16_t* out;
+  float* part_o;                             // as in JoinArgs
+  float2* part_ml;
+  PieceJoin* join;
+  int32_t* status;
+  long long q_stride;
+  int Hq, G;
+  int tile_rows;                             // a unit's first rows; the rest are tile 1's
+  FastDiv by_G;
+  float scale_log2;
+};
+
+__device__ __forceinline__ void report(int32_t* status, int code) {
+  if (status != nullptr) atomicCAS(status, 0, code);
+}
+
+constexpr int kTokenThreads = 512;
+constexpr int kTokenWarps = kTokenThreads / 32;
+constexpr int kTokenBlock = 128;             // keys per block of work
+constexpr int kTokenHeads = 16;              // query heads of a unit, at most
+constexpr float kTokenBits = 7.0f;           // P is 2^7 times what it is relative to
+
+// D (+)= A B of 16 x 8 x 16 float16 values, float32 sums.
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+
+// N words, or zeros if not wanted.  (Predicated inside: a branch around the load
+// would end in a copy of its result, which waits for it.)
+template <int N>
+__device__ __forceinline__ void load_if(uint32_t (&v)[N], bool wanted, const uint8_t* p) {
+  if constexpr (N == 4) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n mov.u32 %0, 0;\n mov.u32 %1, 0;\n"
+        " mov.u32 %2, 0;\n mov.u32 %3, 0;\n"
+        " @p ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n}\n"
+        : "=&r"(v[0]), "=&r"(v[1]), "=&r"(v[2]), "=&r"(v[3])
+        : "l"(p), "r"(static_cast<uint32_t>(wanted)));
+  } else {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %3, 0;\n mov.u32 %0, 0;\n mov.u32 %1, 0;\n"
+        " @p ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];\n}\n"
+        : "=&r"(v[0]), "=&r"(v[1])
+        : "l"(p), "r"(static_cast<uint32_t>(wanted)));
+  }
+}
+
+template <int D, int NT>
+struct TokenShared {
+  float o[kTokenWarps][8 * NT][D + 4];
+  float m[kTokenWarps][8 * NT], l[kTokenWarps][8 * NT];
+  unsigned upto[PCTREE_KV_MAX_BATCH];
+};
+
+// NT: groups of 8 query heads.
+template <int D, bool F16, int NT>
+__global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs a) {
+  constexpr int kC = D / 64;                     // 16-byte chunks of a key's row a lane has
+  constexpr int kVWords = D / 32;                // words of V a lane has of a key
+  constexpr int kTiles = D / 16;                 // of O^T's rows
+  extern __shared__ uint8_t smem_raw[];
+  TokenShared<D, NT>& sh = *reinterpret_cast<TokenShared<D, NT>*>(smem_raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  const KvRows& rows = a.units.rows;
+  const int Hkv = a.units.Hkv;
+  pdl_launch_dependents();
+  pdl_wait();
+  count_work<kTokenThreads>(a.units, sh.upto, [&](int code) {
+    if (blockIdx.x == 0) report(a.status, code);
+  });
+
+  auto piece = [&](const Piece& it) -> bool {
+    // this lane's share of Q: head g, the dims of its chunks
+    uint32_t qf[NT][kC][4][2];
+    float sc[NT][2];                             // of the heads 2 t and 2 t + 1 (log2 units)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int h = 8 * n + g;
+      float row_sc = a.scale_log2;
+      const uint16_t* q =
+          a.q + it.row0 * a.q_stride + (it.kvh * a.G + min(h, a.G - 1)) * D + t * 16;
+      uint32_t top2 = 0;
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const uint4 lo = *reinterpret_cast<const uint4*>(q + c * 64);
+        const uint4 hi = *reinterpret_cast<const uint4*>(q + c * 64 + 8);
+        const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          qf[n][c][i / 2][i & 1] = h < a.G ? w[i] : 0;
+          top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
+        }
+      }
+      if constexpr (!F16) {
+        // to float16: the row's largest to 2^14 .. 2^15 (as in the kernel for many rows)
+        top2 = __vmaxu2(top2, __shfl_xor_sync(kFull, top2, 1));
+        top2 = __vmaxu2(top2, __shfl_xor_sync(kFull, top2, 2));
+        const int top = static_cast<int>(max(top2 >> 16, top2 & 0xffffu) >> 7) - 127;
+        const int e = max(-100, min(126, top)) - 14;
+        const float by = exp2_of(-e);
+        row_sc *= exp2_of(e);
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float2 f = unpack16<false>(qf[n][c][i / 2][i & 1]);
+            qf[n][c][i / 2][i & 1] = pack16<true>(f.x * by, f.y * by);
+          }
+      }
+      sc[n][0] = __shfl_sync(kFull, row_sc, 8 * t);
+      sc[n][1] = __shfl_sync(kFull, row_sc, 8 * t + 4);
+    }
+    float o[NT][kTiles][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
+    }
+    const int stop = min(it.key_end, it.b1 * kTokenBlock);
+    // lane i < 16 finds the place and the scales of a tile's key i (the others the
+    // same again): -1 past the end and in pages that are none
+    uint32_t at = 0xffffffffu, scales = 0;
+    auto find = [&](int key0) {
+      const int key = key0 + (lane & 15);
+      at = 0xffffffffu;
+      scales = kExpBias | kExpBias << 8;
+      if (key < stop) {
+        const int entry = div_by(key, a.blocks.page), off = key - entry * rows.page_size;
+        const int page = kv_page(rows, it.r, entry);
+        if (page >= 0) {
+          at = (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh;
+          const long long s = (static_cast<long long>(page) * a.blocks.per_page +
+                               (off >> a.blocks.shift)) * Hkv + it.kvh;
+          const uint32_t k = __ldg(a.scale[0] + s), v = __ldg(a.scale[1] + s);
+          if (!scale_ok(k) || !scale_ok(v)) report(a.status, PCTREE_ERR_INVALID_ARG);
+          scales = k | v << 8;
+        } else {
+          report(a.status, PCTREE_ERR_INVALID_ARG);
+        }
+      }
+    };
+    uint32_t k_raw[2][kC][4], v_raw[4][kVWords];
+    auto load_k = [&]() {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t p = __shfl_sync(kFull, at, g + 8 * i);
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+          load_if<4>(k_raw[i][c], p != 0xffffffffu,
+                     a.cache[0] + static_cast<size_t>(p) * D + c * 64 + t * 16);
+      }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t p = __shfl_sync(kFull, at, 2 * t + (i & 1) + 8 * (i >> 1));
+        load_if<kVWords>(v_raw[i], p != 0xffffffffu,
+                         a.cache[1] + static_cast<size_t>(p) * D + g * (D / 8));
+      }
+    };
+    const int first = it.b0 * kTokenBlock + warp * 16;
+    constexpr int kStep = 16 * kTokenWarps;
+    if (first < stop) {
+      find(first);
+      load_k();
+      load_v();
+    }
+#pragma unroll 1
+    for (int key0 = first; key0 < stop; key0 += kStep) {
+      // K Q^T, then the next K on its way
+      const uint32_t here = scales;
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x = k_raw[0][c][w], y = k_raw[1][c][w];
+          const uint32_t a0 = halves2(x), a1 = halves2(y), a2 = halves2(x >> 16),
+                         a3 = halves2(y >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qf[n][c][w][0], qf[n][c][w][1]);
+        }
+      find(key0 + kStep);
+      load_k();
+      // scores with the exponents of K's and V's scales; keys past the end are -inf
+      uint32_t p16[NT][2];
+      float v_off[2], k_by[2], v_by[2];
+      bool in[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t sc2 = __shfl_sync(kFull, here, g + 8 * i);
+        const int ev = scale_exp(sc2 >> 8);
+        k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
+        v_by[i] = exp2_of(-ev);
+        v_off[i] = static_cast<float>(ev);
+        in[i] = key0 + g + 8 * i < stop;
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x[4];
+        bool look = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = in[i >> 1] ? fmaf(s[n][i], sc[n][i & 1] * k_by[i >> 1], v_off[i >> 1]) : -INFINITY;
+          look = look || x[i] > m[n][i & 1] + 8.0f;
+        }
+        if (__any_sync(kFull, look)) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float top = fmaxf(x[r], x[2 + r]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
+            if (top > m[n][r]) {
+              const float alpha = ex2_approx(m[n][r] - top);
+              m[n][r] = top;
+              l[n][r] *= alpha;
+#pragma unroll
+              for (int i = 0; i < kTiles; ++i) {
+                o[n][i][r] *= alpha;
+                o[n][i][2 + r] *= alpha;
+              }
+            }
+          }
+        }
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
+          p[i] = ex2_approx(x[i] - ref + kTokenBits);
+          l[n][i & 1] = fmaf(p[i], v_by[i >> 1], l[n][i & 1]);
+        }
+        p16[n][0] = transposed8x8(pack16<true>(p[0], p[1]));
+        p16[n][1] = transposed8x8(pack16<true>(p[2], p[3]));
+      }
+      // V^T P^T: pairs of keys of a dim, two dims a word
+#pragma unroll
+      for (int w = 0; w < kVWords; ++w)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t sel = j == 0 ? 0x5140u : 0x7362u;
+          const uint32_t lo = __byte_perm(v_raw[0][w], v_raw[1][w], sel);
+          const uint32_t hi = __byte_perm(v_raw[2][w], v_raw[3][w], sel);
+          const uint32_t a0 = halves2(lo), a1 = halves2(lo >> 16), a2 = halves2(hi),
+                         a3 = halves2(hi >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + j], a0, a1, a2, a3, p16[n][0], p16[n][1]);
+        }
+      load_v();
+    }
+    // the warps' parts, in order
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][r] += __shfl_xor_sync(kFull, l[n][r], d);
+        const int h = 8 * n + 2 * t + r;
+        if (g == 0) {
+          sh.m[warp][h] = m[n][r];
+          sh.l[warp][h] = l[n][r];
+        }
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+          *reinterpret_cast<float2*>(&sh.o[warp][h][g * (D / 8) + 2 * i]) =
+              make_float2(o[n][i][r], o[n][i][2 + r]);
+      }
+    }
+    __syncthreads();
+    const bool whole = it.b0 == 0 && it.b1 == it.nblk;
+    const size_t part = static_cast<size_t>(blockIdx.x) * 2 + (it.b0 == 0 ? 1 : 0);
+    constexpr int kQuads = D / 4;
+    for (int i = threadIdx.x; i < a.G * kQuads; i += kTokenThreads) {
+      const int h = i / kQuads, d = (i - h * kQuads) * 4;
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kTokenWarps; ++w)
+        if (sh.l[w][h] != 0.0f) top = fmaxf(top, sh.m[w][h]);
+      float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < kTokenWarps; ++w) {
+        const float lw = sh.l[w][h];
+        if (lw == 0.0f) continue;                // (no finite score, or no keys)
+        const float f = exp2f(sh.m[w][h] - top);
+        const float4 v = *reinterpret_cast<const float4*>(&sh.o[w][h][d]);
+        sum = fmaf(lw, f, sum);
+        y.x = fmaf(v.x, f, y.x);
+        y.y = fmaf(v.y, f, y.y);
+        y.z = fmaf(v.z, f, y.z);
+        y.w = fmaf(v.w, f, y.w);
+      }
+      if (whole) {
+        const float inv = 1.0f / sum;            // (no finite score, sum = 0: NaN)
+        *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(it.row0) * a.Hq + it.kvh * a.G + h) * D +
+                                  d) = make_uint2(pack16<F16>(y.x * inv, y.y * inv),
+                                                  pack16<F16>(y.z * inv, y.w * inv));
+      } else {
+        reinterpret_cast<float4*>(a.part_o)[(part * kQuads + d / 4) * kUnitRows + h] = y;
+        if (d == 0) a.part_ml[part * kUnitRows + h] = make_float2(sum != 0.0f ? top : -INFINITY, sum);
+      }
+    }
+    __syncthreads();
+    return true;
+  };
+  PieceJoin join;
+  plan_pieces(a.units, sh.upto, join, piece);
+  if (threadIdx.x == 0) a.join[blockIdx.x] = join;
+}
+
+template <int D, bool F16, int NT>
+cudaError_t launch_tokens(cudaLaunchConfig_t lc, const Kv8AttnArgs& a) {
+  static SmemLimit limit;
+  const cudaError_t e = limit.ensure(reinterpret_cast<const void*>(kv8_token_kernel<D, F16, NT>),
+                                     sizeof(TokenShared<D, NT>));
+  if (e != cudaSuccess) return e;
+  lc.blockDim = dim3(kTokenThreads);
+  lc.dynamicSmemBytes = sizeof(TokenShared<D, NT>);
+  return cudaLaunchKernelEx(&lc, kv8_token_kernel<D, F16, NT>, a);
+}
+
+}  // namespace
+}  // namespace pct

@@ -17,6 +17,7 @@ namespace pct {
 constexpr int kUnitCharge = 1;               // blocks' worth of a unit's fixed cost
 constexpr int kMinStretch = 2;               // of work per CTA
 constexpr int kMaxCtas = 152;                // SMs of a GB300: partials a workspace holds
+constexpr int kUnitRows = 256;               // (row, query head) pairs of a unit, at most
 
 // A piece of a unit: blocks b0 .. b1-1 of the nblk of a tile whose keys end at
 // key_end.  nblk = 0: no more pieces.
@@ -193,8 +194,8 @@ __device__ __forceinline__ bool plan_pieces(const Units& u, const unsigned* upto
 }
 
 struct JoinArgs {
-  const float* part_o;    // [CTA][2][D / 4][128 rows][4]; a CTA's first piece, its last
-  const float2* part_ml;  // [CTA][2][128]  (max in log2 units, sum)
+  const float* part_o;    // [CTA][2][D / 4][kUnitRows][4]; a CTA's first piece, its last
+  const float2* part_ml;  // [CTA][2][kUnitRows]  (max in log2 units, sum)
   const PieceJoin* join;  // [CTA]
   uint16_t* out;
   int G, Hq;
@@ -230,8 +231,8 @@ __global__ void __launch_bounds__(kJoinThreads, 4) join_pieces_kernel(JoinArgs a
         const bool in = s0 + u < j.pieces;
         // the first piece is its CTA's last, every other one its CTA's first
         const size_t part = static_cast<size_t>(c0 + s0 + u) * 2 + (s0 + u == 0 ? 1 : 0);
-        w[u] = in ? a.part_ml[part * 128 + row] : make_float2(-INFINITY, 0.0f);
-        v[u] = in ? po[(part * kQuads + quad) * 128 + row] : acc;
+        w[u] = in ? a.part_ml[part * kUnitRows + row] : make_float2(-INFINITY, 0.0f);
+        v[u] = in ? po[(part * kQuads + quad) * kUnitRows + row] : acc;
       }
       float mn = m;
 #pragma unroll
@@ -270,7 +271,7 @@ struct PieceWs {
 };
 inline PieceWs piece_ws(int D) {
   PieceWs w{};
-  const size_t slots = static_cast<size_t>(kMaxCtas) * 2 * 128;
+  const size_t slots = static_cast<size_t>(kMaxCtas) * 2 * kUnitRows;
   w.part_o = 0;
   w.part_ml = w.part_o + slots * D * sizeof(float);
   w.join = w.part_ml + slots * sizeof(float2);
