@@ -13,11 +13,12 @@
 //   warp 2        PV issuer: O += P V of each tile (P read from TMEM)
 //   warp 3        where the keys of a block lie and what scales they have, up to
 //                 kPlaceRing blocks ahead
-//   warps 4..7    the next unit's Q and its rows' ancestors, once the last S of a
-//                 piece is done; then O of the finished piece to rows of out or to
-//                 the piece's partial
-//   warps 8..15   softmax, four warps a tile and a thread a row: S is read from
-//                 TMEM, masked and scaled, P = 2^(s - m_used) written back over it
+//   warps 4..7    the next unit's Q as it is and its rows' ancestors, once the last S
+//                 of a piece is done; then O of the finished piece to rows of out or
+//                 to the piece's partial
+//   warps 8..15   softmax, four warps a tile and a thread a row: Q to float16, then S
+//                 is read from TMEM, masked and scaled, P = 2^(s - m_used) written
+//                 back over it
 //   warps 16..19  K, and warps 20..23 V: codes to shared memory two blocks ahead,
 //                 16 bytes a thread and copy, and to float16 (128-byte swizzle, 64
 //                 dims a half)
@@ -71,7 +72,7 @@ struct Places {
 
 struct Tail {
   uint64_t place_full[kPlaceRing], place_empty[kPlaceRing];
-  uint64_t q_full[2], q_empty;               // (full: by piece parity)
+  uint64_t q_raw[2], q_full[2], q_empty;     // (raw: by piece parity; full: by tile)
   uint64_t kv_full[kSlots], kv_empty[kSlots];
   uint64_t s_full[2][2], p_full[2][2], p_empty[2][2];      // [tile][buffer]
   uint64_t o_full[2], o_empty[2];            // [tile]
@@ -83,7 +84,7 @@ struct Tail {
   Piece item[kItemRing];
   Places places[kPlaceRing];
   float row_l[2][128], row_m[2][128];        // [tile]
-  float row_scale[2][2][128];                // of Q's rows (log2 units), [piece parity][tile]
+  float row_scale[2][128];                   // of Q's rows (log2 units), [tile]
   // NaN values at keys that only some rows of the unit see, by place in the item
   // ring: 16 bits of a group of dims, the group << 16, the key (counted from the
   // first that not every row sees) << 20; their number and the first such key.
@@ -252,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     }
     mbar_init(&T->q_empty, 1);
     for (int s = 0; s < 2; ++s) {
+      mbar_init(&T->q_raw[s], 4);
       mbar_init(&T->q_full[s], 4);
       for (int t = 0; t < 2; ++t) {
         mbar_init(&T->s_full[t][s], 1);
@@ -326,12 +328,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       constexpr uint32_t idS = idesc_f16(128, kBK);
       const uint64_t q_desc = desc_kmajor_sw128(smem_u32(sq));
       const uint64_t k_desc = desc_kmajor_sw128(smem_u32(skv));
-      int g = 0, gt[2] = {0, 0};                   // blocks, and of each tile
+      int g = 0, gt[2] = {0, 0}, kt[2] = {0, 0};   // blocks, of each tile; pieces of each
       bool ok = true;
       Piece it;
       for (int k = 0; ok; ++k) {
         if (!(ok = fetch_one(k, it)) || it.nblk == 0) break;
-        if (!(ok = wait_one(T, &T->q_full[k & 1], (k >> 1) & 1))) break;
         const int tiles = it.n_rows > a.tile_rows ? 2 : 1;
         for (int b = it.b0; ok && b < it.b1; ++b, ++g) {
           const int slot = (2 * g) % kSlots;
@@ -340,7 +341,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
 #pragma unroll 1
           for (int t = 0; t < tiles; ++t) {
             const int n = t == 0 ? gt[0]++ : gt[1]++, sb = n & 1;
-            if (!(ok = wait_one(T, &T->p_empty[t][sb], ((n >> 1) & 1) ^ 1))) break;
+            ok = wait_one(T, &T->p_empty[t][sb], ((n >> 1) & 1) ^ 1) &&
+                 (b > it.b0 || wait_one(T, &T->q_full[t], (t == 0 ? kt[0]++ : kt[1]++) & 1));
+            if (!ok) break;
             tc_fence_after_sync();
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
@@ -552,58 +555,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       const uint16_t* q = a.q + it.row0 * a.q_stride + it.kvh * a.G * D + c * 8;
       auto place_of = [&](int row) {               // of a row of the unit
         const int n = div_by(row, a.by_G);
-        return q + n * a.q_stride + (row - n * a.G) * D;
+        return reinterpret_cast<const uint8_t*>(q + n * a.q_stride + (row - n * a.G) * D);
       };
-      // on their way to L2 while the last S is under way
-      for (int row = t; row < rows; row += 128) {
-        const uint16_t* p = place_of(row) - c * 8;
-        for (int i = 0; i < D; i += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + i));
-      }
       if (!wwait_long(T, &T->q_empty, (k & 1) ^ 1)) return false;
-      constexpr int kDeep = 4;                     // rows in flight
       // rows past the last one's are zeros up to the end of their tile
       const int all = it.n_rows > a.tile_rows ? 2 * R : R;
-      // (few instructions: they come from memory again for every piece)
-#pragma unroll 1
-      for (int r0 = t / kLanes; r0 < all + t / kLanes; r0 += kDeep * kRows) {
-        uint4 x[kDeep];
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u)
-          x[u] = *reinterpret_cast<const uint4*>(place_of(min(r0 + u * kRows, rows - 1)));
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-          const int row = r0 + u * kRows;
-          const uint32_t keep = row < rows ? ~0u : 0u;
-          uint32_t w[4] = {x[u].x & keep, x[u].y & keep, x[u].z & keep, x[u].w & keep};
-          float sc = a.scale_log2;
-          if constexpr (!F16) {
-            // (magnitudes of bfloat16 are ordered as the integers they are)
-            uint32_t top2 = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
-#pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1)
-              top2 = __vmaxu2(top2, __shfl_xor_sync(kFull, top2, o));
-            const int top = static_cast<int>(max(top2 >> 16, top2 & 0xffffu) >> 7) - 127;
-            // (a row with an infinity or NaN is NaN in the end, whatever its others are)
-            const int e = max(-100, min(126, top)) - 14;
-            const float by = exp2_of(-e);
-            sc *= exp2_of(e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 f = unpack16<false>(w[i]);
-              w[i] = pack16<true>(f.x * by, f.y * by);
-            }
-          }
-          if (row < all) {
-            const int tile = row >= R ? 1 : 0, in = row - tile * R;
-            *reinterpret_cast<uint4*>(sq + tile * kQBytes + (c >> 3) * kQHalf + in * 128 +
-                                      (((c & 7) ^ (in & 7)) * 16)) =
-                make_uint4(w[0], w[1], w[2], w[3]);
-            if (c == 0) T->row_scale[qb][tile][in] = sc;
-          }
-        }
+#pragma unroll 2
+      for (int row = t / kLanes; row < all; row += kRows) {
+        const int tile = row >= R ? 1 : 0, in = row - tile * R;
+        copy16_if(row < rows,
+                  sq + tile * kQBytes + (c >> 3) * kQHalf + in * 128 + (((c & 7) ^ (in & 7)) * 16),
+                  place_of(min(row, rows - 1)));
       }
+      copies_commit();
       if (a.parent != nullptr) {
         // ancestors of the unit's rows, from the parents of the request's first rows
         const int n = it.j0 + it.n_rows;
@@ -624,9 +588,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
           for (int m = it.j0 + j; m >= 0; m = T->par[m]) path[m >> 5] |= 1u << (m & 31);
         }
       }
+      copies_wait<0>();
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&T->q_full[qb]);
+      if (lane == 0) mbar_arrive(&T->q_raw[qb]);
       return true;
     };
     Piece it;
@@ -738,7 +703,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     const int tile = (warp - 8) >> 2;
     const int quad = warp & 3;
     const int t = quad * 32 + lane;
-    const int R = a.G * a.tile_rows;
     const int nl = tile * a.tile_rows + div_by(t, a.by_G);     // row of the unit
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const uint32_t o_col = lane_base + kOCol + tile * D;
@@ -749,9 +713,44 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (!(ok = peek_warp(k, it))) break;
       release_warp(k);
       if (it.nblk == 0) break;
-      if (!(ok = wwait_long(T, &T->q_full[k & 1], (k >> 1) & 1))) break;
+      if (!(ok = wwait_long(T, &T->q_raw[k & 1], (k >> 1) & 1))) break;
       if (it.n_rows <= tile * a.tile_rows) continue;
-      const float sc = t < R ? T->row_scale[k & 1][tile][t] : a.scale_log2;
+      float sc = a.scale_log2;
+      if constexpr (!F16) {
+        // this warp's 32 rows of the tile to float16, the row's largest to 2^14 .. 2^15
+        constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+        const int c = lane % kLanes;
+#pragma unroll 2
+        for (int r0 = 0; r0 < 32; r0 += kRows) {
+          const int row = quad * 32 + r0 + lane / kLanes;
+          uint4* at = reinterpret_cast<uint4*>(sq + tile * kQBytes + (c >> 3) * kQHalf + row * 128 +
+                                               (((c & 7) ^ (row & 7)) * 16));
+          const uint4 x = *at;
+          uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          // (magnitudes of bfloat16 are ordered as the integers they are)
+          uint32_t top2 = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1)
+            top2 = __vmaxu2(top2, __shfl_xor_sync(kFull, top2, o));
+          const int top = static_cast<int>(max(top2 >> 16, top2 & 0xffffu) >> 7) - 127;
+          // (a row with an infinity or NaN is NaN in the end, whatever its others are)
+          const int e = max(-100, min(126, top)) - 14;
+          const float by = exp2_of(-e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack16<false>(w[i]);
+            w[i] = pack16<true>(f.x * by, f.y * by);
+          }
+          *at = make_uint4(w[0], w[1], w[2], w[3]);
+          if (c == 0) T->row_scale[tile][row] = a.scale_log2 * exp2_of(e);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        sc = T->row_scale[tile][t];
+      }
+      if (lane == 0) mbar_arrive(&T->q_full[tile]);
       // keys this row sees: slots below `end`, and of those from the prefix on (in
       // a tree) its ancestors
       const int end = min(it.key_end, it.prefix + it.j0 + nl + 1);
