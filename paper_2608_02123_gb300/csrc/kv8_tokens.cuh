@@ -48,7 +48,7 @@ __device__ __forceinline__ void report(int32_t* status, int code) {
   if (status != nullptr) atomicCAS(status, 0, code);
 }
 
-constexpr int kTokenThreads = 512;
+constexpr int kTokenThreads = 384;
 constexpr int kTokenWarps = kTokenThreads / 32;
 constexpr int kTokenBlock = 128;             // keys per block of work
 constexpr int kTokenHeads = 16;              // query heads of a unit, at most
@@ -164,58 +164,57 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
     const int stop = min(it.key_end, it.b1 * kTokenBlock);
-    // lane i < 16 finds the place and the scales of a tile's key i (the others the
-    // same again): -1 past the end and in pages that are none
-    uint32_t at = 0xffffffffu, scales = 0;
-    auto find = [&](int key0) {
+    // What is on its way of a tile of keys, two tiles ahead of its use: its codes and
+    // (lane i < 16) its key i's scales and place, none past the end and in pages that
+    // are none.  Page numbers are read a tile earlier.
+    constexpr uint32_t kNone = 0xffffffffu;
+    struct Ahead {
+      uint32_t k[2][kC][4], v[4][kVWords];
+      uint32_t scales, at;
+    };
+    int page = -2;                               // -2: past the end
+    auto find_page = [&](int key0) {
       const int key = key0 + (lane & 15);
-      at = 0xffffffffu;
-      scales = kExpBias | kExpBias << 8;
-      if (key < stop) {
-        const int entry = div_by(key, a.blocks.page), off = key - entry * rows.page_size;
-        const int page = kv_page(rows, it.r, entry);
-        if (page >= 0) {
-          at = (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh;
-          const long long s = (static_cast<long long>(page) * a.blocks.per_page +
-                               (off >> a.blocks.shift)) * Hkv + it.kvh;
-          const uint32_t k = __ldg(a.scale[0] + s), v = __ldg(a.scale[1] + s);
-          if (!scale_ok(k) || !scale_ok(v)) report(a.status, PCTREE_ERR_INVALID_ARG);
-          scales = k | v << 8;
-        } else {
-          report(a.status, PCTREE_ERR_INVALID_ARG);
-        }
+      page = key < stop ? kv_page(rows, it.r, div_by(key, a.blocks.page)) : -2;
+    };
+    auto find = [&](Ahead& x, int key0) {
+      const int key = key0 + (lane & 15);
+      x.at = kNone;
+      x.scales = kExpBias | kExpBias << 8;
+      if (page >= 0) {
+        const int off = key - div_by(key, a.blocks.page) * rows.page_size;
+        x.at = (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh;
+        const long long s = (static_cast<long long>(page) * a.blocks.per_page +
+                             (off >> a.blocks.shift)) * Hkv + it.kvh;
+        x.scales = __ldg(a.scale[0] + s) | __ldg(a.scale[1] + s) << 8;
+      } else if (page == -1) {
+        report(a.status, PCTREE_ERR_INVALID_ARG);
       }
     };
-    uint32_t k_raw[2][kC][4], v_raw[4][kVWords];
-    auto load_k = [&]() {
+    auto load_k = [&](Ahead& x) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t p = __shfl_sync(kFull, at, g + 8 * i);
+        const uint32_t p = __shfl_sync(kFull, x.at, g + 8 * i);
 #pragma unroll
         for (int c = 0; c < kC; ++c)
-          load_if<4>(k_raw[i][c], p != 0xffffffffu,
+          load_if<4>(x.k[i][c], p != kNone,
                      a.cache[0] + static_cast<size_t>(p) * D + c * 64 + t * 16);
       }
     };
-    auto load_v = [&]() {
+    auto load_v = [&](Ahead& x) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t p = __shfl_sync(kFull, at, 2 * t + (i & 1) + 8 * (i >> 1));
-        load_if<kVWords>(v_raw[i], p != 0xffffffffu,
+        const uint32_t p = __shfl_sync(kFull, x.at, 2 * t + (i & 1) + 8 * (i >> 1));
+        load_if<kVWords>(x.v[i], p != kNone,
                          a.cache[1] + static_cast<size_t>(p) * D + g * (D / 8));
       }
     };
     const int first = it.b0 * kTokenBlock + warp * 16;
     constexpr int kStep = 16 * kTokenWarps;
-    if (first < stop) {
-      find(first);
-      load_k();
-      load_v();
-    }
-#pragma unroll 1
-    for (int key0 = first; key0 < stop; key0 += kStep) {
-      // K Q^T, then the next K on its way
-      const uint32_t here = scales;
+    // one tile, whose registers then take the one after the next
+    auto step = [&](Ahead& cur, int key0) {
+      // K Q^T, then the K after the next on its way
+      const uint32_t here = cur.scales;
       float s[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
@@ -223,14 +222,15 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       for (int c = 0; c < kC; ++c)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const uint32_t x = k_raw[0][c][w], y = k_raw[1][c][w];
+          const uint32_t x = cur.k[0][c][w], y = cur.k[1][c][w];
           const uint32_t a0 = halves2(x), a1 = halves2(y), a2 = halves2(x >> 16),
                          a3 = halves2(y >> 16);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qf[n][c][w][0], qf[n][c][w][1]);
         }
-      find(key0 + kStep);
-      load_k();
+      find(cur, key0 + 2 * kStep);
+      find_page(key0 + 3 * kStep);
+      load_k(cur);
       // scores with the exponents of K's and V's scales; keys past the end are -inf
       uint32_t p16[NT][2];
       float v_off[2], k_by[2], v_by[2];
@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t sc2 = __shfl_sync(kFull, here, g + 8 * i);
+        if (!scale_ok(sc2 & 0xffu) || !scale_ok(sc2 >> 8)) report(a.status, PCTREE_ERR_INVALID_ARG);
         const int ev = scale_exp(sc2 >> 8);
         k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
         v_by[i] = exp2_of(-ev);
@@ -287,14 +288,29 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint32_t sel = j == 0 ? 0x5140u : 0x7362u;
-          const uint32_t lo = __byte_perm(v_raw[0][w], v_raw[1][w], sel);
-          const uint32_t hi = __byte_perm(v_raw[2][w], v_raw[3][w], sel);
+          const uint32_t lo = __byte_perm(cur.v[0][w], cur.v[1][w], sel);
+          const uint32_t hi = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
           const uint32_t a0 = halves2(lo), a1 = halves2(lo >> 16), a2 = halves2(hi),
                          a3 = halves2(hi >> 16);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + j], a0, a1, a2, a3, p16[n][0], p16[n][1]);
         }
-      load_v();
+      load_v(cur);
+    };
+    Ahead x0, x1;
+    find_page(first);
+    find(x0, first);
+    find_page(first + kStep);
+    load_k(x0);
+    load_v(x0);
+    find(x1, first + kStep);
+    find_page(first + 2 * kStep);
+    load_k(x1);
+    load_v(x1);
+#pragma unroll 1
+    for (int key0 = first; key0 < stop; key0 += 2 * kStep) {
+      step(x0, key0);
+      if (key0 + kStep < stop) step(x1, key0 + kStep);
     }
     // the warps' parts, in order
 #pragma unroll
