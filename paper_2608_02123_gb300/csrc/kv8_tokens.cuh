@@ -88,6 +88,26 @@ __device__ __forceinline__ void load_if(uint32_t (&v)[N], bool wanted, const uin
   }
 }
 
+__device__ __forceinline__ int load_int_if(bool wanted, const int32_t* p, int otherwise) {
+  int v;
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.u32 %0, %3;\n"
+      " @p ld.global.nc.u32 %0, [%1];\n}\n"
+      : "=&r"(v)
+      : "l"(p), "r"(static_cast<uint32_t>(wanted)), "r"(otherwise));
+  return v;
+}
+__device__ __forceinline__ uint32_t load_byte_if(bool wanted, const uint8_t* p,
+                                                 uint32_t otherwise) {
+  uint32_t v;
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.u32 %0, %3;\n"
+      " @p ld.global.nc.u8 %0, [%1];\n}\n"
+      : "=&r"(v)
+      : "l"(p), "r"(static_cast<uint32_t>(wanted)), "r"(otherwise));
+  return v;
+}
+
 template <int D, int NT>
 struct TokenShared {
   float o[kTokenWarps][8 * NT][D + 4];
@@ -170,26 +190,26 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
     constexpr uint32_t kNone = 0xffffffffu;
     struct Ahead {
       uint32_t k[2][kC][4], v[4][kVWords];
-      uint32_t scales, at;
+      uint32_t k_byte, v_byte, at;
     };
-    int page = -2;                               // -2: past the end
+    int page = 0;                                // as it is in the table
     auto find_page = [&](int key0) {
       const int key = key0 + (lane & 15);
-      page = key < stop ? kv_page(rows, it.r, div_by(key, a.blocks.page)) : -2;
+      page = load_int_if(
+          key < stop && rows.page_table != nullptr,
+          rows.page_table + static_cast<size_t>(it.r) * rows.max_pages + div_by(key, a.blocks.page),
+          it.r);
     };
     auto find = [&](Ahead& x, int key0) {
       const int key = key0 + (lane & 15);
-      x.at = kNone;
-      x.scales = kExpBias | kExpBias << 8;
-      if (page >= 0) {
-        const int off = key - div_by(key, a.blocks.page) * rows.page_size;
-        x.at = (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh;
-        const long long s = (static_cast<long long>(page) * a.blocks.per_page +
-                             (off >> a.blocks.shift)) * Hkv + it.kvh;
-        x.scales = __ldg(a.scale[0] + s) | __ldg(a.scale[1] + s) << 8;
-      } else if (page == -1) {
-        report(a.status, PCTREE_ERR_INVALID_ARG);
-      }
+      const bool is = key < stop && page >= 0 && page < rows.n_pages;
+      if (key < stop && !is) report(a.status, PCTREE_ERR_INVALID_ARG);
+      const int off = key - div_by(key, a.blocks.page) * rows.page_size;
+      x.at = is ? (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh : kNone;
+      const long long s = (static_cast<long long>(page) * a.blocks.per_page +
+                           (off >> a.blocks.shift)) * Hkv + it.kvh;
+      x.k_byte = load_byte_if(is, a.scale[0] + s, kExpBias);
+      x.v_byte = load_byte_if(is, a.scale[1] + s, kExpBias);
     };
     auto load_k = [&](Ahead& x) {
 #pragma unroll
@@ -214,7 +234,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
     // one tile, whose registers then take the one after the next
     auto step = [&](Ahead& cur, int key0) {
       // K Q^T, then the K after the next on its way
-      const uint32_t here = cur.scales;
+      const uint32_t here = cur.k_byte | cur.v_byte << 8;
       float s[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
