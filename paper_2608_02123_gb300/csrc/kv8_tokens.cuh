@@ -12,8 +12,8 @@
 //
 // P is relative to the running maximum of score + exponent of the value's scale, so
 // that P V is a product of P with the codes themselves and P fits float16 whatever
-// the scales: 2^7 times, down to 2^-31 of the maximum.  A row's sum adds P 2^-e in
-// float32.
+// the scales: 2^7 times, down to 2^-31 of the maximum.  The reference is a float and
+// what its rounding leaves.  A row's sum adds P 2^-e in float32.
 //
 // A CTA's pieces are kv_pieces.cuh's, planned by every warp alike; a piece's keys
 // are dealt out among its warps, whose (max, sum, O) are added up in order.
@@ -175,10 +175,12 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       sc[n][1] = __shfl_sync(kFull, row_sc, 8 * t + 4);
     }
     float o[NT][kTiles][4];
-    float m[NT][2], l[NT][2];
+    // P's reference is m + m_low: large scores would swallow the values' exponents
+    float m[NT][2], m_low[NT][2], l[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       m[n][0] = m[n][1] = -INFINITY;
+      m_low[n][0] = m_low[n][1] = 0.0f;
       l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
@@ -267,22 +269,40 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[4];
+        // (x: scores; d: with the value's exponent, relative to the reference)
+        float x[4], d[4];
         bool look = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = in[i >> 1] ? fmaf(s[n][i], sc[n][i & 1] * k_by[i >> 1], v_off[i >> 1]) : -INFINITY;
-          look = look || x[i] > m[n][i & 1] + 8.0f;
+          x[i] = in[i >> 1] ? s[n][i] * (sc[n][i & 1] * k_by[i >> 1]) : -INFINITY;
+          const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
+          d[i] = (x[i] - ref) + (v_off[i >> 1] - m_low[n][i & 1]);
+          look = look || d[i] > (m[n][i & 1] == -INFINITY ? -INFINITY : 8.0f);
         }
         if (__any_sync(kFull, look)) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             float top = fmaxf(x[r], x[2 + r]);
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-            if (top > m[n][r]) {
-              const float alpha = ex2_approx(m[n][r] - top);
+            for (int o2 = 4; o2 < 32; o2 <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o2));
+            const bool none = m[n][r] == -INFINITY;
+            if (none && top > -INFINITY) {       // the first keys: their largest score for now
               m[n][r] = top;
+              d[r] = (x[r] - top) + v_off[0];
+              d[2 + r] = (x[2 + r] - top) + v_off[1];
+            }
+            float up = fmaxf(d[r], d[2 + r]);
+#pragma unroll
+            for (int o2 = 4; o2 < 32; o2 <<= 1) up = fmaxf(up, __shfl_xor_sync(kFull, up, o2));
+            if (m[n][r] > -INFINITY && (none || up > 0.0f)) {
+              // m + m_low + up, as a rounded sum and what the rounding left
+              const float low = m_low[n][r] + up, sum = m[n][r] + low;
+              const float back = sum - m[n][r];
+              m_low[n][r] = (m[n][r] - (sum - back)) + (low - back);
+              m[n][r] = sum;
+              d[r] = (x[r] - sum) + (v_off[0] - m_low[n][r]);
+              d[2 + r] = (x[2 + r] - sum) + (v_off[1] - m_low[n][r]);
+              const float alpha = none ? 0.0f : ex2_approx(-up);
               l[n][r] *= alpha;
 #pragma unroll
               for (int i = 0; i < kTiles; ++i) {
@@ -295,8 +315,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
-          p[i] = ex2_approx(x[i] - ref + kTokenBits);
+          p[i] = ex2_approx(d[i] + kTokenBits);
           l[n][i & 1] = fmaf(p[i], v_by[i >> 1], l[n][i & 1]);
         }
         p16[n][0] = transposed8x8(pack16<true>(p[0], p[1]));
@@ -340,14 +359,17 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[n][r] += __shfl_xor_sync(kFull, l[n][r], d);
         const int h = 8 * n + 2 * t + r;
+        // relative to a rounded reference, as other parts are
+        const float ref = m[n][r] + m_low[n][r];
+        const float f = m[n][r] == -INFINITY ? 1.0f : exp2f((m[n][r] - ref) + m_low[n][r]);
         if (g == 0) {
-          sh.m[warp][h] = m[n][r];
-          sh.l[warp][h] = l[n][r];
+          sh.m[warp][h] = ref;
+          sh.l[warp][h] = l[n][r] * f;
         }
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
           *reinterpret_cast<float2*>(&sh.o[warp][h][g * (D / 8) + 2 * i]) =
-              make_float2(o[n][i][r], o[n][i][2 + r]);
+              make_float2(o[n][i][r] * f, o[n][i][2 + r] * f);
       }
     }
     __syncthreads();
