@@ -695,6 +695,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       release_warp(k);
       it = next;
     }
+    copies_wait<0>();                              // copies land before the CTA may exit
     if (!ok && lane == 0) give_up();
   } else if (warp < 16) {
     // ---------------- softmax, a thread per row of a tile ----------------

@@ -32,7 +32,7 @@ struct Kv8CompactArgs {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kCompactThreads, 4) kv8_compact_kernel(Kv8CompactArgs a) {
+__global__ void __launch_bounds__(kCompactThreads, 3) kv8_compact_kernel(Kv8CompactArgs a) {
   constexpr int S = D / 16;                  // lanes per row
   constexpr int kRows = 32 / S;              // rows side by side
   const int lane = threadIdx.x & 31;
@@ -209,7 +209,7 @@ pctree_status pctree_kv8_compact(const pctree_kv8_compact_config* cfg,
   a.layers = c.layers;
   a.Hkv = c.Hkv;
   long long ctas = (a.items + kCompactWarps - 1) / kCompactWarps;
-  if (ctas > 4ll * num_sms) ctas = 4ll * num_sms;
+  if (ctas > 3ll * num_sms) ctas = 3ll * num_sms;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -786,6 +786,22 @@ def _scales(t: torch.Tensor, cfg, device: int, layers: int = 1) -> bool:
             and (t.numel() == n or (t.numel() > n and _whole(t.shape, page))))
 
 
+def _planes(k_cache, v_cache, k_scale, v_scale, cfg, device: int, layers: int = 1) -> bool:
+    """Both planes' codes and scales there."""
+    pages, size, Hkv = cfg.n_pages, cfg.page_size, cfg.Hkv
+    shape, block = (pages, size, Hkv, cfg.D), cfg.scale_block
+    if (layers == 1 and block > 0 and k_cache.shape == shape and v_cache.shape == shape
+            and k_scale.shape == (pages, -(-size // block), Hkv) and v_scale.shape == k_scale.shape
+            and k_cache.dtype in _CODE_TYPES and v_cache.dtype in _CODE_TYPES
+            and k_scale.dtype in _SCALE_TYPES and v_scale.dtype in _SCALE_TYPES):
+        return (k_cache.get_device() == v_cache.get_device() == k_scale.get_device()
+                == v_scale.get_device() == device and k_cache.is_contiguous()
+                and v_cache.is_contiguous() and k_scale.is_contiguous()
+                and v_scale.is_contiguous())
+    return (_codes(k_cache, cfg, device, layers) and _codes(v_cache, cfg, device, layers)
+            and _scales(k_scale, cfg, device, layers) and _scales(v_scale, cfg, device, layers))
+
+
 def _codes_check(name, t, cfg, device, layers=1):
     lead = f"[{layers}]" if layers > 1 else ""
     return (name, _codes(t, cfg, device, layers),
@@ -839,8 +855,7 @@ def pctree_kv8_append(cfg: Kv8AppendConfig, q: Optional[torch.Tensor], k: torch.
                          and _flat(q_out, dt, n * Hq * D, dev, Hq * D)))
             and _rows(k, dt, n, Hkv, D, cfg.k_stride, dev)
             and _rows(v, dt, n, Hkv, D, cfg.v_stride, dev)
-            and _codes(k_cache, cfg, dev) and _codes(v_cache, cfg, dev)
-            and _scales(k_scale, cfg, dev) and _scales(v_scale, cfg, dev)
+            and _planes(k_cache, v_cache, k_scale, v_scale, cfg, dev)
             and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
             and _flat(prefix_len, i32, batch, dev)
             and _table(page_table, batch, cfg.max_pages, dev)
@@ -907,8 +922,7 @@ def pctree_kv8_attention(cfg: Kv8AttnConfig, q: torch.Tensor, k_cache: torch.Ten
     n, D, Hq, batch, i32 = cfg.total_rows, cfg.D, cfg.Hq, cfg.batch, torch.int32
     if not (_rows(q, dt, n, Hq, D, cfg.q_stride, dev)
             and _flat(out, dt, n * Hq * D, dev, Hq * D)
-            and _codes(k_cache, cfg, dev) and _codes(v_cache, cfg, dev)
-            and _scales(k_scale, cfg, dev) and _scales(v_scale, cfg, dev)
+            and _planes(k_cache, v_cache, k_scale, v_scale, cfg, dev)
             and _flat(row_start, i32, batch, dev) and _flat(n_rows, i32, batch, dev)
             and _flat(prefix_len, i32, batch, dev)
             and _table(page_table, batch, cfg.max_pages, dev) and _flat(parent, i32, n, dev)
@@ -964,9 +978,7 @@ def pctree_kv8_compact(cfg: Kv8CompactConfig, accepted_idx: torch.Tensor,
                  and cfg.scale_layer_stride == cfg.n_pages * _scale_page(cfg)))
     if not (dense and _flat(accepted_idx, i32, batch * (cfg.B + 1), dev, cfg.B + 1)
             and _flat(accepted_len, i32, batch, dev) and _flat(prefix_len, i32, batch, dev)
-            and _codes(k_cache, cfg, dev, cfg.layers) and _codes(v_cache, cfg, dev, cfg.layers)
-            and _scales(k_scale, cfg, dev, cfg.layers)
-            and _scales(v_scale, cfg, dev, cfg.layers)
+            and _planes(k_cache, v_cache, k_scale, v_scale, cfg, dev, cfg.layers)
             and _table(page_table, batch, cfg.max_pages, dev) and _flat(status, i32, 1, dev)):
         _refuse("pctree_kv8_compact", dev, [
             ("cfg", dense, "a config of dense layers"),
