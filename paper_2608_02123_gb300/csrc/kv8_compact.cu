@@ -9,6 +9,12 @@
 //
 // A warp moves one head of a request, layer and plane: 16 bytes a lane, 32 / (D /
 // 16) rows side by side, all rows of a window of up to 32 slots in flight.
+//
+// What bounds it (one GB300, us): 32 requests of 40 layers (53 MB) 29.4, 0.26 of the
+// measured copy rate: a warp's chain of dependent reads (path, pages, scales, codes),
+// with three CTAs an SM; four of 64 registers spill (30.5), two have too few warps
+// (35.0), and a warp's items of one request, with one look at its path, lie apart in
+// memory from its neighbours' (36.0).
 #include "kv8.cuh"
 #include "sm103_ptx.cuh"
 
