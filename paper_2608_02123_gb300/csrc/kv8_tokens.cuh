@@ -193,57 +193,57 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
     const int stop = min(it.key_end, it.b1 * kTokenBlock);
-    // What is on its way of a tile of keys, two tiles ahead of its use: its codes and
-    // (lane i < 16) its key i's scales and place, none past the end and in pages that
-    // are none.  Page numbers are read a tile earlier.
+    // Keys come to a warp 32 at a time, as two tiles of 16; lane i finds the place and
+    // the scales of key i, none past the end and in pages that are none.  Codes are on
+    // their way from 32 keys ahead, page numbers from 32 more.
     constexpr uint32_t kNone = 0xffffffffu;
     struct Ahead {
       uint32_t k[2][kC][4], v[4][kVWords];
-      uint32_t k_byte, v_byte, at;
     };
     int page = 0;                                // as it is in the table
     auto find_page = [&](int key0) {
-      const int key = key0 + (lane & 15);
+      const int key = key0 + lane;
       page = load_int_if(
           key < stop && rows.page_table != nullptr,
           rows.page_table + static_cast<size_t>(it.r) * rows.max_pages + div_by(key, a.blocks.page),
           it.r);
     };
-    auto find = [&](Ahead& x, int key0) {
-      const int key = key0 + (lane & 15);
+    uint32_t at = kNone, k_byte = kExpBias, v_byte = kExpBias;
+    auto find = [&](int key0) {
+      const int key = key0 + lane;
       const bool is = key < stop && page >= 0 && page < rows.n_pages;
       if (key < stop && !is) report(a.status, PCTREE_ERR_INVALID_ARG);
       const int off = key - div_by(key, a.blocks.page) * rows.page_size;
-      x.at = is ? (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh : kNone;
+      at = is ? (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh : kNone;
       const long long s = (static_cast<long long>(page) * a.blocks.per_page +
                            (off >> a.blocks.shift)) * Hkv + it.kvh;
-      x.k_byte = load_byte_if(is, a.scale[0] + s, kExpBias);
-      x.v_byte = load_byte_if(is, a.scale[1] + s, kExpBias);
+      k_byte = load_byte_if(is, a.scale[0] + s, kExpBias);
+      v_byte = load_byte_if(is, a.scale[1] + s, kExpBias);
     };
-    auto load_k = [&](Ahead& x) {
+    // codes of the keys from lane `half` on
+    auto load_k = [&](Ahead& x, int half) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t p = __shfl_sync(kFull, x.at, g + 8 * i);
+        const uint32_t p = __shfl_sync(kFull, at, half + g + 8 * i);
 #pragma unroll
         for (int c = 0; c < kC; ++c)
           load_if<4>(x.k[i][c], p != kNone,
                      a.cache[0] + static_cast<size_t>(p) * D + c * 64 + t * 16);
       }
     };
-    auto load_v = [&](Ahead& x) {
+    auto load_v = [&](Ahead& x, int half) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t p = __shfl_sync(kFull, x.at, 2 * t + (i & 1) + 8 * (i >> 1));
+        const uint32_t p = __shfl_sync(kFull, at, half + 2 * t + (i & 1) + 8 * (i >> 1));
         load_if<kVWords>(x.v[i], p != kNone,
                          a.cache[1] + static_cast<size_t>(p) * D + g * (D / 8));
       }
     };
-    const int first = it.b0 * kTokenBlock + warp * 16;
-    constexpr int kStep = 16 * kTokenWarps;
-    // one tile, whose registers then take the one after the next
-    auto step = [&](Ahead& cur, int key0) {
-      // K Q^T, then the K after the next on its way
-      const uint32_t here = cur.k_byte | cur.v_byte << 8;
+    const int first = it.b0 * kTokenBlock + warp * 32;
+    constexpr int kStep = 32 * kTokenWarps;
+    uint32_t here = 0;                           // the keys' scales, K's byte in front
+    // one tile, whose registers then take the one 32 keys on
+    auto step = [&](Ahead& cur, int key0, int half) {
       float s[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
@@ -257,17 +257,14 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qf[n][c][w][0], qf[n][c][w][1]);
         }
-      find(cur, key0 + 2 * kStep);
-      find_page(key0 + 3 * kStep);
-      load_k(cur);
+      load_k(cur, half);
       // scores with the exponents of K's and V's scales; keys past the end are -inf
       uint32_t p16[NT][2];
       float v_off[2], k_by[2], v_by[2];
       bool in[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t sc2 = __shfl_sync(kFull, here, g + 8 * i);
-        if (!scale_ok(sc2 & 0xffu) || !scale_ok(sc2 >> 8)) report(a.status, PCTREE_ERR_INVALID_ARG);
+        const uint32_t sc2 = __shfl_sync(kFull, here, half + g + 8 * i);
         const int ev = scale_exp(sc2 >> 8);
         k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
         v_by[i] = exp2_of(-ev);
@@ -341,22 +338,27 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + j], a0, a1, a2, a3, p16[n][0], p16[n][1]);
         }
-      load_v(cur);
+      load_v(cur, half);
+    };
+    auto take_scales = [&]() {
+      here = k_byte | v_byte << 8;
+      if (!scale_ok(k_byte) || !scale_ok(v_byte)) report(a.status, PCTREE_ERR_INVALID_ARG);
     };
     Ahead x0, x1;
     find_page(first);
-    find(x0, first);
+    find(first);
     find_page(first + kStep);
-    load_k(x0);
-    load_v(x0);
-    find(x1, first + kStep);
-    find_page(first + 2 * kStep);
-    load_k(x1);
-    load_v(x1);
+    load_k(x0, 0);
+    load_v(x0, 0);
+    load_k(x1, 16);
+    load_v(x1, 16);
 #pragma unroll 1
-    for (int key0 = first; key0 < stop; key0 += 2 * kStep) {
-      step(x0, key0);
-      if (key0 + kStep < stop) step(x1, key0 + kStep);
+    for (int key0 = first; key0 < stop; key0 += kStep) {
+      take_scales();
+      find(key0 + kStep);
+      find_page(key0 + 2 * kStep);
+      step(x0, key0, 0);
+      if (key0 + 16 < stop) step(x1, key0 + 16, 16);
     }
     // the warps' parts, in order
 #pragma unroll
