@@ -34,8 +34,8 @@
 // small against the first are not lost.  Row sums add the unrounded values.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
-//   four prompts of up to 4096 rows 873 (0.48 PFLOP/s), packed trees of 32 requests
-//   197: 3600 cycles a block of 64 keys for two tiles, of which the products take 1280
+//   four prompts of up to 4096 rows 865 (0.49 PFLOP/s), packed trees of 32 requests
+//   195: 3600 cycles a block of 64 keys for two tiles, of which the products take 1280
 //   (S, M = 128, N = 64, reads 6 KB of shared memory a product: 48 cycles instead of
 //   32), the widening's traffic (64 KB) 512, and a softmax warp's chain 2300: two
 //   warps on an SM's quarter issue an instruction in some 7 cycles each, and the
@@ -44,7 +44,7 @@
 // Steps that were measured (prompts): codes to registers with a branch around each
 // load, which waits for it, 4583; places and scales by a warp of their own 1589;
 // copies to shared memory 1290; two tiles a block of K and V 1216; Q in place by
-// asynchronous copies, to float16 by its tile's softmax warps 876.  Not kept: codes in
+// asynchronous copies, to float16 by its tile's softmax warps 870.  Not kept: codes in
 // registers two blocks ahead instead of the copies 997; one warpgroup for K and V both
 // 2147; the rescaling of O unrolled (instructions that run rarely come from memory)
 // 1370.

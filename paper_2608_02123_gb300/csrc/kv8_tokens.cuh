@@ -19,11 +19,13 @@
 // are dealt out among its warps, whose (max, sum, O) are added up in order.
 //
 // What bounds it (one GB300, us; tokens of 32 requests over up to 8192 slots, 40
-// query and 8 KV heads of 128 dims, 431 MB): 99, 0.64 of the measured copy rate; the
-// wait for codes on their way (3.5 of 7.3 warps a quarter of an SM hold per issued
-// instruction), with 12 warps of two tiles (8 KB) each.  Sixteen warps of one tile 107;
-// a scale or page number that is looked at where it is read 104; a unit of all KV
-// heads of a row (neighbouring memory at the same time) 114; codes through L1 132.
+// query and 8 KV heads of 128 dims, 431 MB): 83, 0.77 of the measured copy rate; some
+// 350 instructions a tile of 16 keys, 5 cycles each, by the three warps of a quarter
+// of an SM.  Before: each lane finding its key's place twice over (16 keys at a time)
+// 99; a scale or page number that is looked at where it is read 104; sixteen warps of
+// one tile ahead 107.  Not kept: a unit of all KV heads of a row (neighbouring memory
+// at the same time) 114; codes through L1 132; the codes of no key from an array of
+// zeros instead of predicated loads 87.
 #pragma once
 
 #include "kv8.cuh"
@@ -55,8 +57,9 @@ __device__ __forceinline__ void report(int32_t* status, int code) {
   if (status != nullptr) atomicCAS(status, 0, code);
 }
 
-constexpr int kTokenThreads = 384;
-constexpr int kTokenWarps = kTokenThreads / 32;
+// Threads for NT groups of 8 query heads: as many as their registers allow.
+__host__ __device__ constexpr int token_threads(int NT) { return NT == 1 ? 384 : 256; }
+__host__ __device__ constexpr int token_warps(int NT) { return token_threads(NT) / 32; }
 constexpr int kTokenBlock = 128;             // keys per block of work
 constexpr int kTokenHeads = 16;              // query heads of a unit, at most
 constexpr float kTokenBits = 7.0f;           // P is 2^7 times what it is relative to
@@ -117,14 +120,14 @@ __device__ __forceinline__ uint32_t load_byte_if(bool wanted, const uint8_t* p,
 
 template <int D, int NT>
 struct TokenShared {
-  float o[kTokenWarps][8 * NT][D + 4];
-  float m[kTokenWarps][8 * NT], l[kTokenWarps][8 * NT];
+  float o[token_warps(NT)][8 * NT][D + 4];
+  float m[token_warps(NT)][8 * NT], l[token_warps(NT)][8 * NT];
   unsigned upto[PCTREE_KV_MAX_BATCH];
 };
 
 // NT: groups of 8 query heads.
 template <int D, bool F16, int NT>
-__global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs a) {
+__global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8AttnArgs a) {
   constexpr int kC = D / 64;                     // 16-byte chunks of a key's row a lane has
   constexpr int kVWords = D / 32;                // words of V a lane has of a key
   constexpr int kTiles = D / 16;                 // of O^T's rows
@@ -136,7 +139,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
   const int Hkv = a.units.Hkv;
   pdl_launch_dependents();
   pdl_wait();
-  count_work<kTokenThreads>(a.units, sh.upto, [&](int code) {
+  count_work<token_threads(NT)>(a.units, sh.upto, [&](int code) {
     if (blockIdx.x == 0) report(a.status, code);
   });
 
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       }
     };
     const int first = it.b0 * kTokenBlock + warp * 32;
-    constexpr int kStep = 32 * kTokenWarps;
+    constexpr int kStep = 32 * token_warps(NT);
     uint32_t here = 0;                           // the keys' scales, K's byte in front
     // one tile, whose registers then take the one 32 keys on
     auto step = [&](Ahead& cur, int key0, int half) {
@@ -261,7 +264,6 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
       // scores with the exponents of K's and V's scales; keys past the end are -inf
       uint32_t p16[NT][2];
       float v_off[2], k_by[2], v_by[2];
-      bool in[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t sc2 = __shfl_sync(kFull, here, half + g + 8 * i);
@@ -269,7 +271,6 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
         k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
         v_by[i] = exp2_of(-ev);
         v_off[i] = static_cast<float>(ev);
-        in[i] = key0 + g + 8 * i < stop;
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -278,7 +279,8 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
         bool look = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = in[i >> 1] ? s[n][i] * (sc[n][i & 1] * k_by[i >> 1]) : -INFINITY;
+          x[i] = s[n][i] * (sc[n][i & 1] * k_by[i >> 1]);
+          if (key0 + 16 > stop && key0 + g + 8 * (i >> 1) >= stop) x[i] = -INFINITY;
           const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
           d[i] = (x[i] - ref) + (v_off[i >> 1] - m_low[n][i & 1]);
           look = look || d[i] > (m[n][i & 1] == -INFINITY ? -INFINITY : 8.0f);
@@ -385,15 +387,15 @@ __global__ void __launch_bounds__(kTokenThreads, 1) kv8_token_kernel(Kv8AttnArgs
     const bool whole = it.b0 == 0 && it.b1 == it.nblk;
     const size_t part = static_cast<size_t>(blockIdx.x) * 2 + (it.b0 == 0 ? 1 : 0);
     constexpr int kQuads = D / 4;
-    for (int i = threadIdx.x; i < a.G * kQuads; i += kTokenThreads) {
+    for (int i = threadIdx.x; i < a.G * kQuads; i += token_threads(NT)) {
       const int h = i / kQuads, d = (i - h * kQuads) * 4;
       float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kTokenWarps; ++w)
+      for (int w = 0; w < token_warps(NT); ++w)
         if (sh.l[w][h] != 0.0f) top = fmaxf(top, sh.m[w][h]);
       float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int w = 0; w < kTokenWarps; ++w) {
+      for (int w = 0; w < token_warps(NT); ++w) {
         const float lw = sh.l[w][h];
         if (lw == 0.0f) continue;                // (no finite score, or no keys)
         const float f = exp2f(sh.m[w][h] - top);
@@ -428,7 +430,7 @@ cudaError_t launch_tokens(cudaLaunchConfig_t lc, const Kv8AttnArgs& a) {
   const cudaError_t e = limit.ensure(reinterpret_cast<const void*>(kv8_token_kernel<D, F16, NT>),
                                      sizeof(TokenShared<D, NT>));
   if (e != cudaSuccess) return e;
-  lc.blockDim = dim3(kTokenThreads);
+  lc.blockDim = dim3(token_threads(NT));
   lc.dynamicSmemBytes = sizeof(TokenShared<D, NT>);
   return cudaLaunchKernelEx(&lc, kv8_token_kernel<D, F16, NT>, a);
 }
