@@ -369,7 +369,7 @@ using namespace pct;
 
 extern "C" {
 
-int32_t pctree_version(void) { return 103; }
+int32_t pctree_version(void) { return 104; }
 
 const char* pctree_status_string(int32_t s) {
   switch (s) {

@@ -1068,8 +1068,14 @@ pctree_status attn8_launch(const Kv8AttnArgs& a, bool tokens, int num_sms, cudaS
     if (e != cudaSuccess) return PCTREE_ERR_CUDA;
   } else {
     static SmemLimit limit;
-    if (limit.ensure(reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>), smem) != cudaSuccess)
-      return PCTREE_ERR_CUDA;
+    const void* fn = reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>);
+    if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
+    // (a launch with fewer registers would leave the softmax waiting for its own)
+    static const bool registers = [fn] {
+      cudaFuncAttributes f;
+      return cudaFuncGetAttributes(&f, fn) == cudaSuccess && f.numRegs >= kRegsLaunch;
+    }();
+    if (!registers) return PCTREE_ERR_CUDA;
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = smem;
     if (cudaLaunchKernelEx(&lc, kv8_attn_kernel<D, F16>, a) != cudaSuccess) return PCTREE_ERR_CUDA;

@@ -110,6 +110,10 @@ SHAPES = {
     "one_key": dict(rows=[1], prefix=[0], page=16, heads=(32, 8)),
     "token": dict(rows=[1], prefix=[2047], page=16, heads=(32, 8)),
     "tokens": dict(rows=[1, 1, 1, 1, 1], prefix=[0, 127, 128, 700, 3], page=32, heads=(40, 8)),
+    # two groups of eight heads in the kernel for single tokens
+    "tokens_group_of_9": dict(rows=[1, 1, 1], prefix=[5, 300, 1029], page=16, heads=(18, 2)),
+    "tokens_group_of_16": dict(rows=[1] * 7, prefix=[0, 15, 16, 31, 32, 800, 2100], page=48,
+                               heads=(32, 2)),
     "tokens_contiguous": dict(rows=[1, 1, 1], prefix=[5, 300, 129], page=0, heads=(16, 16)),
     "chains": dict(rows=[8, 8, 3, 0, 8], prefix=[100, 250, 0, 9, 121], page=0, heads=(32, 8)),
     "pairs": dict(rows=[2, 1, 2], prefix=[100, 250, 0], page=16, heads=(16, 4)),
