@@ -12,15 +12,17 @@
 //   blocks  with larger blocks: a block of one request's new slots, keys or
 //           values of the heads that fit a warp.  Its rows are read twice, for
 //           the maximum and for the codes (the second time from L1), four rows'
-//           loads in flight.  Earlier slots of the request in the block are
+//           loads in flight.  Sines and cosines of a CTA's blocks are found once,
+//           in shared memory.  Earlier slots of the request in the block are
 //           divided by what their scale has to grow.
 //
-// What bounds it (one GB300, us): prompts (fp16, blocks of 16, 311 MB) 99.7, 0.46 of the
-// measured copy rate: instructions (56 million warp instructions, 0.45 of the issue
-// slots with four warps on a quarter of an SM); trees (blocks of one, 87 MB) 30.6, as
-// the append in 16 bits: the rows a warp takes one after the other.  Blocks by a team
-// of warps that keep their rows in registers took the same 99.6, chains 17.0 instead
-// of 14.5.
+// What bounds it (one GB300, us): prompts (fp16, blocks of 16, 311 MB) 90, 0.51 of the
+// measured copy rate: instructions, with four warps on a quarter of an SM (of 15000
+// rows of 16 and 2 x 16 heads in blocks of 16, 89: 20 are the queries, 14 the keys'
+// rotation; the same in blocks of one slot, read once, 68); trees (blocks of one, 87
+// MB) 31, as the append in 16 bits: the rows a warp takes one after the other.  Angles
+// by every warp for its own heads 99.7; blocks by a team of warps that keep their
+// rows in registers 99.6, chains 17.0 instead of 14.
 #include "kv8.cuh"
 #include "sm103_ptx.cuh"
 
@@ -31,6 +33,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kCtas = 2;            // an SM
 constexpr int kAhead = 4;           // heads or rows a lane has loads in flight for
+constexpr int kBlocks = 32;         // that a CTA takes at once, at most
 
 struct Kv8AppendArgs {
   KvRows rows;
@@ -60,7 +63,13 @@ struct Kv8AppendShared {
   int start[PCTREE_KV_MAX_BATCH], end[PCTREE_KV_MAX_BATCH], prefix[PCTREE_KV_MAX_BATCH];
   int upto[PCTREE_KV_MAX_BATCH];                 // blocks of requests 0 .. r
   int blocks;                                    // of all; -1: too many rows
+  // a CTA's blocks: their requests, pages (-1: none), first and last new slots
+  int r[kBlocks], page[kBlocks], base[kBlocks], first[kBlocks], stop[kBlocks];
 };
+
+// Sines and cosines of the blocks' rows, [row][sin, cos][pair].
+constexpr int kTableRows = 128;
+using AngleTable = float[kTableRows][2][64];
 
 // A lane's share of a head: two pieces of eight elements, two at a time.
 struct Piece2 {
@@ -302,139 +311,175 @@ __global__ void __launch_bounds__(kThreads, kCtas) kv8_append_kernel(Kv8AppendAr
   // (dims past rotary_dim: pieces 2 s and 2 s + 1 lie past it, since
   // s >= rotary_dim / 16)
   const long long row_items = static_cast<long long>(a.rows.total_rows) * a.parts;
-  const long long items = row_items + blocks * 2 * a.groups;
   bool bad = false;                              // a key or value is not finite
-  for (long long item = static_cast<long long>(blockIdx.x) * kWarps + warp; item < items;
+  for (long long item = static_cast<long long>(blockIdx.x) * kWarps + warp; item < row_items;
        item += static_cast<long long>(gridDim.x) * kWarps) {
-    if (item < row_items) {
-      // ---------------- a run of a row's heads ----------------
-      const int row = static_cast<int>(item / a.parts);
-      const int part = static_cast<int>(item - static_cast<long long>(row) * a.parts);
-      int r = -1;
-      for (int b = 0; b < a.rows.batch; b += 32) {
-        const int x = b + lane;
-        const unsigned in = __ballot_sync(
-            kFull, x < a.rows.batch && row >= sh.start[x] && row < sh.end[x]);
-        if (in != 0) {
-          r = b + __ffs(in) - 1;
-          break;
+    // ---------------- a run of a row's heads ----------------
+    const int row = static_cast<int>(item / a.parts);
+    const int part = static_cast<int>(item - static_cast<long long>(row) * a.parts);
+    int r = -1;
+    for (int b = 0; b < a.rows.batch; b += 32) {
+      const int x = b + lane;
+      const unsigned in = __ballot_sync(
+          kFull, x < a.rows.batch && row >= sh.start[x] && row < sh.end[x]);
+      if (in != 0) {
+        r = b + __ffs(in) - 1;
+        break;
+      }
+    }
+    if (r < 0) continue;                       // a row of no request
+    const int h_end = min(a.heads, (part + 1) * a.heads_per_part);
+    const uint16_t* q_row = a.q + row * a.q_stride;
+    const uint16_t* k_row = a.k + row * a.k_stride;
+    const uint16_t* v_row = a.v + row * a.v_stride;
+    uint4 x0[kAhead], x1[kAhead];
+    auto load = [&](int hb) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int h = hb + u * kGroups + group;
+        const bool is_v = h >= a.Hq + a.Hkv;
+        const uint16_t* src = h < a.Hq ? q_row + h * D
+                              : !is_v  ? k_row + (h - a.Hq) * D
+                                       : v_row + (h - a.Hq - a.Hkv) * D;
+        if (h < h_end) {
+          x0[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s : c0) * 8);
+          x1[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s + 1 : c1) * 8);
+        } else {
+          x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
         }
       }
-      if (r < 0) continue;                       // a row of no request
-      const int h_end = min(a.heads, (part + 1) * a.heads_per_part);
-      const uint16_t* q_row = a.q + row * a.q_stride;
-      const uint16_t* k_row = a.k + row * a.k_stride;
-      const uint16_t* v_row = a.v + row * a.v_stride;
-      uint4 x0[kAhead], x1[kAhead];
-      auto load = [&](int hb) {
+    };
+    // the first heads are under way while the place and the angles are found
+    load(part * a.heads_per_part);
+    const int slot = sh.prefix[r] + row - sh.start[r];
+    int page = 0, off = 0;
+    if (a.groups == 0) {
+      const int entry = div_by(slot, a.blocks.page);
+      off = slot - entry * a.rows.page_size;
+      page = kv_page(a.rows, r, entry);
+      if (page < 0 && lane == 0) report(PCTREE_ERR_INVALID_ARG);
+    }
+    const long long place = (static_cast<long long>(page) * a.rows.page_size + off) * a.Hkv;
+    uint64_t cs[4], sn[4];
+    if (a.rotary > 0)
+      angles<S>(sh.turn, a.positions != nullptr ? a.positions[row] : slot, s, group,
+                a.rope_scale, cs, sn);
+    // every lane runs the same number of rounds: the reductions are warp-wide
+    for (int hb = part * a.heads_per_part;;) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int h = hb + u * kGroups + group;
-          const bool is_v = h >= a.Hq + a.Hkv;
-          const uint16_t* src = h < a.Hq ? q_row + h * D
-                                : !is_v  ? k_row + (h - a.Hq) * D
-                                         : v_row + (h - a.Hq - a.Hkv) * D;
-          if (h < h_end) {
-            x0[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s : c0) * 8);
-            x1[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 2 * s + 1 : c1) * 8);
-          } else {
-            x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+      for (int u = 0; u < kAhead; ++u) {
+        const int h = hb + u * kGroups + group;
+        const bool is_q = h < a.Hq, is_v = h >= a.Hq + a.Hkv;
+        Piece2 f = widened<F16>(x0[u], x1[u]);
+        const float sum = head_square<S>(f);
+        if (!is_v) {
+          if ((is_q ? a.q_weight : a.k_weight) != nullptr)
+            scaled(f, rsqrtf(sum * (1.0f / D) + a.eps), &sh.weight[is_q ? 0 : 1][c0 * 8],
+                   &sh.weight[is_q ? 0 : 1][c1 * 8]);
+          if (rotated) rotate(f, cs, sn, a.interleaved != 0);
+        }
+        if (a.groups == 0) {                   // (the reductions are warp-wide)
+          const bool code = !is_q && h < h_end && page >= 0;
+          bool odd = false;
+          float top = is_q ? 0.0f : finite_top(f, odd);
+#pragma unroll
+          for (int o = S / 2; o > 0; o >>= 1)
+            top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+          if (code) {
+            const int kv = is_v ? 1 : 0, hk = h - a.Hq - kv * a.Hkv;
+            const int e = least_exp(top);
+            const float by = exp2_of(-e);
+            uint8_t* dst = a.cache[kv] + (place + hk) * D;
+            *reinterpret_cast<uint2*>(dst + (is_v ? 2 * s : c0) * 8) = coded(f.a, by);
+            *reinterpret_cast<uint2*>(dst + (is_v ? 2 * s + 1 : c1) * 8) = coded(f.b, by);
+            if (s == 0) a.scale[kv][place + hk] = static_cast<uint8_t>(e + kExpBias);
+            bad = bad || odd;
           }
         }
-      };
-      // the first heads are under way while the place and the angles are found
-      load(part * a.heads_per_part);
-      const int slot = sh.prefix[r] + row - sh.start[r];
-      int page = 0, off = 0;
-      if (a.groups == 0) {
-        const int entry = div_by(slot, a.blocks.page);
-        off = slot - entry * a.rows.page_size;
-        page = kv_page(a.rows, r, entry);
-        if (page < 0 && lane == 0) report(PCTREE_ERR_INVALID_ARG);
-      }
-      const long long place = (static_cast<long long>(page) * a.rows.page_size + off) * a.Hkv;
-      uint64_t cs[4], sn[4];
-      if (a.rotary > 0)
-        angles<S>(sh.turn, a.positions != nullptr ? a.positions[row] : slot, s, group,
-                  a.rope_scale, cs, sn);
-      // every lane runs the same number of rounds: the reductions are warp-wide
-      for (int hb = part * a.heads_per_part;;) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int h = hb + u * kGroups + group;
-          const bool is_q = h < a.Hq, is_v = h >= a.Hq + a.Hkv;
-          Piece2 f = widened<F16>(x0[u], x1[u]);
-          const float sum = head_square<S>(f);
-          if (!is_v) {
-            if ((is_q ? a.q_weight : a.k_weight) != nullptr)
-              scaled(f, rsqrtf(sum * (1.0f / D) + a.eps), &sh.weight[is_q ? 0 : 1][c0 * 8],
-                     &sh.weight[is_q ? 0 : 1][c1 * 8]);
-            if (rotated) rotate(f, cs, sn, a.interleaved != 0);
-          }
-          if (a.groups == 0) {                   // (the reductions are warp-wide)
-            const bool code = !is_q && h < h_end && page >= 0;
-            bool odd = false;
-            float top = is_q ? 0.0f : finite_top(f, odd);
-#pragma unroll
-            for (int o = S / 2; o > 0; o >>= 1)
-              top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-            if (code) {
-              const int kv = is_v ? 1 : 0, hk = h - a.Hq - kv * a.Hkv;
-              const int e = least_exp(top);
-              const float by = exp2_of(-e);
-              uint8_t* dst = a.cache[kv] + (place + hk) * D;
-              *reinterpret_cast<uint2*>(dst + (is_v ? 2 * s : c0) * 8) = coded(f.a, by);
-              *reinterpret_cast<uint2*>(dst + (is_v ? 2 * s + 1 : c1) * 8) = coded(f.b, by);
-              if (s == 0) a.scale[kv][place + hk] = static_cast<uint8_t>(e + kExpBias);
-              bad = bad || odd;
-            }
-          }
-          if (is_q && h < h_end) {
-            uint16_t* dst = a.q_out + (static_cast<size_t>(row) * a.Hq + h) * D;
-            *reinterpret_cast<uint4*>(dst + c0 * 8) = narrowed<F16>(f.a);
-            *reinterpret_cast<uint4*>(dst + c1 * 8) = narrowed<F16>(f.b);
-          }
+        if (is_q && h < h_end) {
+          uint16_t* dst = a.q_out + (static_cast<size_t>(row) * a.Hq + h) * D;
+          *reinterpret_cast<uint4*>(dst + c0 * 8) = narrowed<F16>(f.a);
+          *reinterpret_cast<uint4*>(dst + c1 * 8) = narrowed<F16>(f.b);
         }
-        hb += kGroups * kAhead;
-        if (hb >= h_end) break;
-        load(hb);
       }
-    } else {
-      // ---------------- keys or values of a block ----------------
-      const long long of = item - row_items;
-      const int g = static_cast<int>(of % a.groups);
-      const int kv = static_cast<int>((of / a.groups) & 1);
-      const int nth = static_cast<int>(of / a.groups / 2);
+      hb += kGroups * kAhead;
+      if (hb >= h_end) break;
+      load(hb);
+    }
+  }
+  // ---------------- keys or values of blocks ----------------
+  // as many at a time as give every CTA some, and as the table holds
+  extern __shared__ float4 dynamic[];
+  AngleTable& table = *reinterpret_cast<AngleTable*>(dynamic);
+  const int block_slots = 1 << a.blocks.shift;
+  const int nb = static_cast<int>(
+      min(static_cast<long long>(min(kBlocks, kTableRows >> a.blocks.shift)),
+          max(1ll, (blocks + gridDim.x - 1) / gridDim.x)));
+  for (long long b_first = static_cast<long long>(blockIdx.x) * nb; b_first < blocks;
+       b_first += static_cast<long long>(gridDim.x) * nb) {
+    const int here = static_cast<int>(min(static_cast<long long>(nb), blocks - b_first));
+    __syncthreads();                             // the blocks before are done
+    if (threadIdx.x < here) {
+      const int nth = static_cast<int>(b_first) + threadIdx.x;
       int lo = 0, hi = a.rows.batch - 1;         // the request that holds it
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (sh.upto[mid] <= nth) lo = mid + 1; else hi = mid;
       }
-      const int r = lo, prefix = sh.prefix[r];
-      const int last = prefix + sh.end[r] - sh.start[r];
-      const int block = block_of(prefix) + nth - (r > 0 ? sh.upto[r - 1] : 0);
-      const int entry = block / a.blocks.per_page, in_page = block - entry * a.blocks.per_page;
-      const int page = kv_page(a.rows, r, entry);
-      if (page < 0) {
-        if (lane == 0) report(PCTREE_ERR_INVALID_ARG);
-        continue;
+      const int prefix = sh.prefix[lo], last = prefix + sh.end[lo] - sh.start[lo];
+      const int block = block_of(prefix) + nth - (lo > 0 ? sh.upto[lo - 1] : 0);
+      const int entry = block / a.blocks.per_page;
+      const int base = entry * a.rows.page_size +
+                       ((block - entry * a.blocks.per_page) << a.blocks.shift);
+      const int page = kv_page(a.rows, lo, entry);
+      if (page < 0) report(PCTREE_ERR_INVALID_ARG);
+      sh.r[threadIdx.x] = lo;
+      sh.page[threadIdx.x] = page;
+      sh.base[threadIdx.x] = base;
+      sh.first[threadIdx.x] = max(base, prefix);
+      sh.stop[threadIdx.x] =
+          min(min(base + block_slots, (entry + 1) * a.rows.page_size), last);
+    }
+    __syncthreads();
+    if (a.rotary > 0) {
+      for (int i = threadIdx.x; i < (here << a.blocks.shift) * half; i += kThreads) {
+        const int row = i / half, pair = i - row * half;
+        const int b = row >> a.blocks.shift, slot = sh.base[b] + (row & (block_slots - 1));
+        if (slot < sh.first[b] || slot >= sh.stop[b]) continue;
+        const int r = sh.r[b];
+        const long long pos = a.positions != nullptr
+                                  ? a.positions[sh.start[r] + slot - sh.prefix[r]] : slot;
+        const unsigned long long ph = static_cast<unsigned long long>(pos) * sh.turn[pair];
+        float sine, cosine;                      // (half turns in [-1, 1))
+        sincospif(static_cast<float>(static_cast<int>(ph >> 32)) * (1.0f / 2147483648.0f), &sine,
+                  &cosine);
+        table[row][0][pair] = sine * a.rope_scale;
+        table[row][1][pair] = cosine * a.rope_scale;
       }
-      const int base = entry * a.rows.page_size + (in_page << a.blocks.shift);
-      const int first = max(base, prefix);
-      const int stop = min(min(base + (1 << a.blocks.shift), (entry + 1) * a.rows.page_size), last);
+      __syncthreads();
+    }
+    for (int task = warp; task < here * 2 * a.groups; task += kWarps) {
+      const int b = task / (2 * a.groups), part = task - b * 2 * a.groups;
+      const int kv = part >= a.groups ? 1 : 0, g = part - kv * a.groups;
+      const int page = sh.page[b];
+      if (page < 0) continue;
+      const int r = sh.r[b], base = sh.base[b], first = sh.first[b], stop = sh.stop[b];
+      const int prefix = sh.prefix[r];
+      const int entry = div_by(base, a.blocks.page), page0 = entry * a.rows.page_size;
       const int hk = g * kGroups + group;
       const bool mine = hk < a.Hkv;
       const int b0 = kv ? 2 * s : c0, b1 = kv ? 2 * s + 1 : c1;
       const uint16_t* src = (kv ? a.v : a.k) + hk * D;
       const long long stride = kv ? a.v_stride : a.k_stride;
       const int row0 = sh.start[r] - prefix;     // row of slot 0
-      const bool norm = kv == 0 && a.k_weight != nullptr, turn = kv == 0 && a.rotary > 0;
+      const bool norm = kv == 0 && a.k_weight != nullptr, turn = kv == 0 && rotated;
       float top = 0.0f;
       int e = 0;
       uint8_t* dst = a.cache[kv] +
                      (static_cast<long long>(page) * a.rows.page_size * a.Hkv + hk) * D;
       uint8_t* scale = a.scale[kv] +
-                       (static_cast<long long>(page) * a.blocks.per_page + in_page) * a.Hkv + hk;
+                       (static_cast<long long>(page) * a.blocks.per_page +
+                        ((base - page0) >> a.blocks.shift)) * a.Hkv + hk;
       // the largest magnitude, then the codes
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
@@ -459,10 +504,18 @@ __global__ void __launch_bounds__(kThreads, kCtas) kv8_append_kernel(Kv8AppendAr
               scaled(f, rsqrtf(head_square<S>(f) * (1.0f / D) + a.eps), &sh.weight[1][c0 * 8],
                      &sh.weight[1][c1 * 8]);
             if (turn) {
+              const auto& angle = table[(b << a.blocks.shift) + x + u - base];
               uint64_t cs[4], sn[4];
-              angles<S>(sh.turn, a.positions != nullptr ? a.positions[row0 + x + u] : x + u, s,
-                        group, a.rope_scale, cs, sn);
-              if (rotated) rotate(f, cs, sn, a.interleaved != 0);
+#pragma unroll
+              for (int i = 0; i < 4; i += 2) {
+                const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&angle[0][8 * s + 2 * i]);
+                const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(&angle[1][8 * s + 2 * i]);
+                sn[i] = q.x;
+                sn[i + 1] = q.y;
+                cs[i] = c.x;
+                cs[i + 1] = c.y;
+              }
+              rotate(f, cs, sn, a.interleaved != 0);
             }
             bool odd = false;
             const float t = finite_top(f, odd);
@@ -471,8 +524,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) kv8_append_kernel(Kv8AppendAr
               bad = bad || (mine && odd);
             } else if (mine) {
               const float by = exp2_of(-e);
-              uint8_t* to = dst + static_cast<long long>(x + u - entry * a.rows.page_size) *
-                                      a.Hkv * D;
+              uint8_t* to = dst + static_cast<long long>(x + u - page0) * a.Hkv * D;
               *reinterpret_cast<uint2*>(to + b0 * 8) = coded(f.a, by);
               *reinterpret_cast<uint2*>(to + b1 * 8) = coded(f.b, by);
             }
@@ -490,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) kv8_append_kernel(Kv8AppendAr
             const float by = exp2_of(old - e);
             for (int x = base; x < prefix; ++x) {
               uint4* p = reinterpret_cast<uint4*>(
-                  dst + static_cast<long long>(x - entry * a.rows.page_size) * a.Hkv * D + s * 16);
+                  dst + static_cast<long long>(x - page0) * a.Hkv * D + s * 16);
               *p = rescaled16(*p, by);
             }
           }
@@ -525,10 +577,12 @@ pctree_status append8_check(const pctree_kv8_append_config* c) {
   return PCTREE_OK;
 }
 
-template <bool F16>
-const void* append8_kernel(int D) {
-  return D == 64 ? reinterpret_cast<const void*>(kv8_append_kernel<F16, 64>)
-                 : reinterpret_cast<const void*>(kv8_append_kernel<F16, 128>);
+// The kernel, ready to be launched with the table; NULL if it cannot be.
+template <bool F16, int D>
+const void* append8_kernel() {
+  static SmemLimit limit;
+  const void* fn = reinterpret_cast<const void*>(kv8_append_kernel<F16, D>);
+  return limit.ensure(fn, sizeof(AngleTable)) == cudaSuccess ? fn : nullptr;
 }
 
 }  // namespace
@@ -623,10 +677,14 @@ pctree_status pctree_kv8_append(const pctree_kv8_append_config* cfg, const void*
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3(static_cast<unsigned>(ctas));
   lc.blockDim = dim3(kThreads);
+  lc.dynamicSmemBytes = a.groups > 0 && c.rotary_dim > 0 ? sizeof(AngleTable) : 0;
   lc.stream = static_cast<cudaStream_t>(stream);
   lc.attrs = attr;
   lc.numAttrs = 1;
-  const void* fn = c.dtype == PCTREE_F16 ? append8_kernel<true>(c.D) : append8_kernel<false>(c.D);
+  const bool f16 = c.dtype == PCTREE_F16;
+  const void* fn = c.D == 64 ? (f16 ? append8_kernel<true, 64>() : append8_kernel<false, 64>())
+                             : (f16 ? append8_kernel<true, 128>() : append8_kernel<false, 128>());
+  if (fn == nullptr) return PCTREE_ERR_CUDA;
   void* params[] = {&a};
   return cudaLaunchKernelExC(&lc, fn, params) == cudaSuccess ? PCTREE_OK : PCTREE_ERR_CUDA;
 }
