@@ -88,7 +88,9 @@ struct Places {
 
 struct Tail {
   uint64_t place_full[kPlaceRing], place_empty[kPlaceRing];
-  uint64_t q_raw[2], q_full[2], q_empty;     // (raw: by piece parity; full: by tile)
+  // (raw: by place in the item ring, whose places are given back after the wait for
+  // it: a warp without a part in a piece cannot fall a phase behind; full: by tile)
+  uint64_t q_raw[kItemRing], q_full[2], q_empty;
   uint64_t kv_full[kSlots], kv_empty[kSlots];
   uint64_t s_full[2][2], p_full[2][2], p_empty[2][2];      // [tile][buffer]
   uint64_t o_full[2], o_empty[2];            // [tile]
@@ -269,7 +271,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     }
     mbar_init(&T->q_empty, 1);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&T->q_raw[s], 4);
       mbar_init(&T->q_full[s], 4);
       for (int t = 0; t < 2; ++t) {
         mbar_init(&T->s_full[t][s], 1);
@@ -280,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       mbar_init(&T->o_empty[s], 4);
     }
     for (int s = 0; s < kItemRing; ++s) {
+      mbar_init(&T->q_raw[s], 4);
       mbar_init(&T->item_full[s], 1);
       mbar_init(&T->item_empty[s], 2 + 1 + 4 + 8);
     }
@@ -607,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       copies_wait<0>();
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&T->q_raw[qb]);
+      if (lane == 0) mbar_arrive(&T->q_raw[k % kItemRing]);
       return true;
     };
     Piece it;
@@ -728,9 +730,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
     Piece it;
     for (int k = 0; ok; ++k) {
       if (!(ok = peek_warp(k, it))) break;
+      if (it.nblk == 0) {
+        release_warp(k);
+        break;
+      }
+      if (!(ok = wwait_long(T, &T->q_raw[k % kItemRing], (k / kItemRing) & 1))) break;
       release_warp(k);
-      if (it.nblk == 0) break;
-      if (!(ok = wwait_long(T, &T->q_raw[k & 1], (k >> 1) & 1))) break;
       if (it.n_rows <= tile * a.tile_rows) continue;
       float sc = a.scale_log2;
       if constexpr (!F16) {
