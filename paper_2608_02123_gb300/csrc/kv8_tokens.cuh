@@ -123,6 +123,8 @@ struct TokenShared {
   float o[token_warps(NT)][8 * NT][D + 4];
   float m[token_warps(NT)][8 * NT], l[token_warps(NT)][8 * NT];
   unsigned upto[PCTREE_KV_MAX_BATCH];
+  int16_t par[PCTREE_ATTN_MAX_N];
+  uint32_t path[PCTREE_ATTN_MAX_N / 32];         // the row and its ancestors
 };
 
 // NT: groups of 8 query heads.
@@ -196,9 +198,30 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
       for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
     const int stop = min(it.key_end, it.b1 * kTokenBlock);
+    int edge = stop;                             // from here on not every key is seen
+    if (a.parent != nullptr) {
+      const int32_t* parent = a.parent + it.row0 - it.j0;
+      for (int i = threadIdx.x; i <= it.j0; i += token_threads(NT)) {
+        int p = parent[i];
+        if (p < -1 || p >= i) {                  // parents precede children
+          report(a.status, PCTREE_ERR_INVALID_ARG);
+          p = -1;
+        }
+        sh.par[i] = static_cast<int16_t>(p);
+      }
+      __syncthreads();
+      if (warp == 0) {
+        uint32_t word = 0;                       // lane i finds word i
+        for (int i = it.j0; i >= 0; i = sh.par[i])
+          if (i >> 5 == lane) word |= 1u << (i & 31);
+        if (lane < PCTREE_ATTN_MAX_N / 32) sh.path[lane] = word;
+      }
+      __syncthreads();
+      edge = min(edge, it.prefix);
+    }
     // Keys come to a warp 32 at a time, as two tiles of 16; lane i finds the place and
-    // the scales of key i, none past the end and in pages that are none.  Codes are on
-    // their way from 32 keys ahead, page numbers from 32 more.
+    // the scales of key i, none where the row does not see it and in pages that are
+    // none.  Codes are on their way from 32 keys ahead, page numbers from 32 more.
     constexpr uint32_t kNone = 0xffffffffu;
     struct Ahead {
       uint32_t k[2][kC][4], v[4][kVWords];
@@ -212,10 +235,17 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
           it.r);
     };
     uint32_t at = kNone, k_byte = kExpBias, v_byte = kExpBias;
+    bool seen = false;
     auto find = [&](int key0) {
       const int key = key0 + lane;
-      const bool is = key < stop && page >= 0 && page < rows.n_pages;
-      if (key < stop && !is) report(a.status, PCTREE_ERR_INVALID_ARG);
+      seen = key < stop;
+      bool is = seen && page >= 0 && page < rows.n_pages;
+      if (seen && !is) report(a.status, PCTREE_ERR_INVALID_ARG);
+      if (a.parent != nullptr && key0 + 32 > edge) {
+        const int node = key - it.prefix;
+        if (seen && node >= 0) seen = (sh.path[node >> 5] >> (node & 31)) & 1u;
+        is = is && seen;
+      }
       const int off = key - div_by(key, a.blocks.page) * rows.page_size;
       at = is ? (static_cast<uint32_t>(page) * rows.page_size + off) * Hkv + it.kvh : kNone;
       const long long s = (static_cast<long long>(page) * a.blocks.per_page +
@@ -244,7 +274,8 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
     };
     const int first = it.b0 * kTokenBlock + warp * 32;
     constexpr int kStep = 32 * token_warps(NT);
-    uint32_t here = 0;                           // the keys' scales, K's byte in front
+    uint32_t here = 0;                           // the keys' scales, K's byte in front, and
+                                                 // whether the row does not see them
     // one tile, whose registers then take the one 32 keys on
     auto step = [&](Ahead& cur, int key0, int half) {
       float s[NT][4];
@@ -261,13 +292,15 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
           for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qf[n][c][w][0], qf[n][c][w][1]);
         }
       load_k(cur, half);
-      // scores with the exponents of K's and V's scales; keys past the end are -inf
+      // scores with the exponents of K's and V's scales; keys not seen are -inf
       uint32_t p16[NT][2];
       float v_off[2], k_by[2], v_by[2];
+      bool hide[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t sc2 = __shfl_sync(kFull, here, half + g + 8 * i);
-        const int ev = scale_exp(sc2 >> 8);
+        const int ev = scale_exp(sc2 >> 8 & 0xffu);
+        hide[i] = key0 + 16 > edge && sc2 >> 16 != 0;
         k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
         v_by[i] = exp2_of(-ev);
         v_off[i] = static_cast<float>(ev);
@@ -280,7 +313,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[i] = s[n][i] * (sc[n][i & 1] * k_by[i >> 1]);
-          if (key0 + 16 > stop && key0 + g + 8 * (i >> 1) >= stop) x[i] = -INFINITY;
+          if (hide[i >> 1]) x[i] = -INFINITY;
           const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
           d[i] = (x[i] - ref) + (v_off[i >> 1] - m_low[n][i & 1]);
           look = look || d[i] > (m[n][i & 1] == -INFINITY ? -INFINITY : 8.0f);
@@ -343,7 +376,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
       load_v(cur, half);
     };
     auto take_scales = [&]() {
-      here = k_byte | v_byte << 8;
+      here = k_byte | v_byte << 8 | (seen ? 0u : 1u << 16);
       if (!scale_ok(k_byte) || !scale_ok(v_byte)) report(a.status, PCTREE_ERR_INVALID_ARG);
     };
     Ahead x0, x1;
