@@ -610,9 +610,7 @@ PCTREE_API pctree_status pctree_kv8_append(
  *
  * Slots no row of the request sees are never used.  A row without a finite score
  * is NaN.  A NaN code reaches the rows that see its slot (a key's every dim, a
- * value's own dim; where 2 * (128 / G) neighbouring new rows hold NaN values in more
- * than 64 groups of 16 dims of a head, every dim of the rows that see the first of
- * them) and no others.  Scores, row maxima and sums and the output's
+ * value's own dim) and no others.  Scores, row maxima and sums and the output's
  * accumulation are float32; what else is rounded before the end is stated at the
  * kernels and stays below half a step of float16 for each probability.
  */

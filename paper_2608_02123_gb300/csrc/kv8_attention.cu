@@ -64,7 +64,6 @@ constexpr int kSlots = 6;                    // K and V blocks in the ring, in t
 constexpr int kAhead = 2;                    // blocks of codes under way
 constexpr int kItemRing = 8;
 constexpr int kPlaceRing = 4;
-constexpr int kMaxBad = 64;                  // groups of 16 values of V told apart
 constexpr uint32_t kTmemCols = 512;
 // Registers a thread: of the launch, and what the groups of four warps make of
 // them (their sum must not exceed the launch's).
@@ -103,11 +102,9 @@ struct Tail {
   Places places[kPlaceRing];
   float row_l[2][128], row_m[2][128];        // [tile]
   float row_scale[2][128];                   // of Q's rows (log2 units), [tile]
-  // NaN values at keys that only some rows of the unit see, by place in the item
-  // ring: 16 bits of a group of dims, the group << 16, the key (counted from the
-  // first that not every row sees) << 20; their number and the first such key.
-  int bad_n[kItemRing], bad_first[kItemRing];
-  uint32_t bad[kItemRing][kMaxBad];
+  // keys with NaN values that only some rows of the unit see, by place in the item
+  // ring: a bit each, counted from the first key that not every row sees
+  uint32_t bad[kItemRing][PCTREE_ATTN_MAX_N / 32];
   int16_t par[PCTREE_ATTN_MAX_N];
   uint32_t path[2][256][PCTREE_ATTN_MAX_N / 32];   // rows' ancestors, by piece parity
   alignas(16) uint8_t stage[4][32 * 32];
@@ -188,22 +185,24 @@ __device__ __forceinline__ bool any_nan(const uint4& x) {
   return (nan_tops(x.x) | nan_tops(x.y) | nan_tops(x.z) | nan_tops(x.w)) != 0;
 }
 
-// Sixteen codes of V with the NaN among them replaced by 0 and noted.
-__device__ __noinline__ uint4 without_nan(uint4 x, Tail* T, int ring, int key, int dim0) {
+// Sixteen codes of V with the NaN among them replaced by 0, their key noted.
+__device__ __noinline__ uint4 without_nan(uint4 x, Tail* T, int ring, int key) {
   uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= ~((nan_tops(w[i]) >> 7) * 0xffu);   // 0xff in those bytes
+  atomicOr(&T->bad[ring][key >> 5], 1u << (key & 31));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Which of sixteen codes are NaN, a bit each.
+__device__ __forceinline__ uint32_t nan_bits(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t bits = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t nan = (nan_tops(w[i]) >> 7) * 0xffu;      // 0xff in those bytes
-    w[i] &= ~nan;
+    const uint32_t nan = (nan_tops(w[i]) >> 7) * 0xffu;
     bits |= (((nan & 0x08040201u) * 0x01010101u) >> 24 & 15u) << (4 * i);
   }
-  atomicMin(&T->bad_first[ring], key);
-  const int n = atomicAdd(&T->bad_n[ring], 1);
-  if (n < kMaxBad)
-    T->bad[ring][n] =
-        bits | static_cast<uint32_t>(dim0 / 16) << 16 | static_cast<uint32_t>(key) << 20;
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return bits;
 }
 
 // Scores (in log2 units) whose floats are half an octave apart: from here on the
@@ -422,9 +421,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       auto post = [&](const Piece& it) -> bool {   // lane 0 writes the k-th piece
         const int s = k % kItemRing;
         if (!wwait_long(T, &T->item_empty[s], ((k / kItemRing) & 1) ^ 1)) return false;
+        if (lane < PCTREE_ATTN_MAX_N / 32) T->bad[s][lane] = 0;
+        __syncwarp();
         if (lane == 0) {
-          T->bad_n[s] = 0;
-          T->bad_first[s] = PCTREE_ATTN_MAX_N;
           T->item[s] = it;
           mbar_arrive(&T->item_full[s]);
         }
@@ -628,7 +627,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       for (int tile = 0; tile < tiles; ++tile) {
         if (!(ok = wwait_long(T, &T->o_full[tile], (tile == 0 ? kt[0]++ : kt[1]++) & 1))) break;
         tc_fence_after_sync();
-        const int n_bad = T->bad_n[ring];
+        uint32_t any_bad = 0;
+        for (int i = 0; i < PCTREE_ATTN_MAX_N / 32; ++i) any_bad |= T->bad[ring][i];
         const int nl = tile * a.tile_rows + div_by(t, a.by_G);   // row of the unit
         const int n_end = min(it.n_rows, (tile + 1) * a.tile_rows);
         // (rows of the next tile lie past this one's R)
@@ -652,19 +652,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) f[i] = 0.0f;
           }
-          if (n_bad != 0) {
-            // NaN values that were taken out of V reach the rows that see their keys
-            auto sees = [&](int key) {
-              return a.parent == nullptr
-                         ? key < nl
-                         : ((T->path[k & 1][min(nl, 255)][key >> 5] >> (key & 31)) & 1) != 0;
-            };
+          if (any_bad != 0) {
+            // NaN values that were taken out of V reach the rows that see their keys:
+            // the codes are looked at once more
+            const int first = a.parent != nullptr ? it.prefix : it.prefix + it.j0 + 1;
             uint32_t nan = 0;
-            for (int i = 0; i < min(n_bad, kMaxBad); ++i) {
-              const uint32_t e = T->bad[ring][i];
-              if (static_cast<int>((e >> 16) & 15) == c && sees(e >> 20)) nan |= e & 0xffffu;
+            for (int i = 0; i < PCTREE_ATTN_MAX_N / 32; ++i) {
+              uint32_t keys = T->bad[ring][i] &
+                              (a.parent != nullptr     ? T->path[k & 1][min(nl, 255)][i]
+                               : nl >= 32 * (i + 1) ? ~0u
+                               : nl > 32 * i        ? (1u << (nl - 32 * i)) - 1
+                                                    : 0u);
+              for (; in_tile && keys != 0; keys &= keys - 1) {
+                const int key = first + 32 * i + __ffs(keys) - 1;
+                const int entry = div_by(key, a.blocks.page);
+                const long long at =
+                    (static_cast<long long>(kv_page(a.units.rows, it.r, entry)) *
+                         a.units.rows.page_size + key - entry * a.units.rows.page_size) *
+                        a.units.Hkv + it.kvh;
+                // (a page that is none has no NaN)
+                nan |= nan_bits(__ldg(reinterpret_cast<const uint4*>(a.cache[1] + at * D + c * 16)));
+              }
             }
-            if (n_bad > kMaxBad && sees(T->bad_first[ring])) nan = 0xffffu;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if ((nan >> i) & 1u) f[i] = __int_as_float(0x7fc00000);
@@ -963,11 +972,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
         by[u] = (cur.by[u * kRows + row_in] >> (16 * is_v) & 0xffffu) * 0x10001u;
       }
       if (is_v != 0 && cur.key0 + kBK > cur.all) {
-        // keys that not every row sees: their NaN values are taken out and noted
+        // keys that not every row sees: their NaN values are taken out, the keys noted
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
           const int key = cur.key0 + u * kRows + row_in - cur.all;
-          if (key >= 0 && any_nan(x[u])) x[u] = without_nan(x[u], T, cur.ring, key, dim0);
+          if (key >= 0 && any_nan(x[u])) x[u] = without_nan(x[u], T, cur.ring, key);
         }
       }
       uint8_t* dst = mine + slot * kKBytes;
