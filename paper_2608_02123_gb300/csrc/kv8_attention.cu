@@ -165,18 +165,6 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Two float16 values times a float16 pair.
-__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
-// 2^e as float16, e in -15 .. 7.
-__device__ __forceinline__ uint16_t half_exp(int e) {
-  return static_cast<uint16_t>(e >= -14 ? (e + 15) << 10 : 0x200);
-}
-
 // Whether a word holds the code NaN (a carry into the byte's top bit).
 __device__ __forceinline__ uint32_t nan_tops(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;

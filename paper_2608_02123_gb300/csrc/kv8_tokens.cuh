@@ -10,10 +10,14 @@
 // (tcgen05 would take them from there, widened, for tiles of 128 rows of which G
 // are real: the kernel for many rows takes 245 us for the batch below.)
 //
-// P is relative to the running maximum of score + exponent of the value's scale, so
-// that P V is a product of P with the codes themselves and P fits float16 whatever
-// the scales: 2^7 times, down to 2^-31 of the maximum.  The reference is a float and
-// what its rounding leaves.  A row's sum adds P 2^-e in float32.
+// P is 2^7 times the probability relative to the running maximum of the scores, and
+// its row's sum adds it in float32.  For the product, in float16, V's scales are
+// relative to the largest exponent the warp has met.  Where those of 32 keys are at
+// most 3 below it, P takes them, 2^-3 .. 1, and V is the codes themselves (11 bits
+// of P down to 2^-18 of the maximum, and 2^-29 of it).  Else V takes as many as
+// float16 holds exactly with every code, 15, and P the rest: never more than 7, with
+// 11 bits down to 2^-14 and 2^-25 of the maximum, as the type has for the probability
+// itself.
 //
 // A CTA's pieces are kv_pieces.cuh's, planned by every warp alike; a piece's keys
 // are dealt out among its warps, whose (max, sum, O) are added up in order.
@@ -27,6 +31,8 @@
 // at the same time) 114; codes through L1 132; the codes of no key from an array of
 // zeros instead of predicated loads 87.
 #pragma once
+
+#include <type_traits>
 
 #include "kv8.cuh"
 #include "kv_pieces.cuh"
@@ -63,6 +69,7 @@ __host__ __device__ constexpr int token_warps(int NT) { return token_threads(NT)
 constexpr int kTokenBlock = 128;             // keys per block of work
 constexpr int kTokenHeads = 16;              // query heads of a unit, at most
 constexpr float kTokenBits = 7.0f;           // P is 2^7 times what it is relative to
+constexpr int kTokenLift = 3;                // of V's exponents that P takes where all are near
 
 // D (+)= A B of 16 x 8 x 16 float16 values, float32 sums.
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
@@ -71,6 +78,17 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       "{%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two float16 values times a float16 pair.
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// 2^e as float16, e in -15 .. 7.
+__device__ __forceinline__ uint16_t half_exp(int e) {
+  return static_cast<uint16_t>(e >= -14 ? (e + 15) << 10 : 0x200);
 }
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
   uint32_t r;
@@ -186,13 +204,12 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
       sc[n][0] = __shfl_sync(kFull, row_sc, 8 * t);
       sc[n][1] = __shfl_sync(kFull, row_sc, 8 * t + 4);
     }
-    float o[NT][kTiles][4];
-    // P's reference is m + m_low: large scores would swallow the values' exponents
-    float m[NT][2], m_low[NT][2], l[NT][2];
+    float o[NT][kTiles][4];                      // times 2^-e_ref
+    float m[NT][2], l[NT][2];
+    int e_ref = kMinExp;                         // the largest exponent of V so far
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       m[n][0] = m[n][1] = -INFINITY;
-      m_low[n][0] = m_low[n][1] = 0.0f;
       l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
@@ -274,8 +291,10 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
     };
     const int first = it.b0 * kTokenBlock + warp * 32;
     constexpr int kStep = 32 * token_warps(NT);
-    uint32_t here = 0;                           // the keys' scales, K's byte in front, and
-                                                 // whether the row does not see them
+    // Of a lane's key: K's scale as the upper half of a float, the part of V's that P
+    // takes as the lower half (0: not seen); V's own part; whether there is any.
+    uint32_t here = 0, v_part = 0;
+    bool parted = false;
     // one tile, whose registers then take the one 32 keys on
     auto step = [&](Ahead& cur, int key0, int half) {
       float s[NT][4];
@@ -292,22 +311,20 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
           for (int n = 0; n < NT; ++n) mma_f16(s[n], a0, a1, a2, a3, qf[n][c][w][0], qf[n][c][w][1]);
         }
       load_k(cur, half);
-      // scores with the exponents of K's and V's scales; keys not seen are -inf
+      // scores with K's scales; keys not seen are -inf
       uint32_t p16[NT][2];
-      float v_off[2], k_by[2], v_by[2];
+      float k_by[2], p_by[2];
       bool hide[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t sc2 = __shfl_sync(kFull, here, half + g + 8 * i);
-        const int ev = scale_exp(sc2 >> 8 & 0xffu);
-        hide[i] = key0 + 16 > edge && sc2 >> 16 != 0;
-        k_by[i] = exp2_of(scale_exp(sc2 & 0xffu));
-        v_by[i] = exp2_of(-ev);
-        v_off[i] = static_cast<float>(ev);
+        const uint32_t by = __shfl_sync(kFull, here, half + g + 8 * i);
+        k_by[i] = __uint_as_float(by & 0xffff0000u);
+        p_by[i] = __uint_as_float(by << 16);
+        hide[i] = key0 + 16 > edge && p_by[i] == 0.0f;
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        // (x: scores; d: with the value's exponent, relative to the reference)
+        // (x: scores; d: relative to the reference)
         float x[4], d[4];
         bool look = false;
 #pragma unroll
@@ -315,7 +332,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
           x[i] = s[n][i] * (sc[n][i & 1] * k_by[i >> 1]);
           if (hide[i >> 1]) x[i] = -INFINITY;
           const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
-          d[i] = (x[i] - ref) + (v_off[i >> 1] - m_low[n][i & 1]);
+          d[i] = x[i] - ref;
           look = look || d[i] > (m[n][i & 1] == -INFINITY ? -INFINITY : 8.0f);
         }
         if (__any_sync(kFull, look)) {
@@ -324,24 +341,11 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
             float top = fmaxf(x[r], x[2 + r]);
 #pragma unroll
             for (int o2 = 4; o2 < 32; o2 <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o2));
-            const bool none = m[n][r] == -INFINITY;
-            if (none && top > -INFINITY) {       // the first keys: their largest score for now
+            if (top > m[n][r]) {
+              const float alpha = ex2_approx(m[n][r] - top);
               m[n][r] = top;
-              d[r] = (x[r] - top) + v_off[0];
-              d[2 + r] = (x[2 + r] - top) + v_off[1];
-            }
-            float up = fmaxf(d[r], d[2 + r]);
-#pragma unroll
-            for (int o2 = 4; o2 < 32; o2 <<= 1) up = fmaxf(up, __shfl_xor_sync(kFull, up, o2));
-            if (m[n][r] > -INFINITY && (none || up > 0.0f)) {
-              // m + m_low + up, as a rounded sum and what the rounding left
-              const float low = m_low[n][r] + up, sum = m[n][r] + low;
-              const float back = sum - m[n][r];
-              m_low[n][r] = (m[n][r] - (sum - back)) + (low - back);
-              m[n][r] = sum;
-              d[r] = (x[r] - sum) + (v_off[0] - m_low[n][r]);
-              d[2 + r] = (x[2 + r] - sum) + (v_off[1] - m_low[n][r]);
-              const float alpha = none ? 0.0f : ex2_approx(-up);
+              d[r] = x[r] - top;
+              d[2 + r] = x[2 + r] - top;
               l[n][r] *= alpha;
 #pragma unroll
               for (int i = 0; i < kTiles; ++i) {
@@ -355,29 +359,65 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           p[i] = ex2_approx(d[i] + kTokenBits);
-          l[n][i & 1] = fmaf(p[i], v_by[i >> 1], l[n][i & 1]);
+          l[n][i & 1] += p[i];
         }
-        p16[n][0] = transposed8x8(pack16<true>(p[0], p[1]));
-        p16[n][1] = transposed8x8(pack16<true>(p[2], p[3]));
+        p16[n][0] = transposed8x8(pack16<true>(p[0] * p_by[0], p[1] * p_by[0]));
+        p16[n][1] = transposed8x8(pack16<true>(p[2] * p_by[1], p[3] * p_by[1]));
       }
       // V^T P^T: pairs of keys of a dim, two dims a word
+      auto product = [&](auto with_parts) {
+        uint32_t part[2] = {0, 0};               // of V's scales, pairs of keys
+        if constexpr (with_parts.value) {
 #pragma unroll
-      for (int w = 0; w < kVWords; ++w)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t sel = j == 0 ? 0x5140u : 0x7362u;
-          const uint32_t lo = __byte_perm(cur.v[0][w], cur.v[1][w], sel);
-          const uint32_t hi = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
-          const uint32_t a0 = halves2(lo), a1 = halves2(lo >> 16), a2 = halves2(hi),
-                         a3 = halves2(hi >> 16);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16(o[n][2 * w + j], a0, a1, a2, a3, p16[n][0], p16[n][1]);
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t lo = __shfl_sync(kFull, v_part, half + 2 * t + 8 * i);
+            part[i] = lo | __shfl_sync(kFull, v_part, half + 2 * t + 1 + 8 * i) << 16;
+          }
         }
+        auto halves = [&](uint32_t codes, int i) {
+          const uint32_t h = halves2(codes);
+          if constexpr (with_parts.value) return mul_h2(h, part[i]);
+          return h;
+        };
+#pragma unroll
+        for (int w = 0; w < kVWords; ++w)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t sel = j == 0 ? 0x5140u : 0x7362u;
+            const uint32_t lo = __byte_perm(cur.v[0][w], cur.v[1][w], sel);
+            const uint32_t hi = __byte_perm(cur.v[2][w], cur.v[3][w], sel);
+            const uint32_t a0 = halves(lo, 0), a1 = halves(lo >> 16, 0), a2 = halves(hi, 1),
+                           a3 = halves(hi >> 16, 1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              mma_f16(o[n][2 * w + j], a0, a1, a2, a3, p16[n][0], p16[n][1]);
+          }
+      };
+      if (parted) product(std::true_type{}); else product(std::false_type{});
       load_v(cur, half);
     };
+    // the scales of the 32 keys that come next
     auto take_scales = [&]() {
-      here = k_byte | v_byte << 8 | (seen ? 0u : 1u << 16);
       if (!scale_ok(k_byte) || !scale_ok(v_byte)) report(a.status, PCTREE_ERR_INVALID_ARG);
+      const bool none = at == kNone;             // no codes: any scale does
+      const int e = none ? kMinExp : scale_exp(v_byte);
+      const int top = __reduce_max_sync(kFull, e);
+      if (top > e_ref) {
+        const float by = exp2_of(e_ref - top);
+        e_ref = top;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[n][i][r] *= by;
+      }
+      const int off = none ? 0 : e - e_ref;      // -22 .. 0
+      parted = __any_sync(kFull, off < -kTokenLift);
+      const int p_exp = parted ? min(0, off - kMinExp) : off;
+      v_part = half_exp(off - p_exp);            // (-15 .. 0: exact with every code)
+      here = __float_as_uint(exp2_of(scale_exp(k_byte))) |
+             (seen ? __float_as_uint(exp2_of(p_exp)) >> 16 : 0u);
     };
     Ahead x0, x1;
     find_page(first);
@@ -396,6 +436,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
       if (key0 + 16 < stop) step(x1, key0 + 16, 16);
     }
     // the warps' parts, in order
+    const float f = exp2_of(e_ref);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -403,12 +444,9 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[n][r] += __shfl_xor_sync(kFull, l[n][r], d);
         const int h = 8 * n + 2 * t + r;
-        // relative to a rounded reference, as other parts are
-        const float ref = m[n][r] + m_low[n][r];
-        const float f = m[n][r] == -INFINITY ? 1.0f : exp2f((m[n][r] - ref) + m_low[n][r]);
         if (g == 0) {
-          sh.m[warp][h] = ref;
-          sh.l[warp][h] = l[n][r] * f;
+          sh.m[warp][h] = m[n][r];
+          sh.l[warp][h] = l[n][r];
         }
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
