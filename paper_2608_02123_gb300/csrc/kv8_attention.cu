@@ -49,6 +49,7 @@
 // 2147; the rescaling of O unrolled (instructions that run rarely come from memory)
 // 1370.
 #include <algorithm>
+#include <atomic>
 
 #include "kv8_tokens.cuh"
 
@@ -1072,12 +1073,18 @@ pctree_status attn8_launch(const Kv8AttnArgs& a, bool tokens, int num_sms, cudaS
     static SmemLimit limit;
     const void* fn = reinterpret_cast<const void*>(kv8_attn_kernel<D, F16>);
     if (limit.ensure(fn, smem) != cudaSuccess) return PCTREE_ERR_CUDA;
-    // (a launch with fewer registers would leave the softmax waiting for its own)
-    static const bool registers = [fn] {
+    // (a launch with fewer registers would leave the softmax waiting for its own; a
+    // query that fails is asked again by the next call)
+    static std::atomic<bool> registers{false};
+    if (!registers.load(std::memory_order_relaxed)) {
       cudaFuncAttributes f;
-      return cudaFuncGetAttributes(&f, fn) == cudaSuccess && f.numRegs >= kRegsLaunch;
-    }();
-    if (!registers) return PCTREE_ERR_CUDA;
+      if (cudaFuncGetAttributes(&f, fn) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return PCTREE_ERR_CUDA;
+      }
+      if (f.numRegs < kRegsLaunch) return PCTREE_ERR_CUDA;
+      registers.store(true, std::memory_order_relaxed);
+    }
     lc.blockDim = dim3(kThreads);
     lc.dynamicSmemBytes = smem;
     if (cudaLaunchKernelEx(&lc, kv8_attn_kernel<D, F16>, a) != cudaSuccess) return PCTREE_ERR_CUDA;
