@@ -71,7 +71,8 @@ __global__ void __launch_bounds__(kCompactThreads, 3) kv8_compact_kernel(Kv8Comp
       for (int j = lane; j <= L; j += 32) {
         const int x = idx[j];
         long long place, at;
-        bad = bad || x < 0 || x >= a.N || (j == 0 ? x != 0 : x <= idx[j - 1]) ||
+        // (j <= x < N: both slots are among the request's)
+        bad = bad || x < j || x >= a.N || (j == 0 ? x != 0 : x <= idx[j - 1]) ||
               !find(T + j, place, at) || !find(T + x, place, at);
       }
     if (__any_sync(kFull, bad)) {
