@@ -674,7 +674,7 @@ PCTREE_API pctree_status pctree_kv8_attention(
 typedef struct {
   int32_t batch;         /* requests, <= PCTREE_KV_MAX_BATCH                 */
   int32_t B;             /* accepted_idx rows hold B + 1 ints                */
-  int32_t N;             /* packed tree size: T + N slots exist              */
+  int32_t N;             /* packed tree size, <= max_pages * page_size       */
   int32_t layers;
   int32_t Hkv, D;        /* D 64, 128                                        */
   int32_t page_size, n_pages, max_pages;
@@ -690,10 +690,11 @@ typedef struct {
  *   page_table      [batch][max_pages] int32 (device) or NULL, of all layers
  *   k_cache, v_cache   [layers] caches, 16-byte aligned; k_scale, v_scale
  *   status          one device int32 or NULL.  A request whose accepted path is
- *                   not one pctree_accept can return, with T < 0 or T + N >
- *                   max_pages * page_size, or with a bad page among those of its
- *                   rows, is left untouched and sets it to
- *                   PCTREE_ERR_INVALID_ARG; otherwise it is not written.
+ *                   not one pctree_accept can return, with T < 0, with accepted
+ *                   rows past its max_pages * page_size slots, or with a bad page
+ *                   among those of its rows, is left untouched and sets it to
+ *                   PCTREE_ERR_INVALID_ARG; otherwise it is not written.  (Trees of
+ *                   fewer than N nodes may end at the last slot.)
  * Returns PCTREE_ERR_INVALID_ARG / PCTREE_ERR_UNSUPPORTED for bad arguments
  * (nothing enqueued) and PCTREE_ERR_CUDA if the launch fails.  No workspace.
  */

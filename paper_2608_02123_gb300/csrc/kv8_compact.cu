@@ -64,15 +64,14 @@ __global__ void __launch_bounds__(kCompactThreads, 3) kv8_compact_kernel(Kv8Comp
       at = static_cast<long long>(page) * a.blocks.per_page + (off >> a.blocks.shift);
       return page >= 0;
     };
-    bool bad = L < 0 || L > a.B || T < 0 ||
-               static_cast<long long>(T) + a.N >
-                   static_cast<long long>(a.rows.max_pages) * a.rows.page_size;
+    const int slots = a.rows.max_pages * a.rows.page_size;     // <= 2^30
+    bool bad = L < 0 || L > a.B || T < 0 || T >= slots;
     if (!bad)
       for (int j = lane; j <= L; j += 32) {
         const int x = idx[j];
         long long place, at;
-        // (j <= x < N: both slots are among the request's)
-        bad = bad || x < j || x >= a.N || (j == 0 ? x != 0 : x <= idx[j - 1]) ||
+        // (the tree may be smaller than N: its rows' slots must be there, and j <= x)
+        bad = bad || x < j || x >= a.N || x >= slots - T || (j == 0 ? x != 0 : x <= idx[j - 1]) ||
               !find(T + j, place, at) || !find(T + x, place, at);
       }
     if (__any_sync(kFull, bad)) {
