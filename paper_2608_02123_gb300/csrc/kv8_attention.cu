@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
             w[i] = pack16<true>(f.x * by, f.y * by);
           }
           *at = make_uint4(w[0], w[1], w[2], w[3]);
-          if (c == 0) T->row_scale[tile][row] = a.scale_log2 * exp2_of(e);
+          if (c == 0) T->row_scale[tile][row] = row_scale(a.scale_log2, e);
         }
         fence_proxy_async_smem();
         __syncwarp();

@@ -32,6 +32,7 @@
 // zeros instead of predicated loads 87.
 #pragma once
 
+#include <cfloat>
 #include <type_traits>
 
 #include "kv8.cuh"
@@ -79,6 +80,13 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The softmax scale of a row of Q times 2^e: a normal number, so that neither a masked
+// score's infinity nor a score of 0 becomes NaN.  (Below the smallest all scores are 0
+// but for 2^-80; past the largest those that are not equal are 2^70 apart.)
+__device__ __forceinline__ float row_scale(float scale_log2, int e) {
+  return fminf(fmaxf(scale_log2 * exp2_of(e), FLT_MIN), FLT_MAX);
+}
+
 // Two float16 values times a float16 pair.
 __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -192,7 +200,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
         const int top = static_cast<int>(max(top2 >> 16, top2 & 0xffffu) >> 7) - 127;
         const int e = max(-100, min(126, top)) - 14;
         const float by = exp2_of(-e);
-        row_sc *= exp2_of(e);
+        row_sc = row_scale(row_sc, e);
 #pragma unroll
         for (int c = 0; c < kC; ++c)
 #pragma unroll
@@ -329,7 +337,7 @@ __global__ void __launch_bounds__(token_threads(NT), 1) kv8_token_kernel(Kv8Attn
         bool look = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = s[n][i] * (sc[n][i & 1] * k_by[i >> 1]);
+          x[i] = (s[n][i] * k_by[i >> 1]) * sc[n][i & 1];
           if (hide[i >> 1]) x[i] = -INFINITY;
           const float ref = m[n][i & 1] == -INFINITY ? 0.0f : m[n][i & 1];
           d[i] = x[i] - ref;
