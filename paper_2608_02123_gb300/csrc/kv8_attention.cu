@@ -27,20 +27,27 @@
 //
 // Numbers: code * 2^e is exact in float16 for every exponent of the format, so the
 // products' K and V are the cache's values.  A bfloat16 row of Q is multiplied by
-// a power of two that brings its largest element to 2^14 .. 2^15, which float16
-// holds to 2^-39 of the largest; the power goes into the row's softmax scale.  P is
-// 2^7 times the probability relative to the row's running maximum, in float16 (11
-// bits; down to 2^-31 of the maximum): far keys of a long context that are each
-// small against the first are not lost.  Row sums add the unrounded values.
+// a power of two that brings its largest element to 2^14 .. 2^15 (exact in float16
+// but for elements below 2^-31 of the largest, and those to 2^-39 of it); the power
+// goes into the row's softmax scale.  P is 2^7 times the probability relative to the
+// row's running maximum, by ex2.approx (2^-22 of it), in float16 (11 bits; down to
+// 2^-31 of the maximum): far keys of a long context that are each small against the
+// first are not lost.  (A product's operands have one type, and float16 holds V
+// exactly.  P's rounding is below that of a bfloat16 output; to a float16 output's
+// error it adds a fifth.)  Row sums add the unrounded values.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
-//   four prompts of up to 4096 rows 865 (0.49 PFLOP/s), packed trees of 32 requests
-//   195: 3600 cycles a block of 64 keys for two tiles, of which the products take 1280
-//   (S, M = 128, N = 64, reads 6 KB of shared memory a product: 48 cycles instead of
-//   32), the widening's traffic (64 KB) 512, and a softmax warp's chain 2300: two
-//   warps on an SM's quarter issue an instruction in some 7 cycles each, and the
-//   roles' code, 140 KB, is more than the instruction cache holds;
-//   16 chains of 8 rows (32 query heads) 35: one tile, 40 of its 128 rows.
+//   four prompts of up to 4096 rows 863 to 884 by box (0.48 to 0.49 PFLOP/s), packed
+//   trees of 32 requests 195 to 200.  With longer prefixes a block of 64 keys costs
+//   2950 cycles for two tiles (at the 2070 MHz sampled meanwhile), of which the
+//   products take 1280 (S, M = 128, N = 64, reads 6 KB of shared memory a product: 48
+//   cycles instead of 32), the widening's traffic (64 KB) 512, and a softmax warp's
+//   chain 2300: two warps on an SM's quarter issue an instruction in some 7 cycles
+//   each, and the roles' code, 140 KB, is more than the instruction cache holds.  That
+//   is 506 us of the prompts' (354 blocks a CTA) and 89 of the trees' (62); the rest
+//   is 18 to 25 us for each of a CTA's 14 and 5 pieces: queries, first block, output;
+//   16 chains of 8 rows (32 query heads) 35: one tile, 16 to 32 of its 128 rows real;
+//   2100 cycles a block.
 // Steps that were measured (prompts): codes to registers with a branch around each
 // load, which waits for it, 4583; places and scales by a warp of their own 1589;
 // copies to shared memory 1290; two tiles a block of K and V 1216; Q in place by
@@ -199,7 +206,7 @@ __device__ __forceinline__ uint32_t nan_bits(const uint4& x) {
 // powers of two that P's type does not hold.
 constexpr float kWideScore = 4194304.0f;
 
-// The 64 scores of a block half at TMEM columns s_col .. (those not in `see` are
+// The 64 scores of a block at TMEM columns s_col .. (those not in `see` are
 // -inf) become what, times sc, is the rounded score less the reference.
 __device__ __noinline__ void wide_scores(uint32_t s_col, float sc, float mref, uint64_t see) {
   const float inv = 1.0f / sc;
@@ -430,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_attn_kernel(Kv8AttnArgs a) {
       if (!ok && lane == 0) give_up();
     } else if (warp == 3) {
       // ---------------- places and scales of the keys ----------------
-      // Four keys a lane.  Page numbers are read a block ahead of their use, and a
+      // Two keys a lane.  Page numbers are read a block ahead of their use, and a
       // block's scales are under way while the block before it is written down.
       constexpr int kKeys = kBK / 32;
       const KvRows& rows = a.units.rows;

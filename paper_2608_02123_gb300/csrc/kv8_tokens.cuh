@@ -8,10 +8,10 @@
 // share of K is 16 neighbouring dims of a key and of V 16 neighbouring dims of
 // four keys: codes are widened where they were loaded, without shared memory.
 // (tcgen05 would take them from there, widened, for tiles of 128 rows of which G
-// are real: the kernel for many rows takes 245 us for the batch below.)
+// are real: the kernel for many rows takes 230 us for the batch below.)
 //
-// P is 2^7 times the probability relative to the running maximum of the scores, and
-// its row's sum adds it in float32.  For the product, in float16, V's scales are
+// P is 2^7 times the probability relative to the running maximum of the scores, by
+// ex2.approx (2^-22 of it), and its row's sum adds it in float32.  For the product, in float16, V's scales are
 // relative to the largest exponent the warp has met.  Where those of 32 keys are at
 // most 3 below it, P takes them, 2^-3 .. 1, and V is the codes themselves (11 bits
 // of P down to 2^-18 of the maximum, and 2^-29 of it).  Else V takes as many as
@@ -23,9 +23,10 @@
 // are dealt out among its warps, whose (max, sum, O) are added up in order.
 //
 // What bounds it (one GB300, us; tokens of 32 requests over up to 8192 slots, 40
-// query and 8 KV heads of 128 dims, 431 MB): 83, 0.77 of the measured copy rate; some
-// 350 instructions a tile of 16 keys, 5 cycles each, by the three warps of a quarter
-// of an SM.  Before: each lane finding its key's place twice over (16 keys at a time)
+// query and 8 KV heads of 128 dims, 431 MB): 83 to 86 by box, 0.74 to 0.77 of the
+// measured copy rate; some 350 instructions a tile of 16 keys, 5 cycles each, by the
+// three warps of a quarter of an SM.  Groups of 9 to 16 heads have eight warps: 119 to
+// 121 where eight heads take 96 (L2 flushed).  Before: each lane finding its key's place twice over (16 keys at a time)
 // 99; a scale or page number that is looked at where it is read 104; sixteen warps of
 // one tile ahead 107.  Not kept: a unit of all KV heads of a row (neighbouring memory
 // at the same time) 114; codes through L1 132; the codes of no key from an array of
