@@ -37,8 +37,8 @@
 // error it adds a fifth.)  Row sums add the unrounded values.
 //
 // What bounds it (one GB300, us; 40 query and 8 KV heads of 128 dims, bf16):
-//   four prompts of up to 4096 rows 863 to 884 by box (0.48 to 0.49 PFLOP/s), packed
-//   trees of 32 requests 195 to 200.  With longer prefixes a block of 64 keys costs
+//   four prompts of up to 4096 rows 874 to 884 by box (0.48 PFLOP/s), packed trees of 32
+//   requests 197 to 200.  With longer prefixes a block of 64 keys costs
 //   2950 cycles for two tiles (at the 2070 MHz sampled meanwhile), of which the
 //   products take 1280 (S, M = 128, N = 64, reads 6 KB of shared memory a product: 48
 //   cycles instead of 32), the widening's traffic (64 KB) 512, and a softmax warp's

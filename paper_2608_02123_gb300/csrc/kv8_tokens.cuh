@@ -23,7 +23,7 @@
 // are dealt out among its warps, whose (max, sum, O) are added up in order.
 //
 // What bounds it (one GB300, us; tokens of 32 requests over up to 8192 slots, 40
-// query and 8 KV heads of 128 dims, 431 MB): 83 to 86 by box, 0.74 to 0.77 of the
+// query and 8 KV heads of 128 dims, 431 MB): 84.5 to 86.6 by box, 0.74 of the
 // measured copy rate; some 350 instructions a tile of 16 keys, 5 cycles each, by the
 // three warps of a quarter of an SM.  Groups of 9 to 16 heads have eight warps: 119 to
 // 121 where eight heads take 96 (L2 flushed).  Before: each lane finding its key's place twice over (16 keys at a time)
